@@ -428,6 +428,118 @@ enum { GSN_STAT_ROUNDS = 0, GSN_STAT_ROUNDS_MAX = 1, GSN_STAT_UPDATES = 2,
        GSN_STAT_LOOP_RECORDS = 6 };
 int gsn_stat(gsn_net* net, int32_t key, int64_t* value, void* stream);
 
+/* ------------------------------------------------------------ mixture of local experts --
+ *
+ * Local models on top of the units: a token (the features of a signal) is normed, routed to
+ * the K best of E experts and passed through their products.  Routing of the negative squared
+ * distances to the units with K = 2 gives the winner and the second of gsn_find_winners.
+ * These calls need no handle.  They are async, may be captured into a HIP graph, allocate
+ * nothing, and give the same bits on every run.  Matrices are row-major; a stride is the
+ * number of elements from one row to the next.  Sums are binary32; a result is rounded once,
+ * to its type, to nearest even. */
+enum { GSN_F32 = 0, GSN_BF16 = 1, GSN_F16 = 2 };
+
+/* Layer norm of every row of x [rows][dim]:
+ *     mean = sum x / dim,  r = 1 / sqrt(sum (x - mean)^2 / dim + eps),
+ *     y = (x - mean) * r * weight + bias.
+ * dtype: the type of x and y; param_dtype: that of weight and bias, GSN_F32 or dtype.  weight
+ * and bias may be NULL (1 and 0).  stats (device float [2][rows], or NULL) receives the means,
+ * then the r's, which the backward pass takes.  x and y may be the same memory.  rows >= 0,
+ * dim >= 1, eps >= 0. */
+int gsn_layer_norm(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim, const void* x,
+                   int64_t x_stride, const void* weight, const void* bias, float eps, void* y,
+                   int64_t y_stride, float* stats, void* stream);
+
+/* Device workspace of the backward pass; 0 if the arguments are invalid. */
+size_t gsn_layer_norm_workspace_bytes(int64_t rows, int32_t dim);
+
+/* Gradients of gsn_layer_norm from dy: dx, and the sums over the rows dweight = sum dy n,
+ * dbias = sum dy with n = (x - mean) * r.  Each output may be NULL (not computed); dx may be
+ * the memory of dy.  workspace: 256-byte aligned, needed for dweight or dbias. */
+int gsn_layer_norm_backward(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim,
+                            const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
+                            const void* weight, const float* stats, void* dx, int64_t dx_stride,
+                            void* dweight, void* dbias, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Routing of tokens to experts.  With s = softmax(logits) or sigmoid(logits) of a token:
+ *   - an expert whose logit is -inf or NaN is shut out; +inf counts as the largest float;
+ *   - experts are ordered by s + balance, or by the logit where there is no balance (the same
+ *     order without rounding); ties go to the lowest index; one whose s + balance is -inf or
+ *     NaN is shut out;
+ *   - with groups > top_groups, group g holds experts [g, g + 1) * experts / groups; its value
+ *     is its best expert's place in that order (best = 1) or the sum of s + balance of its two
+ *     best (best = 2); only experts of the top_groups best groups are left, ties to the lowest;
+ *   - ids receives the top best of what is left, -1 where nothing is left; weights their s
+ *     (without the balance), over the sum of the chosen s if renormalise is not 0, times
+ *     scale; 0 where the id is -1.
+ * A token whose valid byte is 0 has no experts, whatever its logits (valid may be NULL).
+ * experts 1 to 1024, top 1 to 64 and at most top_groups * experts / groups, groups a divisor
+ * of experts, 1 to 64. */
+enum { GSN_SCORE_SOFTMAX = 0, GSN_SCORE_SIGMOID = 1 };
+typedef struct gsn_route_params {
+  int32_t experts, top;
+  int32_t score;
+  int32_t groups, top_groups, best;
+  int32_t renormalise;
+  float scale;
+} gsn_route_params;
+
+/* logits: device [tokens][experts] of dtype with the given row stride; balance: device
+ * float [experts] or NULL; valid: device uint8 [tokens] or NULL; ids: device int32
+ * [tokens][top]; weights: device float [tokens][top]. */
+int gsn_route(const gsn_route_params* params, int32_t dtype, int64_t tokens, const void* logits,
+              int64_t stride, const float* balance, const uint8_t* valid, int32_t* ids,
+              float* weights, void* stream);
+
+/* Gradient of the weights with respect to the logits, the choice held fixed: dlogits
+ * [tokens][experts] of dtype, every element written.  ids out of range count as -1. */
+int gsn_route_backward(const gsn_route_params* params, int32_t dtype, int64_t tokens,
+                       const float* dweights, const void* logits, int64_t stride,
+                       const int32_t* ids, void* dlogits, int64_t dlogits_stride, void* stream);
+
+/* Number of pairs that went to each expert: counts, device int32 [experts]. */
+int gsn_route_counts(int64_t pairs, int32_t experts, const int32_t* ids, int32_t* counts,
+                     void* stream);
+
+/* Moves the balance of every expert by rate: up where counts is below its mean, down where it
+ * is above. */
+int gsn_route_balance(int32_t experts, const int32_t* counts, float rate, float* balance,
+                      void* stream);
+
+/* The experts' products of routed tokens:
+ *     (gate, up) = w1[e] x[t],  out[t] = sum over k of weights[t][k] * w2[e] (silu(gate) * up)
+ * with e = ids[t][k], silu(v) = v / (1 + exp(-v)); a pair whose id is out of range adds nothing.
+ * x [tokens][dim] with a row stride, w1 [experts][2 * hidden][dim] (the gate's rows first),
+ * w2 [experts][dim][hidden] and out [tokens][dim] are of type dtype; silu(gate) * up is rounded
+ * to dtype between the two products, the sum over k is in binary32.  tokens up to 2^23,
+ * tokens * top up to 2^26, experts 1 to 1024, top 1 to 64, dim and hidden 1 to 2^20. */
+typedef struct gsn_experts_params {
+  int32_t dtype;
+  int32_t experts, top, dim, hidden;
+  int64_t tokens;
+} gsn_experts_params;
+
+/* Device bytes of a call's workspace (backward: 0 or 1), and of what the forward pass saves for
+ * the backward pass; 0 if the parameters are invalid.  Both buffers are 256-byte aligned. */
+size_t gsn_experts_workspace_bytes(const gsn_experts_params* params, int32_t backward);
+size_t gsn_experts_saved_bytes(const gsn_experts_params* params);
+
+/* saved may be NULL (no backward pass will follow). */
+int gsn_experts(const gsn_experts_params* params, const void* x, int64_t x_stride,
+                const int32_t* ids, const float* weights, const void* w1, const void* w2,
+                void* out, void* saved, size_t saved_bytes, void* workspace,
+                size_t workspace_bytes, void* stream);
+
+/* Gradients from dout [tokens][dim], with the arguments and the saved buffer of the forward
+ * call: dx [tokens][dim], dweights float [tokens][top], dw1, dw2 (every element written; 0 for
+ * an expert without tokens).  Each may be NULL (not computed). */
+int gsn_experts_backward(const gsn_experts_params* params, const void* dout, const void* x,
+                         int64_t x_stride, const float* weights, const void* w1, const void* w2,
+                         const void* saved, size_t saved_bytes, void* dx, float* dweights,
+                         void* dw1, void* dw2, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,6 @@ import importlib
 
 
 def __getattr__(name):
-    if name in ("gsn", "clouds"):
+    if name in ("gsn", "clouds", "mixture"):
         return importlib.import_module(f"{__name__}.{name}")
     raise AttributeError(name)

@@ -1,0 +1,63 @@
+// The experts' products: what the host passes to the kernels of one type of element.
+#pragma once
+
+#include "mixture.h"
+
+namespace gsn {
+
+constexpr int kPlanExperts = 1024;  // experts at most
+
+// Pairs (token, place k), number token * top + k, sorted by expert and then by number: row r of
+// the products is pair rows[r], pair j is row pos[j] (-1 for a pair without an expert), expert
+// e's rows are offsets[e] .. offsets[e + 1] - 1.  Blocks of `block` rows that hold one expert's
+// rows alone are listed in tiles as (expert, first row); *tile_count of them.
+struct Plan {
+  int32_t* offsets;     // experts + 1
+  int32_t* tile_count;  // 1
+  int2* tiles;          // most_tiles
+  int32_t* rows;        // pairs
+  int32_t* pos;         // pairs
+  int32_t block;
+  int32_t most_tiles;
+};
+
+struct Experts {
+  int64_t tokens;
+  int32_t experts, top, dim, hidden;
+  int64_t pairs;
+  const void* x;
+  int64_t x_stride;
+  const int32_t* ids;
+  const float* weights;
+  const void* w1;
+  const void* w2;
+  Plan plan;
+  // forward
+  void* out;
+  float* pre;    // [pairs][2 hidden] the products with w1, kept for the backward pass, or null
+  void* act;     // [pairs][hidden]
+  float* y;      // [pairs][dim]
+  // backward
+  const void* dout;
+  void* dpre;    // [pairs][2 hidden]
+  void* wact;    // [pairs][hidden], the activation times the pair's weight
+  float* dots;   // [pairs][dot_tiles] parts of the weights' gradients
+  int32_t dot_tiles;
+  float* dxr;    // [pairs][dim]
+  void* dx;
+  float* dweights;
+  void* dw1;
+  void* dw2;
+};
+
+hipError_t launch_plan(const Experts& x, hipStream_t st);
+
+template <typename T>
+hipError_t launch_experts(const Experts& x, hipStream_t st);
+template <typename T>
+hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
+
+// columns of one partial dot product of the weights' gradient
+constexpr int kDotColumns = 128;
+
+}  // namespace gsn

@@ -58,6 +58,12 @@ GSN_STAT_RESOLVED = 4
 GSN_STAT_ACCEPTED = 5
 GSN_STAT_LOOP_RECORDS = 6
 
+GSN_F32 = 0
+GSN_BF16 = 1
+GSN_F16 = 2
+GSN_SCORE_SOFTMAX = 0
+GSN_SCORE_SIGMOID = 1
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with __graft_entry__.build() "
                       "(hipcc --offload-arch=gfx950); there is no fallback path")
@@ -120,8 +126,34 @@ class gsn_schedule_result(ctypes.Structure):
     ]
 
 
+class gsn_route_params(ctypes.Structure):
+    _fields_ = [
+        ("experts", ctypes.c_int32),
+        ("top", ctypes.c_int32),
+        ("score", ctypes.c_int32),
+        ("groups", ctypes.c_int32),
+        ("top_groups", ctypes.c_int32),
+        ("best", ctypes.c_int32),
+        ("renormalise", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class gsn_experts_params(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("experts", ctypes.c_int32),
+        ("top", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("hidden", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+    ]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
+_Z = ctypes.c_size_t
 _sig = {
     "gsn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(gsn_params)]),
     "gsn_create": (ctypes.c_int, [ctypes.POINTER(gsn_params), _P, ctypes.c_size_t, _I, _P, _P,
@@ -152,6 +184,23 @@ _sig = {
     "gsn_timing_read": (ctypes.c_int, [_P, _I, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(_I)]),
     "gsn_stat": (ctypes.c_int, [_P, _I, ctypes.POINTER(ctypes.c_int64), _P]),
+    "gsn_layer_norm": (ctypes.c_int, [_I, _I, _L, _I, _P, _L, _P, _P, ctypes.c_float, _P, _L,
+                                      _P, _P]),
+    "gsn_layer_norm_workspace_bytes": (_Z, [_L, _I]),
+    "gsn_layer_norm_backward": (ctypes.c_int, [_I, _I, _L, _I, _P, _L, _P, _L, _P, _P, _P, _L,
+                                               _P, _P, _P, _Z, _P]),
+    "gsn_route": (ctypes.c_int, [ctypes.POINTER(gsn_route_params), _I, _L, _P, _L, _P, _P, _P,
+                                 _P, _P]),
+    "gsn_route_backward": (ctypes.c_int, [ctypes.POINTER(gsn_route_params), _I, _L, _P, _P, _L,
+                                          _P, _P, _L, _P]),
+    "gsn_route_counts": (ctypes.c_int, [_L, _I, _P, _P, _P]),
+    "gsn_route_balance": (ctypes.c_int, [_I, _P, ctypes.c_float, _P, _P]),
+    "gsn_experts_workspace_bytes": (_Z, [ctypes.POINTER(gsn_experts_params), _I]),
+    "gsn_experts_saved_bytes": (_Z, [ctypes.POINTER(gsn_experts_params)]),
+    "gsn_experts": (ctypes.c_int, [ctypes.POINTER(gsn_experts_params), _P, _L, _P, _P, _P, _P,
+                                   _P, _P, _Z, _P, _Z, _P]),
+    "gsn_experts_backward": (ctypes.c_int, [ctypes.POINTER(gsn_experts_params), _P, _P, _L, _P,
+                                            _P, _P, _P, _Z, _P, _P, _P, _P, _P, _Z, _P]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -387,6 +436,187 @@ def gsn_stat(net, key: int, stream=None) -> int:
     v = ctypes.c_int64()
     _check(_lib.gsn_stat(net, key, ctypes.byref(v), _stream(stream)), "gsn_stat")
     return v.value
+
+
+# ------------------------------------------- C-named calls: mixture of local experts ----
+# (paper_1503_08294_amd.mixture holds the calls on torch tensors that allocate their outputs.)
+
+_DTYPES = {torch.float32: GSN_F32, torch.bfloat16: GSN_BF16, torch.float16: GSN_F16}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _matrix(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
+    """(pointer, row stride) of a device matrix with contiguous rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{what} must be ({rows}, {cols}), got {tuple(t.shape)}")
+    row, col = t.stride()
+    if col != 1 and cols > 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    if rows <= 1:
+        row = cols  # (torch gives such a tensor any stride)
+    if row < cols:
+        raise ValueError(f"{what} must not have overlapping rows")
+    return t.data_ptr(), row
+
+
+def _flat(t: torch.Tensor | None, dtype, shape, what: str):
+    """Pointer of a contiguous device tensor of this shape, None for None."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return t.data_ptr()
+
+
+def _params_type(x_dtype, weight, bias) -> torch.dtype:
+    got = {t.dtype for t in (weight, bias) if t is not None}
+    if len(got) > 1:
+        raise ValueError("weight and bias must be of the same type")
+    return got.pop() if got else x_dtype
+
+
+def gsn_layer_norm(x, weight, bias, eps: float, y, stats=None, stream=None):
+    """x, y: (rows, dim); weight, bias: (dim,) or None; stats: (2, rows) float32 or None."""
+    code = _type(x, "x")
+    rows, dim = x.shape
+    xp, xs = _matrix(x, x.dtype, rows, dim, "x")
+    yp, ys = _matrix(y, x.dtype, rows, dim, "y")
+    pt = _params_type(x.dtype, weight, bias)
+    return _check(_lib.gsn_layer_norm(
+        code, _DTYPES.get(pt, -1), rows, dim, xp, xs, _flat(weight, pt, (dim,), "weight"),
+        _flat(bias, pt, (dim,), "bias"), eps, yp, ys,
+        _flat(stats, torch.float32, (2, rows), "stats"), _stream(stream)), "gsn_layer_norm")
+
+
+def gsn_layer_norm_workspace_bytes(rows: int, dim: int) -> int:
+    return int(_lib.gsn_layer_norm_workspace_bytes(rows, dim))
+
+
+def gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, workspace, stream=None):
+    """Gradients of gsn_layer_norm; dx, dweight and dbias may be None."""
+    code = _type(x, "x")
+    rows, dim = x.shape
+    dyp, dys = _matrix(dy, x.dtype, rows, dim, "dy")
+    xp, xs = _matrix(x, x.dtype, rows, dim, "x")
+    dxp, dxs = (None, dim) if dx is None else _matrix(dx, x.dtype, rows, dim, "dx")
+    pt = _params_type(x.dtype, weight if weight is not None else dweight, dbias)
+    return _check(_lib.gsn_layer_norm_backward(
+        code, _DTYPES.get(pt, -1), rows, dim, dyp, dys, xp, xs,
+        _flat(weight, pt, (dim,), "weight"), _flat(stats, torch.float32, (2, rows), "stats"),
+        dxp, dxs, _flat(dweight, pt, (dim,), "dweight"), _flat(dbias, pt, (dim,), "dbias"),
+        _dev(workspace, torch.uint8), 0 if workspace is None else workspace.numel(),
+        _stream(stream)), "gsn_layer_norm_backward")
+
+
+def make_route(experts: int, top: int, score="softmax", groups=1, top_groups=1, best=1,
+               renormalise=True, scale=1.0) -> gsn_route_params:
+    codes = {"softmax": GSN_SCORE_SOFTMAX, "sigmoid": GSN_SCORE_SIGMOID}
+    if score not in codes:
+        raise ValueError(f"score must be 'softmax' or 'sigmoid', got {score!r}")
+    return gsn_route_params(experts, top, codes[score], groups, top_groups, best,
+                            1 if renormalise else 0, scale)
+
+
+def gsn_route(params: gsn_route_params, logits, balance, valid, ids, weights, stream=None):
+    """logits: (tokens, experts); balance: (experts,) float32 or None; valid: (tokens,) uint8 or
+    None; ids, weights: (tokens, top)."""
+    tokens = logits.shape[0]
+    lp, ls = _matrix(logits, logits.dtype, tokens, params.experts, "logits")
+    return _check(_lib.gsn_route(
+        params, _type(logits, "logits"), tokens, lp, ls,
+        _flat(balance, torch.float32, (params.experts,), "balance"),
+        _flat(valid, torch.uint8, (tokens,), "valid"),
+        _flat(ids, torch.int32, (tokens, params.top), "ids"),
+        _flat(weights, torch.float32, (tokens, params.top), "weights"), _stream(stream)),
+        "gsn_route")
+
+
+def gsn_route_backward(params: gsn_route_params, dweights, logits, ids, dlogits, stream=None):
+    tokens = logits.shape[0]
+    lp, ls = _matrix(logits, logits.dtype, tokens, params.experts, "logits")
+    dp, ds = _matrix(dlogits, logits.dtype, tokens, params.experts, "dlogits")
+    return _check(_lib.gsn_route_backward(
+        params, _type(logits, "logits"), tokens,
+        _flat(dweights, torch.float32, (tokens, params.top), "dweights"), lp, ls,
+        _flat(ids, torch.int32, (tokens, params.top), "ids"), dp, ds, _stream(stream)),
+        "gsn_route_backward")
+
+
+def gsn_route_counts(ids, counts, stream=None):
+    return _check(_lib.gsn_route_counts(
+        ids.numel(), counts.numel(), _dev(ids, torch.int32, what="ids"),
+        _dev(counts, torch.int32, what="counts"), _stream(stream)), "gsn_route_counts")
+
+
+def gsn_route_balance(counts, rate: float, balance, stream=None):
+    return _check(_lib.gsn_route_balance(
+        counts.numel(), _dev(counts, torch.int32, what="counts"), rate,
+        _dev(balance, torch.float32, counts.numel(), "balance"), _stream(stream)),
+        "gsn_route_balance")
+
+
+def make_experts(x, ids, w1, w2) -> gsn_experts_params:
+    """Parameters of the experts' products of these tensors."""
+    code = _type(x, "x")
+    if w1.dim() != 3 or w2.dim() != 3 or ids.dim() != 2:
+        raise ValueError("w1 and w2 must be 3-dimensional, ids 2-dimensional")
+    return gsn_experts_params(code, w2.shape[0], ids.shape[1], x.shape[1], w2.shape[2],
+                              x.shape[0])
+
+
+def gsn_experts_workspace_bytes(params: gsn_experts_params, backward: bool) -> int:
+    return int(_lib.gsn_experts_workspace_bytes(params, 1 if backward else 0))
+
+
+def gsn_experts_saved_bytes(params: gsn_experts_params) -> int:
+    return int(_lib.gsn_experts_saved_bytes(params))
+
+
+def gsn_experts(params: gsn_experts_params, x, ids, weights, w1, w2, out, saved, workspace,
+                stream=None):
+    p = params
+    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    pairs = (p.tokens, p.top)
+    return _check(_lib.gsn_experts(
+        p, xp, xs, _flat(ids, torch.int32, pairs, "ids"),
+        _flat(weights, torch.float32, pairs, "weights"),
+        _flat(w1, x.dtype, (p.experts, 2 * p.hidden, p.dim), "w1"),
+        _flat(w2, x.dtype, (p.experts, p.dim, p.hidden), "w2"),
+        _flat(out, x.dtype, (p.tokens, p.dim), "out"), _dev(saved, torch.uint8, what="saved"),
+        0 if saved is None else saved.numel(), _dev(workspace, torch.uint8, what="workspace"),
+        workspace.numel(), _stream(stream)), "gsn_experts")
+
+
+def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, saved, dx,
+                         dweights, dw1, dw2, workspace, stream=None):
+    p = params
+    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    pairs = (p.tokens, p.top)
+    s1, s2 = (p.experts, 2 * p.hidden, p.dim), (p.experts, p.dim, p.hidden)
+    return _check(_lib.gsn_experts_backward(
+        p, _flat(dout, x.dtype, (p.tokens, p.dim), "dout"), xp, xs,
+        _flat(weights, torch.float32, pairs, "weights"), _flat(w1, x.dtype, s1, "w1"),
+        _flat(w2, x.dtype, s2, "w2"), _dev(saved, torch.uint8, what="saved"), saved.numel(),
+        _flat(dx, x.dtype, (p.tokens, p.dim), "dx"),
+        _flat(dweights, torch.float32, pairs, "dweights"), _flat(dw1, x.dtype, s1, "dw1"),
+        _flat(dw2, x.dtype, s2, "dw2"), _dev(workspace, torch.uint8, what="workspace"),
+        workspace.numel(), _stream(stream)), "gsn_experts_backward")
 
 
 # ------------------------------------------------------------------ convenience ----

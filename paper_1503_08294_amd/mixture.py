@@ -1,0 +1,220 @@
+"""Local experts on torch tensors: layer norm, routing of tokens to experts, and the experts'
+products, through the C calls of ``include/gsn.h``.
+
+A network of units answers with the nearest units of a signal; a mixture of local experts
+answers with what the models of its best units say about it.  ``route`` picks every token's
+experts (of the negative squared distances to the units with ``top=2``: the winner and the
+second of ``Network.find_winners``), ``experts`` runs their products, ``layer_norm`` goes before
+them.  ``layer_norm``, ``route`` and ``experts`` take part in autograd; the ``_forward`` and
+``_backward`` calls are their two halves for programs that keep their own order.
+
+Tensors are on one HIP device; work goes to torch's current stream, where the outputs and
+workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import gsn
+
+
+def _same_device(x, **others):
+    for name, t in others.items():
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, not on {x.device}")
+
+
+def _rows(x: torch.Tensor, what: str) -> torch.Tensor:
+    if x.dim() != 2:
+        raise ValueError(f"{what} must be 2-dimensional, got {tuple(x.shape)}")
+    return x
+
+
+def _bytes(n: int, x: torch.Tensor) -> torch.Tensor:
+    # torch's allocator aligns to 512 bytes
+    return torch.empty(n, dtype=torch.uint8, device=x.device)
+
+
+# ----------------------------------------------------------------------- layer norm ----
+
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
+    """(y, stats): the norm of every row of x (rows, dim) and what its backward pass takes."""
+    _rows(x, "x")
+    _same_device(x, weight=weight, bias=bias)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device)
+    gsn.gsn_layer_norm(x, weight, bias, eps, y, stats)
+    return y, stats
+
+
+def layer_norm_backward(dy, x, weight, bias, stats, need=(True, True, True)):
+    """(dx, dweight, dbias) from dy; None for what is not needed or has no parameter."""
+    _rows(x, "x")
+    _same_device(x, dy=dy, weight=weight, bias=bias, stats=stats)
+    rows, dim = x.shape
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
+    dweight = torch.empty_like(weight) if need[1] and weight is not None else None
+    dbias = torch.empty_like(bias) if need[2] and bias is not None else None
+    ws = None
+    if dweight is not None or dbias is not None:
+        ws = _bytes(gsn.gsn_layer_norm_workspace_bytes(rows, dim), x)
+    gsn.gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, ws)
+    return dx, dweight, dbias
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, stats = layer_norm_forward(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, bias, stats)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, bias, stats = ctx.saved_tensors
+        if dy.stride(-1) != 1 or (dy.shape[0] > 1 and dy.stride(0) < dy.shape[1]):
+            dy = dy.contiguous()  # (an expanded gradient, as that of a sum)
+        return (*layer_norm_backward(dy, x, weight, bias, stats, ctx.needs_input_grad), None)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last dimension of x (rows, dim).  weight and bias: (dim,), float32 or
+    of x's type, or None.  Rows may be those of a wider tensor (any row stride)."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad
+                                       for t in (x, weight, bias)):
+        return _LayerNorm.apply(x, weight, bias, eps)
+    _rows(x, "x")
+    _same_device(x, weight=weight, bias=bias)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    gsn.gsn_layer_norm(x, weight, bias, eps, y)
+    return y
+
+
+# -------------------------------------------------------------------------- routing ----
+
+def _route(logits, params, balance, valid):
+    _same_device(logits, balance=balance, valid=valid)
+    tokens = logits.shape[0]
+    ids = torch.empty((tokens, params.top), dtype=torch.int32, device=logits.device)
+    weights = torch.empty((tokens, params.top), dtype=torch.float32, device=logits.device)
+    gsn.gsn_route(params, logits, balance, valid, ids, weights)
+    return ids, weights
+
+
+def _route_backward(dweights, logits, ids, params):
+    _same_device(logits, dweights=dweights, ids=ids)
+    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    gsn.gsn_route_backward(params, dweights, logits, ids, dlogits)
+    return dlogits
+
+
+class _Route(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, params, balance, valid):
+        ids, weights = _route(logits, params, balance, valid)
+        ctx.params = params
+        ctx.save_for_backward(logits, ids)
+        ctx.mark_non_differentiable(ids)
+        return ids, weights
+
+    @staticmethod
+    def backward(ctx, _, dweights):
+        logits, ids = ctx.saved_tensors
+        return _route_backward(dweights.contiguous(), logits, ids, ctx.params), None, None, None
+
+
+def route(logits, top, *, score="softmax", balance=None, groups=1, top_groups=1, best=1,
+          renormalise=True, scale=1.0, valid=None):
+    """(ids, weights), each (tokens, top): the best experts of every token, by descending order,
+    and their weights; see gsn_route in include/gsn.h for the order, masks and ties.  The weights
+    are differentiable with respect to the logits."""
+    _rows(logits, "logits")
+    params = gsn.make_route(logits.shape[1], top, score, groups, top_groups, best, renormalise,
+                            scale)
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return _Route.apply(logits, params, balance, valid)
+    return _route(logits, params, balance, valid)
+
+
+def route_backward(dweights, logits, ids, *, score="softmax", groups=1, top_groups=1, best=1,
+                   renormalise=True, scale=1.0):
+    """dlogits of ``route`` with the same options (those of the choice alone do not matter)."""
+    _rows(logits, "logits")
+    params = gsn.make_route(logits.shape[1], ids.shape[1], score, groups, top_groups, best,
+                            renormalise, scale)
+    return _route_backward(dweights, logits, ids, params)
+
+
+def route_counts(ids, experts):
+    """Pairs of each expert, int32 (experts,)."""
+    counts = torch.empty(experts, dtype=torch.int32, device=ids.device)
+    gsn.gsn_route_counts(ids, counts)
+    return counts
+
+
+def route_balance(counts, balance, rate=1e-3):
+    """Moves balance in place by rate towards the experts with fewer pairs than the mean."""
+    gsn.gsn_route_balance(counts, rate, balance)
+    return balance
+
+
+# ------------------------------------------------------------------- experts' products ----
+
+def _experts_forward(x, ids, weights, w1, w2, save):
+    _rows(x, "x")
+    _same_device(x, ids=ids, weights=weights, w1=w1, w2=w2)
+    p = gsn.make_experts(x, ids, w1, w2)
+    size = gsn.gsn_experts_workspace_bytes(p, False)
+    if size == 0:
+        raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    saved = _bytes(gsn.gsn_experts_saved_bytes(p), x) if save else None
+    gsn.gsn_experts(p, x, ids, weights, w1, w2, out, saved, _bytes(size, x))
+    return out, saved
+
+
+def experts_forward(x, ids, weights, w1, w2):
+    """(out, saved): the experts' products and what their backward pass takes."""
+    return _experts_forward(x, ids, weights, w1, w2, True)
+
+
+def experts_backward(dout, x, ids, weights, w1, w2, saved, need=(True, True, True, True)):
+    """(dx, dweights, dw1, dw2) from dout; None for what is not needed."""
+    _rows(x, "x")
+    _same_device(x, dout=dout, ids=ids, weights=weights, w1=w1, w2=w2, saved=saved)
+    p = gsn.make_experts(x, ids, w1, w2)
+    size = gsn.gsn_experts_workspace_bytes(p, True)
+    if size == 0:
+        raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
+    dx, dweights, dw1, dw2 = (
+        torch.empty(t.shape, dtype=t.dtype, device=x.device) if n else None
+        for t, n in zip((x, weights, w1, w2), need))
+    gsn.gsn_experts_backward(p, dout, x, weights, w1, w2, saved, dx, dweights, dw1, dw2,
+                             _bytes(size, x))
+    return dx, dweights, dw1, dw2
+
+
+class _Experts(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, ids, weights, w1, w2):
+        out, saved = experts_forward(x, ids, weights, w1, w2)
+        ctx.save_for_backward(x, ids, weights, w1, w2, saved)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        x, ids, weights, w1, w2, saved = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dweights, dw1, dw2 = experts_backward(dout.contiguous(), x, ids, weights, w1, w2,
+                                                  saved, (need[0], *need[2:5]))
+        return dx, None, dweights, dw1, dw2
+
+
+def experts(x, ids, weights, w1, w2):
+    """out[t] = sum_k weights[t, k] * w2[e] (silu(gate) * up), (gate, up) = w1[e] x[t] and
+    e = ids[t, k].  x (tokens, dim), ids int32 and weights float32 (tokens, top), w1 (experts,
+    2 * hidden, dim) with the gate's rows first, w2 (experts, dim, hidden).  A pair whose id is
+    not an expert's adds nothing."""
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, weights, w1, w2)):
+        return _Experts.apply(x, ids, weights, w1, w2)
+    return _experts_forward(x, ids, weights, w1, w2, False)[0]

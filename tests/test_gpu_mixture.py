@@ -1,0 +1,587 @@
+"""The mixture's operators on the GPU against their 64-bit definitions: types, odd sizes,
+strides, masks, empty experts and rows, gradients against the formulas and against differences,
+other streams, recorded graphs."""
+import numpy as np
+import pytest
+import torch
+
+import mixture_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+
+
+@pytest.fixture(scope="module")
+def mix():
+    from paper_1503_08294_amd import mixture
+    return mixture
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(*shape, seed, dtype=F32, scale=1.0):
+    return (torch.randn(shape, generator=gen(seed)) * scale).to(dtype)
+
+
+def close(got, want, tol, what):
+    """|got - want| <= tol elementwise, no NaN."""
+    got = got.detach().double().cpu()
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    over = ((got - want).abs() - tol).max().item() if got.numel() else 0.0
+    assert over <= 0, f"{what}: {over} beyond the tolerance"
+
+
+def near(got, want, rel, what):
+    """Norm of the difference at most rel of the norm of want; every element within 16 rel of
+    the larger of itself and the root mean square (rounding errors of random data)."""
+    got = got.detach().double().cpu()
+    assert got.shape == want.shape, what
+    assert torch.isfinite(got).all(), f"{what}: not finite"
+    if not want.numel():
+        return
+    norm = want.norm().item()
+    d = (got - want)
+    assert d.norm().item() <= rel * norm, f"{what}: {d.norm().item() / max(norm, 1e-300)}"
+    size = want.abs().clamp(min=norm / want.numel() ** 0.5)
+    assert (d.abs() <= 16 * rel * size).all(), f"{what}: {(d.abs() / size).max().item()}"
+
+
+# -------------------------------------------------------------------------- layer norm ----
+
+def norm_tolerance(x, w, b, eps, dtype, y):
+    """One rounding of the result, and binary32 sums of D terms taken at most D / 64 at a time by
+    a lane and then joined in six or eight steps: errors of (D / 64 + 16) units of 2^-24 in the
+    mean, relative to the mean size of x, and in r and the products, relative to the value."""
+    u = (x.shape[1] / 64 + 16) * 2.0 ** -24
+    x = x.double()
+    r = 1 / torch.sqrt(x.var(1, correction=0, keepdim=True) + eps)
+    n = (x - x.mean(1, keepdim=True)) * r
+    wd = 1.0 if w is None else w.double().abs()
+    bd = 0.0 if b is None else b.double().abs()
+    return ref.HALF_ULP[dtype] * y.abs() + u * ((n.abs() + x.abs().mean(1, keepdim=True) * r)
+                                                * wd + bd) + 2.0 ** -25 * (dtype == F16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,dim", [(1, 1), (3, 1), (5, 2), (4, 63), (7, 64), (2, 65), (9, 500),
+                                      (5, 1001), (6, 1024), (3, 1025), (2, 2048), (3, 2056),
+                                      (2, 4096), (2, 8192), (1, 8200), (2, 20_003), (1, 70_000)])
+def test_norm_forward_and_backward(mix, dtype, rows, dim):
+    x = randn(rows, dim, seed=1, dtype=dtype, scale=2.0) + 0.5
+    for w_type in {F32, dtype}:
+        w = (1 + 0.2 * randn(dim, seed=2)).to(w_type)
+        b = randn(dim, seed=3, dtype=w_type)
+        dy = randn(rows, dim, seed=4, dtype=dtype)
+        y, stats = mix.layer_norm_forward(x.cuda(), w.cuda(), b.cuda(), 1e-5)
+        want, dx, dw, db = ref.layer_norm(x, w, b, 1e-5, dy)
+        close(y, want, norm_tolerance(x, w, b, 1e-5, dtype, want), "y")
+        got = mix.layer_norm_backward(dy.cuda(), x.cuda(), w.cuda(), b.cuda(), stats)
+        # sums of D (or of rows) products in binary32, one rounding of the result; a width of one
+        # or two has gradients that cancel to about nothing: absolute, in units of dy w r
+        u = ref.HALF_ULP[dtype]
+        r = 1 / torch.sqrt(x.double().var(1, correction=0, keepdim=True) + 1e-5)
+        n = (x.double() - x.double().mean(1, keepdim=True)) * r
+        g = dy.double().abs() * w.double().abs()
+        size = r * (g + g.mean(1, keepdim=True)
+                    + n.abs() * (g * n.abs()).mean(1, keepdim=True))
+        f = (dim / 64 + 24) * 2.0 ** -24
+        # (an error in the mean, of f mean|x|, shifts every n by r times that)
+        shift = f * x.double().abs().mean(1, keepdim=True) * r
+        close(got[0], dx, u * dx.abs() + f * size + shift * 3 * size + 2.0 ** -25 * (dtype == F16),
+              "dx")
+        f = (rows + 16) * 2.0 ** -24
+        uw = ref.HALF_ULP[w_type]
+        ny = (dy.double().abs() * (n.abs() * (f + (dim / 64 + 16) * 2.0 ** -24) + shift)).sum(0)
+        close(got[1], dw, uw * dw.abs() + ny + 2.0 ** -25 * (w_type == F16), "dweight")
+        close(got[2], db, uw * db.abs() + f * dy.double().abs().sum(0)
+              + 2.0 ** -25 * (w_type == F16), "dbias")
+
+
+@pytest.mark.parametrize("rows,dim", [(3000, 96), (70_001, 8), (1025, 1000)])
+def test_norm_many_rows(mix, rows, dim):
+    x, dy = randn(rows, dim, seed=5) + 1.0, randn(rows, dim, seed=6)
+    w, b = 1 + 0.1 * randn(dim, seed=7), randn(dim, seed=8)
+    y, stats = mix.layer_norm_forward(x.cuda(), w.cuda(), b.cuda(), 1e-5)
+    want, dx, dw, db = ref.layer_norm(x, w, b, 1e-5, dy)
+    got = mix.layer_norm_backward(dy.cuda(), x.cuda(), w.cuda(), b.cuda(), stats)
+    # root-sum-square growth of binary32 rounding over the rows, 8 for the safe side
+    rel = 8 * max(rows, dim) ** 0.5 * 2.0 ** -24
+    for g, v, name in zip((y, *got), (want, dx, dw, db), ("y", "dx", "dweight", "dbias")):
+        near(g, v, rel, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,pad", [(64, 3), (1000, 8), (2048, 64), (4096, 1), (33, 31)])
+def test_norm_strides_and_missing_parameters(mix, dtype, dim, pad):
+    wide = randn(6, dim + pad, seed=9, dtype=dtype)
+    wide[:, dim:] = float("nan")  # what is beside a row is not its own
+    x = wide[:, :dim]
+    out = torch.full((6, dim + pad), 7.0, dtype=dtype, device="cuda")
+    from paper_1503_08294_amd import gsn
+    w = randn(dim, seed=10)
+    for weight, bias in ((None, None), (w, None), (None, w)):
+        gw, gb = (None if t is None else t.cuda() for t in (weight, bias))
+        gsn.gsn_layer_norm(wide.cuda()[:, :dim], gw, gb, 1e-5, out[:, :dim])
+        want = ref.layer_norm(x, weight, bias, 1e-5)
+        close(out[:, :dim], want, norm_tolerance(x, weight, bias, 1e-5, dtype, want), "y")
+        assert (out[:, dim:] == 7.0).all()
+    # parts that start at any element
+    flat = randn(5 * dim + 3, seed=11, dtype=dtype).cuda()
+    x = flat[3:].view(5, dim)
+    want = ref.layer_norm(x.cpu(), None, None, 1e-5)
+    close(mix.layer_norm(x), want, norm_tolerance(x.cpu(), None, None, 1e-5, dtype, want), "y")
+
+
+def test_norm_in_place_empty_and_large_values(mix):
+    from paper_1503_08294_amd import gsn
+    x = randn(5, 300, seed=12, scale=1e15).cuda() + 1e16  # squares beyond 2^100
+    want = ref.layer_norm(x.cpu(), None, None, 1e-5)
+    tol = norm_tolerance(x.cpu(), None, None, 1e-5, F32, want)
+    gsn.gsn_layer_norm(x, None, None, 1e-5, x)
+    close(x, want, tol, "y")
+    empty = torch.empty((0, 64), device="cuda")
+    w = torch.ones(64, device="cuda")
+    y, stats = mix.layer_norm_forward(empty, w, w)
+    assert y.shape == (0, 64)
+    dx, dw, db = mix.layer_norm_backward(empty, empty, w, w, stats)
+    assert dx.shape == (0, 64) and not dw.any() and not db.any()
+    const = torch.full((3, 70), 4.0, device="cuda")
+    assert not mix.layer_norm(const).any()
+    # a row that holds NaN or inf spoils itself alone
+    bad = randn(4, 128, seed=13).cuda()
+    bad[1, 5] = float("nan")
+    bad[2, 7] = float("inf")
+    y = mix.layer_norm(bad)
+    assert torch.isnan(y[1]).all() and torch.isnan(y[2]).any()
+    assert torch.isfinite(y[0]).all() and torch.isfinite(y[3]).all()
+
+
+def test_norm_gradient_against_differences(mix):
+    x = randn(4, 24, seed=14).double()
+    w, b, dy = (randn(*s, seed=15 + i).double() for i, s in enumerate(((24,), (24,), (4, 24))))
+    t = [v.float().cuda().requires_grad_() for v in (x, w, b)]
+    mix.layer_norm(*t, 1e-5).backward(dy.float().cuda())
+    h = 1e-5
+    base = [x.float().double(), w.float().double(), b.float().double()]
+    for i, name in enumerate(("dx", "dweight", "dbias")):
+        got = t[i].grad.double().cpu().flatten()
+        for j in range(0, got.numel(), 5):
+            lo, hi = [v.clone() for v in base], [v.clone() for v in base]
+            lo[i].view(-1)[j] -= h
+            hi[i].view(-1)[j] += h
+            d = ((ref.layer_norm(*hi, 1e-5) - ref.layer_norm(*lo, 1e-5)) * dy).sum() / (2 * h)
+            # differences: h^2 and 1e-16 / h; binary32 sums of 24 terms of size one
+            assert abs(got[j] - d) < 1e-5 * (1 + abs(d)), (name, j)
+
+
+# ---------------------------------------------------------------------------- routing ----
+
+def route_case(mix, logits, k, score="softmax", balance=None, groups=1, top_groups=1, best=1,
+               renorm=True, scale=1.0, valid=None, logits_gpu=None):
+    ids, w = mix.route(logits.cuda() if logits_gpu is None else logits_gpu, k, score=score,
+                       balance=None if balance is None else balance.cuda(), groups=groups,
+                       top_groups=top_groups, best=best, renormalise=renorm, scale=scale,
+                       valid=None if valid is None else valid.cuda())
+    ids, w = ids.cpu(), w.cpu()
+    bal = None if balance is None else balance.double().numpy()
+    for t in range(logits.shape[0]):
+        want_i, want_w = ref.route_token(logits[t].double().numpy(), k, score, bal, groups,
+                                         top_groups, best, renorm, scale,
+                                         valid is None or bool(valid[t]))
+        assert ids[t].tolist() == want_i, (t, ids[t].tolist(), want_i)
+        # exponentials of arguments up to 30 (2 + 30 units in the last place), sums of at most
+        # 1,024 terms (16 a lane, then six steps), a division: under 64 units of 2^-24
+        np.testing.assert_allclose(w[t].double().numpy(), want_w, rtol=64 * 2.0 ** -24,
+                                   atol=1e-36)
+    return ids, w
+
+
+def apart(rows, experts, seed, dtype=F32):
+    """Logits whose scores, plus a bias that is a multiple of a thousandth, are never nearer than
+    32 bits resolve: a permutation of well separated values in each row."""
+    g = gen(seed)
+    return torch.stack([(torch.randperm(experts, generator=g).float() / experts * 6 - 3)
+                        for _ in range(rows)]).to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("experts,k", [(1, 1), (2, 2), (3, 1), (8, 2), (63, 5), (64, 8), (65, 6),
+                                       (100, 10), (128, 64), (255, 3), (256, 8), (257, 8),
+                                       (384, 6), (512, 1), (1000, 40), (1024, 64)])
+def test_route_choice_and_weights(mix, dtype, experts, k):
+    logits = randn(9, experts, seed=20, dtype=dtype, scale=2.0)
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            route_case(mix, logits, k, score, renorm=renorm, scale=1.5)
+
+
+@pytest.mark.parametrize("experts,groups,top_groups,k", [(8, 4, 2, 3), (16, 8, 1, 2),
+                                                         (64, 8, 4, 6), (100, 4, 2, 8),
+                                                         (256, 8, 4, 8), (320, 64, 7, 9),
+                                                         (1024, 16, 3, 64)])
+@pytest.mark.parametrize("best", [1, 2])
+def test_route_groups_and_balance(mix, experts, groups, top_groups, k, best):
+    logits = apart(5, experts, 21)
+    # (a bias apart from every difference of two scores: irrational steps)
+    balance = torch.tensor([(i * 0.0137) % 0.2 for i in range(experts)])
+    for score in ("softmax", "sigmoid"):
+        for b in (None, balance):
+            if score == "softmax" and b is not None and experts > 300:
+                continue  # scores of 1 / 1,024: the bias alone would order them
+            route_case(mix, logits, k, score, b, groups, top_groups, best, scale=2.5)
+
+
+def test_route_ties_go_to_the_lowest_index(mix):
+    logits = torch.zeros(3, 256)
+    logits[1, 200:] = 1.0
+    logits[2] = torch.arange(256) % 4
+    logits[2, 0] = -0.0
+    for score in ("softmax", "sigmoid"):
+        ids, _ = route_case(mix, logits, 8, score)
+        assert ids[0].tolist() == list(range(8))
+        route_case(mix, logits, 8, score, groups=8, top_groups=2, best=2)
+        route_case(mix, logits, 8, score, balance=torch.zeros(256), groups=8, top_groups=2)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("experts", [4, 64, 200, 600])
+def test_route_masks_and_extreme_logits(mix, dtype, experts):
+    inf, low = float("inf"), torch.finfo(dtype).min
+    logits = randn(12, experts, seed=22, dtype=dtype)
+    logits[0] = -inf
+    logits[1] = float("nan")
+    logits[2, 1:] = -inf                      # one expert left
+    logits[3] = low                           # a mask of the type's lowest value: all equal
+    logits[4, :3] = low
+    logits[5, 2] = inf
+    logits[6, 1], logits[6, 3] = inf, float("nan")
+    logits[7] = float("nan")
+    valid = torch.ones(12, dtype=torch.uint8)
+    valid[7:9] = 0
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            ids, w = route_case(mix, logits, 3, score, renorm=renorm, valid=valid)
+            for t in (0, 1, 7, 8):
+                assert (ids[t] == -1).all() and not w[t].any()
+    shut = torch.zeros(experts)
+    shut[::2] = -inf
+    ids, _ = mix.route(logits.cuda(), 2, balance=shut.cuda(), valid=valid.cuda())
+    assert not ((ids >= 0) & (ids % 2 == 0)).any()
+    ids, w = route_case(mix, torch.full((2, experts), -95.0), 3, "sigmoid")
+    assert torch.allclose(w, torch.full_like(w, 1 / 3))
+
+
+@pytest.mark.parametrize("tokens", [0, 1, 2, 5, 1000])
+def test_route_rows_and_strides(mix, tokens):
+    wide = randn(tokens, 70, seed=23)
+    wide[:, 48:] = 50.0
+    gpu = wide.cuda()[:, :48]
+    ids, w = route_case(mix, wide[:, :48], 4, logits_gpu=gpu)
+    counts = mix.route_counts(ids.cuda(), 48).cpu()
+    assert counts.tolist() == torch.bincount(ids.flatten().long(), minlength=48).tolist()
+
+
+def test_route_counts_and_balance(mix):
+    ids = torch.randint(-1, 10, (40_000, 3), generator=gen(24), dtype=torch.int32)
+    ids[5] = 17  # no expert: not counted
+    counts = mix.route_counts(ids.cuda(), 10)
+    want = torch.bincount(ids[(ids >= 0) & (ids < 10)].long(), minlength=10)
+    assert counts.cpu().tolist() == want.tolist()
+    counts = torch.tensor([4, 2, 3, 3], dtype=torch.int32, device="cuda")
+    balance = torch.zeros(4, device="cuda")
+    mix.route_balance(counts, balance, 0.25)
+    assert balance.tolist() == [-0.25, 0.25, 0.0, 0.0]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("experts,k", [(3, 2), (64, 2), (100, 8), (256, 8), (700, 5)])
+def test_route_gradient(mix, dtype, score, renorm, experts, k):
+    logits = randn(17, experts, seed=25, dtype=dtype, scale=1.5)
+    logits[3, 1:] = -float("inf")
+    logits[4] = float("nan")
+    logits[5, 2] = float("nan")
+    kw = dict(score=score, renormalise=renorm, scale=1.7)
+    g = logits.cuda().requires_grad_()
+    ids, w = mix.route(g, k, **kw)
+    dw = randn(17, k, seed=26)
+    w.backward(dw.cuda())
+    l = logits.double().nan_to_num(nan=-1e4, neginf=-1e4).requires_grad_()
+    ref.route_weights(l, ids.cpu().long(), score, renorm, 1.7).backward(dw.double())
+    # a few exponentials and sums in binary32, relative to the largest term of the row's
+    # gradient; one rounding of the result
+    size = 1.7 * dw.double().abs().max(1, keepdim=True)[0]
+    close(g.grad, l.grad, ref.HALF_ULP[dtype] * l.grad.abs() + 128 * 2.0 ** -24 * size
+          + 2.0 ** -25 * (dtype == F16), "dlogits")
+    with torch.no_grad():
+        out = mix.route_backward(dw.cuda(), logits.cuda(), ids, **kw)
+    assert torch.equal(out, g.grad)
+
+
+def test_route_gradient_against_differences(mix):
+    logits = randn(3, 12, seed=27)
+    dw = randn(3, 4, seed=28).double()
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            ids, _ = mix.route(logits.cuda(), 4, score=score, renormalise=renorm)
+            got = mix.route_backward(dw.float().cuda(), logits.cuda(), ids, score=score,
+                                     renormalise=renorm).cpu()
+            h = 1e-5
+            for j in range(36):
+                lo, hi = logits.double(), logits.double()
+                lo.view(-1)[j] -= h
+                hi.view(-1)[j] += h
+                d = ((ref.route_weights(hi, ids.cpu(), score, renorm, 1.0)
+                      - ref.route_weights(lo, ids.cpu(), score, renorm, 1.0)) * dw).sum() / (2 * h)
+                assert abs(got.view(-1)[j] - d) < 1e-5 * (1 + abs(d))
+
+
+def test_route_of_distances_finds_the_winners(mix):
+    """Routing of -d^2 with top 2 is the network's search: winner and second."""
+    from paper_1503_08294_amd import gsn
+    from paper_1503_08294_amd.clouds import torus_cloud
+    cloud = torus_cloud(4000, 3)
+    units = torch.from_numpy(np.ascontiguousarray(cloud[:300].T)).cuda()
+    sig = torch.from_numpy(np.ascontiguousarray(cloud[300:1300].T)).cuda()
+    net = gsn.Network(gsn.make_params(n_max=300, e_max=1200, m_max=1000), units)
+    winner, second, _, _ = net.find_winners(sig)
+    d = (sig[:, :, None] - units[:, None, :])
+    d2 = (d[0] * d[0] + d[1] * d[1]) + d[2] * d[2]
+    ids, _ = mix.route(-d2, 2)
+    assert torch.equal(ids[:, 0], winner) and torch.equal(ids[:, 1], second)
+
+
+# ------------------------------------------------------------------- experts' products ----
+
+def expert_inputs(dtype, tokens, experts, k, dim, hidden, seed, empty=True):
+    g = gen(seed)
+    x = (torch.randn(tokens, dim, generator=g)).to(dtype)
+    w1 = (torch.randn(experts, 2 * hidden, dim, generator=g) / dim ** 0.5).to(dtype)
+    w2 = (torch.randn(experts, dim, hidden, generator=g) / hidden ** 0.5).to(dtype)
+    # (an expert in the middle, and the last, stay without tokens)
+    rank = torch.rand(tokens, experts, generator=g)
+    if empty and experts > k + 1:
+        rank[:, experts // 2] = 2.0
+        rank[:, -1] = 2.0
+    ids = rank.argsort(1)[:, :k].to(torch.int32).contiguous()
+    weights = torch.rand(tokens, k, generator=g) + 0.1
+    dout = torch.randn(tokens, dim, generator=g).to(dtype)
+    return x, ids, weights, w1, w2, dout
+
+
+def expert_tolerance(dtype, dim, hidden, rows):
+    """Norm-wise: one rounding of the intermediate and one of the result (each at most HALF_ULP,
+    0.4 of it in the mean square; two of them, added), and binary32 sums of the longest product's
+    n terms, whose errors grow as sqrt(n) 2^-24, times 4 for the chain of three products."""
+    n = max(dim, 2 * hidden, rows, 16)
+    return (2 * ref.HALF_ULP[dtype] if dtype != F32 else 0.0) + 4 * n ** 0.5 * 2.0 ** -24
+
+
+def check_experts(mix, dtype, x, ids, weights, w1, w2, dout, what="", xg=None):
+    names = ("out", "dx", "dweights", "dw1", "dw2")
+    xd, wd, w1d, w2d = (t.double().requires_grad_() for t in (x, weights, w1, w2))
+    want = ref.experts(xd, ids, wd, w1d, w2d)
+    want.backward(dout.double()) if want.requires_grad else None
+    zero = [torch.zeros_like(t) if t.grad is None else t.grad for t in (xd, wd, w1d, w2d)]
+    a = [(x.cuda() if xg is None else xg), ids.cuda(), weights.cuda(), w1.cuda(), w2.cuda()]
+    plain = mix.experts(*a)
+    out, saved = mix.experts_forward(*a)
+    got = mix.experts_backward(dout.cuda(), *a, saved)
+    rel = expert_tolerance(dtype, x.shape[1], w2.shape[2], x.shape[0])
+    near(plain, want.detach(), rel, what + " out without a backward pass")
+    for g, v, name in zip((out, *got), (want.detach(), *zero), names):
+        near(g, v, rel, f"{what} {name}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (1, 1, 1, 1, 1), (1, 4, 2, 64, 64), (2, 3, 3, 5, 7), (3, 8, 2, 33, 17), (17, 5, 2, 100, 36),
+    (40, 6, 3, 72, 130), (130, 4, 2, 129, 65), (64, 64, 8, 64, 128), (300, 3, 1, 136, 72),
+    (9, 16, 4, 264, 200), (33, 4, 2, 256, 128), (150, 2, 2, 64, 264)])
+def test_experts_forward_and_backward(mix, dtype, tokens, experts, k, dim, hidden):
+    a = expert_inputs(dtype, tokens, experts, k, dim, hidden, 30)
+    check_experts(mix, dtype, *a, what=f"{tokens} {experts} {k} {dim} {hidden}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,hidden", [(64, 64), (40, 24), (35, 9)])
+def test_experts_dropped_repeated_and_foreign_ids(mix, dtype, dim, hidden):
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, 50, 6, 3, dim, hidden, 31)
+    ids[4] = -1                 # no expert at all: its row of x is not read
+    x[4] = float("nan")
+    ids[7, 1] = -1
+    ids[9, 2] = 6               # not an expert
+    ids[10, 0] = -7
+    ids[11] = ids[11, 0]        # one expert three times
+    ids[12:30, 0] = 1
+    safe = x.clone()
+    safe[4] = 0.0
+    xg = x.cuda()
+    check_experts(mix, dtype, safe, ids, weights, w1, w2, dout, xg=xg)
+    # nobody has an expert
+    none = torch.full_like(ids, -1)
+    a = [t.cuda() for t in (x, none, weights, w1, w2)]
+    out, saved = mix.experts_forward(*a)
+    got = mix.experts_backward(dout.cuda(), *a, saved)
+    assert not out.any() and not any(g.any() for g in got)
+    assert not mix.experts(*a).any()
+
+
+def test_experts_rows_do_not_touch_each_other(mix):
+    """A token with NaN or inf spoils its own output alone, whatever shares its tile."""
+    for dtype in TYPES:
+        x, ids, weights, w1, w2, _ = expert_inputs(dtype, 40, 3, 2, 72, 40, 32)
+        good = mix.experts(*(t.cuda() for t in (x, ids, weights, w1, w2)))
+        x[13] = float("nan")
+        x[20, 3] = float("inf")
+        bad = mix.experts(*(t.cuda() for t in (x, ids, weights, w1, w2)))
+        rest = [t for t in range(40) if t not in (13, 20)]
+        assert torch.equal(bad[rest], good[rest])
+        assert torch.isnan(bad[13]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim,pad", [(64, 8), (64, 3), (50, 14)])
+def test_experts_strided_tokens(mix, dtype, dim, pad):
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, 45, 5, 2, dim, 32, 33)
+    wide = torch.full((45, dim + pad), float("nan"), dtype=dtype)
+    wide[:, :dim] = x
+    check_experts(mix, dtype, x, ids, weights, w1, w2, dout, xg=wide.cuda()[:, :dim])
+
+
+def test_experts_no_tokens(mix):
+    x, ids, weights, w1, w2, dout = expert_inputs(F32, 0, 4, 2, 24, 16, 34)
+    a = [t.cuda() for t in (x, ids, weights, w1, w2)]
+    out, saved = mix.experts_forward(*a)
+    assert out.shape == (0, 24) and mix.experts(*a).shape == (0, 24)
+    dx, dweights, dw1, dw2 = mix.experts_backward(dout.cuda(), *a, saved)
+    assert dx.shape == (0, 24) and dweights.shape == (0, 2)
+    assert not dw1.any() and not dw2.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (1500, 3, 2, 512, 320), (700, 2, 1, 384, 576), (2100, 16, 2, 264, 136), (777, 7, 3, 501, 333),
+    (900, 40, 4, 1024, 256)])
+def test_experts_larger_sizes(mix, dtype, tokens, experts, k, dim, hidden):
+    """Several tiles in every direction, against products in float64 on the GPU."""
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, tokens, experts, k, dim, hidden, 35)
+    ids[5] = -1
+    xg, ig, wg, w1g, w2g, dg = (t.cuda() for t in (x, ids, weights, w1, w2, dout))
+    xd, wd, w1d, w2d = (t.double().requires_grad_() for t in (xg, wg, w1g, w2g))
+    want = torch.zeros_like(xd)
+    for e in range(experts):
+        t, j = (ig == e).nonzero(as_tuple=True)
+        h = xd[t] @ w1d[e].t()
+        a = torch.nn.functional.silu(h[:, :hidden]) * h[:, hidden:]
+        want = want.index_add(0, t, (a @ w2d[e].t()) * wd[t, j][:, None])
+    want.backward(dg.double())
+    out, saved = mix.experts_forward(xg, ig, wg, w1g, w2g)
+    got = mix.experts_backward(dg, xg, ig, wg, w1g, w2g, saved)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    near(mix.experts(xg, ig, wg, w1g, w2g), want.detach().cpu(), rel, "out alone")
+    for g, v, name in zip((out, *got), (want, xd.grad, wd.grad, w1d.grad, w2d.grad),
+                          ("out", "dx", "dweights", "dw1", "dw2")):
+        near(g, v.detach().cpu(), rel, name)
+
+
+def test_experts_gradient_against_differences(mix):
+    x, ids, weights, w1, w2, dout = expert_inputs(F32, 6, 3, 2, 7, 5, 36, empty=False)
+    a = [x, weights, w1, w2]
+    t = [v.cuda().requires_grad_() for v in a]
+    mix.experts(t[0], ids.cuda(), t[1], t[2], t[3]).backward(dout.cuda())
+    h = 1e-5
+    f = lambda v: (ref.experts(v[0], ids, v[1], v[2], v[3]) * dout.double()).sum()  # noqa: E731
+    for i in range(4):
+        got = t[i].grad.double().cpu().flatten()
+        for j in range(0, got.numel(), 3):
+            lo, hi = [v.double().clone() for v in a], [v.double().clone() for v in a]
+            lo[i].view(-1)[j] -= h
+            hi[i].view(-1)[j] += h
+            d = (f(hi) - f(lo)) / (2 * h)
+            assert abs(got[j] - d) < 1e-5 * (1 + abs(d)), (i, j)
+
+
+# ------------------------------------------------------------------------ use of the GPU ----
+
+def everything(mix, x, logits, w, b, w1, w2, dout):
+    y, stats = mix.layer_norm_forward(x, w, b)
+    ids, weights = mix.route(logits, 2, score="sigmoid", scale=1.5)
+    out, saved = mix.experts_forward(y, ids, weights, w1, w2)
+    dy, dweights, dw1, dw2 = mix.experts_backward(dout, y, ids, weights, w1, w2, saved)
+    dlogits = mix.route_backward(dweights, logits, ids, score="sigmoid", scale=1.5)
+    dx, dw, db = mix.layer_norm_backward(dy, x, w, b, stats)
+    return y, ids, weights, out, dy, dweights, dw1, dw2, dlogits, dx, dw, db
+
+
+def layer_inputs(dtype, tokens=200, experts=8, dim=96, hidden=64):
+    x, _, _, w1, w2, dout = expert_inputs(dtype, tokens, experts, 2, dim, hidden, 40)
+    logits = randn(tokens, experts, seed=41)
+    return [t.cuda() for t in (x, logits, 1 + 0.1 * randn(dim, seed=42), randn(dim, seed=43),
+                               w1, w2, dout)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_results_repeat_bit_for_bit_and_on_other_streams(mix, dtype):
+    a = layer_inputs(dtype)
+    first = everything(mix, *a)
+    torch.cuda.synchronize()
+    second = everything(mix, *a)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        third = everything(mix, *a)
+    side.synchronize()
+    for p, q, r in zip(first, second, third):
+        assert torch.equal(p, q) and torch.equal(p, r)
+
+
+@pytest.mark.parametrize("tokens", [2, 200])
+def test_a_recorded_graph_replays(mix, tokens):
+    a = layer_inputs(BF16, tokens=tokens)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        everything(mix, *a)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = everything(mix, *a)
+    for i in range(4):
+        a[0].copy_(randn(*a[0].shape, seed=50 + i, dtype=BF16))
+        a[1].copy_(randn(*a[1].shape, seed=60 + i))
+        graph.replay()
+        torch.cuda.synchronize()
+        copies = [t.clone() for t in got]
+        want = everything(mix, *a)
+        for p, q in zip(copies, want):
+            assert torch.equal(p, q), i
+
+
+def test_autograd_of_the_whole_layer(mix):
+    """Norm, router, choice, experts and the residual sum, differentiated by torch, against the
+    same in float64."""
+    x, _, w, b, w1, w2, dout = layer_inputs(F32, tokens=30, experts=5, dim=20, hidden=12)
+    wr = randn(5, 20, seed=44).cuda()
+
+    def layer(x, w, b, wr, w1, w2):
+        y = mix.layer_norm(x, w, b)
+        ids, weights = mix.route(y @ wr.t(), 2)
+        return x + mix.experts(y, ids, weights, w1, w2), ids
+
+    t = [v.clone().requires_grad_() for v in (x, w, b, wr, w1, w2)]
+    out, ids = layer(*t)
+    out.backward(dout)
+    d = [v.detach().double().cpu().requires_grad_() for v in (x, w, b, wr, w1, w2)]
+    n = torch.nn.functional.layer_norm(d[0], (20,), d[1], d[2], 1e-5)
+    weights = ref.route_weights(n @ d[3].t(), ids.cpu().long(), "softmax", True, 1.0)
+    want = d[0] + ref.experts(n, ids.cpu(), weights, d[4], d[5])
+    want.backward(dout.double().cpu())
+    near(out, want.detach(), 1e-5, "out")
+    for p, q, name in zip(t, d, ("x", "w", "b", "router", "w1", "w2")):
+        near(p.grad, q.grad, 1e-5, name)
