@@ -6,18 +6,19 @@
 namespace gsn {
 
 constexpr int kPlanExperts = 1024;  // experts at most
+constexpr int kPlanRows = 256;      // rows of a listed block
 
 // Pairs (token, place k), number token * top + k, sorted by expert and then by number: row r of
 // the products is pair rows[r], pair j is row pos[j] (-1 for a pair without an expert), expert
-// e's rows are offsets[e] .. offsets[e + 1] - 1.  Blocks of `block` rows that hold one expert's
+// e's rows are offsets[e] .. offsets[e + 1] - 1.  Blocks of kPlanRows rows that hold one expert's
 // rows alone are listed in tiles as (expert, first row); *tile_count of them.
 struct Plan {
   int32_t* offsets;     // experts + 1
   int32_t* tile_count;  // 1
   int2* tiles;          // most_tiles
   int32_t* rows;        // pairs
+  int32_t* token;       // pairs: rows[r] / top
   int32_t* pos;         // pairs
-  int32_t block;
   int32_t most_tiles;
 };
 
@@ -57,7 +58,7 @@ hipError_t launch_experts(const Experts& x, hipStream_t st);
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
 
-// columns of one partial dot product of the weights' gradient
+// columns of one partial dot product of the weights' gradient, at least
 constexpr int kDotColumns = 128;
 
 }  // namespace gsn

@@ -14,6 +14,7 @@ static_assert(kPlanExperts <= kPlanThreads);
 // own rows begin), then to place its own, each wave a stretch of the pairs in their order.  No
 // workgroup waits for another, and the order is that of the pairs.
 __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t experts,
+                                                        int32_t top,
                                                         const int32_t* __restrict__ ids,
                                                         Plan plan) {
   __shared__ int32_t count[kPlanExperts];
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t e
   __syncthreads();
   // rows and tiles before every expert
   const int32_t c = tid < experts ? count[tid] : 0;
-  int32_t rows = c, tiles = (c + plan.block - 1) / plan.block;
+  int32_t rows = c, tiles = (c + kPlanRows - 1) / kPlanRows;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
     const int32_t r = __shfl_up(rows, o), t = __shfl_up(tiles, o);
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t e
     rows += sums[w].x;
     tiles += sums[w].y;
   }
-  if (tid == e) at = int4{rows - c, c, tiles - (c + plan.block - 1) / plan.block, 0};
+  if (tid == e) at = int4{rows - c, c, tiles - (c + kPlanRows - 1) / kPlanRows, 0};
   if (e == 0) {
     if (tid < experts) plan.offsets[tid + 1] = rows;
     if (tid == 0) plan.offsets[0] = 0;
@@ -61,8 +62,8 @@ __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t e
   }
   __syncthreads();
   const int4 a = at;
-  for (int32_t k = tid; k * plan.block < a.y; k += kPlanThreads)
-    plan.tiles[a.z + k] = int2{e, a.x + k * plan.block};
+  for (int32_t k = tid; k * kPlanRows < a.y; k += kPlanThreads)
+    plan.tiles[a.z + k] = int2{e, a.x + k * kPlanRows};
   int32_t r = a.x;
   for (int w = 0; w < wave; ++w) r += mine[w];
   for (int64_t i = i0; i < i1; i += kWave) {
@@ -71,14 +72,12 @@ __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t e
     if (hit) {
       const int32_t at_row = r + __popcll(m & ((uint64_t{1} << lane) - 1));
       plan.rows[at_row] = static_cast<int32_t>(i + lane);
+      plan.token[at_row] = static_cast<int32_t>(i + lane) / top;
       plan.pos[i + lane] = at_row;
     }
     r += __popcll(m);
   }
 }
-
-// rows of a tile
-int32_t block_rows(int64_t, int32_t) { return 128; }
 
 constexpr size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -95,13 +94,13 @@ struct Carver {
 void carve_plan(Carver* c, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs);
   Plan& p = x->plan;
-  p.block = block_rows(x->pairs, x->experts);
   p.most_tiles = static_cast<int32_t>(
-      x->pairs / p.block + (x->pairs < x->experts ? x->pairs : x->experts));
+      x->pairs / kPlanRows + (x->pairs < x->experts ? x->pairs : x->experts));
   p.offsets = static_cast<int32_t*>(c->take(4 * (static_cast<size_t>(x->experts) + 1)));
   p.tile_count = static_cast<int32_t*>(c->take(4));
   p.tiles = static_cast<int2*>(c->take(8 * static_cast<size_t>(p.most_tiles)));
   p.rows = static_cast<int32_t*>(c->take(4 * n));
+  p.token = static_cast<int32_t*>(c->take(4 * n));
   p.pos = static_cast<int32_t*>(c->take(4 * n));
 }
 
@@ -169,8 +168,8 @@ bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 
 }  // namespace
 
 hipError_t launch_plan(const Experts& x, hipStream_t st) {
-  ex_plan<<<x.experts, kPlanThreads, 0, st>>>(static_cast<int32_t>(x.pairs), x.experts, x.ids,
-                                              x.plan);
+  ex_plan<<<x.experts, kPlanThreads, 0, st>>>(static_cast<int32_t>(x.pairs), x.experts, x.top,
+                                              x.ids, x.plan);
   return hipGetLastError();
 }
 
