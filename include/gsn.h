@@ -493,7 +493,8 @@ int gsn_route(const gsn_route_params* params, int32_t dtype, int64_t tokens, con
               float* weights, void* stream);
 
 /* Gradient of the weights with respect to the logits, the choice held fixed: dlogits
- * [tokens][experts] of dtype, every element written.  ids out of range count as -1. */
+ * [tokens][experts] of dtype, every element written.  ids are those of gsn_route (a token's
+ * differ from each other); out of range they count as -1. */
 int gsn_route_backward(const gsn_route_params* params, int32_t dtype, int64_t tokens,
                        const float* dweights, const void* logits, int64_t stride,
                        const int32_t* ids, void* dlogits, int64_t dlogits_stride, void* stream);

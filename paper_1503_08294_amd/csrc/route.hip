@@ -1,9 +1,16 @@
 // Routing of tokens to experts: scores, the choice of K of E experts, their weights, and the
 // gradient of the logits.
 //
-// A token's logits lie in the lanes of one wave (expert lane + 64 j).  An expert's place in the
-// order is one 64-bit key, the float's bits in unsigned order above the complemented index, so
-// the largest key is the best expert and ties go to the lowest index; 0 is an expert shut out.
+// A token's logits lie in SUB lanes of a wave (16: four tokens a wave; 64: one), NPL experts in a
+// row each.  An expert's place in the order is its float's bits in unsigned order, 0 if it is shut
+// out; ties go to the lower lane and the earlier of its experts, which is the lower index.
+// Every lane keeps its two best; each of the K rounds takes the largest of the lanes' first ones
+// (16 lanes: four instructions that move data between lanes), and only a lane whose two are both
+// taken looks through its experts again.
+//
+// Bound by instructions, and by the latency of their chain where tokens are few: 16,384 tokens of
+// 256 experts, 8 chosen of 4 of 8 groups, sigmoid with a balance: 19 us (8 MB of logits would take
+// 2); one such token 9 us; 65,536 tokens of 64 experts, 2 chosen, softmax: 8 us, backward 7.
 #include "mixture.h"
 
 #pragma clang fp contract(fast)
@@ -12,12 +19,9 @@ namespace gsn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kMostExperts = 1024;
-constexpr int kMostTop = 64;  // one chosen expert a lane
+constexpr int kMostTop = 64;
 constexpr int kMostGroups = 64;
-
-using u64 = unsigned long long;
 
 struct RouteArgs {
   int32_t experts, top, groups, top_groups, best;
@@ -32,19 +36,63 @@ struct RouteArgs {
   float* weights;
 };
 
-// unsigned order of the bits = order of the floats (-0 equals +0)
+// unsigned order of the bits = order of the floats (-0 equals +0), and back
 __device__ __forceinline__ uint32_t ordered(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);
   return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float unordered(uint32_t k) {
+  return __uint_as_float(k ^ (static_cast<uint32_t>(static_cast<int32_t>(~k) >> 31) | 0x80000000u));
+}
 
-__device__ __forceinline__ u64 wave_max_key(u64 k) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const u64 other = __shfl_xor(k, o);
-    k = other > k ? other : k;
+// The value of a lane of this row of 16: its neighbour (lane ^ 1), lane ^ 2, and the mirror
+// images in 8 and in 16 lanes; after a reduction's four steps all 16 hold the result.
+template <int STEP>
+__device__ __forceinline__ uint32_t other(uint32_t v) {
+  constexpr int kCtrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+  return __builtin_amdgcn_mov_dpp(static_cast<int>(v), kCtrl, 0xf, 0xf, true);
+}
+template <int SUB, typename F>
+__device__ __forceinline__ uint32_t reduce(uint32_t v, F f) {
+  v = f(v, other<0>(v));
+  v = f(v, other<1>(v));
+  v = f(v, other<2>(v));
+  v = f(v, other<3>(v));
+  if constexpr (SUB == kWave) {
+    v = f(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16)));
+    v = f(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32)));
   }
-  return k;
+  return v;
+}
+template <int SUB>
+__device__ __forceinline__ uint32_t max_u32(uint32_t v) {
+  return reduce<SUB>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int SUB>
+__device__ __forceinline__ float max_f32(float v) {
+  return __uint_as_float(reduce<SUB>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+template <int SUB>
+__device__ __forceinline__ float sum_f32(float v) {
+  return __uint_as_float(reduce<SUB>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+// the lowest of this token's lanes where p holds, -1 for none
+template <int SUB>
+__device__ __forceinline__ int first_lane(bool p) {
+  const uint64_t m = __ballot(p);
+  if constexpr (SUB == kWave) return __ffsll(static_cast<unsigned long long>(m)) - 1;
+  return __ffs(static_cast<int>((m >> ((threadIdx.x % kWave) & 48)) & 0xffff)) - 1;
+}
+
+// What a wave's lanes wrote to LDS before it, they may read from each other after it.
+__device__ __forceinline__ void lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
 // a logit as the scores take it: NaN is shut out like -inf, +inf is the largest float
@@ -58,122 +106,214 @@ __device__ __forceinline__ float sigmoid_from(float l, float low) {
   return l > 0.0f ? sigmoid(l) : __expf(l - low) * __builtin_amdgcn_rcpf(1.0f + __expf(l));
 }
 
+// A lane's NPL elements of a row of n at i; rows start at any element.
 template <typename T, int NPL>
+__device__ __forceinline__ void load_row(const T* row, int i, int n, float none, float (&v)[NPL]) {
+  constexpr int kW = NPL * sizeof(T) >= 16 ? 16 / sizeof(T) : NPL;
+  typedef T Some __attribute__((ext_vector_type(kW), aligned(sizeof(T))));
+  if (NPL > 1 && i + NPL <= n) {
+#pragma unroll
+    for (int h = 0; h < NPL; h += kW) {
+      const Some c = *reinterpret_cast<const Some*>(row + i + h);
+#pragma unroll
+      for (int k = 0; k < kW; ++k) v[h + k] = to_float(c[k]);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NPL; ++k) v[k] = i + k < n ? to_float(row[i + k]) : none;
+  }
+}
+template <typename T, int NPL>
+__device__ __forceinline__ void store_row(T* row, int i, int n, const float (&v)[NPL]) {
+  constexpr int kW = NPL * sizeof(T) >= 16 ? 16 / sizeof(T) : NPL;
+  typedef T Some __attribute__((ext_vector_type(kW), aligned(sizeof(T))));
+  if (NPL > 1 && i + NPL <= n) {
+#pragma unroll
+    for (int h = 0; h < NPL; h += kW) {
+      Some c;
+#pragma unroll
+      for (int k = 0; k < kW; ++k) c[k] = from_float<T>(v[h + k]);
+      *reinterpret_cast<Some*>(row + i + h) = c;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NPL; ++k)
+      if (i + k < n) row[i + k] = from_float<T>(v[k]);
+  }
+}
+
+// a lane's two best after (k, at) in the order; 0 where there is none
+struct Two {
+  uint32_t k1, k2;
+  int p1, p2;
+};
+template <int NPL>
+__device__ __forceinline__ Two two_after(const uint32_t (&key)[NPL], uint32_t k, int at) {
+  Two t{0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < NPL; ++j) {
+    const uint32_t c = key[j] < k || (key[j] == k && j > at) ? key[j] : 0;
+    const bool first = c > t.k1, second = c > t.k2;
+    t.k2 = first ? t.k1 : second ? c : t.k2;
+    t.p2 = first ? t.p1 : second ? j : t.p2;
+    t.k1 = first ? c : t.k1;
+    t.p1 = first ? j : t.p1;
+  }
+  return t;
+}
+
+template <typename T, int SUB, int NPL>
 __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
-  __shared__ u64 keys[kWaves][NPL * kWave];
-  __shared__ float pick[kWaves][NPL * kWave];
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-  if (t >= a.tokens) return;
+  constexpr int kTokens = kThreads / SUB;
+  __shared__ int32_t picked[kTokens][SUB];
+  // only for groups whose experts are not whole lanes
+  __shared__ uint32_t keys[kTokens][SUB * NPL];
+  __shared__ uint32_t values[kTokens][kMostGroups];
+  const int sub = threadIdx.x / SUB, lane = threadIdx.x % SUB;
+  // (a token past the end is worked on like the last one, and not written)
+  const int64_t mine = static_cast<int64_t>(blockIdx.x) * kTokens + sub;
+  const int64_t t = mine < a.tokens ? mine : a.tokens - 1;
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
   const float ninf = -__builtin_inff();
+  const int e0 = lane * NPL;
+  const bool live = !a.valid || a.valid[t] != 0;
   float l[NPL];
+  load_row(row, e0, a.experts, ninf, l);
 #pragma unroll
-  for (int j = 0; j < NPL; ++j) {
-    const int e = lane + kWave * j;
-    l[j] = e < a.experts ? clean(to_float(row[e])) : ninf;
-  }
-  if (a.valid && a.valid[t] == 0) {
+  for (int j = 0; j < NPL; ++j) l[j] = live ? clean(l[j]) : ninf;
+  const bool grouped = a.groups > 1 && a.top_groups < a.groups;
+  // softmax over all experts, where a bias or a group's sum or the weights take it
+  float most = 0.0f, inv = 0.0f;
+  if (a.softmax && (a.balance || !a.renorm || (grouped && a.best == 2))) {
+    most = ninf;
 #pragma unroll
-    for (int j = 0; j < NPL; ++j) l[j] = ninf;
-  }
-  float most = ninf;
-#pragma unroll
-  for (int j = 0; j < NPL; ++j) most = fmaxf(most, l[j]);
-  most = fmaxf(wave_max(most), -__FLT_MAX__);
-  float total = 0.0f;
-  if (a.softmax) {
+    for (int j = 0; j < NPL; ++j) most = fmaxf(most, l[j]);
+    most = fmaxf(max_f32<SUB>(most), -__FLT_MAX__);
+    float total = 0.0f;
 #pragma unroll
     for (int j = 0; j < NPL; ++j) total += __expf(l[j] - most);
-    total = wave_sum(total);
+    total = sum_f32<SUB>(total);
+    inv = total > 0.0f ? 1.0f / total : 0.0f;
   }
-  const float inv = total > 0.0f ? 1.0f / total : 0.0f;
-  // choice: score + bias; key: the logits give the same order where there is no bias
-  u64 key[NPL];
+  const auto score = [&](float v) { return a.softmax ? __expf(v - most) * inv : sigmoid(v); };
+  uint32_t key[NPL];
+  if (a.balance) {
+    float b[NPL];
+    load_row(a.balance, e0, a.experts, ninf, b);
 #pragma unroll
-  for (int j = 0; j < NPL; ++j) {
-    const int e = lane + kWave * j;
-    float c = a.softmax ? __expf(l[j] - most) * inv : sigmoid(l[j]);
-    float k = l[j];
-    if (a.balance) {
-      c += e < a.experts ? a.balance[e] : 0.0f;
-      k = c;
+    for (int j = 0; j < NPL; ++j) {
+      const float c = score(l[j]) + b[j];
+      key[j] = l[j] > ninf && c > ninf ? ordered(c) : 0;
     }
-    const bool shut = !(l[j] > ninf) || !(k > ninf);
-    key[j] = shut ? 0 : (static_cast<u64>(ordered(k)) << 32) | (0xffffffffu - e);
-    keys[wave][e] = key[j];
-    pick[wave][e] = c;
+  } else {
+#pragma unroll
+    for (int j = 0; j < NPL; ++j) key[j] = l[j] > ninf ? ordered(l[j]) : 0;
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  if (a.groups > 1 && a.top_groups < a.groups) {
+  Two top = two_after(key, 0xffffffffu, -1);
+
+  if (grouped) {
     const int width = a.experts / a.groups;
-    u64 value = 0;  // of the group of this lane
-    if (lane < a.groups) {
-      u64 k1 = 0, k2 = 0;
-      for (int i = 0; i < width; ++i) {
-        const u64 k = keys[wave][lane * width + i];
-        if (k > k1) {
-          k2 = k1;
-          k1 = k;
-        } else if (k > k2) {
-          k2 = k;
+    // the value of a group whose two best are k1, k2
+    const auto value_of = [&](uint32_t k1, uint32_t k2) -> uint32_t {
+      if (k1 == 0 || a.best == 1) return k1;
+      float v = unordered(k1), w = unordered(k2);
+      if (!a.balance) {
+        v = score(v);
+        w = score(w);
+      }
+      return ordered(k2 != 0 ? v + w : v);
+    };
+    const int lanes = width / NPL;
+    if (lanes * NPL == width && (lanes == 1 || lanes == 2 || lanes == 4)) {
+      // whole lanes: the two best of a group, then one round of the largest value for each kept
+      uint32_t k1 = top.k1, k2 = top.k2;
+      const auto join = [&](uint32_t o1, uint32_t o2) {
+        const uint32_t low = k1 < o1 ? k1 : o1, high = k2 > o2 ? k2 : o2;
+        k1 = k1 > o1 ? k1 : o1;
+        k2 = low > high ? low : high;
+      };
+      if (lanes > 1) join(other<0>(k1), other<0>(k2));
+      if (lanes > 2) join(other<1>(k1), other<1>(k2));
+      uint32_t value = e0 < a.experts ? value_of(k1, k2) : 0;
+      bool kept = false;
+      for (int g = 0; g < a.top_groups; ++g) {
+        const uint32_t best = max_u32<SUB>(value);
+        const int first = first_lane<SUB>(best != 0 && value == best);
+        if (first >= 0 && first / lanes == lane / lanes) {
+          kept = true;
+          value = 0;
         }
       }
-      if (k1 != 0) {
-        uint32_t v = static_cast<uint32_t>(k1 >> 32);
-        if (a.best == 2) {
-          float s = pick[wave][0xffffffffu - static_cast<uint32_t>(k1)];
-          if (k2 != 0) s += pick[wave][0xffffffffu - static_cast<uint32_t>(k2)];
-          v = ordered(s);
-        }
-        value = (static_cast<u64>(v) << 32) | (0xffffffffu - lane);
-      }
-    }
-    int rank = 0;
-    for (int g = 0; g < a.groups; ++g) rank += __shfl(value, g) > value;
-    const u64 kept = __ballot(value != 0 && rank < a.top_groups);
 #pragma unroll
-    for (int j = 0; j < NPL; ++j) {
-      const int e = lane + kWave * j;
-      if (e < a.experts && !((kept >> (e / width)) & 1)) key[j] = 0;
+      for (int j = 0; j < NPL; ++j) key[j] = kept ? key[j] : 0;
+      if (!kept) top = Two{0, 0, 0, 0};
+    } else {
+#pragma unroll
+      for (int j = 0; j < NPL; ++j) keys[sub][e0 + j] = key[j];
+      lds_fence();
+      for (int g = lane; g < a.groups; g += SUB) {
+        uint32_t k1 = 0, k2 = 0;
+        for (int i = 0; i < width; ++i) {
+          const uint32_t k = keys[sub][g * width + i];
+          const uint32_t low = k < k1 ? k : k1;
+          k1 = k > k1 ? k : k1;
+          k2 = low > k2 ? low : k2;
+        }
+        values[sub][g] = value_of(k1, k2);
+      }
+      lds_fence();
+#pragma unroll
+      for (int j = 0; j < NPL; ++j) {
+        const int e = e0 + j;
+        if (e >= a.experts) continue;
+        const int g = e / width;
+        const uint32_t v = values[sub][g];
+        int rank = 0;
+        for (int i = 0; i < a.groups; ++i) {
+          const uint32_t o = values[sub][i];
+          rank += o > v || (o == v && i < g);
+        }
+        if (rank >= a.top_groups) key[j] = 0;
+      }
+      top = two_after(key, 0xffffffffu, -1);
     }
   }
-  // K rounds of the largest key; lane k holds the k-th
-  int32_t id = -1;
-  float logit = ninf;
+
+  // K rounds
+  uint32_t last = 0xffffffffu;
+  int last_at = -1;
+  picked[sub][lane] = -1;
+  lds_fence();
   for (int k = 0; k < a.top; ++k) {
-    u64 b = 0;
-#pragma unroll
-    for (int j = 0; j < NPL; ++j) b = key[j] > b ? key[j] : b;
-    b = wave_max_key(b);
-    if (b == 0) break;
-    const int32_t e = static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(b));
-    float v = ninf;
-#pragma unroll
-    for (int j = 0; j < NPL; ++j) {
-      if (key[j] == b) {
-        key[j] = 0;
-        v = l[j];
-      }
+    const uint32_t best = max_u32<SUB>(top.k1);
+    const int first = first_lane<SUB>(best != 0 && top.k1 == best);
+    const bool won = first == lane;
+    if (won) {
+      picked[sub][k] = e0 + top.p1;
+      last = top.k1;
+      last_at = top.p1;
+      top.k1 = top.k2;
+      top.p1 = top.p2;
+      top.k2 = 0;
     }
-    v = __shfl(v, e % kWave);
-    if (lane == k) {
-      id = e;
-      logit = v;
+    if (NPL > 2 && __any(won && top.k1 == 0)) {
+      const Two next = two_after(key, last, last_at);
+      if (won && top.k1 == 0) top = next;
     }
   }
-  const float top = fmaxf(wave_max(logit), -__FLT_MAX__);
+  lds_fence();
+  const int32_t id = lane < a.top ? picked[sub][lane] : -1;
+  const float logit = id >= 0 ? clean(to_float(row[id])) : ninf;
   float s = 0.0f;
-  if (id >= 0) {
-    if (a.softmax) s = a.renorm ? __expf(logit - top) : __expf(logit - most) * inv;
-    else s = a.renorm ? sigmoid_from(logit, fminf(top, 0.0f)) : sigmoid(logit);
-  }
   if (a.renorm) {
-    const float sum = wave_sum(s);
+    const float high = fmaxf(max_f32<SUB>(logit), -__FLT_MAX__);
+    if (id >= 0) s = a.softmax ? __expf(logit - high) : sigmoid_from(logit, fminf(high, 0.0f));
+    const float sum = sum_f32<SUB>(s);
     s = sum > 0.0f ? s / sum : 0.0f;
+  } else if (id >= 0) {
+    s = score(logit);
   }
-  if (lane < a.top) {
+  if (lane < a.top && mine < a.tokens) {
     a.ids[t * a.top + lane] = id;
     a.weights[t * a.top + lane] = s * a.scale;
   }
@@ -194,15 +334,20 @@ struct RouteBackArgs {
 
 // softmax: dl = s (G - sum G s), G the chosen experts' scaled gradients; renormalised, over the
 // chosen alone, dl_k = p_k (g_k - sum g p).  sigmoid: dl_k = g_k s_k (1 - s_k); renormalised
-// dl_k = p_k (g_k - sum g p) (1 - s_k), since d log s = (1 - s) dl.
-template <typename T, int NPL>
+// dl_k = p_k (g_k - sum g p) (1 - s_k), since d log s = (1 - s) dl.  The chosen experts' values
+// reach the lanes that write their places through a row in LDS.
+template <typename T, int SUB, int NPL>
 __global__ __launch_bounds__(kThreads) void rt_backward(RouteBackArgs a) {
-  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-  if (t >= a.tokens) return;
+  constexpr int kTokens = kThreads / SUB;
+  __shared__ __attribute__((aligned(16))) float rows[kTokens][SUB * NPL];
+  const int sub = threadIdx.x / SUB, lane = threadIdx.x % SUB;
+  const int64_t mine = static_cast<int64_t>(blockIdx.x) * kTokens + sub;
+  const int64_t t = mine < a.tokens ? mine : a.tokens - 1;
   const T* row = static_cast<const T*>(a.logits) + t * a.stride;
-  T* out = static_cast<T*>(a.dlogits) + t * a.dstride;
   const float ninf = -__builtin_inff();
+  const int e0 = lane * NPL;
+#pragma unroll
+  for (int j = 0; j < NPL; ++j) rows[sub][e0 + j] = 0.0f;
   int32_t id = -1;
   float g = 0.0f;
   if (lane < a.top) {
@@ -211,60 +356,52 @@ __global__ __launch_bounds__(kThreads) void rt_backward(RouteBackArgs a) {
     if (id >= 0) g = a.dweights[t * a.top + lane] * a.scale;
   }
   const float logit = id >= 0 ? clean(to_float(row[id])) : ninf;
-  const bool any = __ballot(id >= 0) != 0;
+  const bool any = first_lane<SUB>(id >= 0) >= 0;
+  const bool dense = a.softmax && !a.renorm;  // every expert has a gradient
   float l[NPL], most = 0.0f, inv = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NPL; ++j) l[j] = ninf;
-  if (a.softmax && !a.renorm && any) {
+  if (dense) {
+    load_row(row, e0, a.experts, ninf, l);
     most = ninf;
 #pragma unroll
     for (int j = 0; j < NPL; ++j) {
-      const int e = lane + kWave * j;
-      if (e < a.experts) l[j] = clean(to_float(row[e]));
+      l[j] = any ? clean(l[j]) : ninf;
       most = fmaxf(most, l[j]);
     }
-    most = fmaxf(wave_max(most), -__FLT_MAX__);
+    most = fmaxf(max_f32<SUB>(most), -__FLT_MAX__);
     float total = 0.0f;
 #pragma unroll
     for (int j = 0; j < NPL; ++j) total += __expf(l[j] - most);
-    total = wave_sum(total);
+    total = sum_f32<SUB>(total);
     inv = total > 0.0f ? 1.0f / total : 0.0f;
   }
   float back = 0.0f, mean = 0.0f;
   if (a.renorm) {
-    const float top = fmaxf(wave_max(logit), -__FLT_MAX__);
+    const float high = fmaxf(max_f32<SUB>(logit), -__FLT_MAX__);
     float p = 0.0f;
-    if (id >= 0)
-      p = a.softmax ? __expf(logit - top) : sigmoid_from(logit, fminf(top, 0.0f));
-    const float sum = wave_sum(p);
+    if (id >= 0) p = a.softmax ? __expf(logit - high) : sigmoid_from(logit, fminf(high, 0.0f));
+    const float sum = sum_f32<SUB>(p);
     p = sum > 0.0f ? p / sum : 0.0f;
-    mean = wave_sum(g * p);
+    mean = sum_f32<SUB>(g * p);
     back = p * (g - mean);
     // 1 - sigmoid(l) = sigmoid(-l), without the cancellation
     if (!a.softmax) back *= sigmoid(-logit);
   } else if (a.softmax) {
-    mean = wave_sum(id >= 0 ? g * (__expf(logit - most) * inv) : 0.0f);
+    mean = sum_f32<SUB>(id >= 0 ? g * (__expf(logit - most) * inv) : 0.0f);
     back = g;
   } else {
     back = g * sigmoid(logit) * sigmoid(-logit);
   }
-  if (id < 0) back = 0.0f;
+  lds_fence();
+  if (id >= 0) rows[sub][id] = back;
+  lds_fence();
   float d[NPL];
 #pragma unroll
-  for (int j = 0; j < NPL; ++j) d[j] = 0.0f;
-  for (int k = 0; k < a.top; ++k) {
-    const int32_t e = __shfl(id, k);
-    const float b = __shfl(back, k);
-#pragma unroll
-    for (int j = 0; j < NPL; ++j) d[j] += e == lane + kWave * j ? b : 0.0f;
-  }
-#pragma unroll
   for (int j = 0; j < NPL; ++j) {
-    const int e = lane + kWave * j;
-    if (a.softmax && !a.renorm)
-      d[j] = l[j] > ninf ? __expf(l[j] - most) * inv * (d[j] - mean) : 0.0f;
-    if (e < a.experts) out[e] = from_float<T>(d[j]);
+    d[j] = rows[sub][e0 + j];
+    if (dense) d[j] = l[j] > ninf ? __expf(l[j] - most) * inv * (d[j] - mean) : 0.0f;
   }
+  if (mine < a.tokens)
+    store_row(static_cast<T*>(a.dlogits) + t * a.dstride, e0, a.experts, d);
 }
 
 __global__ __launch_bounds__(kThreads) void rt_clear(int32_t n, int32_t* __restrict__ c) {
@@ -308,21 +445,46 @@ __global__ __launch_bounds__(kThreads) void rt_balance(int32_t experts,
   }
 }
 
+// 16 lanes a token where they hold its experts and chosen ones, else a wave.
 template <typename T>
 hipError_t choose(const RouteArgs& a, hipStream_t st) {
-  const uint32_t nb = static_cast<uint32_t>((a.tokens + kWaves - 1) / kWaves);
-  if (a.experts <= 64) rt_choose<T, 1><<<nb, kThreads, 0, st>>>(a);
-  else if (a.experts <= 256) rt_choose<T, 4><<<nb, kThreads, 0, st>>>(a);
-  else rt_choose<T, 16><<<nb, kThreads, 0, st>>>(a);
+  const auto blocks = [&](int sub) {
+    const int per = kThreads / sub;
+    return static_cast<uint32_t>((a.tokens + per - 1) / per);
+  };
+  if (a.top <= 16 && a.experts <= 64)
+    rt_choose<T, 16, 4><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.top <= 16 && a.experts <= 128)
+    rt_choose<T, 16, 8><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.top <= 16 && a.experts <= 256)
+    rt_choose<T, 16, 16><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.experts <= 256)
+    rt_choose<T, 64, 4><<<blocks(64), kThreads, 0, st>>>(a);
+  else if (a.experts <= 512)
+    rt_choose<T, 64, 8><<<blocks(64), kThreads, 0, st>>>(a);
+  else
+    rt_choose<T, 64, 16><<<blocks(64), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t backward(const RouteBackArgs& a, hipStream_t st) {
-  const uint32_t nb = static_cast<uint32_t>((a.tokens + kWaves - 1) / kWaves);
-  if (a.experts <= 64) rt_backward<T, 1><<<nb, kThreads, 0, st>>>(a);
-  else if (a.experts <= 256) rt_backward<T, 4><<<nb, kThreads, 0, st>>>(a);
-  else rt_backward<T, 16><<<nb, kThreads, 0, st>>>(a);
+  const auto blocks = [&](int sub) {
+    const int per = kThreads / sub;
+    return static_cast<uint32_t>((a.tokens + per - 1) / per);
+  };
+  if (a.top <= 16 && a.experts <= 64)
+    rt_backward<T, 16, 4><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.top <= 16 && a.experts <= 128)
+    rt_backward<T, 16, 8><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.top <= 16 && a.experts <= 256)
+    rt_backward<T, 16, 16><<<blocks(16), kThreads, 0, st>>>(a);
+  else if (a.experts <= 256)
+    rt_backward<T, 64, 4><<<blocks(64), kThreads, 0, st>>>(a);
+  else if (a.experts <= 512)
+    rt_backward<T, 64, 8><<<blocks(64), kThreads, 0, st>>>(a);
+  else
+    rt_backward<T, 64, 16><<<blocks(64), kThreads, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -338,7 +500,7 @@ bool params_ok(const gsn_route_params* p) {
   return p->scale == p->scale && p->scale - p->scale == 0.0f;  // finite
 }
 
-constexpr int64_t kMostTokens = int64_t{1} << 25;  // a wave each, in a grid of 2^31 threads
+constexpr int64_t kMostTokens = int64_t{1} << 25;  // a wave each at most, in a grid of 2^31 threads
 
 bool dtype_ok(int32_t d) { return d >= GSN_F32 && d <= GSN_F16; }
 

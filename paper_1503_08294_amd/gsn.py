@@ -451,14 +451,21 @@ def _type(t: torch.Tensor, what: str) -> int:
     return code
 
 
-def _matrix(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
-    """(pointer, row stride) of a device matrix with contiguous rows."""
+def _refuse(t, dtype, shape, what: str):
+    """The first reason why t is not a device tensor of this type and shape."""
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what} must be ({rows}, {cols}), got {tuple(t.shape)}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must be {shape}, got {tuple(t.shape)}")
+
+
+# (a few hundred nanoseconds a tensor: the calls below are made for single tokens)
+def _matrix(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
+    """(pointer, row stride) of a device matrix with contiguous rows."""
+    if not t.is_cuda or t.dtype is not dtype or t.shape != (rows, cols):
+        _refuse(t, dtype, (rows, cols), what)
     row, col = t.stride()
     if col != 1 and cols > 1:
         raise ValueError(f"{what} must have contiguous rows")
@@ -473,15 +480,21 @@ def _flat(t: torch.Tensor | None, dtype, shape, what: str):
     """Pointer of a contiguous device tensor of this shape, None for None."""
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a device tensor")
-    if t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{what} must be {shape}, got {tuple(t.shape)}")
+    if not t.is_cuda or t.dtype is not dtype or t.shape != shape:
+        _refuse(t, dtype, shape, what)
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     return t.data_ptr()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _on(t: torch.Tensor, stream) -> int | ctypes.c_void_p:
+    """The stream's handle; without one, torch's current stream of t's device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(t.device.index)
+    return _stream(stream)
 
 
 def _params_type(x_dtype, weight, bias) -> torch.dtype:
@@ -501,7 +514,7 @@ def gsn_layer_norm(x, weight, bias, eps: float, y, stats=None, stream=None):
     return _check(_lib.gsn_layer_norm(
         code, _DTYPES.get(pt, -1), rows, dim, xp, xs, _flat(weight, pt, (dim,), "weight"),
         _flat(bias, pt, (dim,), "bias"), eps, yp, ys,
-        _flat(stats, torch.float32, (2, rows), "stats"), _stream(stream)), "gsn_layer_norm")
+        _flat(stats, torch.float32, (2, rows), "stats"), _on(x, stream)), "gsn_layer_norm")
 
 
 def gsn_layer_norm_workspace_bytes(rows: int, dim: int) -> int:
@@ -521,7 +534,7 @@ def gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, workspace,
         _flat(weight, pt, (dim,), "weight"), _flat(stats, torch.float32, (2, rows), "stats"),
         dxp, dxs, _flat(dweight, pt, (dim,), "dweight"), _flat(dbias, pt, (dim,), "dbias"),
         _dev(workspace, torch.uint8), 0 if workspace is None else workspace.numel(),
-        _stream(stream)), "gsn_layer_norm_backward")
+        _on(x, stream)), "gsn_layer_norm_backward")
 
 
 def make_route(experts: int, top: int, score="softmax", groups=1, top_groups=1, best=1,
@@ -543,7 +556,7 @@ def gsn_route(params: gsn_route_params, logits, balance, valid, ids, weights, st
         _flat(balance, torch.float32, (params.experts,), "balance"),
         _flat(valid, torch.uint8, (tokens,), "valid"),
         _flat(ids, torch.int32, (tokens, params.top), "ids"),
-        _flat(weights, torch.float32, (tokens, params.top), "weights"), _stream(stream)),
+        _flat(weights, torch.float32, (tokens, params.top), "weights"), _on(logits, stream)),
         "gsn_route")
 
 
@@ -554,20 +567,20 @@ def gsn_route_backward(params: gsn_route_params, dweights, logits, ids, dlogits,
     return _check(_lib.gsn_route_backward(
         params, _type(logits, "logits"), tokens,
         _flat(dweights, torch.float32, (tokens, params.top), "dweights"), lp, ls,
-        _flat(ids, torch.int32, (tokens, params.top), "ids"), dp, ds, _stream(stream)),
+        _flat(ids, torch.int32, (tokens, params.top), "ids"), dp, ds, _on(logits, stream)),
         "gsn_route_backward")
 
 
 def gsn_route_counts(ids, counts, stream=None):
     return _check(_lib.gsn_route_counts(
         ids.numel(), counts.numel(), _dev(ids, torch.int32, what="ids"),
-        _dev(counts, torch.int32, what="counts"), _stream(stream)), "gsn_route_counts")
+        _dev(counts, torch.int32, what="counts"), _on(ids, stream)), "gsn_route_counts")
 
 
 def gsn_route_balance(counts, rate: float, balance, stream=None):
     return _check(_lib.gsn_route_balance(
         counts.numel(), _dev(counts, torch.int32, what="counts"), rate,
-        _dev(balance, torch.float32, counts.numel(), "balance"), _stream(stream)),
+        _dev(balance, torch.float32, counts.numel(), "balance"), _on(counts, stream)),
         "gsn_route_balance")
 
 
@@ -600,7 +613,7 @@ def gsn_experts(params: gsn_experts_params, x, ids, weights, w1, w2, out, saved,
         _flat(w2, x.dtype, (p.experts, p.dim, p.hidden), "w2"),
         _flat(out, x.dtype, (p.tokens, p.dim), "out"), _dev(saved, torch.uint8, what="saved"),
         0 if saved is None else saved.numel(), _dev(workspace, torch.uint8, what="workspace"),
-        workspace.numel(), _stream(stream)), "gsn_experts")
+        workspace.numel(), _on(x, stream)), "gsn_experts")
 
 
 def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, saved, dx,
@@ -616,7 +629,7 @@ def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, s
         _flat(dx, x.dtype, (p.tokens, p.dim), "dx"),
         _flat(dweights, torch.float32, pairs, "dweights"), _flat(dw1, x.dtype, s1, "dw1"),
         _flat(dw2, x.dtype, s2, "dw2"), _dev(workspace, torch.uint8, what="workspace"),
-        workspace.numel(), _stream(stream)), "gsn_experts_backward")
+        workspace.numel(), _on(x, stream)), "gsn_experts_backward")
 
 
 # ------------------------------------------------------------------ convenience ----

@@ -32,7 +32,7 @@ def _rows(x: torch.Tensor, what: str) -> torch.Tensor:
 
 def _bytes(n: int, x: torch.Tensor) -> torch.Tensor:
     # torch's allocator aligns to 512 bytes
-    return torch.empty(n, dtype=torch.uint8, device=x.device)
+    return x.new_empty(n, dtype=torch.uint8)
 
 
 # ----------------------------------------------------------------------- layer norm ----
@@ -41,8 +41,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     """(y, stats): the norm of every row of x (rows, dim) and what its backward pass takes."""
     _rows(x, "x")
     _same_device(x, weight=weight, bias=bias)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((2, x.shape[0]), dtype=torch.float32, device=x.device)
+    y = x.new_empty(x.shape)
+    stats = x.new_empty((2, x.shape[0]), dtype=torch.float32)
     gsn.gsn_layer_norm(x, weight, bias, eps, y, stats)
     return y, stats
 
@@ -52,7 +52,7 @@ def layer_norm_backward(dy, x, weight, bias, stats, need=(True, True, True)):
     _rows(x, "x")
     _same_device(x, dy=dy, weight=weight, bias=bias, stats=stats)
     rows, dim = x.shape
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
+    dx = x.new_empty(x.shape) if need[0] else None
     dweight = torch.empty_like(weight) if need[1] and weight is not None else None
     dbias = torch.empty_like(bias) if need[2] and bias is not None else None
     ws = None
@@ -85,7 +85,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
         return _LayerNorm.apply(x, weight, bias, eps)
     _rows(x, "x")
     _same_device(x, weight=weight, bias=bias)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = x.new_empty(x.shape)
     gsn.gsn_layer_norm(x, weight, bias, eps, y)
     return y
 
@@ -95,15 +95,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 def _route(logits, params, balance, valid):
     _same_device(logits, balance=balance, valid=valid)
     tokens = logits.shape[0]
-    ids = torch.empty((tokens, params.top), dtype=torch.int32, device=logits.device)
-    weights = torch.empty((tokens, params.top), dtype=torch.float32, device=logits.device)
+    ids = logits.new_empty((tokens, params.top), dtype=torch.int32)
+    weights = logits.new_empty((tokens, params.top), dtype=torch.float32)
     gsn.gsn_route(params, logits, balance, valid, ids, weights)
     return ids, weights
 
 
 def _route_backward(dweights, logits, ids, params):
     _same_device(logits, dweights=dweights, ids=ids)
-    dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    dlogits = logits.new_empty(logits.shape)
     gsn.gsn_route_backward(params, dweights, logits, ids, dlogits)
     return dlogits
 
@@ -167,7 +167,7 @@ def _experts_forward(x, ids, weights, w1, w2, save):
     size = gsn.gsn_experts_workspace_bytes(p, False)
     if size == 0:
         raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    out = x.new_empty(x.shape)
     saved = _bytes(gsn.gsn_experts_saved_bytes(p), x) if save else None
     gsn.gsn_experts(p, x, ids, weights, w1, w2, out, saved, _bytes(size, x))
     return out, saved
@@ -187,7 +187,7 @@ def experts_backward(dout, x, ids, weights, w1, w2, saved, need=(True, True, Tru
     if size == 0:
         raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
     dx, dweights, dw1, dw2 = (
-        torch.empty(t.shape, dtype=t.dtype, device=x.device) if n else None
+        t.new_empty(t.shape) if n else None
         for t, n in zip((x, weights, w1, w2), need))
     gsn.gsn_experts_backward(p, dout, x, weights, w1, w2, saved, dx, dweights, dw1, dw2,
                              _bytes(size, x))
