@@ -11,11 +11,12 @@ constexpr int kPlanRows = 256;      // rows of a listed block
 // Pairs (token, place k), number token * top + k, sorted by expert and then by number: row r of
 // the products is pair rows[r], pair j is row pos[j] (-1 for a pair without an expert), expert
 // e's rows are offsets[e] .. offsets[e + 1] - 1.  Blocks of kPlanRows rows that hold one expert's
-// rows alone are listed in tiles as (expert, first row); *tile_count of them.
+// rows alone are listed in tiles as (expert, the expert's first row, its first block, its
+// blocks), expert by expert; *tile_count of them.
 struct Plan {
   int32_t* offsets;     // experts + 1
   int32_t* tile_count;  // 1
-  int2* tiles;          // most_tiles
+  int4* tiles;          // most_tiles
   int32_t* rows;        // pairs
   int32_t* token;       // pairs: rows[r] / top
   int32_t* pos;         // pairs

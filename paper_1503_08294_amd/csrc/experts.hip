@@ -63,7 +63,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_plan(int32_t pairs, int32_t e
   __syncthreads();
   const int4 a = at;
   for (int32_t k = tid; k * kPlanRows < a.y; k += kPlanThreads)
-    plan.tiles[a.z + k] = int2{e, a.x + k * kPlanRows};
+    plan.tiles[a.z + k] = int4{e, a.x, a.z, (a.y + kPlanRows - 1) / kPlanRows};
   int32_t r = a.x;
   for (int w = 0; w < wave; ++w) r += mine[w];
   for (int64_t i = i0; i < i1; i += kWave) {
@@ -98,7 +98,7 @@ void carve_plan(Carver* c, Experts* x) {
       x->pairs / kPlanRows + (x->pairs < x->experts ? x->pairs : x->experts));
   p.offsets = static_cast<int32_t*>(c->take(4 * (static_cast<size_t>(x->experts) + 1)));
   p.tile_count = static_cast<int32_t*>(c->take(4));
-  p.tiles = static_cast<int2*>(c->take(8 * static_cast<size_t>(p.most_tiles)));
+  p.tiles = static_cast<int4*>(c->take(16 * static_cast<size_t>(p.most_tiles)));
   p.rows = static_cast<int32_t*>(c->take(4 * n));
   p.token = static_cast<int32_t*>(c->take(4 * n));
   p.pos = static_cast<int32_t*>(c->take(4 * n));
@@ -113,11 +113,12 @@ size_t carve_saved(void* base, Experts* x) {
   return c.used;
 }
 
+// (rows past the last one may be read, for results that are not stored)
 size_t carve_forward(void* base, int32_t dtype, bool saved, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs);
   Carver c{static_cast<char*>(base)};
   if (!saved) carve_plan(&c, x);
-  x->act = c.take(size_of(dtype) * n * x->hidden);
+  x->act = c.take(size_of(dtype) * (n + kPlanRows) * x->hidden);
   x->y = static_cast<float*>(c.take(4 * n * x->dim));
   return c.used;
 }
@@ -126,7 +127,7 @@ size_t carve_backward(void* base, int32_t dtype, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs), s = size_of(dtype);
   Carver c{static_cast<char*>(base)};
   x->dot_tiles = (x->hidden + kDotColumns - 1) / kDotColumns;
-  x->dpre = c.take(2 * s * n * x->hidden);
+  x->dpre = c.take(2 * s * (n + kPlanRows) * x->hidden);
   x->wact = c.take(s * n * x->hidden);
   x->dots = static_cast<float*>(c.take(4 * n * x->dot_tiles));
   x->dxr = static_cast<float*>(c.take(4 * n * x->dim));

@@ -13,6 +13,8 @@
 
 #include "experts.h"
 
+#include <type_traits>
+
 #pragma clang fp contract(fast)
 
 namespace gsn {
@@ -30,7 +32,12 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define EX_WM 2
 #define EX_WN 4
 #endif
-constexpr int kRowBytes = 128;  // bytes of k (contiguous operands) staged at a time
+#ifndef EX_SA
+#define EX_SA 3
+#endif
+constexpr int64_t kFewTokens = 2;    // tokens up to which one launch makes the second product and the sum
+constexpr int64_t kFewPairs = 2048;  // pairs that a workgroup lists at most
+constexpr int kRowBytes = 128;  // bytes of k (contiguous operands) in a stage
 
 // 16 bytes of an operand in a lane: 8 or 4 values of k of row (lane & 15)
 union Frag {
@@ -59,15 +66,16 @@ __device__ __forceinline__ f32x4 multiply(const Frag& n, const Frag& m, f32x4 ac
 // Place of 16-byte chunk c in row r of a staged operand with k contiguous (8 chunks a row): the
 // 16 rows that a quarter wave reads at one k fall on different banks.
 __device__ __forceinline__ int chunk_k(int r, int c) { return c ^ ((r >> 1) & 7); }
-// The same with k as the row, `chunks` a row: the 4 (2-byte types) or 1 rows that 16 lanes read
-// 32 or 64 bytes of, and those of the wave's other quarters, fall on different banks.
+// The same with k as the row: the 4 (2-byte types) or 1 rows that 16 lanes read 32 or 64 bytes
+// of, and those of the wave's other quarters, fall on different banks.
 template <typename T>
 __device__ __forceinline__ int chunk_n(int k, int c) {
   if constexpr (sizeof(T) == 2) return c ^ (((k & 3) | ((k >> 1) & 4)) << 1);
   else return c ^ (((k >> 2) & 3) << 2);
 }
 
-// Fragment of 16 rows at `r0` and the s-th half of the staged k
+// Fragment of 16 rows at `r0` and the s-th half of a stage's k; R rows (k contiguous) or columns
+// (k as the row) in all.
 template <typename T, bool TR, int R>
 __device__ __forceinline__ Frag fragment(const char* tile, int r0, int s, int lane) {
   const int g = lane >> 4, i = lane & 15;
@@ -107,35 +115,32 @@ enum Kind {
 };
 
 // Four results of a row at column n, N columns in all
-template <bool VEC, typename T>
+template <typename T>
 __device__ __forceinline__ void store4(T* row, int32_t n, int32_t N, const float* v) {
-  if constexpr (VEC) {
-    Vec<T, 4> o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o.v[i] = from_float<T>(v[i]);
-    if (n < N) *reinterpret_cast<Vec<T, 4>*>(row + n) = o;
-    return;
-  }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (n + i < N) row[n + i] = from_float<T>(v[i]);
 }
-template <bool VEC, typename T>
+template <typename T>
 __device__ __forceinline__ void load4(const T* row, int32_t n, int32_t N, float* v) {
-  if constexpr (VEC) {
-    Vec<T, 4> o{};
-    if (n < N) o = *reinterpret_cast<const Vec<T, 4>*>(row + n);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = to_float(o.v[i]);
-    return;
-  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = n + i < N ? to_float(row[n + i]) : 0.0f;
 }
 
+// What the backward pass makes of d = dout . w2 at a pair's gate and up: the gradients of both,
+// the activation times the pair's weight, and the term of the weight's gradient.
+struct Gated {
+  float dg, du, wa, dot;
+};
+__device__ __forceinline__ Gated gated(float d, float g, float u, float w) {
+  const float s = sigmoid(g), sg = g * s, act = sg * u;
+  // silu' = s (1 + g (1 - s)), 1 - s without the cancellation
+  return Gated{w * d * u * (s + sg * sigmoid(-g)), w * d * sg, w * act, d * act};
+}
+
 // Results of a tile: rows m0 + 0 .. mrows - 1 of the weights' products, or rows row0 + 0 .. of
-// the others; columns from n0.  VEC: four results are one access.  Uses WN * BM floats of LDS.
-template <typename T, Kind KIND, int BM, int BN, int WM, int WN, bool VEC>
+// the others; columns from n0.  Uses WN * BM floats of LDS.
+template <typename T, Kind KIND, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 16][BN / WN / 16],
                                        float* dot, int32_t e, int32_t m0, int32_t mrows,
                                        int32_t n0, int64_t row0) {
@@ -163,10 +168,10 @@ __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 
             u[q] = acc[i][j + NT / 2][q];
             v[q] = g[q] * sigmoid(g[q]) * u[q];
           }
-          store4<VEC>(static_cast<T*>(x.act) + (row0 + m) * F, f, F, v);
+          store4(static_cast<T*>(x.act) + (row0 + m) * F, f, F, v);
           if (x.pre) {
-            store4<VEC>(x.pre + (row0 + m) * 2 * F, f, F, g);
-            store4<VEC>(x.pre + (row0 + m) * 2 * F + F, f, F, u);
+            store4(x.pre + (row0 + m) * 2 * F, f, F, g);
+            store4(x.pre + (row0 + m) * 2 * F + F, f, F, u);
           }
         }
       } else if constexpr (KIND == kBackwardGate) {
@@ -175,20 +180,19 @@ __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 
         for (int j = 0; j < NT; ++j) {
           const int32_t f = n0 + wn * (BN / WN) + j * 16 + lg;
           float g[4], u[4], dg[4], du[4], wa[4];
-          load4<VEC>(x.pre + (row0 + m) * 2 * F, f, F, g);
-          load4<VEC>(x.pre + (row0 + m) * 2 * F + F, f, F, u);
+          load4(x.pre + (row0 + m) * 2 * F, f, F, g);
+          load4(x.pre + (row0 + m) * 2 * F + F, f, F, u);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float s = sigmoid(g[q]), d = acc[i][j][q], sg = g[q] * s;
-            part += f + q < F ? d * (sg * u[q]) : 0.0f;
-            wa[q] = w * (sg * u[q]);
-            du[q] = w * d * sg;
-            // s (1 + g (1 - s)), 1 - s without the cancellation
-            dg[q] = w * d * u[q] * (s + sg * sigmoid(-g[q]));
+            const Gated r = gated(acc[i][j][q], g[q], u[q], w);
+            part += f + q < F ? r.dot : 0.0f;
+            wa[q] = r.wa;
+            du[q] = r.du;
+            dg[q] = r.dg;
           }
-          store4<VEC>(static_cast<T*>(x.wact) + (row0 + m) * F, f, F, wa);
-          store4<VEC>(static_cast<T*>(x.dpre) + (row0 + m) * 2 * F, f, F, dg);
-          store4<VEC>(static_cast<T*>(x.dpre) + (row0 + m) * 2 * F + F, f, F, du);
+          store4(static_cast<T*>(x.wact) + (row0 + m) * F, f, F, wa);
+          store4(static_cast<T*>(x.dpre) + (row0 + m) * 2 * F, f, F, dg);
+          store4(static_cast<T*>(x.dpre) + (row0 + m) * 2 * F + F, f, F, du);
         }
       } else {
         constexpr bool kF32 = KIND == kForwardOut || KIND == kBackwardIn;
@@ -201,8 +205,8 @@ __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 
           float v[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q];
-          if constexpr (kF32) store4<VEC>(c32 + (row0 + m) * N, n, N, v);
-          else store4<VEC>(ct + (e * M + m0 + m) * N, n, N, v);
+          if constexpr (kF32) store4(c32 + (row0 + m) * N, n, N, v);
+          else store4(ct + (e * M + m0 + m) * N, n, N, v);
         }
       }
     }
@@ -264,10 +268,10 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
     const int32_t id = blockIdx.x / tiles_n;
     if (id >= *x.plan.tile_count * (kPlanRows / BM)) return;
     n0 = blockIdx.x % tiles_n * kCols;
-    const int2 t = x.plan.tiles[id / (kPlanRows / BM)];
+    const int4 t = x.plan.tiles[id / (kPlanRows / BM)];
     e = t.x;
     m0 = 0;
-    row0 = t.y + id % (kPlanRows / BM) * BM;
+    row0 = t.y + (id - t.z * (kPlanRows / BM)) * BM;
     mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
     if (mrows <= 0) return;
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
@@ -371,8 +375,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
     __syncthreads();
   }
 
-  finish<T, KIND, BM, BN, WM, WN, false>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0,
-                                         row0);
+  finish<T, KIND, BM, BN, WM, WN>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0, row0);
 }
 
 // ------------------------------------------------------------------ aligned operands ----
@@ -381,7 +384,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
 __device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
 
 // 16 bytes a lane from its address to LDS offset `at` + 16 lane, without a register between.
-// The compiler does not count these loads: await_loads() does (with the builtin of this load the
+// The compiler does not count these loads: meet() does (with the builtin of this load the
 // compiler waits for all of them before every read of LDS, as it cannot tell the buffers apart).
 // m0 is a reserved register, which the compiler sets right before an instruction that reads it;
 // no other instruction of these kernels does.
@@ -391,22 +394,266 @@ __device__ __forceinline__ void load_to_lds(const void* p, uint32_t at) {
                : "s"(at), "v"(p)
                : "memory");
 }
-// Waits until they and this wave's reads of LDS are done.
-__device__ __forceinline__ void await_loads() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+__device__ __forceinline__ void load_word_to_lds(const void* p, uint32_t at) {  // 4 bytes a lane
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(at), "v"(p)
+               : "memory");
+}
+// Waits for the workgroup's other waves; before that until this wave's reads of LDS are done, or
+// its loads too.  One block of asm each, so that no access of LDS comes between.
+__device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
+__device__ __forceinline__ void meet_read() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+template <int LEFT>  // but for so many of the last loads
+__device__ __forceinline__ void meet_loaded() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
-// The tile's place in the XCD that runs it: workgroups go round the 8 XCDs, so each XCD takes a
-// contiguous eighth of the tiles, whose operands then stay in its own L2.
-__device__ __forceinline__ int32_t spread(int32_t total) {
-  const int32_t per = (total + 7) / 8;
-  const int32_t in = blockIdx.x >> 3, id = (blockIdx.x & 7) * per + in;
-  return in < per && id < total ? id : -1;
+// Waits until at most LEFT of this wave's loads and stores are under way; until its reads of LDS
+// are done.
+template <int LEFT>
+__device__ __forceinline__ void await_own() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ void await_reads() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// Workgroups go round the 8 XCDs.  Runs of `run` tiles go to one XCD, where the 32 tiles that its
+// CUs work on at a time share operands through its L2; the next run goes to the next XCD.
+__device__ __forceinline__ int32_t spread(int32_t total, int32_t run) {
+  const int32_t in = blockIdx.x >> 3;
+  const int32_t id = (in / run * 8 + (blockIdx.x & 7)) * run + in % run;
+  return id < total ? id : -1;
+}
+// Workgroups that cover `total` tiles in that order.
+inline uint32_t spread_grid(uint32_t total, uint32_t run) {
+  return (total + 8 * run - 1) / (8 * run) * (8 * run);
+}
+constexpr int32_t kRun = 32;
+// Place of a tile in a block of tiles_m x tiles_n, taken 4 tiles of m by all of n at a time, m
+// first: 32 tiles in a row have 4 + 8 tiles of operands.
+constexpr int32_t kTall = 4;
+__device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t tiles_n) {
+  const int32_t g = id / (kTall * tiles_n), in = id - g * kTall * tiles_n;
+  const int32_t left = tiles_m - g * kTall, tall = left < kTall ? left : kTall;
+  return int2{g * kTall + in % tall, in / tall};
+}
+
+// What a wave's lanes wrote to LDS before it, they may read from each other after it.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// 16 rows of COLS results of a wave, turned round in its own LDS: a lane has four columns of one
+// row, and 4 lanes of 64 share it, so stores from the lanes would go out in pieces of 32 or 64
+// bytes; from here they go out in whole rows of 64 to 256 bytes.
+template <typename U, int COLS>
+struct Turn {
+  static constexpr int kRow = COLS * static_cast<int>(sizeof(U)) + 16;  // (spreads the banks)
+  static constexpr int kBytes = 16 * kRow;
+  static constexpr int kW = 16 / static_cast<int>(sizeof(U));
+  static constexpr int kLanes = COLS / kW;  // of a row
+  static constexpr int kStores = 16 * kLanes / kWave;
+  char* at;
+  __device__ __forceinline__ void put(int row, int col, const float* v) const {
+    Vec<U, 4> o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.v[i] = from_float<U>(v[i]);
+    *reinterpret_cast<Vec<U, 4>*>(at + row * kRow + col * static_cast<int>(sizeof(U))) = o;
+  }
+  // rows `rows` of the 16, columns `cols` of a matrix with rows of ld elements
+  __device__ __forceinline__ void out(U* to, int64_t ld, int32_t rows, int32_t cols,
+                                      int lane) const {
+#pragma unroll
+    for (int i = 0; i < kStores; ++i) {
+      const int row = i * (kWave / kLanes) + lane / kLanes, col = lane % kLanes * kW;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(at + row * kRow + col * static_cast<int>(sizeof(U)));
+      if (row < rows && col < cols) *reinterpret_cast<u32x4*>(to + row * ld + col) = v;
+    }
+  }
+};
+
+// Results of a tile, as finish() makes them, by way of the stages' LDS, an equal part a wave.
+template <typename T, Kind KIND, int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void finish_rows(const Experts& x,
+                                            f32x4 (&acc)[BM / WM / 16][BN / WN / 16], char* smem,
+                                            uint32_t lds, int32_t e, int32_t m0, int32_t mrows,
+                                            int32_t n0, int64_t row0) {
+  constexpr int kThr = WM * WN * kWave, MT = BM / WM / 16, NT = BN / WN / 16, kW = BN / WN;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int wm = wave / WN, wn = wave % WN;
+  const int32_t D = x.dim, F = x.hidden;
+  const int32_t N = KIND == kForwardGate || KIND == kBackwardGate || KIND == kWeightsOut ? F : D;
+  const int li = lane & 15, lg = (lane >> 4) * 4;
+  constexpr int kRoom = 2 * (BM + BN) * kRowBytes / (WM * WN);  // of a wave
+  char* const room = smem + wave * kRoom;
+  const int32_t n = n0 + wn * (KIND == kForwardGate ? kW / 2 : kW);  // the wave's first column
+  const int32_t cols = N - n;
+
+  if constexpr (KIND == kForwardGate) {
+    constexpr int kC = kW / 2;
+    using Wide = Turn<float, kC>;
+    using Narrow = Turn<T, kC>;
+    static_assert(2 * Wide::kBytes + Narrow::kBytes <= kRoom);
+    const Narrow act{room};
+    const Wide gate{room + Narrow::kBytes}, up{room + Narrow::kBytes + Wide::kBytes};
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int32_t m = wm * (BM / WM) + i * 16;
+#pragma unroll
+      for (int j = 0; j < NT / 2; ++j) {
+        float g[4], u[4], v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          g[q] = acc[i][j][q];
+          u[q] = acc[i][j + NT / 2][q];
+          v[q] = g[q] * sigmoid(g[q]) * u[q];
+        }
+        act.put(li, j * 16 + lg, v);
+        if (x.pre) {
+          gate.put(li, j * 16 + lg, g);
+          up.put(li, j * 16 + lg, u);
+        }
+      }
+      wave_fence();
+      const int64_t row = row0 + m;
+      act.out(static_cast<T*>(x.act) + row * F + n, F, mrows - m, cols, lane);
+      if (x.pre) {
+        gate.out(x.pre + row * 2 * F + n, 2 * F, mrows - m, cols, lane);
+        up.out(x.pre + row * 2 * F + F + n, 2 * F, mrows - m, cols, lane);
+      }
+      wave_fence();
+    }
+  } else if constexpr (KIND == kBackwardGate) {
+    // The gates and ups of 16 rows come to LDS while the rows before are worked on.
+    using Narrow = Turn<T, kW>;
+    constexpr int kPre = 16 * kW * 4;  // bytes of 16 rows of gates, or of ups
+    // three results turned at once, or (4-byte ones) one after another in the same place
+    constexpr int kTurns = sizeof(T) == 2 ? 3 : 1;
+    static_assert(2 * kPre + kTurns * Narrow::kBytes <= kRoom && kPre % 1024 == 0);
+    const char* const pre = room;
+    char* const turns = room + 2 * kPre;
+    const Narrow dgate{turns}, dup{turns + (kTurns > 1 ? 1 : 0) * Narrow::kBytes},
+        wact{turns + (kTurns > 1 ? 2 : 0) * Narrow::kBytes};
+    const uint32_t pre_at = lds + wave * kRoom;
+    constexpr int kLanes = kW / 4;  // of a row of 4-byte elements
+    const auto fetch = [&](int i) {
+      // (rows and columns past the ends load the last ones)
+      const int32_t m = wm * (BM / WM) + i * 16;
+      const int col = lane % kLanes * 4;
+      const int32_t f = col < cols ? n + col : F - 4;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int v = 0; v < kPre / 1024; ++v) {
+          int32_t r = m + v * (kWave / kLanes) + lane / kLanes;
+          if (r >= mrows) r = mrows - 1;
+          load_to_lds(x.pre + (row0 + r) * 2 * F + h * F + f, pre_at + h * kPre + v * 1024);
+        }
+    };
+    fetch(0);
+    float parts[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int32_t m = wm * (BM / WM) + i * 16;
+      const float w = m + li < mrows ? x.weights[x.plan.rows[row0 + m + li]] : 0.0f;
+      // (the stores since then count too)
+      if (i == 0) await_own<0>();
+      else await_own<kTurns * Narrow::kStores>();
+      const int64_t row = row0 + m;
+      T* const to_dg = static_cast<T*>(x.dpre) + row * 2 * F + n;
+      T* const to_wa = static_cast<T*>(x.wact) + row * F + n;
+      float part = 0.0f;
+#pragma unroll
+      for (int turn = 0; turn < 4 - kTurns; ++turn) {  // 0: all at once, or the gate's gradient
+        if (turn > 0) {
+          (turn == 1 ? dgate.out(to_dg, 2 * F, mrows - m, cols, lane)
+                     : dup.out(to_dg + F, 2 * F, mrows - m, cols, lane));
+          wave_fence();
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const int at = (li * kW + j * 16 + lg) * 4;
+          const f32x4 g = *reinterpret_cast<const f32x4*>(pre + at);
+          const f32x4 u = *reinterpret_cast<const f32x4*>(pre + kPre + at);
+          float dg[4], du[4], wa[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const Gated r = gated(acc[i][j][q], g[q], u[q], w);
+            if (turn == 0) part += j * 16 + lg < cols ? r.dot : 0.0f;
+            dg[q] = r.dg;
+            du[q] = r.du;
+            wa[q] = r.wa;
+          }
+          if (turn == 0) dgate.put(li, j * 16 + lg, dg);
+          if (kTurns > 1 || turn == 1) dup.put(li, j * 16 + lg, du);
+          if (kTurns > 1 || turn == 2) wact.put(li, j * 16 + lg, wa);
+        }
+        wave_fence();
+      }
+      parts[i] = part;
+      if (i + 1 < MT) {
+        await_reads();
+        fetch(i + 1);
+      }
+      if constexpr (kTurns > 1) {
+        dgate.out(to_dg, 2 * F, mrows - m, cols, lane);
+        dup.out(to_dg + F, 2 * F, mrows - m, cols, lane);
+      }
+      wact.out(to_wa, F, mrows - m, cols, lane);
+      wave_fence();
+    }
+    __syncthreads();
+    float* const dot = reinterpret_cast<float*>(smem);  // [WN][BM]
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      float part = parts[i];
+      part += __shfl_xor(part, 16);
+      part += __shfl_xor(part, 32);
+      if (lane < 16) dot[wn * BM + wm * (BM / WM) + i * 16 + li] = part;
+    }
+    __syncthreads();
+    for (int32_t m = tid; m < BM && m < mrows; m += kThr) {
+      float s = 0.0f;
+#pragma unroll
+      for (int q = 0; q < WN; ++q) s += dot[q * BM + m];
+      x.dots[(row0 + m) * x.dot_tiles + n0 / BN] = s;
+    }
+  } else {
+    constexpr bool kF32 = KIND == kForwardOut || KIND == kBackwardIn;
+    using U = std::conditional_t<kF32, float, T>;
+    const Turn<U, kW> turn{room};
+    static_assert(Turn<U, kW>::kBytes <= kRoom);
+    U* const to = static_cast<U*>(KIND == kForwardOut    ? static_cast<void*>(x.y)
+                                  : KIND == kBackwardIn  ? static_cast<void*>(x.dxr)
+                                  : KIND == kWeightsIn   ? x.dw1
+                                                         : x.dw2);
+    const int64_t M = KIND == kWeightsIn ? 2 * F : D;
+    const int64_t first = kF32 ? row0 : e * M + m0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int32_t m = wm * (BM / WM) + i * 16;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        turn.put(li, j * 16 + lg, v);
+      }
+      wave_fence();
+      turn.out(to + (first + m) * N + n, N, mrows - m, cols, lane);
+      wave_fence();
+    }
+  }
 }
 
 // One tile of BM x BN by WM x WN waves.  Rows of every operand start at a multiple of 16 bytes
 // and hold a multiple of 16 bytes.
-template <typename T, Kind KIND, int BM, int BN, int WM, int WN>
+template <typename T, Kind KIND, int BM, int BN, int WM, int WN, int SA, int SB>
 __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   constexpr int kThr = WM * WN * kWave, kWaves = WM * WN;
   constexpr int kE = 16 / sizeof(T);          // elements of a chunk
@@ -416,8 +663,11 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   constexpr bool kTrB = kWeightsKind || KIND == kBackwardGate || KIND == kBackwardIn;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;  // chunks a lane loads of each operand
-  constexpr int kStage = (BM + BN) * kRowBytes;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage];
+  // SA and SB places for a stage of A and of B; of gathered k, the tokens of four stages
+  constexpr int kSlotA = BM * kRowBytes, kSlotB = BN * kRowBytes;
+  static_assert(SB == 2 && (SA == 2 || SA == 3));
+  __shared__ __attribute__((aligned(1024))) char
+      smem[SA * kSlotA + SB * kSlotB + (kWeightsKind ? 4 * kWave * 4 : 0)];
 
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -432,154 +682,153 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    int32_t id = spread(x.experts * tiles_m * tiles_n);
+    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun);
     if (id < 0) return;
-    n0 = id % tiles_n * BN;
-    id /= tiles_n;
-    m0 = id % tiles_m * BM;
-    e = id / tiles_m;
+    e = id / (tiles_m * tiles_n);
+    const int2 at = tile_place(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    m0 = at.x * BM;
+    n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
     constexpr int kParts = kPlanRows / BM;
-    int32_t id = spread(*x.plan.tile_count * kParts * tiles_n);
+    const int32_t id = spread(*x.plan.tile_count * kParts * tiles_n, kRun);
     if (id < 0) return;
-    n0 = id % tiles_n * kCols;
-    id /= tiles_n;
-    const int2 t = x.plan.tiles[id / kParts];
+    const int4 t = x.plan.tiles[id / (kParts * tiles_n)];
+    const int2 at = tile_place(id - t.z * kParts * tiles_n, t.w * kParts, tiles_n);
     e = t.x;
     m0 = 0;
-    row0 = t.y + id % kParts * BM;
+    row0 = t.y + at.x * BM;
+    n0 = at.y * kCols;
     mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
     if (mrows <= 0) return;
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
-  // What this lane loads.  k contiguous: chunk (row, c) of the staged rows, at a pointer that
-  // moves on by 128 bytes; rows past the last load the last one (their results are not stored).
-  // k as rows: chunk c of row k, at a pointer that moves on by kBK rows, or of a gathered row.
-  const char* pa[LA];
-  const char* pb[LB];
-  int32_t ka[LA], kb[LB];  // k of the chunk in the first stage
+  // What this lane loads of an operand: chunk i = j kThr + tid of a stage for j = 0, 1, ..  With k
+  // contiguous that is chunk c of row r + j kStepK, c the same for all j; with k as the row, chunk
+  // c of row r + j kStep of the stage.  An address is the lane's own, which moves on from stage to
+  // stage, and the same step for all lanes from one j to the next; gathered rows have their
+  // token's row instead.  What lies outside loads zeros, except rows past an expert's last ones,
+  // whose results are not stored (act and dpre have room for them).
   const char* const zeros = reinterpret_cast<const char*>(kZeros);
-#pragma unroll
-  for (int j = 0; j < LA; ++j) {
-    const int i = (j * kWaves + wave) * kWave + lane;
-    if constexpr (!kTrA) {
-      const int r = i >> 3, c = chunk_k(r, i & 7);
-      const int64_t row = row0 + (r < mrows ? r : mrows - 1);
-      const T* p;
-      if constexpr (KIND == kForwardGate)
-        p = static_cast<const T*>(x.x) + x.plan.token[row] * x.x_stride;
-      else if constexpr (KIND == kForwardOut)
-        p = static_cast<const T*>(x.act) + row * F;
-      else if constexpr (KIND == kBackwardGate)
-        p = static_cast<const T*>(x.dout) + static_cast<int64_t>(x.plan.token[row]) * D;
-      else
-        p = static_cast<const T*>(x.dpre) + row * 2 * F;
-      ka[j] = c * kE;
-      pa[j] = reinterpret_cast<const char*>(p + c * kE);
-    } else {
-      constexpr int kC = BM / kE;
-      const int r = i / kC, c = chunk_n<T>(r, i % kC);
-      ka[j] = r;
-      const int32_t m = m0 + c * kE;
-      // past the last column: no k (zeros)
-      if (c * kE >= mrows) ka[j] = INT32_MAX / 2;
-      if constexpr (KIND == kWeightsIn)
-        pa[j] = reinterpret_cast<const char*>(static_cast<const T*>(x.dpre) + (row0 + r) * 2 * F +
-                                              m);
-      else
-        pa[j] = reinterpret_cast<const char*>(static_cast<const T*>(x.dout) + m);
-    }
+  constexpr int kStepK = kThr / 8, kCA = BM / kE, kCB = BN / kE;
+  constexpr int kStepA = kTrA ? kThr / kCA : kStepK, kStepB = kTrB ? kThr / kCB : kStepK;
+  constexpr int kSize = static_cast<int>(sizeof(T));
+  constexpr bool kGatherA = KIND == kForwardGate || KIND == kBackwardGate || KIND == kWeightsOut;
+  constexpr bool kGatherB = KIND == kWeightsIn;
+  const int ra = kTrA ? tid / kCA : tid >> 3, rb = kTrB ? tid / kCB : tid >> 3;
+  const auto col_a = [&](int j) { return chunk_n<T>(ra + j * kStepA, tid % kCA); };
+  const auto col_b = [&](int j) { return chunk_n<T>(rb + j * kStepB, tid % kCB); };
+  // (2-byte types: kStep is a multiple of 16, which leaves the chunk's place alone)
+  constexpr bool kSame = sizeof(T) == 2;
+  const int ca = kTrA ? col_a(0) : chunk_k(ra, tid & 7);
+  const int cb = kTrB ? col_b(0) : chunk_k(rb, tid & 7);
+  const int32_t ka = kTrA ? ra : ca * kE, kb = kTrB ? rb : cb * kE;  // k of j = 0 in stage 0
+  int64_t lda, ldb;  // bytes from row to row
+  const T *a0, *b0;
+  if constexpr (KIND == kForwardGate) {
+    a0 = static_cast<const T*>(x.x);
+    lda = x.x_stride * kSize;
+    // a wave's columns: half of them gates, half the same columns' ups
+    constexpr int kW = BN / WN, kHalf = kW / 2;
+    static_assert(kW == kStepK);
+    b0 = static_cast<const T*>(x.w1) +
+         (static_cast<int64_t>(e) * 2 * F + rb / kHalf * F + n0 + rb % kHalf) * D;
+    ldb = int64_t{kSize} * D;
+  } else if constexpr (KIND == kForwardOut) {
+    a0 = static_cast<const T*>(x.act) + (row0 + ra) * F;
+    lda = int64_t{kSize} * F;
+    b0 = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n0 + rb) * F;
+    ldb = lda;
+  } else if constexpr (KIND == kBackwardGate) {
+    a0 = static_cast<const T*>(x.dout);
+    lda = int64_t{kSize} * D;
+    b0 = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + rb) * F + n0;
+    ldb = int64_t{kSize} * F;
+  } else if constexpr (KIND == kBackwardIn) {
+    a0 = static_cast<const T*>(x.dpre) + (row0 + ra) * 2 * F;
+    lda = int64_t{kSize} * 2 * F;
+    b0 = static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + rb) * D + n0;
+    ldb = int64_t{kSize} * D;
+  } else if constexpr (KIND == kWeightsIn) {
+    a0 = static_cast<const T*>(x.dpre) + (row0 + ra) * 2 * F + m0;
+    lda = int64_t{kSize} * 2 * F;
+    b0 = static_cast<const T*>(x.x) + n0;
+    ldb = x.x_stride * kSize;
+  } else {
+    a0 = static_cast<const T*>(x.dout) + m0;
+    lda = int64_t{kSize} * D;
+    b0 = static_cast<const T*>(x.wact) + (row0 + rb) * F + n0;
+    ldb = int64_t{kSize} * F;
   }
-#pragma unroll
-  for (int j = 0; j < LB; ++j) {
-    const int i = (j * kWaves + wave) * kWave + lane;
-    if constexpr (!kTrB) {
-      const int r = i >> 3, c = chunk_k(r, i & 7);
-      const T* p;
-      if constexpr (KIND == kForwardGate) {
-        constexpr int kW = BN / WN, kHalf = kW / 2;
-        int32_t f = n0 + r / kW * kHalf + r % kHalf;
-        if (f >= F) f = F - 1;
-        p = static_cast<const T*>(x.w1) +
-            (static_cast<int64_t>(e) * 2 * F + r % kW / kHalf * F + f) * D;
-      } else {
-        const int32_t n = n0 + r < D ? n0 + r : D - 1;
-        p = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n) * F;
-      }
-      kb[j] = c * kE;
-      pb[j] = reinterpret_cast<const char*>(p + c * kE);
-    } else {
-      constexpr int kC = BN / kE;
-      const int r = i / kC, c = chunk_n<T>(r, i % kC);
-      kb[j] = r;
-      const int32_t n = n0 + c * kE;
-      if (n >= N) kb[j] = INT32_MAX / 2;
-      const T* p;
-      if constexpr (KIND == kWeightsIn) p = static_cast<const T*>(x.x) + n;
-      else if constexpr (KIND == kWeightsOut)
-        p = static_cast<const T*>(x.wact) + (row0 + r) * F + n;
-      else if constexpr (KIND == kBackwardGate)
-        p = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + r) * F + n;
-      else
-        p = static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + r) * D + n;
-      pb[j] = reinterpret_cast<const char*>(p);
-    }
-  }
-  // bytes from one stage to the next
-  const int64_t step_a = !kTrA ? kRowBytes : int64_t{kBK} * 2 * F * sizeof(T);
-  const int64_t step_b = !kTrB ? kRowBytes
-                         : KIND == kBackwardIn ? int64_t{kBK} * D * sizeof(T)
-                                               : int64_t{kBK} * F * sizeof(T);
+  const char* pa = reinterpret_cast<const char*>(a0 + ca * kE);
+  const char* pb = reinterpret_cast<const char*>(b0 + cb * kE);
+  const int64_t step_a = !kTrA ? kRowBytes : kGatherA ? 0 : kBK * lda;
+  const int64_t step_b = !kTrB ? kRowBytes : kGatherB ? 0 : kBK * ldb;
+  // rows of B with k contiguous: of w1 the next kHalf gates and ups, of w2 the next kStepK columns
+  constexpr int kNextB = KIND == kForwardGate ? kStepK / 2 : kStepB;
+  const int32_t nb = n0 + (KIND == kForwardGate ? rb % kNextB : rb);
   const uint32_t lds = static_cast<uint32_t>(
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem));
+  const uint32_t at_a = lds + wave * (kWave * 16), at_b = at_a + SA * kSlotA;
 
-  // Rows gathered as k: the tokens of the next stage to load are read one stage before.
-  constexpr int LG = KIND == kWeightsIn ? LB : KIND == kWeightsOut ? LA : 1;
-  int32_t token[LG];
-  const auto gather = [&](int32_t k0) {
-    if constexpr (kWeightsKind) {
-#pragma unroll
-      for (int j = 0; j < LG; ++j) {
-        const int32_t k = k0 + (KIND == kWeightsIn ? kb[j] : ka[j]);
-        token[j] = k < K ? x.plan.token[row0 + k] : 0;
-      }
-    }
+  // Rows gathered as k: their tokens come to LDS too, a stage before the loads that need them, by
+  // every wave alike (the same values to the same place; of 64 a stage uses the first kBK).
+  const int32_t* const tokens = reinterpret_cast<const int32_t*>(smem + SA * kSlotA + SB * kSlotB);
+  const auto load_tokens = [&](int32_t h) {
+    const int32_t k = h * kBK + lane;
+    load_word_to_lds(x.plan.token + row0 + (k < K ? k : K - 1),
+                     lds + SA * kSlotA + SB * kSlotB + (h & 3) * (kWave * 4));
   };
-  const int64_t row_bytes =
-      (KIND == kWeightsIn ? x.x_stride : static_cast<int64_t>(D)) * static_cast<int>(sizeof(T));
-  const auto issue = [&](int32_t k0, int buf) {
-    const uint32_t at = lds + buf * kStage + wave * (kWave * 16);
-    const char* p[LA + LB];
+  int32_t token[kGatherB ? LB : LA];  // of the gathered operand
+  const auto read_tokens = [&](int32_t h) {
+#pragma unroll
+    for (int j = 0; j < (kGatherB ? LB : LA); ++j)
+      token[j] = tokens[(h & 3) * kWave + (kGatherB ? rb + j * kStepB : ra + j * kStepA)];
+  };
+  if constexpr (kGatherA && !kTrA) {
 #pragma unroll
     for (int j = 0; j < LA; ++j) {
-      p[j] = zeros;
-      if constexpr (KIND == kWeightsOut) {
-        if (k0 + ka[j] < K) p[j] = pa[j] + token[j] * row_bytes;
-      } else {
-        if (k0 + ka[j] < K) p[j] = pa[j];
-        pa[j] += step_a;
-      }
+      const int32_t r = ra + j * kStepA;
+      token[j] = x.plan.token[row0 + (r < mrows ? r : mrows - 1)];
     }
+  }
+  // Loads of stage h to their slots; then the addresses are those of the next stage.
+  const auto load_a = [&](int32_t h, int slot) {
+#pragma unroll
+    for (int j = 0; j < LA; ++j) {
+      const char* p = pa;
+      if constexpr (kGatherA) p += token[j] * lda;
+      else p += j * (kStepA * lda);
+      bool in = h * kBK + ka + (kTrA ? j * kStepA : 0) < K;
+      if constexpr (kTrA) {
+        const int c = kSame ? ca : col_a(j);
+        if constexpr (!kSame) p += (c - ca) * 16;
+        in = in && c * kE < mrows;
+      }
+      load_to_lds(in ? p : zeros, at_a + slot * kSlotA + j * (kThr * 16));
+    }
+    pa += step_a;
+  };
+  const auto load_b = [&](int32_t h, int slot) {
 #pragma unroll
     for (int j = 0; j < LB; ++j) {
-      p[LA + j] = zeros;
-      if constexpr (KIND == kWeightsIn) {
-        if (k0 + kb[j] < K) p[LA + j] = pb[j] + token[j] * row_bytes;
+      const char* p = pb;
+      if constexpr (kGatherB) p += token[j] * ldb;
+      else p += j * (kNextB * ldb);
+      bool in = h * kBK + kb + (kTrB ? j * kStepB : 0) < K;
+      if constexpr (kTrB) {
+        const int c = kSame ? cb : col_b(j);
+        if constexpr (!kSame) p += (c - cb) * 16;
+        in = in && n0 + c * kE < N;
       } else {
-        if (k0 + kb[j] < K) p[LA + j] = pb[j];
-        pb[j] += step_b;
+        in = in && nb + j * kNextB < N;
       }
+      load_to_lds(in ? p : zeros, at_b + slot * kSlotB + j * (kThr * 16));
     }
-#pragma unroll
-    for (int j = 0; j < LA; ++j) load_to_lds(p[j], at + j * (kThr * 16));
-#pragma unroll
-    for (int j = 0; j < LB; ++j)
-      load_to_lds(p[LA + j], at + BM * kRowBytes + j * (kThr * 16));
-    gather(k0 + kBK);
+    pb += step_b;
   };
 
   f32x4 acc[MT][NT];
@@ -588,34 +837,311 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  gather(0);
-  if (K > 0) issue(0, 0);
-  int buf = 0;
-  for (int32_t k0 = 0; k0 < K; k0 += kBK, buf ^= 1) {
-    await_loads();
-    __builtin_amdgcn_s_barrier();
-    if (k0 + kBK < K) issue(k0 + kBK, buf ^ 1);
-    const char* const sa = smem + buf * kStage;
-    const char* const sb = sa + BM * kRowBytes;
+  // Each SIMD has a wave of the workgroup's first half and one of its second.  The halves work in
+  // opposite phases, with a barrier at the end of each: while one multiplies, the other reads the
+  // fragments of its next products from LDS and sends loads out, so neither waits in the other's
+  // way.  A stage is four phases of a wave: read half of k, multiply, read the other half,
+  // multiply.  With three places for A its loads go out in the third phase, two stages ahead, and
+  // those of B in the first, one ahead; with two, all in the first.  They are awaited at the end
+  // of the third phase, which is before either half reads what they bring; a place is loaded again
+  // when the later half has read its last fragment of it, a phase before.  The scheduling barriers
+  // hold the compiler to the phases.
+  const bool late = wave >= kWaves / 2;
+  Frag fa[MT], fb[NT];
+  const auto read = [&](int s, int slot_a, int slot_b) {
+    const char* const sa = smem + slot_a * kSlotA;
+    const char* const sb = smem + SA * kSlotA + slot_b * kSlotB;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      Frag fa[MT], fb[NT];
+    for (int j = 0; j < NT; ++j)
+      fb[j] = fragment<T, kTrB, BN>(sb, wn * (BN / WN) + j * 16, s, lane);
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-        fa[i] = fragment<T, kTrA, BM>(sa, wm * (BM / WM) + i * 16, s, lane);
+    for (int i = 0; i < MT; ++i)
+      fa[i] = fragment<T, kTrA, BM>(sa, wm * (BM / WM) + i * 16, s, lane);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto multiply_all = [&] {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        fb[j] = fragment<T, kTrB, BN>(sb, wn * (BN / WN) + j * 16, s, lane);
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+      for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int sa = 0, sb = 0;  // this stage's places
+  const auto after_a = [&](int n) { return sa + n >= SA ? sa + n - SA : sa + n; };
+  // next_a: A of stage h + SA - 1 is loaded; next_b: B of stage h + 1
+  const auto stage = [&](auto next_a, auto next_b, int32_t h) {
+    constexpr bool kNextA = decltype(next_a)::value, kMore = decltype(next_b)::value;
+    read(0, sa, sb);
+    if constexpr (kMore) {
+      if constexpr (SA == 2) load_a(h + 1, sa ^ 1);
+      load_b(h + 1, sb ^ 1);
+      if constexpr (kWeightsKind) load_tokens(h + 3);
     }
+    meet_read();
+    multiply_all();
+    meet();
+    read(1, sa, sb);
+    if constexpr (SA == 3 && kNextA) load_a(h + 2, after_a(2));
+    if constexpr (kMore && kWeightsKind) read_tokens(h + 2);
+    if constexpr (SA == 3 && kNextA) meet_loaded<LA>();
+    else if constexpr (kMore) meet_loaded<0>();
+    else meet_read();
+    multiply_all();
+    meet();
+    sa = after_a(1);
+    sb ^= 1;
+  };
+
+  if (K > 0) {
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    const int32_t stages = (K + kBK - 1) / kBK;
+    if constexpr (kWeightsKind) {
+      load_tokens(0);
+      load_tokens(1);
+      load_tokens(2);
+      meet_loaded<0>();
+      read_tokens(0);
+    }
+    load_a(0, 0);
+    load_b(0, 0);
+    if constexpr (SA == 3) load_a(1, 1);
+    if constexpr (kWeightsKind) read_tokens(1);
+    meet_loaded<SA == 3 ? LA : 0>();
+    if (late) meet();
+    int32_t h = 0;
+    for (; h + SA - 1 < stages; ++h) stage(yes, yes, h);
+    if (SA == 3 && h + 1 < stages) {
+      stage(no, yes, h);
+      ++h;
+    }
+    stage(no, no, h);
+    if (!late) meet();
   }
-  if constexpr (KIND == kBackwardGate) __syncthreads();
-  finish<T, KIND, BM, BN, WM, WN, true>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0,
-                                        row0);
+  __syncthreads();
+  finish_rows<T, KIND, BM, BN, WM, WN>(x, acc, smem, lds, e, m0, mrows, n0, row0);
 }
+// ------------------------------------------------------------------------- few pairs ----
+
+// A lane's 16 bytes of a row of K elements at k, zeros past its end (INSIDE: there is none in
+// them).  Rows start at any element.
+template <bool INSIDE, typename T>
+__device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
+  constexpr int kE = 16 / sizeof(T);
+  typedef T Loose __attribute__((ext_vector_type(kE), aligned(sizeof(T))));
+  Frag f;
+  if (INSIDE || k + kE <= K) {
+    f.u = __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose*>(row + k));
+  } else {
+    Vec<T, kE> v;
+#pragma unroll
+    for (int j = 0; j < kE; ++j) v.v[j] = k + j < K ? row[k + j] : from_float<T>(0.0f);
+    f.u = __builtin_bit_cast(u32x4, v);
+  }
+  return f;
+}
+
+// With a few pairs an expert the products read every weight once and are bound by that: no
+// staging, a wave loads 16 rows of weights straight into fragments and multiplies them with 16
+// rows of tokens.  A workgroup takes one expert and 16 GT columns; its four waves each take a
+// quarter of k, joined through LDS.  An expert's pairs are listed from all ids by every workgroup
+// (rows of act and y are the pairs' numbers: no plan), 16 MT at a time.
+template <typename T, bool GATE, int MT, int GT>
+__global__ __launch_bounds__(256) void ex_few(Experts x) {
+  constexpr int kE = 16 / sizeof(T), kStep = 8 * kE;  // 128 bytes of k a step
+  constexpr int NT = GATE ? 2 * GT : GT;
+  constexpr int kCols = 16 * GT, kRows = 16 * MT;
+  __shared__ int32_t list[kFewPairs];
+  __shared__ int32_t found[5];
+  __shared__ float part[4][MT * NT][64][4];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int g = lane >> 4, i = lane & 15;
+  const int32_t D = x.dim, F = x.hidden, pairs = static_cast<int32_t>(x.pairs);
+  const int32_t N = GATE ? F : D, K = GATE ? D : F;
+  const int32_t n0 = blockIdx.x * kCols;
+
+  // the expert: of a pair (unless an earlier one has it), where there are fewer pairs than experts
+  int32_t e = blockIdx.y;
+  const bool by_pair = pairs <= x.experts;
+  if (by_pair) {
+    e = x.ids[blockIdx.y];
+    if (e < 0 || e >= x.experts) return;
+  }
+  int32_t count = 0;
+  bool again = false;
+  for (int32_t j0 = 0; j0 < pairs; j0 += 256) {
+    const int32_t j = j0 + tid;
+    const bool hit = j < pairs && x.ids[j] == e;
+    again |= by_pair && hit && j < static_cast<int32_t>(blockIdx.y);
+    const uint64_t m = __ballot(hit);
+    if (lane == 0) found[wave] = __popcll(m);
+    __syncthreads();
+    int32_t at = count;
+    for (int w = 0; w < wave; ++w) at += found[w];
+    if (hit) list[at + __popcll(m & ((uint64_t{1} << lane) - 1))] = j;
+    count += found[0] + found[1] + found[2] + found[3];
+    __syncthreads();
+  }
+  if (__syncthreads_or(again) || count == 0) return;
+
+  const T* w[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    int32_t n = n0 + t % GT * 16 + i;
+    if (n >= N) n = N - 1;
+    w[t] = GATE ? static_cast<const T*>(x.w1) +
+                      (static_cast<int64_t>(e) * 2 * F + (t >= GT ? F : 0) + n) * D
+                : static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n) * F;
+  }
+  const int32_t steps = (K + kStep - 1) / kStep, per = (steps + 3) / 4;
+  const int32_t k_begin = wave * per * kStep;
+  const int32_t k_end = (wave + 1) * per * kStep < K ? (wave + 1) * per * kStep : K;
+
+  for (int32_t r0 = 0; r0 < count; r0 += kRows) {
+    const T* a[MT];
+    bool live[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int32_t r = r0 + t * 16 + i;
+      live[t] = r < count;
+      const int32_t j = list[live[t] ? r : 0];
+      a[t] = GATE ? static_cast<const T*>(x.x) + static_cast<int64_t>(j / x.top) * x.x_stride
+                  : static_cast<const T*>(x.act) + static_cast<int64_t>(j) * F;
+    }
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const auto step = [&](auto inside, int32_t k0) {
+      constexpr bool kIn = decltype(inside)::value;
+      Frag fw[2][NT], fa[2][MT];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int32_t k = k0 + (4 * h + g) * kE;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) fw[h][n] = row_chunk<kIn>(w[n], k, K);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          fa[h][t].u = u32x4{0, 0, 0, 0};
+          if (live[t]) fa[h][t] = row_chunk<kIn>(a[t], k, K);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[t][n] = multiply<T>(fw[h][n], fa[h][t], acc[t][n]);
+    };
+    int32_t k0 = k_begin;
+    for (; k0 + kStep <= k_end; k0 += kStep) step(std::true_type(), k0);
+    if (k0 < k_end) step(std::false_type(), k0);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        *reinterpret_cast<f32x4*>(part[wave][t * NT + n][lane]) = acc[t][n];
+    __syncthreads();
+    const int32_t rows = count - r0 < kRows ? count - r0 : kRows;
+    for (int o = tid; o < rows * kCols; o += 256) {
+      const int m = o / kCols, c = o % kCols, n = n0 + c;
+      if (n >= N) continue;
+      const int32_t j = list[r0 + m];
+      const int at = ((c & 15) >> 2) * 16 + (m & 15);
+      const auto sum = [&](int t) {
+        float s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s += part[v][(m >> 4) * NT + t][at][c & 3];
+        return s;
+      };
+      if constexpr (GATE) {
+        const float gate = sum(c >> 4), up = sum(GT + (c >> 4));
+        static_cast<T*>(x.act)[static_cast<int64_t>(j) * F + n] =
+            from_float<T>(gate * sigmoid(gate) * up);
+      } else {
+        x.y[static_cast<int64_t>(j) * D + n] = sum(c >> 4);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The second product and the sum over a token's experts in one launch, for one or two tokens (with
+// 2 tokens 41 us a call, 47 us as two launches; with 4 as long, with 16 164 us and 135 us): a
+// workgroup takes 16 columns of one token, two waves an expert (half of k each).
+template <typename T>
+__global__ __launch_bounds__(1024) void ex_few_join(Experts x) {
+  constexpr int kE = 16 / sizeof(T), kStep = 8 * kE;
+  __shared__ float part[2][64][16];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int waves = blockDim.x / kWave;
+  const int g = lane >> 4, i = lane & 15;
+  const int32_t D = x.dim, F = x.hidden;
+  const int32_t n0 = blockIdx.x * 16, half = wave & 1;
+  const int64_t t = blockIdx.y;
+  const int32_t n = n0 + i < D ? n0 + i : D - 1;
+  const int32_t steps = (F + kStep - 1) / kStep, per = (steps + 1) / 2;
+  const int32_t k_begin = half * per * kStep;
+  const int32_t k_end = (half + 1) * per * kStep < F ? (half + 1) * per * kStep : F;
+  for (int q = wave >> 1; q < x.top; q += waves >> 1) {
+    const int64_t j = t * x.top + q;
+    const int32_t e = x.ids[j];
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (e >= 0 && e < x.experts) {
+      const T* w = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n) * F;
+      const T* a = static_cast<const T*>(x.act) + j * F;
+      const auto step = [&](auto inside, int32_t k0) {
+        constexpr bool kIn = decltype(inside)::value;
+        Frag fw[2], fa[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int32_t k = k0 + (4 * h + g) * kE;
+          fw[h] = row_chunk<kIn>(w, k, F);
+          fa[h].u = u32x4{0, 0, 0, 0};
+          if (i == 0) fa[h] = row_chunk<kIn>(a, k, F);
+        }
+        acc = multiply<T>(fw[0], fa[0], acc);
+        acc = multiply<T>(fw[1], fa[1], acc);
+      };
+      int32_t k0 = k_begin;
+      for (; k0 + kStep <= k_end; k0 += kStep) step(std::true_type(), k0);
+      if (k0 < k_end) step(std::false_type(), k0);
+    }
+    if (i == 0) *reinterpret_cast<f32x4*>(&part[half][q][g * 4]) = acc;
+  }
+  __syncthreads();
+  if (threadIdx.x < 16 && n0 + static_cast<int>(threadIdx.x) < D) {
+    float s = 0.0f;
+    for (int q = 0; q < x.top; ++q) {
+      const int64_t j = t * x.top + q;
+      const int32_t e = x.ids[j];
+      if (e >= 0 && e < x.experts)
+        s += x.weights[j] * (part[0][q][threadIdx.x] + part[1][q][threadIdx.x]);
+    }
+    static_cast<T*>(x.out)[t * D + n0 + threadIdx.x] = from_float<T>(s);
+  }
+}
+
+// The sum over a token's pairs where rows of y are the pairs' numbers.
+template <typename T>
+__global__ __launch_bounds__(256) void ex_pairs_join(Experts x) {
+  const int64_t t = blockIdx.y;
+  const int32_t d = blockIdx.x * 256 + threadIdx.x;
+  if (d >= x.dim) return;
+  float s = 0.0f;
+  for (int k = 0; k < x.top; ++k) {
+    const int64_t j = t * x.top + k;
+    const int32_t e = x.ids[j];
+    if (e >= 0 && e < x.experts) s += x.weights[j] * x.y[j * x.dim + d];
+  }
+  static_cast<T*>(x.out)[t * x.dim + d] = from_float<T>(s);
+}
+
 // out[t] = sum_k weight[t, k] y[row of (t, k)], k ascending, in binary32, rounded once
 template <typename T, bool WEIGHTED>
 __global__ __launch_bounds__(256) void ex_join(Experts x, const float* __restrict__ y,
@@ -669,8 +1195,8 @@ void product(Experts x, hipStream_t st) {
     uint32_t grid = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
                     : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
                                           : x.plan.most_tiles * (kPlanRows / BM) * n;
-    grid = (grid + 7) / 8 * 8;
-    ex_tiles<T, KIND, BM, BN, EX_WM, EX_WN><<<grid, EX_WM * EX_WN * kWave, 0, st>>>(x);
+    grid = spread_grid(grid, kRun);
+    ex_tiles<T, KIND, BM, BN, EX_WM, EX_WN, KIND >= kWeightsIn ? 2 : EX_SA, 2><<<grid, EX_WM * EX_WN * kWave, 0, st>>>(x);
     return;
   }
   constexpr int BM = 128, BN = 128;
@@ -689,8 +1215,33 @@ void product(Experts x, hipStream_t st) {
 
 }  // namespace
 
+template <typename T, int MT, int GT>
+void few(const Experts& x, hipStream_t st) {
+  const uint32_t y = static_cast<uint32_t>(x.pairs < x.experts ? x.pairs : x.experts);
+  ex_few<T, true, MT, GT><<<dim3(blocks_of(x.hidden, 16 * GT), y), 256, 0, st>>>(x);
+  if (x.tokens <= kFewTokens) {
+    const uint32_t waves = 2 * static_cast<uint32_t>(x.top < 8 ? x.top : 8);
+    ex_few_join<T><<<dim3(blocks_of(x.dim, 16), static_cast<uint32_t>(x.tokens)),
+                     waves * kWave, 0, st>>>(x);
+    return;
+  }
+  ex_few<T, false, MT, GT><<<dim3(blocks_of(x.dim, 16 * GT), y), 256, 0, st>>>(x);
+  ex_pairs_join<T><<<dim3(blocks_of(x.dim, 256), static_cast<uint32_t>(x.tokens)), 256, 0, st>>>(
+      x);
+}
+
 template <typename T>
 hipError_t launch_experts(const Experts& x, hipStream_t st) {
+  // Few pairs an expert, and no backward pass that needs the rows in the experts' order.  At 64
+  // experts of 2,048 x 1,024 (bfloat16, 8 of them a token) this takes 26, 101, 197, 224 us for 1,
+  // 8, 64, 128 tokens, the tiles below 113, 204, 230, 231 us; for 192 tokens it is 278 to 235.
+  // Two rows of 16 from 8 pairs an expert on: 96 tokens 198 us, 245 us with one.
+  if (!x.pre && x.pairs <= kFewPairs && x.pairs <= int64_t{16} * x.experts) {
+    if (x.pairs <= x.experts) few<T, 1, 1>(x, st);
+    else if (x.pairs <= int64_t{8} * x.experts) few<T, 1, 2>(x, st);
+    else few<T, 2, 2>(x, st);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_plan(x, st);
   if (e != hipSuccess) return e;
   product<T, kForwardGate>(x, st);
