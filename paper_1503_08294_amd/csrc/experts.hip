@@ -126,7 +126,7 @@ size_t carve_forward(void* base, int32_t dtype, bool saved, Experts* x) {
 size_t carve_backward(void* base, int32_t dtype, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs), s = size_of(dtype);
   Carver c{static_cast<char*>(base)};
-  x->dot_tiles = (x->hidden + kDotColumns - 1) / kDotColumns;
+  x->dot_tiles = (x->hidden + kSmallRows - 1) / kSmallRows;
   x->dpre = c.take(2 * s * (n + kPlanRows) * x->hidden);
   x->wact = c.take(s * n * x->hidden);
   x->dots = static_cast<float*>(c.take(4 * n * x->dot_tiles));
@@ -156,12 +156,13 @@ Experts experts_of(const gsn_experts_params& p) {
 }
 
 // Whether every product's grid stays below 2^32 threads.
-bool grids_ok(const gsn_experts_params& p, const Experts& x) {
-  const auto tiles = [](int64_t n) { return (n + 127) / 128; };
-  const int64_t rows = x.pairs / 64 + x.experts;
-  const int64_t most = std::max(std::max(rows * tiles(2 * int64_t{p.hidden}), rows * tiles(p.dim)),
-                                p.experts * tiles(2 * int64_t{p.hidden}) * tiles(p.dim));
-  return most < (1 << 23);
+bool grids_ok(const Experts& x) {
+  const int64_t side = x.aligned ? kTileRows : kSmallRows, threads = x.aligned ? 512 : 256;
+  const auto tiles = [&](int64_t n) { return (n + side - 1) / side; };
+  const int64_t rows = (x.pairs / kPlanRows + x.experts) * (kPlanRows / side);
+  const int64_t wide = tiles(2 * static_cast<int64_t>(x.hidden)) + 1, deep = tiles(x.dim);
+  const int64_t most = std::max(std::max(rows * wide, rows * deep), x.experts * wide * deep);
+  return most + 256 < (int64_t{1} << 32) / threads;
 }
 
 bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256 == 0; }
@@ -208,7 +209,6 @@ int gsn_experts(const gsn_experts_params* p, const void* x, int64_t x_stride,
   if (!gsn::workspace_ok(workspace) || (saved && !gsn::workspace_ok(saved))) return GSN_E_INVAL;
   if (a.tokens > 0 && (!x || !ids || !weights || !w1 || !w2 || !out || x_stride < p->dim))
     return GSN_E_INVAL;
-  if (!gsn::grids_ok(*p, a)) return GSN_E_CAPACITY;
   if (workspace_bytes < gsn_experts_workspace_bytes(p, 0) ||
       (saved && saved_bytes < gsn_experts_saved_bytes(p)))
     return GSN_E_CAPACITY;
@@ -219,6 +219,8 @@ int gsn_experts(const gsn_experts_params* p, const void* x, int64_t x_stride,
   a.w1 = w1;
   a.w2 = w2;
   a.out = out;
+  a.aligned = gsn::aligned(a, p->dtype);
+  if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   if (saved) gsn::carve_saved(saved, &a);
   gsn::carve_forward(workspace, p->dtype, saved != nullptr, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -240,7 +242,6 @@ int gsn_experts_backward(const gsn_experts_params* p, const void* dout, const vo
   if (!gsn::workspace_ok(workspace) || !gsn::workspace_ok(saved)) return GSN_E_INVAL;
   if (a.tokens > 0 && (!dout || !x || !weights || !w1 || !w2 || x_stride < p->dim))
     return GSN_E_INVAL;
-  if (!gsn::grids_ok(*p, a)) return GSN_E_CAPACITY;
   if (workspace_bytes < gsn_experts_workspace_bytes(p, 1) ||
       saved_bytes < gsn_experts_saved_bytes(p))
     return GSN_E_CAPACITY;
@@ -254,6 +255,8 @@ int gsn_experts_backward(const gsn_experts_params* p, const void* dout, const vo
   a.dweights = dweights;
   a.dw1 = dw1;
   a.dw2 = dw2;
+  a.aligned = gsn::aligned(a, p->dtype);
+  if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   gsn::carve_saved(const_cast<void*>(saved), &a);
   gsn::carve_backward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);

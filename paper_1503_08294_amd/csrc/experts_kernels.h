@@ -26,15 +26,6 @@ typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-#ifndef EX_BM
-#define EX_BM 256
-#define EX_BN 256
-#define EX_WM 2
-#define EX_WN 4
-#endif
-#ifndef EX_SA
-#define EX_SA 3
-#endif
 constexpr int64_t kFewTokens = 2;    // tokens up to which one launch makes the second product and the sum
 constexpr int64_t kFewPairs = 2048;  // pairs that a workgroup lists at most
 constexpr int kRowBytes = 128;  // bytes of k (contiguous operands) in a stage
@@ -68,9 +59,10 @@ __device__ __forceinline__ f32x4 multiply(const Frag& n, const Frag& m, f32x4 ac
 __device__ __forceinline__ int chunk_k(int r, int c) { return c ^ ((r >> 1) & 7); }
 // The same with k as the row: the 4 (2-byte types) or 1 rows that 16 lanes read 32 or 64 bytes
 // of, and those of the wave's other quarters, fall on different banks.
-template <typename T>
+template <typename T, int CHUNKS = 16>  // CHUNKS of a row, at least
 __device__ __forceinline__ int chunk_n(int k, int c) {
-  if constexpr (sizeof(T) == 2) return c ^ (((k & 3) | ((k >> 1) & 4)) << 1);
+  if constexpr (sizeof(T) == 2 && CHUNKS < 16) return c ^ ((k & 3) << 1);
+  else if constexpr (sizeof(T) == 2) return c ^ (((k & 3) | ((k >> 1) & 4)) << 1);
   else return c ^ (((k >> 2) & 3) << 2);
 }
 
@@ -89,7 +81,7 @@ __device__ __forceinline__ Frag fragment(const char* tile, int r0, int s, int la
     for (int j = 0; j < 2; ++j) {
       const int k = 32 * s + 8 * g + 4 * j + (i >> 2);
       const int col = r0 + (i & 3) * 4;
-      const char* p = tile + (k * R + (chunk_n<T>(k, col >> 3) << 3) + (col & 7)) * 2;
+      const char* p = tile + (k * R + (chunk_n<T, R / 8>(k, col >> 3) << 3) + (col & 7)) * 2;
       f.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
           (__attribute__((address_space(3))) s16x4*)(p));
     }
@@ -227,8 +219,26 @@ __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 
   }
 }
 
-// One tile of BM x BN by WM x WN waves, for any sizes and alignment: elements are loaded one by
-// one.
+// A lane's 16 bytes of a row of K elements at k, zeros past its end (INSIDE: there is none in
+// them).  Rows start at any element.
+template <bool INSIDE, typename T>
+__device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
+  constexpr int kE = 16 / sizeof(T);
+  typedef T Loose __attribute__((ext_vector_type(kE), aligned(sizeof(T))));
+  Frag f;
+  if (INSIDE || k + kE <= K) {
+    f.u = __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose*>(row + k));
+  } else {
+    Vec<T, kE> v;
+#pragma unroll
+    for (int j = 0; j < kE; ++j) v.v[j] = k + j < K ? row[k + j] : from_float<T>(0.0f);
+    f.u = __builtin_bit_cast(u32x4, v);
+  }
+  return f;
+}
+
+// One tile of BM x BN by WM x WN waves, for any sizes and alignment: a stage's 16-byte chunks are
+// loaded into registers while the stage before is multiplied, and from there to LDS.
 template <typename T, Kind KIND, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   constexpr int kThr = WM * WN * kWave;
@@ -238,7 +248,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   constexpr bool kTrA = kWeightsKind;
   constexpr bool kTrB = kWeightsKind || KIND == kBackwardGate || KIND == kBackwardIn;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
-  static_assert(BN >= kDotColumns || KIND != kBackwardGate);
+  constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;
   __shared__ __attribute__((aligned(16))) char smem[(BM + BN) * kRowBytes];
   char* const sa = smem;
   char* const sb = smem + BM * kRowBytes;
@@ -277,32 +287,45 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
-  // element (row, k) of the operands, 0 outside
+  // Rows of the operands: with k contiguous, this lane's LA (LB) rows, null outside; with k as the
+  // row, row k (from its first column in the tile).
   const auto token = [&](int64_t r) { return x.plan.token[r]; };
-  const auto row_a = [&](int32_t m) -> const T* {  // k contiguous
-    if (m >= mrows) return nullptr;
-    if constexpr (KIND == kForwardGate)
-      return static_cast<const T*>(x.x) + token(row0 + m) * x.x_stride;
-    else if constexpr (KIND == kForwardOut)
-      return static_cast<const T*>(x.act) + (row0 + m) * F;
-    else if constexpr (KIND == kBackwardGate)
-      return static_cast<const T*>(x.dout) + static_cast<int64_t>(token(row0 + m)) * D;
-    else
-      return static_cast<const T*>(x.dpre) + (row0 + m) * 2 * F;
-  };
-  const auto row_b = [&](int32_t c) -> const T* {  // k contiguous
-    if constexpr (KIND == kForwardGate) {
-      // a wave's columns: half of them gates, half the same columns' ups
-      constexpr int kW = BN / WN, kHalf = kW / 2;
-      const int32_t f = n0 + c / kW * kHalf + c % kHalf;
-      const int q = c % kW / kHalf;
-      if (f >= F) return nullptr;
-      return static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + q * F + f) * D;
-    } else {
-      if (n0 + c >= D) return nullptr;
-      return static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n0 + c) * F;
+  const T* rows_a[LA];
+  const T* rows_b[LB];
+  if constexpr (!kTrA) {
+#pragma unroll
+    for (int j = 0; j < LA; ++j) {
+      const int32_t m = (j * kThr + tid) >> 3;
+      rows_a[j] = nullptr;
+      if (m >= mrows) continue;
+      if constexpr (KIND == kForwardGate)
+        rows_a[j] = static_cast<const T*>(x.x) + token(row0 + m) * x.x_stride;
+      else if constexpr (KIND == kForwardOut)
+        rows_a[j] = static_cast<const T*>(x.act) + (row0 + m) * F;
+      else if constexpr (KIND == kBackwardGate)
+        rows_a[j] = static_cast<const T*>(x.dout) + static_cast<int64_t>(token(row0 + m)) * D;
+      else
+        rows_a[j] = static_cast<const T*>(x.dpre) + (row0 + m) * 2 * F;
     }
-  };
+  }
+  if constexpr (!kTrB) {
+#pragma unroll
+    for (int j = 0; j < LB; ++j) {
+      const int32_t c = (j * kThr + tid) >> 3;
+      rows_b[j] = nullptr;
+      if constexpr (KIND == kForwardGate) {
+        // a wave's columns: half of them gates, half the same columns' ups
+        constexpr int kW = BN / WN, kHalf = kW / 2;
+        const int32_t f = n0 + c / kW * kHalf + c % kHalf;
+        const int q = c % kW / kHalf;
+        if (f < F)
+          rows_b[j] = static_cast<const T*>(x.w1) +
+                      (static_cast<int64_t>(e) * 2 * F + q * F + f) * D;
+      } else if (n0 + c < D) {
+        rows_b[j] = static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + n0 + c) * F;
+      }
+    }
+  }
   const auto krow_a = [&](int32_t k) -> const T* {  // m contiguous
     if constexpr (KIND == kWeightsIn)
       return static_cast<const T*>(x.dpre) + (row0 + k) * 2 * F + m0;
@@ -319,30 +342,33 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
     else
       return static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + k) * D + n0;
   };
-  const auto stage_k = [&](char* tile, int rows, int32_t k0, const auto& row) {
-    for (int i = tid; i < rows * 8; i += kThr) {
-      const int r = i >> 3, c = chunk_k(r, i & 7);
-      const T* p = row(r);
-      Vec<T, kE> v;
+  Frag ca[LA], cb[LB];
+  const auto load = [&](int32_t k0) {
 #pragma unroll
-      for (int j = 0; j < kE; ++j) {
-        const int32_t k = k0 + c * kE + j;
-        v.v[j] = p && k < K ? p[k] : from_float<T>(0.0f);
+    for (int j = 0; j < LA; ++j) {
+      const int i = j * kThr + tid;
+      ca[j].u = u32x4{0, 0, 0, 0};
+      if constexpr (!kTrA) {
+        if (rows_a[j]) ca[j] = row_chunk<false>(rows_a[j], k0 + chunk_k(i >> 3, i & 7) * kE, K);
+      } else {
+        constexpr int kC = BM / kE;
+        const int r = i / kC;
+        if (k0 + r < K)
+          ca[j] = row_chunk<false>(krow_a(k0 + r), chunk_n<T, kC>(r, i % kC) * kE, mrows);
       }
-      *reinterpret_cast<Vec<T, kE>*>(tile + i * 16) = v;
     }
-  };
-  const auto stage_n = [&](char* tile, auto width, int32_t k0, int32_t cols, const auto& row) {
-    constexpr int kC = decltype(width)::value / kE;  // chunks of a row
-    for (int i = tid; i < kBK * kC; i += kThr) {
-      const int r = i / kC, c = chunk_n<T>(r, i % kC);
-      const int32_t k = k0 + r;
-      const T* p = k < K ? row(k) : nullptr;
-      Vec<T, kE> v;
 #pragma unroll
-      for (int j = 0; j < kE; ++j)
-        v.v[j] = p && c * kE + j < cols ? p[c * kE + j] : from_float<T>(0.0f);
-      *reinterpret_cast<Vec<T, kE>*>(tile + i * 16) = v;
+    for (int j = 0; j < LB; ++j) {
+      const int i = j * kThr + tid;
+      cb[j].u = u32x4{0, 0, 0, 0};
+      if constexpr (!kTrB) {
+        if (rows_b[j]) cb[j] = row_chunk<false>(rows_b[j], k0 + chunk_k(i >> 3, i & 7) * kE, K);
+      } else {
+        constexpr int kC = BN / kE;
+        const int r = i / kC;
+        if (k0 + r < K)
+          cb[j] = row_chunk<false>(krow_b(k0 + r), chunk_n<T, kC>(r, i % kC) * kE, N - n0);
+      }
     }
   };
 
@@ -352,12 +378,16 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+  if (K > 0) load(0);
   for (int32_t k0 = 0; k0 < K; k0 += kBK) {
-    if constexpr (kTrA) stage_n(sa, std::integral_constant<int, BM>(), k0, mrows, krow_a);
-    else stage_k(sa, BM, k0, row_a);
-    if constexpr (kTrB) stage_n(sb, std::integral_constant<int, BN>(), k0, N - n0, krow_b);
-    else stage_k(sb, BN, k0, row_b);
+#pragma unroll
+    for (int j = 0; j < LA; ++j)
+      *reinterpret_cast<u32x4*>(sa + (j * kThr + tid) * 16) = ca[j].u;
+#pragma unroll
+    for (int j = 0; j < LB; ++j)
+      *reinterpret_cast<u32x4*>(sb + (j * kThr + tid) * 16) = cb[j].u;
     __syncthreads();
+    if (k0 + kBK < K) load(k0 + kBK);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Frag fa[MT], fb[NT];
@@ -926,24 +956,6 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
 }
 // ------------------------------------------------------------------------- few pairs ----
 
-// A lane's 16 bytes of a row of K elements at k, zeros past its end (INSIDE: there is none in
-// them).  Rows start at any element.
-template <bool INSIDE, typename T>
-__device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
-  constexpr int kE = 16 / sizeof(T);
-  typedef T Loose __attribute__((ext_vector_type(kE), aligned(sizeof(T))));
-  Frag f;
-  if (INSIDE || k + kE <= K) {
-    f.u = __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose*>(row + k));
-  } else {
-    Vec<T, kE> v;
-#pragma unroll
-    for (int j = 0; j < kE; ++j) v.v[j] = k + j < K ? row[k + j] : from_float<T>(0.0f);
-    f.u = __builtin_bit_cast(u32x4, v);
-  }
-  return f;
-}
-
 // With a few pairs an expert the products read every weight once and are bound by that: no
 // staging, a wave loads 16 rows of weights straight into fragments and multiplies them with 16
 // rows of tokens.  A workgroup takes one expert and 16 GT columns; its four waves each take a
@@ -1146,17 +1158,40 @@ __global__ __launch_bounds__(256) void ex_pairs_join(Experts x) {
 template <typename T, bool WEIGHTED>
 __global__ __launch_bounds__(256) void ex_join(Experts x, const float* __restrict__ y,
                                                T* __restrict__ out) {
-  const int64_t t = blockIdx.x;
-  for (int32_t d = threadIdx.x; d < x.dim; d += 256) {
-    float s = 0.0f;
+  constexpr int kW = 4;
+  typedef T Some __attribute__((ext_vector_type(kW), aligned(sizeof(T))));
+  typedef float Four __attribute__((ext_vector_type(kW), aligned(4)));
+  const int32_t each = (x.dim + kW - 1) / kW;  // lanes of a token
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < x.tokens * each;
+       at += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t t = at / each;
+    const int32_t d = static_cast<int32_t>(at - t * each) * kW;
+    const bool whole = d + kW <= x.dim;
+    float s[kW] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int k = 0; k < x.top; ++k) {
       const int64_t j = t * x.top + k;
       const int32_t r = x.plan.pos[j];
-      if (r < 0) continue;
-      const float v = y[static_cast<int64_t>(r) * x.dim + d];
-      s += WEIGHTED ? x.weights[j] * v : v;
+      const float w = r < 0 ? 0.0f : WEIGHTED ? x.weights[j] : 1.0f;
+      const float* row = y + static_cast<int64_t>(r < 0 ? 0 : r) * x.dim + d;
+      if (whole) {
+        const Four v = *reinterpret_cast<const Four*>(row);
+#pragma unroll
+        for (int i = 0; i < kW; ++i) s[i] += r < 0 ? 0.0f : w * v[i];
+      } else {
+        for (int i = 0; i < kW; ++i) s[i] += r < 0 || d + i >= x.dim ? 0.0f : w * row[i];
+      }
     }
-    out[t * x.dim + d] = from_float<T>(s);
+    T* to = out + t * x.dim + d;
+    if (whole) {
+      Some v;
+#pragma unroll
+      for (int i = 0; i < kW; ++i) v[i] = from_float<T>(s[i]);
+      *reinterpret_cast<Some*>(to) = v;
+    } else {
+      for (int i = 0; i < kW; ++i)
+        if (d + i < x.dim) to[i] = from_float<T>(s[i]);
+    }
   }
 }
 
@@ -1175,19 +1210,27 @@ inline uint32_t blocks_of(int64_t n, int64_t per) {
   return static_cast<uint32_t>((n + per - 1) / per);
 }
 
-// Whether rows and their starts are multiples of 16 bytes.
-template <typename T>
-bool aligned(const Experts& x) {
-  constexpr int kE = 16 / sizeof(T);
-  return x.dim % kE == 0 && x.hidden % kE == 0 && x.x_stride % kE == 0 && aligned16(x.x) &&
-         aligned16(x.w1) && aligned16(x.w2) && aligned16(x.out) && aligned16(x.dout) &&
-         aligned16(x.dx) && aligned16(x.dw1) && aligned16(x.dw2);
+inline uint32_t join_blocks(const Experts& x) {
+  const int64_t n = (x.tokens * ((x.dim + 3) / 4) + 255) / 256;
+  return static_cast<uint32_t>(n < (1 << 20) ? n : 1 << 20);
+}
+
+template <typename T, Kind KIND, int BM, int BN>
+void product_any(Experts x, hipStream_t st) {
+  x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, BN));
+  const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
+                               KIND == kWeightsOut ? x.hidden : x.dim,
+                               KIND == kForwardGate ? BN / 2 : BN);
+  const uint32_t grid = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
+                        : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
+                                              : x.plan.most_tiles * (kPlanRows / BM) * n;
+  if (grid > 0) ex_product<T, KIND, BM, BN, 2, 2><<<grid, 256, 0, st>>>(x);
 }
 
 template <typename T, Kind KIND>
 void product(Experts x, hipStream_t st) {
-  if (aligned<T>(x)) {
-    constexpr int BM = EX_BM, BN = EX_BN;
+  if (x.aligned) {
+    constexpr int BM = kTileRows, BN = kTileRows;
     x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, BN));
     const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
                                  KIND == kWeightsOut ? x.hidden : x.dim,
@@ -1196,21 +1239,10 @@ void product(Experts x, hipStream_t st) {
                     : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
                                           : x.plan.most_tiles * (kPlanRows / BM) * n;
     grid = spread_grid(grid, kRun);
-    ex_tiles<T, KIND, BM, BN, EX_WM, EX_WN, KIND >= kWeightsIn ? 2 : EX_SA, 2><<<grid, EX_WM * EX_WN * kWave, 0, st>>>(x);
+    ex_tiles<T, KIND, BM, BN, 2, 4, KIND >= kWeightsIn ? 2 : 3, 2><<<grid, 512, 0, st>>>(x);
     return;
   }
-  constexpr int BM = 128, BN = 128;
-  constexpr int kCols = KIND == kForwardGate ? BN / 2 : BN;
-  uint32_t grid;
-  if constexpr (KIND == kWeightsIn)
-    grid = x.experts * blocks_of(2 * x.hidden, BM) * blocks_of(x.dim, BN);
-  else if constexpr (KIND == kWeightsOut)
-    grid = x.experts * blocks_of(x.dim, BM) * blocks_of(x.hidden, BN);
-  else
-    grid = x.plan.most_tiles * (kPlanRows / BM) *
-           blocks_of(KIND == kForwardGate || KIND == kBackwardGate
-                                             ? x.hidden : x.dim, kCols);
-  if (grid > 0) ex_product<T, KIND, BM, BN, 2, 2><<<grid, 256, 0, st>>>(x);
+  product_any<T, KIND, kSmallRows, kSmallRows>(x, st);
 }
 
 }  // namespace
@@ -1246,8 +1278,7 @@ hipError_t launch_experts(const Experts& x, hipStream_t st) {
   if (e != hipSuccess) return e;
   product<T, kForwardGate>(x, st);
   product<T, kForwardOut>(x, st);
-  ex_join<T, true><<<static_cast<uint32_t>(x.tokens), 256, 0, st>>>(x, x.y,
-                                                                    static_cast<T*>(x.out));
+  ex_join<T, true><<<join_blocks(x), 256, 0, st>>>(x, x.y, static_cast<T*>(x.out));
   return hipGetLastError();
 }
 
@@ -1256,13 +1287,12 @@ hipError_t launch_experts_backward(const Experts& x, hipStream_t st) {
   if (x.pairs > 0) {
     product<T, kBackwardGate>(x, st);
     Experts d = x;
-    if (aligned<T>(x)) d.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, EX_BN));
+    if (x.aligned) d.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, kTileRows));
     if (x.dweights) ex_dots<T><<<blocks_of(x.pairs, 256), 256, 0, st>>>(d);
   }
   if (x.dx && x.tokens > 0) {
     product<T, kBackwardIn>(x, st);
-    ex_join<T, false><<<static_cast<uint32_t>(x.tokens), 256, 0, st>>>(x, x.dxr,
-                                                                       static_cast<T*>(x.dx));
+    ex_join<T, false><<<join_blocks(x), 256, 0, st>>>(x, x.dxr, static_cast<T*>(x.dx));
   }
   if (x.dw1) product<T, kWeightsIn>(x, st);
   if (x.dw2) product<T, kWeightsOut>(x, st);
