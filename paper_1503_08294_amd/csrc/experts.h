@@ -20,6 +20,7 @@ struct Plan {
   int32_t* rows;        // pairs
   int32_t* token;       // pairs: rows[r] / top
   int32_t* pos;         // pairs
+  int32_t* counts;      // pairs of each expert in each chunk of them
   int32_t most_tiles;
 };
 
