@@ -39,19 +39,18 @@ union Frag {
   s16x4 s[2];
 };
 
-// acc[i] += sum over the fragment's k of n-row (lane >> 4) * 4 + i and m-row lane & 15
+// acc[i] += sum over the fragment's k of n-row (lane >> 4) * 4 + i and m-row lane & 15; of a 4-byte
+// type part q of four, so that products of one sum do not wait for each other.
 template <typename T>
-__device__ __forceinline__ f32x4 multiply(const Frag& n, const Frag& m, f32x4 acc) {
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(n.f[i], m.f[i], acc, 0, 0, 0);
-    return acc;
-  } else if constexpr (__is_same(T, bf16_t)) {
+constexpr int kParts = sizeof(T) == 4 ? 4 : 1;
+template <typename T>
+__device__ __forceinline__ f32x4 multiply(const Frag& n, const Frag& m, f32x4 acc, int q) {
+  if constexpr (sizeof(T) == 4)
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(n.f[q], m.f[q], acc, 0, 0, 0);
+  else if constexpr (__is_same(T, bf16_t))
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(n.b, m.b, acc, 0, 0, 0);
-  } else {
+  else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(n.h, m.h, acc, 0, 0, 0);
-  }
 }
 
 // Place of 16-byte chunk c in row r of a staged operand with k contiguous (8 chunks a row): the
@@ -219,6 +218,9 @@ __device__ __forceinline__ void finish(const Experts& x, f32x4 (&acc)[BM / WM / 
   }
 }
 
+// 16 zero bytes that lanes load where an operand has no more k
+__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
+
 // A lane's 16 bytes of a row of K elements at k, zeros past its end (INSIDE: there is none in
 // them).  Rows start at any element.
 template <bool INSIDE, typename T>
@@ -227,7 +229,9 @@ __device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
   typedef T Loose __attribute__((ext_vector_type(kE), aligned(sizeof(T))));
   Frag f;
   if (INSIDE || k + kE <= K) {
-    f.u = __builtin_bit_cast(u32x4, *reinterpret_cast<const Loose*>(row + k));
+    // (said to be global: a pointer chosen between two is taken for any, whose loads LDS reads wait
+    // for)
+    f.u = __builtin_bit_cast(u32x4, *(const __attribute__((address_space(1))) Loose*)(row + k));
   } else {
     Vec<T, kE> v;
 #pragma unroll
@@ -238,8 +242,11 @@ __device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
 }
 
 // One tile of BM x BN by WM x WN waves, for any sizes and alignment: a stage's 16-byte chunks are
-// loaded into registers while the stage before is multiplied, and from there to LDS.
-template <typename T, Kind KIND, int BM, int BN, int WM, int WN>
+// loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk that
+// a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so that every
+// load is one instruction without a branch (one with a branch has to be awaited at once); TINY:
+// rows may be shorter than that, and are loaded element by element.
+template <typename T, Kind KIND, int BM, int BN, int WM, int WN, bool TINY>
 __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   constexpr int kThr = WM * WN * kWave;
   constexpr int kE = 16 / sizeof(T);         // elements of a chunk
@@ -249,9 +256,8 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   constexpr bool kTrB = kWeightsKind || KIND == kBackwardGate || KIND == kBackwardIn;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;
-  __shared__ __attribute__((aligned(16))) char smem[(BM + BN) * kRowBytes];
-  char* const sa = smem;
-  char* const sb = smem + BM * kRowBytes;
+  constexpr int kStage = (BM + BN) * kRowBytes;
+  __shared__ __attribute__((aligned(16))) char smem[2 * kStage];
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WN, wn = wave % WN;
@@ -342,34 +348,51 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
     else
       return static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + k) * D + n0;
   };
-  Frag ca[LA], cb[LB];
-  const auto load = [&](int32_t k0) {
+  // chunk j's place in a stage, k0 the stage's first k: k (or the column) where it begins, and the
+  // length of its row from there (0 or less: nothing of it is inside)
+  const T* const zeros = reinterpret_cast<const T*>(kZeros);
+  const auto begin = [&](bool is_a, int j, int32_t k0) {
+    const int i = j * kThr + tid;
+    if (is_a ? !kTrA : !kTrB) return k0 + chunk_k(i >> 3, i & 7) * kE;
+    constexpr int kCA = BM / kE, kCB = BN / kE;
+    return (is_a ? chunk_n<T, kCA>(i / kCA, i % kCA) : chunk_n<T, kCB>(i / kCB, i % kCB)) * kE;
+  };
+  const auto length = [&](bool is_a) { return (is_a ? !kTrA : !kTrB) ? K : is_a ? mrows : N - n0; };
+  Frag ahead[2][LA + LB];
+  const auto load = [&](int32_t k0, Frag (&to)[LA + LB]) {
 #pragma unroll
-    for (int j = 0; j < LA; ++j) {
-      const int i = j * kThr + tid;
-      ca[j].u = u32x4{0, 0, 0, 0};
-      if constexpr (!kTrA) {
-        if (rows_a[j]) ca[j] = row_chunk<false>(rows_a[j], k0 + chunk_k(i >> 3, i & 7) * kE, K);
+    for (int j = 0; j < LA + LB; ++j) {
+      const bool is_a = j < LA;
+      const int q = is_a ? j : j - LA, i = q * kThr + tid;
+      const int32_t at = begin(is_a, q, k0), len = length(is_a);
+      const T* row;
+      if (is_a) {
+        if constexpr (!kTrA) row = rows_a[q];
+        else row = k0 + i / (BM / kE) < K ? krow_a(k0 + i / (BM / kE)) : nullptr;
       } else {
-        constexpr int kC = BM / kE;
-        const int r = i / kC;
-        if (k0 + r < K)
-          ca[j] = row_chunk<false>(krow_a(k0 + r), chunk_n<T, kC>(r, i % kC) * kE, mrows);
+        if constexpr (!kTrB) row = rows_b[q];
+        else row = k0 + i / (BN / kE) < K ? krow_b(k0 + i / (BN / kE)) : nullptr;
+      }
+      if constexpr (TINY) {
+        to[j].u = u32x4{0, 0, 0, 0};
+        if (row) to[j] = row_chunk<false>(row, at, len);
+      } else {
+        const T* p = row + (at + kE <= len ? at : len - kE);
+        to[j] = row_chunk<true>(row && at < len ? p : zeros, 0, kE);
       }
     }
-#pragma unroll
-    for (int j = 0; j < LB; ++j) {
-      const int i = j * kThr + tid;
-      cb[j].u = u32x4{0, 0, 0, 0};
-      if constexpr (!kTrB) {
-        if (rows_b[j]) cb[j] = row_chunk<false>(rows_b[j], k0 + chunk_k(i >> 3, i & 7) * kE, K);
-      } else {
-        constexpr int kC = BN / kE;
-        const int r = i / kC;
-        if (k0 + r < K)
-          cb[j] = row_chunk<false>(krow_b(k0 + r), chunk_n<T, kC>(r, i % kC) * kE, N - n0);
+  };
+  // the elements from the cut on come first, zeros after them
+  const auto shifted = [&](Frag f, bool is_a, int q, int32_t k0) {
+    if constexpr (!TINY) {
+      const int32_t over = begin(is_a, q, k0) + kE - length(is_a);
+      if (over > 0) {  // (a chunk wholly outside is zeros already)
+        unsigned __int128 v = __builtin_bit_cast(unsigned __int128, f.u);
+        v = over < kE ? v >> (over * 8 * static_cast<int>(sizeof(T))) : 0;
+        f.u = __builtin_bit_cast(u32x4, v);
       }
     }
+    return f;
   };
 
   f32x4 acc[MT][NT];
@@ -378,16 +401,17 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  if (K > 0) load(0);
-  for (int32_t k0 = 0; k0 < K; k0 += kBK) {
+  const auto stage = [&](int32_t k0, Frag (&chunks)[LA + LB], char* sa) {
+    char* const sb = sa + BM * kRowBytes;
 #pragma unroll
     for (int j = 0; j < LA; ++j)
-      *reinterpret_cast<u32x4*>(sa + (j * kThr + tid) * 16) = ca[j].u;
+      *reinterpret_cast<u32x4*>(sa + (j * kThr + tid) * 16) = shifted(chunks[j], true, j, k0).u;
 #pragma unroll
     for (int j = 0; j < LB; ++j)
-      *reinterpret_cast<u32x4*>(sb + (j * kThr + tid) * 16) = cb[j].u;
+      *reinterpret_cast<u32x4*>(sb + (j * kThr + tid) * 16) =
+          shifted(chunks[LA + j], false, j, k0).u;
     __syncthreads();
-    if (k0 + kBK < K) load(k0 + kBK);
+    if (k0 + 2 * kBK < K) load(k0 + 2 * kBK, chunks);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Frag fa[MT], fb[NT];
@@ -398,20 +422,25 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
       for (int j = 0; j < NT; ++j)
         fb[j] = fragment<T, kTrB, BN>(sb, wn * (BN / WN) + j * 16, s, lane);
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int q = 0; q < kParts<T>; ++q)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j], q);
     }
-    __syncthreads();
+  };
+  if (K > 0) load(0, ahead[0]);
+  if (K > kBK) load(kBK, ahead[1]);
+  for (int32_t k0 = 0; k0 < K; k0 += 2 * kBK) {
+    stage(k0, ahead[0], smem);
+    if (k0 + kBK < K) stage(k0 + kBK, ahead[1], smem + kStage);
   }
+  __syncthreads();
 
   finish<T, KIND, BM, BN, WM, WN>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0, row0);
 }
 
 // ------------------------------------------------------------------ aligned operands ----
-
-// 16 zero bytes that lanes load where an operand has no more k
-__device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
 
 // 16 bytes a lane from its address to LDS offset `at` + 16 lane, without a register between.
 // The compiler does not count these loads: meet() does (with the builtin of this load the
@@ -893,9 +922,11 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int q = 0; q < kParts<T>; ++q)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j]);
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j], q);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -1048,7 +1079,9 @@ __global__ __launch_bounds__(256) void ex_few(Experts x) {
         for (int t = 0; t < MT; ++t)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            acc[t][n] = multiply<T>(fw[h][n], fa[h][t], acc[t][n]);
+#pragma unroll
+            for (int q = 0; q < kParts<T>; ++q)
+              acc[t][n] = multiply<T>(fw[h][n], fa[h][t], acc[t][n], q);
     };
     int32_t k0 = k_begin;
     for (; k0 + kStep <= k_end; k0 += kStep) step(std::true_type(), k0);
@@ -1117,8 +1150,10 @@ __global__ __launch_bounds__(1024) void ex_few_join(Experts x) {
           fa[h].u = u32x4{0, 0, 0, 0};
           if (i == 0) fa[h] = row_chunk<kIn>(a, k, F);
         }
-        acc = multiply<T>(fw[0], fa[0], acc);
-        acc = multiply<T>(fw[1], fa[1], acc);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int p = 0; p < kParts<T>; ++p) acc = multiply<T>(fw[h], fa[h], acc, p);
       };
       int32_t k0 = k_begin;
       for (; k0 + kStep <= k_end; k0 += kStep) step(std::true_type(), k0);
@@ -1224,7 +1259,12 @@ void product_any(Experts x, hipStream_t st) {
   const uint32_t grid = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
                         : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
                                               : x.plan.most_tiles * (kPlanRows / BM) * n;
-  if (grid > 0) ex_product<T, KIND, BM, BN, 2, 2><<<grid, 256, 0, st>>>(x);
+  if (grid == 0) return;
+  constexpr int kE = 16 / sizeof(T);
+  if (x.dim < kE || x.hidden < kE)
+    ex_product<T, KIND, BM, BN, 2, 2, true><<<grid, 256, 0, st>>>(x);
+  else
+    ex_product<T, KIND, BM, BN, 2, 2, false><<<grid, 256, 0, st>>>(x);
 }
 
 template <typename T, Kind KIND>
