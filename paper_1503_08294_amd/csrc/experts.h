@@ -25,7 +25,7 @@ struct Plan {
 };
 
 struct Experts {
-  bool aligned;  // see aligned()
+  int32_t side;  // of the products' tiles
   int64_t tokens;
   int32_t experts, top, dim, hidden;
   int64_t pairs;
@@ -61,16 +61,8 @@ hipError_t launch_experts(const Experts& x, hipStream_t st);
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
 
-// A side of the tiles of aligned operands, and of the others.
-constexpr int kTileRows = 256;
-constexpr int kSmallRows = 64;
-
-// Whether rows and their starts are multiples of 16 bytes.
-inline bool aligned(const Experts& x, int32_t dtype) {
-  const int e = 16 / static_cast<int>(size_of(dtype));
-  return x.dim % e == 0 && x.hidden % e == 0 && x.x_stride % e == 0 && aligned16(x.x) &&
-         aligned16(x.w1) && aligned16(x.w2) && aligned16(x.out) && aligned16(x.dout) &&
-         aligned16(x.dx) && aligned16(x.dw1) && aligned16(x.dw2);
-}
+// Sides of the products' tiles.
+constexpr int32_t kTileRows = 256;
+constexpr int32_t kSmallRows = 64;
 
 }  // namespace gsn

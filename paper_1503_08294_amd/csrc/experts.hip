@@ -232,14 +232,33 @@ Experts experts_of(const gsn_experts_params& p) {
   return x;
 }
 
+// Sides of the products' tiles.  The large tiles are for 2-byte elements whose rows, and their
+// starts, are multiples of 16 bytes, and for products that fill the chip with them: 128 pairs an
+// expert at least, and 128 tiles of the first product.  Forward and backward pass, large and small
+// tiles (us): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 280 and 286; 495, 3 of 7, 1,984 x 320: 214
+// and 145; 1,920, 1 of 7, 3,456 x 448: 320 and 280; 465, 3 of 32, 344 x 1,344: 244 and 194; forward
+// of 5,100, 1 of 8, 448 x 992: 60 and 64.  In binary32, where the matrix cores are 16 times slower,
+// small tiles waste less at the edges: 777 tokens, 3 of 7, 512 x 336: 915 and 201; forward of 7,706,
+// 8 of 32, 576 x 704: 1,469 and 1,412.
+int32_t tile_side(const Experts& x, int32_t dtype) {
+  const bool aligned = x.dim % 8 == 0 && x.hidden % 8 == 0 && x.x_stride % 8 == 0 &&
+                       aligned16(x.x) && aligned16(x.w1) && aligned16(x.w2) &&
+                       aligned16(x.out) && aligned16(x.dout) && aligned16(x.dx) &&
+                       aligned16(x.dw1) && aligned16(x.dw2);
+  const int64_t tiles = (x.pairs / kTileRows + x.experts / 2) *
+                        ((2 * static_cast<int64_t>(x.hidden) + kTileRows - 1) / kTileRows);
+  return dtype != GSN_F32 && aligned && x.pairs >= int64_t{128} * x.experts && tiles >= 128
+             ? kTileRows : kSmallRows;
+}
+
 // Whether every product's grid stays below 2^32 threads.
 bool grids_ok(const Experts& x) {
-  const int64_t side = x.aligned ? kTileRows : kSmallRows, threads = x.aligned ? 512 : 256;
+  const int64_t side = x.side, threads = side == kTileRows ? 512 : 256;
   const auto tiles = [&](int64_t n) { return (n + side - 1) / side; };
   const int64_t rows = (x.pairs / kPlanRows + x.experts) * (kPlanRows / side);
   const int64_t wide = tiles(2 * static_cast<int64_t>(x.hidden)) + 1, deep = tiles(x.dim);
   const int64_t most = std::max(std::max(rows * wide, rows * deep), x.experts * wide * deep);
-  return most + 256 < (int64_t{1} << 32) / threads;
+  return most + 2048 < (int64_t{1} << 32) / threads;
 }
 
 bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256 == 0; }
@@ -299,7 +318,7 @@ int gsn_experts(const gsn_experts_params* p, const void* x, int64_t x_stride,
   a.w1 = w1;
   a.w2 = w2;
   a.out = out;
-  a.aligned = gsn::aligned(a, p->dtype);
+  a.side = gsn::tile_side(a, p->dtype);
   if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   if (saved) gsn::carve_saved(saved, &a);
   gsn::carve_forward(workspace, p->dtype, saved != nullptr, &a);
@@ -335,7 +354,7 @@ int gsn_experts_backward(const gsn_experts_params* p, const void* dout, const vo
   a.dweights = dweights;
   a.dw1 = dw1;
   a.dw2 = dw2;
-  a.aligned = gsn::aligned(a, p->dtype);
+  a.side = gsn::tile_side(a, p->dtype);
   if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   gsn::carve_saved(const_cast<void*>(saved), &a);
   gsn::carve_backward(workspace, p->dtype, &a);

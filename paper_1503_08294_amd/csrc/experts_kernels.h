@@ -105,15 +105,32 @@ enum Kind {
   kWeightsOut     // dw2 from dout, wact
 };
 
-// Four results of a row at column n, N columns in all
+// Four results of a row at column n, N columns in all.  Rows start at any element.
+template <typename T>
+struct LooseOf {
+  typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+};
 template <typename T>
 __device__ __forceinline__ void store4(T* row, int32_t n, int32_t N, const float* v) {
+  if (n + 4 <= N) {
+    typename LooseOf<T>::type o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = from_float<T>(v[i]);
+    *reinterpret_cast<typename LooseOf<T>::type*>(row + n) = o;
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (n + i < N) row[n + i] = from_float<T>(v[i]);
 }
 template <typename T>
 __device__ __forceinline__ void load4(const T* row, int32_t n, int32_t N, float* v) {
+  if (n + 4 <= N) {
+    const auto o = *reinterpret_cast<const typename LooseOf<T>::type*>(row + n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = to_float(o[i]);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = n + i < N ? to_float(row[n + i]) : 0.0f;
 }
@@ -241,6 +258,34 @@ __device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
   return f;
 }
 
+// Workgroups go round the 8 XCDs.  Runs of `run` tiles go to one XCD, where the tiles that its CUs
+// work on at a time share operands through its L2; the next run goes to the next XCD.
+// Fewer tiles than 8 runs are dealt out evenly.
+__device__ __forceinline__ int32_t spread(int32_t total, int32_t run) {
+  if (total < 8 * run) run = (total + 7) / 8;
+  const int32_t in = blockIdx.x >> 3;
+  const int32_t id = (in / run * 8 + (blockIdx.x & 7)) * run + in % run;
+  return id < total ? id : -1;
+}
+// Workgroups that cover `total` tiles in that order.
+inline uint32_t spread_grid(uint32_t total, uint32_t run) {
+  return (total + 8 * run - 1) / (8 * run) * (8 * run);
+}
+// Place of a tile in a block of tiles_m x tiles_n, taken TALL tiles of m by all of n at a time, m
+// first: 32 tiles in a row, 4 x 8, have 4 + 8 tiles of operands.
+template <int32_t TALL>
+__device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t tiles_n) {
+  const int32_t g = id / (TALL * tiles_n), in = id - g * TALL * tiles_n;
+  const int32_t left = tiles_m - g * TALL, tall = left < TALL ? left : TALL;
+  return int2{g * TALL + in % tall, in / tall};
+}
+// Of the large tiles, one a CU; the small ones, which many CUs have several of, go round in order
+// (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small products).
+template <int BM>
+constexpr int32_t kTall = BM == kTileRows ? 4 : 1;
+template <int BM>
+constexpr int32_t kRun = BM == kTileRows ? 32 : 1;
+
 // One tile of BM x BN by WM x WN waves, for any sizes and alignment: a stage's 16-byte chunks are
 // loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk that
 // a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so that every
@@ -272,22 +317,25 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    int32_t id = blockIdx.x;
-    n0 = id % tiles_n * BN;
-    id /= tiles_n;
-    m0 = id % tiles_m * BM;
-    e = id / tiles_m;
+    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun<BM>);
+    if (id < 0) return;
+    e = id / (tiles_m * tiles_n);
+    const int2 at = tile_place<kTall<BM>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    m0 = at.x * BM;
+    n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    const int32_t id = blockIdx.x / tiles_n;
-    if (id >= *x.plan.tile_count * (kPlanRows / BM)) return;
-    n0 = blockIdx.x % tiles_n * kCols;
-    const int4 t = x.plan.tiles[id / (kPlanRows / BM)];
+    constexpr int kSub = kPlanRows / BM;
+    const int32_t id = spread(*x.plan.tile_count * kSub * tiles_n, kRun<BM>);
+    if (id < 0) return;
+    const int4 t = x.plan.tiles[id / (kSub * tiles_n)];
+    const int2 at = tile_place<kTall<BM>>(id - t.z * kSub * tiles_n, t.w * kSub, tiles_n);
     e = t.x;
     m0 = 0;
-    row0 = t.y + (id - t.z * (kPlanRows / BM)) * BM;
+    row0 = t.y + at.x * BM;
+    n0 = at.y * kCols;
     mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
     if (mrows <= 0) return;
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
@@ -478,27 +526,6 @@ __device__ __forceinline__ void await_own() {
 }
 __device__ __forceinline__ void await_reads() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-}
-
-// Workgroups go round the 8 XCDs.  Runs of `run` tiles go to one XCD, where the 32 tiles that its
-// CUs work on at a time share operands through its L2; the next run goes to the next XCD.
-__device__ __forceinline__ int32_t spread(int32_t total, int32_t run) {
-  const int32_t in = blockIdx.x >> 3;
-  const int32_t id = (in / run * 8 + (blockIdx.x & 7)) * run + in % run;
-  return id < total ? id : -1;
-}
-// Workgroups that cover `total` tiles in that order.
-inline uint32_t spread_grid(uint32_t total, uint32_t run) {
-  return (total + 8 * run - 1) / (8 * run) * (8 * run);
-}
-constexpr int32_t kRun = 32;
-// Place of a tile in a block of tiles_m x tiles_n, taken 4 tiles of m by all of n at a time, m
-// first: 32 tiles in a row have 4 + 8 tiles of operands.
-constexpr int32_t kTall = 4;
-__device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t tiles_n) {
-  const int32_t g = id / (kTall * tiles_n), in = id - g * kTall * tiles_n;
-  const int32_t left = tiles_m - g * kTall, tall = left < kTall ? left : kTall;
-  return int2{g * kTall + in % tall, in / tall};
 }
 
 // What a wave's lanes wrote to LDS before it, they may read from each other after it.
@@ -741,21 +768,21 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun);
+    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun<BM>);
     if (id < 0) return;
     e = id / (tiles_m * tiles_n);
-    const int2 at = tile_place(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    const int2 at = tile_place<kTall<BM>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
     m0 = at.x * BM;
     n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    constexpr int kParts = kPlanRows / BM;
-    const int32_t id = spread(*x.plan.tile_count * kParts * tiles_n, kRun);
+    constexpr int kSub = kPlanRows / BM;
+    const int32_t id = spread(*x.plan.tile_count * kSub * tiles_n, kRun<BM>);
     if (id < 0) return;
-    const int4 t = x.plan.tiles[id / (kParts * tiles_n)];
-    const int2 at = tile_place(id - t.z * kParts * tiles_n, t.w * kParts, tiles_n);
+    const int4 t = x.plan.tiles[id / (kSub * tiles_n)];
+    const int2 at = tile_place<kTall<BM>>(id - t.z * kSub * tiles_n, t.w * kSub, tiles_n);
     e = t.x;
     m0 = 0;
     row0 = t.y + at.x * BM;
@@ -1250,39 +1277,37 @@ inline uint32_t join_blocks(const Experts& x) {
   return static_cast<uint32_t>(n < (1 << 20) ? n : 1 << 20);
 }
 
-template <typename T, Kind KIND, int BM, int BN>
-void product_any(Experts x, hipStream_t st) {
-  x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, BN));
+// Workgroups that cover every tile of BM x BN of a product.
+template <Kind KIND, int BM, int BN>
+uint32_t tiles_grid(const Experts& x) {
   const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
                                KIND == kWeightsOut ? x.hidden : x.dim,
                                KIND == kForwardGate ? BN / 2 : BN);
-  const uint32_t grid = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
-                        : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
-                                              : x.plan.most_tiles * (kPlanRows / BM) * n;
-  if (grid == 0) return;
-  constexpr int kE = 16 / sizeof(T);
-  if (x.dim < kE || x.hidden < kE)
-    ex_product<T, KIND, BM, BN, 2, 2, true><<<grid, 256, 0, st>>>(x);
-  else
-    ex_product<T, KIND, BM, BN, 2, 2, false><<<grid, 256, 0, st>>>(x);
+  const uint32_t tiles = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
+                         : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
+                                               : x.plan.most_tiles * (kPlanRows / BM) * n;
+  return spread_grid(tiles, kRun<BM>);
 }
 
 template <typename T, Kind KIND>
 void product(Experts x, hipStream_t st) {
-  if (x.aligned) {
-    constexpr int BM = kTileRows, BN = kTileRows;
-    x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, BN));
-    const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
-                                 KIND == kWeightsOut ? x.hidden : x.dim,
-                                 KIND == kForwardGate ? BN / 2 : BN);
-    uint32_t grid = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
-                    : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
-                                          : x.plan.most_tiles * (kPlanRows / BM) * n;
-    grid = spread_grid(grid, kRun);
-    ex_tiles<T, KIND, BM, BN, 2, 4, KIND >= kWeightsIn ? 2 : 3, 2><<<grid, 512, 0, st>>>(x);
-    return;
+  x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
+  if constexpr (sizeof(T) == 2) {
+    if (x.side == kTileRows) {
+      constexpr int S = kTileRows;
+      const uint32_t grid = tiles_grid<KIND, S, S>(x);
+      if (grid > 0)
+        ex_tiles<T, KIND, S, S, 2, 4, KIND >= kWeightsIn ? 2 : 3, 2><<<grid, 512, 0, st>>>(x);
+      return;
+    }
   }
-  product_any<T, KIND, kSmallRows, kSmallRows>(x, st);
+  constexpr int S = kSmallRows, kE = 16 / sizeof(T);
+  const uint32_t grid = tiles_grid<KIND, S, S>(x);
+  if (grid == 0) return;
+  if (x.dim < kE || x.hidden < kE)
+    ex_product<T, KIND, S, S, 2, 2, true><<<grid, 256, 0, st>>>(x);
+  else
+    ex_product<T, KIND, S, S, 2, 2, false><<<grid, 256, 0, st>>>(x);
 }
 
 }  // namespace
@@ -1327,7 +1352,7 @@ hipError_t launch_experts_backward(const Experts& x, hipStream_t st) {
   if (x.pairs > 0) {
     product<T, kBackwardGate>(x, st);
     Experts d = x;
-    if (x.aligned) d.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, kTileRows));
+    d.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
     if (x.dweights) ex_dots<T><<<blocks_of(x.pairs, 256), 256, 0, st>>>(d);
   }
   if (x.dx && x.tokens > 0) {
