@@ -4,13 +4,14 @@
 // A token's logits lie in SUB lanes of a wave (16: four tokens a wave; 64: one), NPL experts in a
 // row each.  An expert's place in the order is its float's bits in unsigned order, 0 if it is shut
 // out; ties go to the lower lane and the earlier of its experts, which is the lower index.
-// Every lane keeps its two best; each of the K rounds takes the largest of the lanes' first ones
-// (16 lanes: four instructions that move data between lanes), and only a lane whose two are both
-// taken looks through its experts again.
+// Every lane keeps its four best; each of the K rounds takes the largest of the lanes' first ones
+// (16 lanes: four instructions that move data between lanes), and only a lane whose four are all
+// taken looks through its experts again (with two kept, one of a wave's lanes did in nearly every
+// round, and 16,384 tokens of 256 experts took 19 us in place of 12).
 //
 // Bound by instructions, and by the latency of their chain where tokens are few: 16,384 tokens of
-// 256 experts, 8 chosen of 4 of 8 groups, sigmoid with a balance: 19 us (8 MB of logits would take
-// 2); one such token 9 us; 65,536 tokens of 64 experts, 2 chosen, softmax: 8 us, backward 7.
+// 256 experts, 8 chosen of 4 of 8 groups, sigmoid with a balance: 12 us (8 MB of logits would take
+// 2); one such token 6 us; 65,536 tokens of 64 experts, 2 chosen, softmax: 8 us, backward 7.
 #include "mixture.h"
 
 #pragma clang fp contract(fast)
@@ -142,22 +143,29 @@ __device__ __forceinline__ void store_row(T* row, int i, int n, const float (&v)
   }
 }
 
-// a lane's two best after (k, at) in the order; 0 where there is none
-struct Two {
-  uint32_t k1, k2;
-  int p1, p2;
+// A lane's four best after (k, at) in the order, best first; 0 where there is none.
+struct Best {
+  uint32_t k[4];
+  int p[4];
 };
 template <int NPL>
-__device__ __forceinline__ Two two_after(const uint32_t (&key)[NPL], uint32_t k, int at) {
-  Two t{0, 0, 0, 0};
+__device__ __forceinline__ Best best_after(const uint32_t (&key)[NPL], uint32_t k, int at) {
+  Best t{};
 #pragma unroll
   for (int j = 0; j < NPL; ++j) {
-    const uint32_t c = key[j] < k || (key[j] == k && j > at) ? key[j] : 0;
-    const bool first = c > t.k1, second = c > t.k2;
-    t.k2 = first ? t.k1 : second ? c : t.k2;
-    t.p2 = first ? t.p1 : second ? j : t.p2;
-    t.k1 = first ? c : t.k1;
-    t.p1 = first ? j : t.p1;
+    uint32_t c = key[j] < k || (key[j] == k && j > at) ? key[j] : 0;
+    int p = j;
+    bool up = false;
+#pragma unroll
+    for (int i = 0; i < 4 && i <= j; ++i) {
+      up = up || c > t.k[i];  // (an equal one that came before stays before; the rest move up)
+      const uint32_t ck = t.k[i];
+      const int cp = t.p[i];
+      t.k[i] = up ? c : ck;
+      t.p[i] = up ? p : cp;
+      c = up ? ck : c;
+      p = up ? cp : p;
+    }
   }
   return t;
 }
@@ -166,8 +174,9 @@ template <typename T, int SUB, int NPL>
 __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
   constexpr int kTokens = kThreads / SUB;
   __shared__ int32_t picked[kTokens][SUB];
-  // only for groups whose experts are not whole lanes
-  __shared__ uint32_t keys[kTokens][SUB * NPL];
+  // the logits, where a bias keeps the keys from telling them; before that, for groups whose
+  // experts are not whole lanes, the keys
+  __shared__ __attribute__((aligned(16))) uint32_t words[kTokens][SUB * NPL];
   __shared__ uint32_t values[kTokens][kMostGroups];
   const int sub = threadIdx.x / SUB, lane = threadIdx.x % SUB;
   // (a token past the end is worked on like the last one, and not written)
@@ -177,8 +186,9 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
   const float ninf = -__builtin_inff();
   const int e0 = lane * NPL;
   const bool live = !a.valid || a.valid[t] != 0;
-  float l[NPL];
+  float l[NPL], b[NPL];
   load_row(row, e0, a.experts, ninf, l);
+  if (a.balance) load_row(a.balance, e0, a.experts, ninf, b);
 #pragma unroll
   for (int j = 0; j < NPL; ++j) l[j] = live ? clean(l[j]) : ninf;
   const bool grouped = a.groups > 1 && a.top_groups < a.groups;
@@ -198,8 +208,6 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
   const auto score = [&](float v) { return a.softmax ? __expf(v - most) * inv : sigmoid(v); };
   uint32_t key[NPL];
   if (a.balance) {
-    float b[NPL];
-    load_row(a.balance, e0, a.experts, ninf, b);
 #pragma unroll
     for (int j = 0; j < NPL; ++j) {
       const float c = score(l[j]) + b[j];
@@ -209,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
 #pragma unroll
     for (int j = 0; j < NPL; ++j) key[j] = l[j] > ninf ? ordered(l[j]) : 0;
   }
-  Two top = two_after(key, 0xffffffffu, -1);
+  Best top = best_after(key, 0xffffffffu, -1);
 
   if (grouped) {
     const int width = a.experts / a.groups;
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
     const int lanes = width / NPL;
     if (lanes * NPL == width && (lanes == 1 || lanes == 2 || lanes == 4)) {
       // whole lanes: the two best of a group, then one round of the largest value for each kept
-      uint32_t k1 = top.k1, k2 = top.k2;
+      uint32_t k1 = top.k[0], k2 = top.k[1];
       const auto join = [&](uint32_t o1, uint32_t o2) {
         const uint32_t low = k1 < o1 ? k1 : o1, high = k2 > o2 ? k2 : o2;
         k1 = k1 > o1 ? k1 : o1;
@@ -246,15 +254,15 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < NPL; ++j) key[j] = kept ? key[j] : 0;
-      if (!kept) top = Two{0, 0, 0, 0};
+      if (!kept) top = Best{};
     } else {
 #pragma unroll
-      for (int j = 0; j < NPL; ++j) keys[sub][e0 + j] = key[j];
+      for (int j = 0; j < NPL; ++j) words[sub][e0 + j] = key[j];
       lds_fence();
       for (int g = lane; g < a.groups; g += SUB) {
         uint32_t k1 = 0, k2 = 0;
         for (int i = 0; i < width; ++i) {
-          const uint32_t k = keys[sub][g * width + i];
+          const uint32_t k = words[sub][g * width + i];
           const uint32_t low = k < k1 ? k : k1;
           k1 = k > k1 ? k : k1;
           k2 = low > k2 ? low : k2;
@@ -275,35 +283,44 @@ __global__ __launch_bounds__(kThreads) void rt_choose(RouteArgs a) {
         }
         if (rank >= a.top_groups) key[j] = 0;
       }
-      top = two_after(key, 0xffffffffu, -1);
+      top = best_after(key, 0xffffffffu, -1);
     }
   }
 
   // K rounds
-  uint32_t last = 0xffffffffu;
+  if (a.balance) {
+#pragma unroll
+    for (int j = 0; j < NPL; ++j) words[sub][e0 + j] = __float_as_uint(l[j]);
+  }
+  uint32_t last = 0xffffffffu, mine_key = 0;
   int last_at = -1;
   picked[sub][lane] = -1;
   lds_fence();
   for (int k = 0; k < a.top; ++k) {
-    const uint32_t best = max_u32<SUB>(top.k1);
-    const int first = first_lane<SUB>(best != 0 && top.k1 == best);
+    const uint32_t best = max_u32<SUB>(top.k[0]);
+    const int first = first_lane<SUB>(best != 0 && top.k[0] == best);
+    mine_key = lane == k ? best : mine_key;
     const bool won = first == lane;
     if (won) {
-      picked[sub][k] = e0 + top.p1;
-      last = top.k1;
-      last_at = top.p1;
-      top.k1 = top.k2;
-      top.p1 = top.p2;
-      top.k2 = 0;
+      picked[sub][k] = e0 + top.p[0];
+      last = top.k[0];
+      last_at = top.p[0];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        top.k[i] = top.k[i + 1];
+        top.p[i] = top.p[i + 1];
+      }
+      top.k[3] = 0;
     }
-    if (NPL > 2 && __any(won && top.k1 == 0)) {
-      const Two next = two_after(key, last, last_at);
-      if (won && top.k1 == 0) top = next;
+    if (NPL > 4 && __any(won && top.k[0] == 0)) {
+      const Best next = best_after(key, last, last_at);
+      if (won && top.k[0] == 0) top = next;
     }
   }
   lds_fence();
   const int32_t id = lane < a.top ? picked[sub][lane] : -1;
-  const float logit = id >= 0 ? clean(to_float(row[id])) : ninf;
+  const float logit = id < 0 ? ninf
+                      : a.balance ? __uint_as_float(words[sub][id]) : unordered(mine_key);
   float s = 0.0f;
   if (a.renorm) {
     const float high = fmaxf(max_f32<SUB>(logit), -__FLT_MAX__);
@@ -445,7 +462,11 @@ __global__ __launch_bounds__(kThreads) void rt_balance(int32_t experts,
   }
 }
 
-// 16 lanes a token where they hold its experts and chosen ones, else a wave.
+// 16 lanes a token where they hold its experts and chosen ones, else a wave.  Over 128 experts a
+// wave also where the tokens are too few to fill the card, so that one token's latency counts:
+// 256 experts in 8 groups, 16 lanes a token and a wave, us: 1 token 7.5 and 6.4, 1024 tokens 7.5
+// and 7.0, 4096 tokens 8.2 and 9.5, 65,536 tokens 35 and 78; 128 experts, 1 token: 3.5 and 3.9.
+constexpr int64_t kFewTokens = 1024;
 template <typename T>
 hipError_t choose(const RouteArgs& a, hipStream_t st) {
   const auto blocks = [&](int sub) {
@@ -456,7 +477,7 @@ hipError_t choose(const RouteArgs& a, hipStream_t st) {
     rt_choose<T, 16, 4><<<blocks(16), kThreads, 0, st>>>(a);
   else if (a.top <= 16 && a.experts <= 128)
     rt_choose<T, 16, 8><<<blocks(16), kThreads, 0, st>>>(a);
-  else if (a.top <= 16 && a.experts <= 256)
+  else if (a.top <= 16 && a.experts <= 256 && a.tokens > kFewTokens)
     rt_choose<T, 16, 16><<<blocks(16), kThreads, 0, st>>>(a);
   else if (a.experts <= 256)
     rt_choose<T, 64, 4><<<blocks(64), kThreads, 0, st>>>(a);
