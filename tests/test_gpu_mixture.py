@@ -491,6 +491,126 @@ def test_experts_larger_sizes(mix, dtype, tokens, experts, k, dim, hidden):
         near(g, v.detach().cpu(), rel, name)
 
 
+def experts_in_float64(x, ids, weights, w1, w2, dout):
+    """(out, dx, dweights, dw1, dw2) by products in float64 on the GPU, an expert at a time."""
+    xd, wd, w1d, w2d = (t.double().requires_grad_() for t in (x, weights, w1, w2))
+    hidden = w2.shape[2]
+    want = torch.zeros_like(xd)
+    for e in range(w2.shape[0]):
+        t, j = (ids == e).nonzero(as_tuple=True)
+        h = xd[t] @ w1d[e].t()
+        a = torch.nn.functional.silu(h[:, :hidden]) * h[:, hidden:]
+        want = want.index_add(0, t, (a @ w2d[e].t()) * wd[t, j][:, None])
+    return want, *torch.autograd.grad(want, (xd, wd, w1d, w2d), dout.double())
+
+
+# (tokens, experts, k, dim, hidden): two bytes, rows of 16 whole bytes and 128 pairs an expert and
+# more take tiles of 256 x 256; dim and hidden end inside a tile here and there
+WIDE = [(3000, 4, 2, 1032, 1544), (2600, 5, 2, 2048, 1032), (9000, 3, 1, 520, 1304),
+        (4100, 8, 3, 1024, 512)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", WIDE)
+def test_experts_many_rows(mix, dtype, tokens, experts, k, dim, hidden):
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 50)]
+    x, ids, weights, w1, w2, dout = a
+    ids[5], ids[6, 0], ids[7, 0] = -1, experts, -9
+    ids[8] = int(ids[8, 0])
+    want = experts_in_float64(*a)
+    out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+    got = mix.experts_backward(dout, x, ids, weights, w1, w2, saved)
+    # a gradient of an expert's weights sums up to tokens * k products
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    near(mix.experts(x, ids, weights, w1, w2), want[0].detach().cpu(), rel, "out alone")
+    for g, v, name in zip((out, *got), want, ("out", "dx", "dweights", "dw1", "dw2")):
+        near(g, v.detach().cpu(), rel, name)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_experts_many_rows_uneven_strided_and_repeated(mix, dtype):
+    """One expert with nearly all of the pairs, one with a single one and one with none; the
+    tokens' rows far apart with NaN between them; the same again bit for bit."""
+    tokens, experts, k, dim, hidden = 3000, 4, 2, 1032, 1544
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, tokens, experts, k, dim, hidden, 51)
+    ids[:] = 0
+    ids[:300, 1] = -1
+    ids[77, 1] = 3
+    wide = torch.full((tokens, dim + 24), float("nan"), dtype=dtype)
+    wide[:, :dim] = x
+    a = [t.cuda() for t in (x, ids, weights, w1, w2, dout)]
+    strided = [wide.cuda()[:, :dim], *a[1:5]]
+    want = experts_in_float64(*a)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    first = None
+    for _ in range(2):
+        out, saved = mix.experts_forward(*strided)
+        got = (out, *mix.experts_backward(a[5], *strided, saved))
+        for g, v, name in zip(got, want, ("out", "dx", "dweights", "dw1", "dw2")):
+            near(g, v.detach().cpu(), rel, name)
+        assert not got[3][1].any() and not got[4][2].any()
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_experts_many_rows_do_not_touch_each_other(mix, dtype):
+    tokens, experts, k, dim, hidden = 3000, 4, 2, 1032, 1544
+    a = expert_inputs(dtype, tokens, experts, k, dim, hidden, 52)
+    x, ids, weights, w1, w2, dout = (t.cuda() for t in a)
+
+    def both():
+        out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        return out, *mix.experts_backward(dout, x, ids, weights, w1, w2, saved)[:2]
+
+    good = both()
+    x[1300] = float("nan")
+    x[20, 3] = float("inf")
+    bad = both()
+    rest = torch.ones(tokens, dtype=torch.bool, device="cuda")
+    rest[1300] = rest[20] = False
+    assert all(torch.equal(p[rest], q[rest]) for p, q in zip(bad, good))
+    assert torch.isnan(bad[0][1300]).all()
+
+
+def test_a_recorded_graph_of_many_rows_replays(mix):
+    tokens, experts, k, dim, hidden = 3000, 4, 2, 1032, 1544
+    a = [t.cuda() for t in expert_inputs(torch.bfloat16, tokens, experts, k, dim, hidden, 53)]
+    x, ids, weights, w1, w2, dout = a
+
+    def step():
+        out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        return out, *mix.experts_backward(dout, x, ids, weights, w1, w2, saved)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        x.copy_(randn(tokens, dim, seed=60 + seed, dtype=torch.bfloat16))
+        ids.copy_(torch.randint(-1, experts, (tokens, k), generator=gen(70 + seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        assert all(torch.equal(p, q) for p, q in zip(got, step()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (64, 4, 1, 136, 72), (150, 16, 1, 264, 200), (40, 9, 3, 1000, 96), (200, 33, 2, 65, 129),
+    (2, 2, 2, 2048, 1024)])
+def test_experts_few_rows_an_expert(mix, dtype, tokens, experts, k, dim, hidden):
+    """Experts of one to 64 rows: their weights are read by several blocks of rows."""
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 54)]
+    x, ids, weights, w1, w2, _ = a
+    ids[1:tokens // 2, 0] = 0
+    want = experts_in_float64(*a)[0].detach().cpu()
+    got = mix.experts(x, ids, weights, w1, w2)
+    near(got, want, expert_tolerance(dtype, dim, hidden, tokens * k), "out")
+    assert torch.equal(got, mix.experts(x, ids, weights, w1, w2))
+
+
 def test_experts_gradient_against_differences(mix):
     x, ids, weights, w1, w2, dout = expert_inputs(F32, 6, 3, 2, 7, 5, 36, empty=False)
     a = [x, weights, w1, w2]
