@@ -8,6 +8,6 @@ import importlib
 
 
 def __getattr__(name):
-    if name in ("gsn", "clouds", "mixture"):
+    if name in ("gsn", "clouds", "mixture", "local_experts"):
         return importlib.import_module(f"{__name__}.{name}")
     raise AttributeError(name)
