@@ -471,7 +471,7 @@ def _matrix(t: torch.Tensor, dtype, rows: int, cols: int, what: str):
         raise ValueError(f"{what} must have contiguous rows")
     if rows <= 1:
         row = cols  # (torch gives such a tensor any stride)
-    if row < cols:
+    elif row < cols:
         raise ValueError(f"{what} must not have overlapping rows")
     return t.data_ptr(), row
 
@@ -498,10 +498,9 @@ def _on(t: torch.Tensor, stream) -> int | ctypes.c_void_p:
 
 
 def _params_type(x_dtype, weight, bias) -> torch.dtype:
-    got = {t.dtype for t in (weight, bias) if t is not None}
-    if len(got) > 1:
+    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
         raise ValueError("weight and bias must be of the same type")
-    return got.pop() if got else x_dtype
+    return weight.dtype if weight is not None else bias.dtype if bias is not None else x_dtype
 
 
 def gsn_layer_norm(x, weight, bias, eps: float, y, stats=None, stream=None):

@@ -13,15 +13,19 @@ workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import gsn
 
 
-def _same_device(x, **others):
-    for name, t in others.items():
-        if t is not None and t.device != x.device:
-            raise ValueError(f"{name} is on {t.device}, not on {x.device}")
+# (the checks of a call cost a single token as much as its kernel: they are kept short)
+def _same_device(x, *others):
+    d = x.get_device()
+    for t in others:
+        if t is not None and t.get_device() != d:
+            raise ValueError(f"a tensor of {tuple(t.shape)} is on {t.device}, not on {x.device}")
 
 
 def _rows(x: torch.Tensor, what: str) -> torch.Tensor:
@@ -40,7 +44,7 @@ def _bytes(n: int, x: torch.Tensor) -> torch.Tensor:
 def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     """(y, stats): the norm of every row of x (rows, dim) and what its backward pass takes."""
     _rows(x, "x")
-    _same_device(x, weight=weight, bias=bias)
+    _same_device(x, weight, bias)
     y = x.new_empty(x.shape)
     stats = x.new_empty((2, x.shape[0]), dtype=torch.float32)
     gsn.gsn_layer_norm(x, weight, bias, eps, y, stats)
@@ -50,7 +54,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
 def layer_norm_backward(dy, x, weight, bias, stats, need=(True, True, True)):
     """(dx, dweight, dbias) from dy; None for what is not needed or has no parameter."""
     _rows(x, "x")
-    _same_device(x, dy=dy, weight=weight, bias=bias, stats=stats)
+    _same_device(x, dy, weight, bias, stats)
     rows, dim = x.shape
     dx = x.new_empty(x.shape) if need[0] else None
     dweight = torch.empty_like(weight) if need[1] and weight is not None else None
@@ -84,7 +88,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
                                        for t in (x, weight, bias)):
         return _LayerNorm.apply(x, weight, bias, eps)
     _rows(x, "x")
-    _same_device(x, weight=weight, bias=bias)
+    _same_device(x, weight, bias)
     y = x.new_empty(x.shape)
     gsn.gsn_layer_norm(x, weight, bias, eps, y)
     return y
@@ -92,8 +96,11 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 # -------------------------------------------------------------------------- routing ----
 
+_route_params = functools.lru_cache(maxsize=256)(gsn.make_route)  # (never written to)
+
+
 def _route(logits, params, balance, valid):
-    _same_device(logits, balance=balance, valid=valid)
+    _same_device(logits, balance, valid)
     tokens = logits.shape[0]
     ids = logits.new_empty((tokens, params.top), dtype=torch.int32)
     weights = logits.new_empty((tokens, params.top), dtype=torch.float32)
@@ -102,7 +109,7 @@ def _route(logits, params, balance, valid):
 
 
 def _route_backward(dweights, logits, ids, params):
-    _same_device(logits, dweights=dweights, ids=ids)
+    _same_device(logits, dweights, ids)
     dlogits = logits.new_empty(logits.shape)
     gsn.gsn_route_backward(params, dweights, logits, ids, dlogits)
     return dlogits
@@ -129,8 +136,8 @@ def route(logits, top, *, score="softmax", balance=None, groups=1, top_groups=1,
     and their weights; see gsn_route in include/gsn.h for the order, masks and ties.  The weights
     are differentiable with respect to the logits."""
     _rows(logits, "logits")
-    params = gsn.make_route(logits.shape[1], top, score, groups, top_groups, best, renormalise,
-                            scale)
+    params = _route_params(logits.shape[1], top, score, groups, top_groups, best, renormalise,
+                           scale)
     if torch.is_grad_enabled() and logits.requires_grad:
         return _Route.apply(logits, params, balance, valid)
     return _route(logits, params, balance, valid)
@@ -140,8 +147,8 @@ def route_backward(dweights, logits, ids, *, score="softmax", groups=1, top_grou
                    renormalise=True, scale=1.0):
     """dlogits of ``route`` with the same options (those of the choice alone do not matter)."""
     _rows(logits, "logits")
-    params = gsn.make_route(logits.shape[1], ids.shape[1], score, groups, top_groups, best,
-                            renormalise, scale)
+    params = _route_params(logits.shape[1], ids.shape[1], score, groups, top_groups, best,
+                           renormalise, scale)
     return _route_backward(dweights, logits, ids, params)
 
 
@@ -162,7 +169,7 @@ def route_balance(counts, balance, rate=1e-3):
 
 def _experts_forward(x, ids, weights, w1, w2, save):
     _rows(x, "x")
-    _same_device(x, ids=ids, weights=weights, w1=w1, w2=w2)
+    _same_device(x, ids, weights, w1, w2)
     p = gsn.make_experts(x, ids, w1, w2)
     size = gsn.gsn_experts_workspace_bytes(p, False)
     if size == 0:
@@ -181,7 +188,7 @@ def experts_forward(x, ids, weights, w1, w2):
 def experts_backward(dout, x, ids, weights, w1, w2, saved, need=(True, True, True, True)):
     """(dx, dweights, dw1, dw2) from dout; None for what is not needed."""
     _rows(x, "x")
-    _same_device(x, dout=dout, ids=ids, weights=weights, w1=w1, w2=w2, saved=saved)
+    _same_device(x, dout, ids, weights, w1, w2, saved)
     p = gsn.make_experts(x, ids, w1, w2)
     size = gsn.gsn_experts_workspace_bytes(p, True)
     if size == 0:
