@@ -7,21 +7,24 @@ namespace gsn {
 
 constexpr int kPlanExperts = 1024;  // experts at most
 constexpr int kPlanRows = 256;      // rows of a listed block
+constexpr int kSmallRows = 64;      // of a small one
 
 // Pairs (token, place k), number token * top + k, sorted by expert and then by number: row r of
 // the products is pair rows[r], pair j is row pos[j] (-1 for a pair without an expert), expert
 // e's rows are offsets[e] .. offsets[e + 1] - 1.  Blocks of kPlanRows rows that hold one expert's
 // rows alone are listed in tiles as (expert, the expert's first row, its first block, its
-// blocks), expert by expert; *tile_count of them.
+// blocks), expert by expert, tile_count[0] of them; blocks of kSmallRows in small as (expert,
+// the block's first row, its rows), tile_count[1] of them.
 struct Plan {
   int32_t* offsets;     // experts + 1
-  int32_t* tile_count;  // 1
+  int32_t* tile_count;  // 2
   int4* tiles;          // most_tiles
+  int4* small;          // most_small
   int32_t* rows;        // pairs
   int32_t* token;       // pairs: rows[r] / top
   int32_t* pos;         // pairs
   int32_t* counts;      // pairs of each expert in each chunk of them
-  int32_t most_tiles;
+  int32_t most_tiles, most_small;
 };
 
 struct Experts {
@@ -61,8 +64,7 @@ hipError_t launch_experts(const Experts& x, hipStream_t st);
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
 
-// Sides of the products' tiles.
-constexpr int32_t kTileRows = 256;
-constexpr int32_t kSmallRows = 64;
+// Side of the products' large tiles (kSmallRows: the small ones).
+constexpr int32_t kTileRows = kPlanRows;
 
 }  // namespace gsn

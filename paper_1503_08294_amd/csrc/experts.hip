@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_place(int32_t pairs, int32_t 
                                                          Plan plan) {
   __shared__ int32_t total[kPlanExperts], before[kPlanExperts];
   __shared__ int32_t next[kPlanWaves][kPlanExperts];  // a wave's next row of an expert
-  __shared__ int2 sums[kPlanWaves];
+  __shared__ int32_t sums[3][kPlanWaves];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int32_t chunks = gridDim.x, chunk = blockIdx.x;
   for (int e = tid; e < experts; e += kPlanThreads) {
@@ -81,36 +81,38 @@ __global__ __launch_bounds__(kPlanThreads) void ex_place(int32_t pairs, int32_t 
   }
   __syncthreads();
   // first rows and blocks of the experts, kPlanEach experts a thread
-  int2 mine = {0, 0};
+  const auto blocks = [](int32_t c, int32_t rows) { return (c + rows - 1) / rows; };
+  int32_t mine[3] = {0, 0, 0}, first[3];  // rows, blocks, small blocks
 #pragma unroll
   for (int k = 0; k < kPlanEach; ++k) {
     const int e = tid * kPlanEach + k;
     const int32_t c = e < experts ? total[e] : 0;
-    mine.x += c;
-    mine.y += (c + kPlanRows - 1) / kPlanRows;
+    mine[0] += c;
+    mine[1] += blocks(c, kPlanRows);
+    mine[2] += blocks(c, kSmallRows);
   }
-  int32_t rows = mine.x, tiles = mine.y;
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int32_t r = __shfl_up(rows, o), t = __shfl_up(tiles, o);
-    if (lane >= o) {
-      rows += r;
-      tiles += t;
+  for (int q = 0; q < 3; ++q) {
+    first[q] = mine[q];
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int32_t v = __shfl_up(first[q], o);
+      if (lane >= o) first[q] += v;
     }
+    if (lane == kWave - 1) sums[q][wave] = first[q];
   }
-  if (lane == kWave - 1) sums[wave] = int2{rows, tiles};
   __syncthreads();
-  for (int w = 0; w < wave; ++w) {
-    rows += sums[w].x;
-    tiles += sums[w].y;
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    for (int w = 0; w < wave; ++w) first[q] += sums[q][w];
+    first[q] -= mine[q];
   }
-  rows -= mine.x;
-  tiles -= mine.y;
 #pragma unroll
   for (int k = 0; k < kPlanEach; ++k) {
     const int e = tid * kPlanEach + k;
     if (e >= experts) break;
-    const int32_t c = total[e], blocks = (c + kPlanRows - 1) / kPlanRows;
+    const int32_t c = total[e], rows = first[0];
+    const int32_t large = blocks(c, kPlanRows), small = blocks(c, kSmallRows);
     int32_t at = rows + before[e];
 #pragma unroll
     for (int w = 0; w < kPlanWaves; ++w) {
@@ -122,12 +124,20 @@ __global__ __launch_bounds__(kPlanThreads) void ex_place(int32_t pairs, int32_t 
       plan.offsets[e] = rows;
       if (e == experts - 1) {
         plan.offsets[experts] = rows + c;
-        *plan.tile_count = tiles + blocks;
+        plan.tile_count[0] = first[1] + large;
+        plan.tile_count[1] = first[2] + small;
       }
-      for (int32_t b = 0; b < blocks; ++b) plan.tiles[tiles + b] = int4{e, rows, tiles, blocks};
     }
-    rows += c;
-    tiles += blocks;
+    // (each chunk lists a part of the blocks)
+    for (int32_t b = chunk; b < large; b += chunks)
+      plan.tiles[first[1] + b] = int4{e, rows, first[1], large};
+    for (int32_t b = chunk; b < small; b += chunks) {
+      const int32_t r = b * kSmallRows;
+      plan.small[first[2] + b] = int4{e, rows + r, c - r < kSmallRows ? c - r : kSmallRows, 0};
+    }
+    first[0] += c;
+    first[1] += large;
+    first[2] += small;
   }
   __syncthreads();
   // a wave's pairs in their order: the lanes that hold the same expert are found bit by bit
@@ -169,11 +179,13 @@ struct Carver {
 void carve_plan(Carver* c, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs);
   Plan& p = x->plan;
-  p.most_tiles = static_cast<int32_t>(
-      x->pairs / kPlanRows + (x->pairs < x->experts ? x->pairs : x->experts));
+  const int64_t cut = x->pairs < x->experts ? x->pairs : x->experts;
+  p.most_tiles = static_cast<int32_t>(x->pairs / kPlanRows + cut);
+  p.most_small = static_cast<int32_t>(x->pairs / kSmallRows + cut);
   p.offsets = static_cast<int32_t*>(c->take(4 * (static_cast<size_t>(x->experts) + 1)));
-  p.tile_count = static_cast<int32_t*>(c->take(4));
+  p.tile_count = static_cast<int32_t*>(c->take(8));
   p.tiles = static_cast<int4*>(c->take(16 * static_cast<size_t>(p.most_tiles)));
+  p.small = static_cast<int4*>(c->take(16 * static_cast<size_t>(p.most_small)));
   p.rows = static_cast<int32_t*>(c->take(4 * n));
   p.token = static_cast<int32_t*>(c->take(4 * n));
   p.pos = static_cast<int32_t*>(c->take(4 * n));
@@ -251,14 +263,14 @@ int32_t tile_side(const Experts& x, int32_t dtype) {
              ? kTileRows : kSmallRows;
 }
 
-// Whether every product's grid stays below 2^32 threads.
+// Whether every launch's grid stays below 2^32 threads.
 bool grids_ok(const Experts& x) {
   const int64_t side = x.side, threads = side == kTileRows ? 512 : 256;
   const auto tiles = [&](int64_t n) { return (n + side - 1) / side; };
-  const int64_t rows = (x.pairs / kPlanRows + x.experts) * (kPlanRows / side);
+  const int64_t rows = x.pairs / side + x.experts;
   const int64_t wide = tiles(2 * static_cast<int64_t>(x.hidden)) + 1, deep = tiles(x.dim);
-  const int64_t most = std::max(std::max(rows * wide, rows * deep), x.experts * wide * deep);
-  return most + 2048 < (int64_t{1} << 32) / threads;
+  const int64_t most = std::max(rows * wide, rows * deep + 2 * x.experts * wide * deep);
+  return most + 4096 < (int64_t{1} << 32) / threads;
 }
 
 bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256 == 0; }

@@ -261,15 +261,11 @@ __device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
 // Workgroups go round the 8 XCDs.  Runs of `run` tiles go to one XCD, where the tiles that its CUs
 // work on at a time share operands through its L2; the next run goes to the next XCD.
 // Fewer tiles than 8 runs are dealt out evenly.
-__device__ __forceinline__ int32_t spread(int32_t total, int32_t run) {
+__device__ __forceinline__ int32_t spread(int32_t block, int32_t total, int32_t run) {
   if (total < 8 * run) run = (total + 7) / 8;
-  const int32_t in = blockIdx.x >> 3;
-  const int32_t id = (in / run * 8 + (blockIdx.x & 7)) * run + in % run;
+  const int32_t in = block >> 3;
+  const int32_t id = (in / run * 8 + (block & 7)) * run + in % run;
   return id < total ? id : -1;
-}
-// Workgroups that cover `total` tiles in that order.
-inline uint32_t spread_grid(uint32_t total, uint32_t run) {
-  return (total + 8 * run - 1) / (8 * run) * (8 * run);
 }
 // Place of a tile in a block of tiles_m x tiles_n, taken TALL tiles of m by all of n at a time, m
 // first: 32 tiles in a row, 4 x 8, have 4 + 8 tiles of operands.
@@ -279,20 +275,36 @@ __device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t 
   const int32_t left = tiles_m - g * TALL, tall = left < TALL ? left : TALL;
   return int2{g * TALL + in % tall, in / tall};
 }
-// Of the large tiles, one a CU; the small ones, which many CUs have several of, go round in order
-// (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small products).
-template <int BM>
-constexpr int32_t kTall = BM == kTileRows ? 4 : 1;
-template <int BM>
-constexpr int32_t kRun = BM == kTileRows ? 32 : 1;
+// Large tiles, one a CU, go in runs; the small ones, which many CUs have several of, go round in
+// order (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small
+// products).
+constexpr int32_t kTall = 4, kRun = 32;
+
+// Gradients of the weights of the pairs from j on, one a thread: the sums of their parts.
+__device__ __forceinline__ void sum_dots(const Experts& x, int64_t j) {
+  j += threadIdx.x;
+  if (j >= x.pairs) return;
+  const int32_t r = x.plan.pos[j];
+  float s = 0.0f;
+  if (r >= 0)
+    for (int i = 0; i < x.dot_tiles; ++i) s += x.dots[static_cast<int64_t>(r) * x.dot_tiles + i];
+  x.dweights[j] = s;
+}
+
+// Workgroups of the backward pass's second launch: for dxr, then dw1, dw2 and dweights.
+struct Shares {
+  int32_t in_x, in_w1, in_w2;
+};
 
 // One tile of BM x BN by WM x WN waves, for any sizes and alignment: a stage's 16-byte chunks are
 // loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk that
 // a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so that every
 // load is one instruction without a branch (one with a branch has to be awaited at once); TINY:
 // rows may be shorter than that, and are loaded element by element.
-template <typename T, Kind KIND, int BM, int BN, int WM, int WN, bool TINY>
-__global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
+constexpr int kSmallLds = 2 * 2 * kSmallRows * kRowBytes;
+template <typename T, Kind KIND, bool TINY>
+__device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* smem) {
+  constexpr int BM = kSmallRows, BN = kSmallRows, WM = 2, WN = 2;
   constexpr int kThr = WM * WN * kWave;
   constexpr int kE = 16 / sizeof(T);         // elements of a chunk
   constexpr int kBK = kRowBytes / sizeof(T);  // k staged at a time
@@ -301,8 +313,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   constexpr bool kTrB = kWeightsKind || KIND == kBackwardGate || KIND == kBackwardIn;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;
-  constexpr int kStage = (BM + BN) * kRowBytes;
-  __shared__ __attribute__((aligned(16))) char smem[2 * kStage];
+  constexpr int kStage = kSmallLds / 2;
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WN, wn = wave % WN;
@@ -317,27 +328,21 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun<BM>);
-    if (id < 0) return;
     e = id / (tiles_m * tiles_n);
-    const int2 at = tile_place<kTall<BM>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
-    m0 = at.x * BM;
-    n0 = at.y * BN;
+    m0 = id / tiles_n % tiles_m * BM;
+    n0 = id % tiles_n * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    constexpr int kSub = kPlanRows / BM;
-    const int32_t id = spread(*x.plan.tile_count * kSub * tiles_n, kRun<BM>);
-    if (id < 0) return;
-    const int4 t = x.plan.tiles[id / (kSub * tiles_n)];
-    const int2 at = tile_place<kTall<BM>>(id - t.z * kSub * tiles_n, t.w * kSub, tiles_n);
+    const int32_t i = id / tiles_n;
+    const int4 t = x.plan.small[i];  // (most_small of them; what follows the listed ones is not used)
+    if (i >= x.plan.tile_count[1]) return;
     e = t.x;
     m0 = 0;
-    row0 = t.y + at.x * BM;
-    n0 = at.y * kCols;
-    mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
-    if (mrows <= 0) return;
+    row0 = t.y;
+    n0 = id % tiles_n * kCols;
+    mrows = t.z;
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
@@ -486,6 +491,24 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_product(Experts x) {
   __syncthreads();
 
   finish<T, KIND, BM, BN, WM, WN>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0, row0);
+}
+
+constexpr int kSmallThreads = 256;
+template <typename T, Kind KIND, bool TINY>
+__global__ __launch_bounds__(kSmallThreads) void ex_small(Experts x) {
+  __shared__ __attribute__((aligned(16))) char smem[kSmallLds];
+  small_tile<T, KIND, TINY>(x, blockIdx.x, smem);
+}
+template <typename T, bool TINY>
+__global__ __launch_bounds__(kSmallThreads) void ex_small_gradients(Experts x, Shares n) {
+  __shared__ __attribute__((aligned(16))) char smem[kSmallLds];
+  int32_t id = blockIdx.x;
+  if (id < n.in_x) return small_tile<T, kBackwardIn, TINY>(x, id, smem);
+  id -= n.in_x;
+  if (id < n.in_w1) return small_tile<T, kWeightsIn, TINY>(x, id, smem);
+  id -= n.in_w1;
+  if (id < n.in_w2) return small_tile<T, kWeightsOut, TINY>(x, id, smem);
+  sum_dots(x, static_cast<int64_t>(id - n.in_w2) * kSmallThreads);
 }
 
 // ------------------------------------------------------------------ aligned operands ----
@@ -739,8 +762,11 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
 
 // One tile of BM x BN by WM x WN waves.  Rows of every operand start at a multiple of 16 bytes
 // and hold a multiple of 16 bytes.
-template <typename T, Kind KIND, int BM, int BN, int WM, int WN, int SA, int SB>
-__global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
+constexpr int kLargeThreads = 512;
+constexpr int kLargeLds = 5 * kTileRows * kRowBytes;
+template <typename T, Kind KIND>
+__device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char* smem) {
+  constexpr int BM = kTileRows, BN = kTileRows, WM = 2, WN = 4;
   constexpr int kThr = WM * WN * kWave, kWaves = WM * WN;
   constexpr int kE = 16 / sizeof(T);          // elements of a chunk
   constexpr int kBK = kRowBytes / sizeof(T);  // k staged at a time
@@ -750,10 +776,10 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;  // chunks a lane loads of each operand
   // SA and SB places for a stage of A and of B; of gathered k, the tokens of four stages
+  constexpr int SA = kWeightsKind ? 2 : 3, SB = 2;
   constexpr int kSlotA = BM * kRowBytes, kSlotB = BN * kRowBytes;
-  static_assert(SB == 2 && (SA == 2 || SA == 3));
-  __shared__ __attribute__((aligned(1024))) char
-      smem[SA * kSlotA + SB * kSlotB + (kWeightsKind ? 4 * kWave * 4 : 0)];
+  static_assert(kThr == kLargeThreads &&
+                SA * kSlotA + SB * kSlotB + (kWeightsKind ? 4 * kWave * 4 : 0) <= kLargeLds);
 
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -768,27 +794,25 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    const int32_t id = spread(x.experts * tiles_m * tiles_n, kRun<BM>);
+    const int32_t id = spread(block, x.experts * tiles_m * tiles_n, kRun);
     if (id < 0) return;
     e = id / (tiles_m * tiles_n);
-    const int2 at = tile_place<kTall<BM>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    const int2 at = tile_place<kTall>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
     m0 = at.x * BM;
     n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    constexpr int kSub = kPlanRows / BM;
-    const int32_t id = spread(*x.plan.tile_count * kSub * tiles_n, kRun<BM>);
+    const int32_t id = spread(block, x.plan.tile_count[0] * tiles_n, kRun);
     if (id < 0) return;
-    const int4 t = x.plan.tiles[id / (kSub * tiles_n)];
-    const int2 at = tile_place<kTall<BM>>(id - t.z * kSub * tiles_n, t.w * kSub, tiles_n);
+    const int4 t = x.plan.tiles[id / tiles_n];
+    const int2 at = tile_place<kTall>(id - t.z * tiles_n, t.w, tiles_n);
     e = t.x;
     m0 = 0;
     row0 = t.y + at.x * BM;
     n0 = at.y * kCols;
     mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
-    if (mrows <= 0) return;
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
@@ -1012,6 +1036,24 @@ __global__ __launch_bounds__(WM* WN* kWave) void ex_tiles(Experts x) {
   __syncthreads();
   finish_rows<T, KIND, BM, BN, WM, WN>(x, acc, smem, lds, e, m0, mrows, n0, row0);
 }
+
+template <typename T, Kind KIND>
+__global__ __launch_bounds__(kLargeThreads) void ex_large(Experts x) {
+  __shared__ __attribute__((aligned(1024))) char smem[kLargeLds];
+  large_tile<T, KIND>(x, blockIdx.x, smem);
+}
+template <typename T>
+__global__ __launch_bounds__(kLargeThreads) void ex_large_gradients(Experts x, Shares n) {
+  __shared__ __attribute__((aligned(1024))) char smem[kLargeLds];
+  int32_t block = blockIdx.x;
+  if (block < n.in_x) return large_tile<T, kBackwardIn>(x, block, smem);
+  block -= n.in_x;
+  if (block < n.in_w1) return large_tile<T, kWeightsIn>(x, block, smem);
+  block -= n.in_w1;
+  if (block < n.in_w2) return large_tile<T, kWeightsOut>(x, block, smem);
+  sum_dots(x, static_cast<int64_t>(block - n.in_w2) * kLargeThreads);
+}
+
 // ------------------------------------------------------------------------- few pairs ----
 
 // With a few pairs an expert the products read every weight once and are bound by that: no
@@ -1257,17 +1299,6 @@ __global__ __launch_bounds__(256) void ex_join(Experts x, const float* __restric
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void ex_dots(Experts x) {
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (j >= x.pairs) return;
-  const int32_t r = x.plan.pos[j];
-  float s = 0.0f;
-  if (r >= 0)
-    for (int i = 0; i < x.dot_tiles; ++i) s += x.dots[static_cast<int64_t>(r) * x.dot_tiles + i];
-  x.dweights[j] = s;
-}
-
 inline uint32_t blocks_of(int64_t n, int64_t per) {
   return static_cast<uint32_t>((n + per - 1) / per);
 }
@@ -1277,37 +1308,62 @@ inline uint32_t join_blocks(const Experts& x) {
   return static_cast<uint32_t>(n < (1 << 20) ? n : 1 << 20);
 }
 
-// Workgroups that cover every tile of BM x BN of a product.
-template <Kind KIND, int BM, int BN>
-uint32_t tiles_grid(const Experts& x) {
+// Workgroups for every tile of a product.
+template <Kind KIND>
+uint32_t product_grid(const Experts& x) {
+  const bool large = x.side == kTileRows;
   const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
                                KIND == kWeightsOut ? x.hidden : x.dim,
-                               KIND == kForwardGate ? BN / 2 : BN);
-  const uint32_t tiles = KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, BM) * n
-                         : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, BM) * n
-                                               : x.plan.most_tiles * (kPlanRows / BM) * n;
-  return spread_grid(tiles, kRun<BM>);
+                               KIND == kForwardGate ? x.side / 2 : x.side);
+  const uint32_t tiles =
+      n * (KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, x.side)
+           : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, x.side)
+           : large ? x.plan.most_tiles : x.plan.most_small);
+  return large ? blocks_of(tiles, 8 * kRun) * 8 * kRun : tiles;
+}
+
+template <typename T>
+bool tiny(const Experts& x) {
+  constexpr int kE = 16 / sizeof(T);
+  return x.dim < kE || x.hidden < kE;
 }
 
 template <typename T, Kind KIND>
 void product(Experts x, hipStream_t st) {
   x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
+  const uint32_t grid = product_grid<KIND>(x);
+  if (grid == 0) return;
   if constexpr (sizeof(T) == 2) {
     if (x.side == kTileRows) {
-      constexpr int S = kTileRows;
-      const uint32_t grid = tiles_grid<KIND, S, S>(x);
-      if (grid > 0)
-        ex_tiles<T, KIND, S, S, 2, 4, KIND >= kWeightsIn ? 2 : 3, 2><<<grid, 512, 0, st>>>(x);
+      ex_large<T, KIND><<<grid, kLargeThreads, 0, st>>>(x);
       return;
     }
   }
-  constexpr int S = kSmallRows, kE = 16 / sizeof(T);
-  const uint32_t grid = tiles_grid<KIND, S, S>(x);
+  if (tiny<T>(x)) ex_small<T, KIND, true><<<grid, kSmallThreads, 0, st>>>(x);
+  else ex_small<T, KIND, false><<<grid, kSmallThreads, 0, st>>>(x);
+}
+
+// What the backward pass makes of dpre, wact and the dots, in one launch, so that one product's
+// last tiles do not leave the chip idle.  All of the backward and forward pass, with a launch for
+// each of the four and with one, us: 2,000 tokens, 2 of 8 experts, 1,024 x 1,024, bfloat16: 245 and
+// 209; 465, 3 of 32, 343 x 1,343: 232 and 196; 16,384, 2 of 32, 2,048 x 2,048: 3,026 and 2,994.
+template <typename T>
+void gradients(Experts x, hipStream_t st) {
+  x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
+  const auto in = [](bool wanted, uint32_t n) { return static_cast<int32_t>(wanted ? n : 0); };
+  const Shares n{in(x.dx, product_grid<kBackwardIn>(x)), in(x.dw1, product_grid<kWeightsIn>(x)),
+                 in(x.dw2, product_grid<kWeightsOut>(x))};
+  const uint32_t threads = x.side == kTileRows ? kLargeThreads : kSmallThreads;
+  const uint32_t grid = n.in_x + n.in_w1 + n.in_w2 + (x.dweights ? blocks_of(x.pairs, threads) : 0);
   if (grid == 0) return;
-  if (x.dim < kE || x.hidden < kE)
-    ex_product<T, KIND, S, S, 2, 2, true><<<grid, 256, 0, st>>>(x);
-  else
-    ex_product<T, KIND, S, S, 2, 2, false><<<grid, 256, 0, st>>>(x);
+  if constexpr (sizeof(T) == 2) {
+    if (x.side == kTileRows) {
+      ex_large_gradients<T><<<grid, threads, 0, st>>>(x, n);
+      return;
+    }
+  }
+  if (tiny<T>(x)) ex_small_gradients<T, true><<<grid, threads, 0, st>>>(x, n);
+  else ex_small_gradients<T, false><<<grid, threads, 0, st>>>(x, n);
 }
 
 }  // namespace
@@ -1349,18 +1405,10 @@ hipError_t launch_experts(const Experts& x, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st) {
-  if (x.pairs > 0) {
-    product<T, kBackwardGate>(x, st);
-    Experts d = x;
-    d.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
-    if (x.dweights) ex_dots<T><<<blocks_of(x.pairs, 256), 256, 0, st>>>(d);
-  }
-  if (x.dx && x.tokens > 0) {
-    product<T, kBackwardIn>(x, st);
+  product<T, kBackwardGate>(x, st);  // (none without pairs)
+  gradients<T>(x, st);
+  if (x.dx && x.tokens > 0)
     ex_join<T, false><<<join_blocks(x), 256, 0, st>>>(x, x.dxr, static_cast<T*>(x.dx));
-  }
-  if (x.dw1) product<T, kWeightsIn>(x, st);
-  if (x.dw2) product<T, kWeightsOut>(x, st);
   return hipGetLastError();
 }
 
