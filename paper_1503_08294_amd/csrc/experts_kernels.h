@@ -346,9 +346,8 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
-  // Rows of the operands: with k contiguous, this lane's LA (LB) rows, null outside; with k as the
-  // row, row k (from its first column in the tile).
-  const auto token = [&](int64_t r) { return x.plan.token[r]; };
+  // With k contiguous: this lane's LA (LB) rows, null outside.
+  const auto token = [&](int64_t r) { return static_cast<int64_t>(x.plan.token[r]); };
   const T* rows_a[LA];
   const T* rows_b[LB];
   if constexpr (!kTrA) {
@@ -362,7 +361,7 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
       else if constexpr (KIND == kForwardOut)
         rows_a[j] = static_cast<const T*>(x.act) + (row0 + m) * F;
       else if constexpr (KIND == kBackwardGate)
-        rows_a[j] = static_cast<const T*>(x.dout) + static_cast<int64_t>(token(row0 + m)) * D;
+        rows_a[j] = static_cast<const T*>(x.dout) + token(row0 + m) * D;
       else
         rows_a[j] = static_cast<const T*>(x.dpre) + (row0 + m) * 2 * F;
     }
@@ -385,22 +384,28 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
       }
     }
   }
-  const auto krow_a = [&](int32_t k) -> const T* {  // m contiguous
-    if constexpr (KIND == kWeightsIn)
-      return static_cast<const T*>(x.dpre) + (row0 + k) * 2 * F + m0;
-    else
-      return static_cast<const T*>(x.dout) + static_cast<int64_t>(token(row0 + k)) * D + m0;
-  };
-  const auto krow_b = [&](int32_t k) -> const T* {  // n contiguous
-    if constexpr (KIND == kWeightsIn)
-      return static_cast<const T*>(x.x) + token(row0 + k) * x.x_stride + n0;
-    else if constexpr (KIND == kWeightsOut)
-      return static_cast<const T*>(x.wact) + (row0 + k) * F + n0;
-    else if constexpr (KIND == kBackwardGate)
-      return static_cast<const T*>(x.w2) + (static_cast<int64_t>(e) * D + k) * F + n0;
-    else
-      return static_cast<const T*>(x.w1) + (static_cast<int64_t>(e) * 2 * F + k) * D + n0;
-  };
+  // With k as the row: rows of A and B (from their first column in the tile) that are not gathered,
+  // and the steps from row to row.
+  constexpr bool kGatherA = KIND == kWeightsOut, kGatherB = KIND == kWeightsIn;
+  const T *base_a = nullptr, *base_b = nullptr;
+  int64_t step_a = 0, step_b = 0;
+  if constexpr (KIND == kWeightsIn) {
+    base_a = static_cast<const T*>(x.dpre) + row0 * 2 * F + m0;
+    step_a = 2 * static_cast<int64_t>(F);
+    base_b = static_cast<const T*>(x.x) + n0;
+    step_b = x.x_stride;
+  } else if constexpr (KIND == kWeightsOut) {
+    base_a = static_cast<const T*>(x.dout) + m0;
+    step_a = D;
+    base_b = static_cast<const T*>(x.wact) + row0 * F + n0;
+    step_b = F;
+  } else if constexpr (KIND == kBackwardGate) {
+    base_b = static_cast<const T*>(x.w2) + static_cast<int64_t>(e) * D * F + n0;
+    step_b = F;
+  } else if constexpr (KIND == kBackwardIn) {
+    base_b = static_cast<const T*>(x.w1) + static_cast<int64_t>(e) * 2 * F * D + n0;
+    step_b = D;
+  }
   // chunk j's place in a stage, k0 the stage's first k: k (or the column) where it begins, and the
   // length of its row from there (0 or less: nothing of it is inside)
   const T* const zeros = reinterpret_cast<const T*>(kZeros);
@@ -411,27 +416,66 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
     return (is_a ? chunk_n<T, kCA>(i / kCA, i % kCA) : chunk_n<T, kCB>(i / kCB, i % kCB)) * kE;
   };
   const auto length = [&](bool is_a) { return (is_a ? !kTrA : !kTrB) ? K : is_a ? mrows : N - n0; };
+  // Chunks with k as the row: their first k in the stage, where k ends for them (0 for columns
+  // outside), and their address, which moves on from stage to stage; gathered rows have their
+  // token's, loaded a stage before it is used and ahead of that stage's chunks, as a wait for a
+  // load is one for all before it.
+  int32_t first[LA + LB], end[LA + LB], tokens[LA + LB];
+  const T* walk[LA + LB];
+  const auto load_tokens = [&](int32_t k0) {
+#pragma unroll
+    for (int j = 0; j < LA + LB; ++j) {
+      if (!(j < LA ? kGatherA : kGatherB)) continue;
+      const int32_t k = k0 + first[j];
+      tokens[j] = x.plan.token[row0 + (k < K ? k : K - 1)];
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < LA + LB; ++j) {
+    const bool is_a = j < LA;
+    if (is_a ? !kTrA : !kTrB) continue;
+    const int q = is_a ? j : j - LA, i = q * kThr + tid;
+    const int32_t at = begin(is_a, q, 0), len = length(is_a);
+    first[j] = i / ((is_a ? BM : BN) / kE);
+    end[j] = at < len ? K : 0;
+    walk[j] = (is_a ? base_a : base_b) + (TINY || at + kE <= len ? at : len - kE);
+    if (!(is_a ? kGatherA : kGatherB)) walk[j] += first[j] * (is_a ? step_a : step_b);
+  }
+  if (K > 0) load_tokens(0);
   Frag ahead[2][LA + LB];
   const auto load = [&](int32_t k0, Frag (&to)[LA + LB]) {
+    const T* from[LA + LB];
 #pragma unroll
     for (int j = 0; j < LA + LB; ++j) {
       const bool is_a = j < LA;
-      const int q = is_a ? j : j - LA, i = q * kThr + tid;
+      if (is_a ? kGatherA : kGatherB)
+        from[j] = walk[j] + tokens[j] * (is_a ? step_a : step_b);
+    }
+    if constexpr (kGatherA || kGatherB) load_tokens(k0 + kBK);
+#pragma unroll
+    for (int j = 0; j < LA + LB; ++j) {
+      const bool is_a = j < LA;
+      const int q = is_a ? j : j - LA;
       const int32_t at = begin(is_a, q, k0), len = length(is_a);
-      const T* row;
-      if (is_a) {
-        if constexpr (!kTrA) row = rows_a[q];
-        else row = k0 + i / (BM / kE) < K ? krow_a(k0 + i / (BM / kE)) : nullptr;
+      bool in;
+      if (is_a ? kTrA : kTrB) {
+        in = k0 + first[j] < end[j];
+        if (!(is_a ? kGatherA : kGatherB)) {
+          from[j] = walk[j];
+          walk[j] += kBK * (is_a ? step_a : step_b);
+        }
       } else {
-        if constexpr (!kTrB) row = rows_b[q];
-        else row = k0 + i / (BN / kE) < K ? krow_b(k0 + i / (BN / kE)) : nullptr;
+        const T* row = nullptr;
+        if constexpr (!kTrA) row = is_a ? rows_a[is_a ? q : 0] : row;
+        if constexpr (!kTrB) row = is_a ? row : rows_b[is_a ? 0 : q];
+        in = row && at < len;
+        from[j] = row + (TINY || at + kE <= len ? at : len - kE);
       }
       if constexpr (TINY) {
         to[j].u = u32x4{0, 0, 0, 0};
-        if (row) to[j] = row_chunk<false>(row, at, len);
+        if (in) to[j] = row_chunk<false>(from[j] - at, at, len);
       } else {
-        const T* p = row + (at + kE <= len ? at : len - kE);
-        to[j] = row_chunk<true>(row && at < len ? p : zeros, 0, kE);
+        to[j] = row_chunk<true>(in ? from[j] : zeros, 0, kE);
       }
     }
   };
