@@ -66,5 +66,6 @@ hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
 
 // Side of the products' large tiles (kSmallRows: the small ones).
 constexpr int32_t kTileRows = kPlanRows;
+constexpr int32_t kMiddleRows = 128;
 
 }  // namespace gsn

@@ -244,23 +244,31 @@ Experts experts_of(const gsn_experts_params& p) {
   return x;
 }
 
-// Sides of the products' tiles.  The large tiles are for 2-byte elements whose rows, and their
-// starts, are multiples of 16 bytes, and for products that fill the chip with them: 128 pairs an
-// expert at least, and 128 tiles of the first product.  Forward and backward pass, large and small
-// tiles (us): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 280 and 286; 495, 3 of 7, 1,984 x 320: 214
-// and 145; 1,920, 1 of 7, 3,456 x 448: 320 and 280; 465, 3 of 32, 344 x 1,344: 244 and 194; forward
-// of 5,100, 1 of 8, 448 x 992: 60 and 64.  In binary32, where the matrix cores are 16 times slower,
-// small tiles waste less at the edges: 777 tokens, 3 of 7, 512 x 336: 915 and 201; forward of 7,706,
-// 8 of 32, 576 x 704: 1,469 and 1,412.
+// Sides of the products' tiles: of 2-byte elements the larger ones, from 128 pairs an expert on and
+// where the first product has enough of them to fill the chip; the largest need rows, and starts of
+// rows, at multiples of 16 bytes.  Forward and backward pass in us,
+// 256 and 64 (128 tiles of 256): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 280 and 286; 495, 3 of 7,
+//   1,984 x 320: 214 and 145; 1,920, 1 of 7, 3,456 x 448: 320 and 280; 465, 3 of 32, 344 x 1,344: 244
+//   and 194; forward of 5,100, 1 of 8, 448 x 992: 60 and 64.
+// 128 and 64 (256 tiles of 128): 16,384, 2 of 32, 2,047 x 2,047: 5,252 and 7,935; 1,500, 2 of 8, 999 x
+//   701 (297 tiles): 177 and 191; 1,500, 1 of 8, 511 x 1,023 (240 tiles): 141 and 110; with fewer pairs
+//   an expert, 2,048, 2 of 64, 511 x 701: 307 and 281.
+// In binary32, where the matrix cores are 16 times slower, small tiles waste less at the edges: 128
+// and 64: 4,096, 2 of 16, 1,024 x 1,024: 1,938 and 1,647; forward of 7,706, 8 of 32, 576 x 704: 1,494
+// and 1,434.
 int32_t tile_side(const Experts& x, int32_t dtype) {
+  const auto tiles = [&](int32_t side) {
+    return (x.pairs / side + x.experts / 2) *
+           ((2 * static_cast<int64_t>(x.hidden) + side - 1) / side);
+  };
+  if (dtype == GSN_F32 || x.pairs < int64_t{128} * x.experts) return kSmallRows;
   const bool aligned = x.dim % 8 == 0 && x.hidden % 8 == 0 && x.x_stride % 8 == 0 &&
                        aligned16(x.x) && aligned16(x.w1) && aligned16(x.w2) &&
                        aligned16(x.out) && aligned16(x.dout) && aligned16(x.dx) &&
                        aligned16(x.dw1) && aligned16(x.dw2);
-  const int64_t tiles = (x.pairs / kTileRows + x.experts / 2) *
-                        ((2 * static_cast<int64_t>(x.hidden) + kTileRows - 1) / kTileRows);
-  return dtype != GSN_F32 && aligned && x.pairs >= int64_t{128} * x.experts && tiles >= 128
-             ? kTileRows : kSmallRows;
+  if (aligned && tiles(kTileRows) >= 128) return kTileRows;
+  // (a row shorter than 16 bytes is loaded by the small tiles alone)
+  return x.dim >= 8 && x.hidden >= 8 && tiles(kMiddleRows) >= 256 ? kMiddleRows : kSmallRows;
 }
 
 // Whether every launch's grid stays below 2^32 threads.

@@ -275,10 +275,15 @@ __device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t 
   const int32_t left = tiles_m - g * TALL, tall = left < TALL ? left : TALL;
   return int2{g * TALL + in % tall, in / tall};
 }
-// Large tiles, one a CU, go in runs; the small ones, which many CUs have several of, go round in
-// order (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small
-// products).
-constexpr int32_t kTall = 4, kRun = 32;
+// Runs of the large tiles, one a CU, and of the middle ones, two a CU; small ones go round in order
+// (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small products).
+// Middle tiles in order, in runs of 16 and of 64, us: 16,384 tokens, 2 of 32 experts, 2,047 x 2,047:
+// 5,353, 5,252, 5,318; forward of 8,192, 4 of 32, 777 x 1,501: 609, 556, 550; 4,096, 2 of 16, 1,023
+// x 1,023: 535, 533, 594.
+template <int SIDE>
+constexpr int32_t kTall = SIDE == kSmallRows ? 1 : 4;
+template <int SIDE>
+constexpr int32_t kRun = SIDE == kTileRows ? 32 : SIDE == kMiddleRows ? 16 : 1;
 
 // Gradients of the weights of the pairs from j on, one a thread: the sums of their parts.
 __device__ __forceinline__ void sum_dots(const Experts& x, int64_t j) {
@@ -301,10 +306,11 @@ struct Shares {
 // a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so that every
 // load is one instruction without a branch (one with a branch has to be awaited at once); TINY:
 // rows may be shorter than that, and are loaded element by element.
-constexpr int kSmallLds = 2 * 2 * kSmallRows * kRowBytes;
-template <typename T, Kind KIND, bool TINY>
-__device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* smem) {
-  constexpr int BM = kSmallRows, BN = kSmallRows, WM = 2, WN = 2;
+template <int SIDE>
+constexpr int kLooseLds = 2 * 2 * SIDE * kRowBytes;
+template <typename T, Kind KIND, int SIDE, bool TINY>
+__device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* smem) {
+  constexpr int BM = SIDE, BN = SIDE, WM = 2, WN = 2;
   constexpr int kThr = WM * WN * kWave;
   constexpr int kE = 16 / sizeof(T);         // elements of a chunk
   constexpr int kBK = kRowBytes / sizeof(T);  // k staged at a time
@@ -313,7 +319,7 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
   constexpr bool kTrB = kWeightsKind || KIND == kBackwardGate || KIND == kBackwardIn;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;
-  constexpr int kStage = kSmallLds / 2;
+  constexpr int kStage = kLooseLds<SIDE> / 2;
 
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int wm = wave / WN, wn = wave % WN;
@@ -328,21 +334,39 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
+    if constexpr (kRun<SIDE> > 1) {
+      id = spread(id, x.experts * tiles_m * tiles_n, kRun<SIDE>);
+      if (id < 0) return;
+    }
     e = id / (tiles_m * tiles_n);
-    m0 = id / tiles_n % tiles_m * BM;
-    n0 = id % tiles_n * BN;
+    const int2 at = tile_place<kTall<SIDE>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    m0 = at.x * BM;
+    n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    const int32_t i = id / tiles_n;
-    const int4 t = x.plan.small[i];  // (most_small of them; what follows the listed ones is not used)
-    if (i >= x.plan.tile_count[1]) return;
-    e = t.x;
     m0 = 0;
-    row0 = t.y;
-    n0 = id % tiles_n * kCols;
-    mrows = t.z;
+    if constexpr (SIDE == kSmallRows) {
+      const int32_t i = id / tiles_n;
+      const int4 t = x.plan.small[i];  // (past the listed ones it is not used)
+      if (i >= x.plan.tile_count[1]) return;
+      e = t.x;
+      row0 = t.y;
+      n0 = id % tiles_n * kCols;
+      mrows = t.z;
+    } else {
+      constexpr int kSub = kPlanRows / SIDE;
+      id = spread(id, x.plan.tile_count[0] * kSub * tiles_n, kRun<SIDE>);
+      if (id < 0) return;
+      const int4 t = x.plan.tiles[id / (kSub * tiles_n)];
+      const int2 at = tile_place<kTall<SIDE>>(id - t.z * kSub * tiles_n, t.w * kSub, tiles_n);
+      e = t.x;
+      row0 = t.y + at.x * SIDE;
+      n0 = at.y * kCols;
+      mrows = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
+      if (mrows <= 0) return;
+    }
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
@@ -537,22 +561,22 @@ __device__ __forceinline__ void small_tile(const Experts& x, int32_t id, char* s
   finish<T, KIND, BM, BN, WM, WN>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0, row0);
 }
 
-constexpr int kSmallThreads = 256;
-template <typename T, Kind KIND, bool TINY>
-__global__ __launch_bounds__(kSmallThreads) void ex_small(Experts x) {
-  __shared__ __attribute__((aligned(16))) char smem[kSmallLds];
-  small_tile<T, KIND, TINY>(x, blockIdx.x, smem);
+constexpr int kLooseThreads = 256;
+template <typename T, Kind KIND, int SIDE, bool TINY>
+__global__ __launch_bounds__(kLooseThreads, 2) void ex_loose(Experts x) {
+  __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
+  loose_tile<T, KIND, SIDE, TINY>(x, blockIdx.x, smem);
 }
-template <typename T, bool TINY>
-__global__ __launch_bounds__(kSmallThreads) void ex_small_gradients(Experts x, Shares n) {
-  __shared__ __attribute__((aligned(16))) char smem[kSmallLds];
+template <typename T, int SIDE, bool TINY>
+__global__ __launch_bounds__(kLooseThreads, 2) void ex_loose_gradients(Experts x, Shares n) {
+  __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
   int32_t id = blockIdx.x;
-  if (id < n.in_x) return small_tile<T, kBackwardIn, TINY>(x, id, smem);
+  if (id < n.in_x) return loose_tile<T, kBackwardIn, SIDE, TINY>(x, id, smem);
   id -= n.in_x;
-  if (id < n.in_w1) return small_tile<T, kWeightsIn, TINY>(x, id, smem);
+  if (id < n.in_w1) return loose_tile<T, kWeightsIn, SIDE, TINY>(x, id, smem);
   id -= n.in_w1;
-  if (id < n.in_w2) return small_tile<T, kWeightsOut, TINY>(x, id, smem);
-  sum_dots(x, static_cast<int64_t>(id - n.in_w2) * kSmallThreads);
+  if (id < n.in_w2) return loose_tile<T, kWeightsOut, SIDE, TINY>(x, id, smem);
+  sum_dots(x, static_cast<int64_t>(id - n.in_w2) * kLooseThreads);
 }
 
 // ------------------------------------------------------------------ aligned operands ----
@@ -838,20 +862,20 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
   if constexpr (kWeightsKind) {
     const int32_t M = KIND == kWeightsIn ? 2 * F : D;
     const int32_t tiles_m = (M + BM - 1) / BM;
-    const int32_t id = spread(block, x.experts * tiles_m * tiles_n, kRun);
+    const int32_t id = spread(block, x.experts * tiles_m * tiles_n, kRun<kTileRows>);
     if (id < 0) return;
     e = id / (tiles_m * tiles_n);
-    const int2 at = tile_place<kTall>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
+    const int2 at = tile_place<kTall<kTileRows>>(id - e * tiles_m * tiles_n, tiles_m, tiles_n);
     m0 = at.x * BM;
     n0 = at.y * BN;
     mrows = M - m0;
     row0 = x.plan.offsets[e];
     K = x.plan.offsets[e + 1] - static_cast<int32_t>(row0);
   } else {
-    const int32_t id = spread(block, x.plan.tile_count[0] * tiles_n, kRun);
+    const int32_t id = spread(block, x.plan.tile_count[0] * tiles_n, kRun<kTileRows>);
     if (id < 0) return;
     const int4 t = x.plan.tiles[id / tiles_n];
-    const int2 at = tile_place<kTall>(id - t.z * tiles_n, t.w, tiles_n);
+    const int2 at = tile_place<kTall<kTileRows>>(id - t.z * tiles_n, t.w, tiles_n);
     e = t.x;
     m0 = 0;
     row0 = t.y + at.x * BM;
@@ -1355,15 +1379,17 @@ inline uint32_t join_blocks(const Experts& x) {
 // Workgroups for every tile of a product.
 template <Kind KIND>
 uint32_t product_grid(const Experts& x) {
-  const bool large = x.side == kTileRows;
   const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
                                KIND == kWeightsOut ? x.hidden : x.dim,
                                KIND == kForwardGate ? x.side / 2 : x.side);
   const uint32_t tiles =
       n * (KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, x.side)
            : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, x.side)
-           : large ? x.plan.most_tiles : x.plan.most_small);
-  return large ? blocks_of(tiles, 8 * kRun) * 8 * kRun : tiles;
+           : x.side == kSmallRows ? x.plan.most_small
+                                  : x.plan.most_tiles * (kPlanRows / x.side));
+  const uint32_t round = x.side == kTileRows     ? 8 * kRun<kTileRows>
+                         : x.side == kMiddleRows ? 8 * kRun<kMiddleRows> : 1;
+  return blocks_of(tiles, round) * round;
 }
 
 template <typename T>
@@ -1383,8 +1409,12 @@ void product(Experts x, hipStream_t st) {
       return;
     }
   }
-  if (tiny<T>(x)) ex_small<T, KIND, true><<<grid, kSmallThreads, 0, st>>>(x);
-  else ex_small<T, KIND, false><<<grid, kSmallThreads, 0, st>>>(x);
+  if (x.side == kMiddleRows)
+    ex_loose<T, KIND, kMiddleRows, false><<<grid, kLooseThreads, 0, st>>>(x);
+  else if (tiny<T>(x))
+    ex_loose<T, KIND, kSmallRows, true><<<grid, kLooseThreads, 0, st>>>(x);
+  else
+    ex_loose<T, KIND, kSmallRows, false><<<grid, kLooseThreads, 0, st>>>(x);
 }
 
 // What the backward pass makes of dpre, wact and the dots, in one launch, so that one product's
@@ -1397,7 +1427,7 @@ void gradients(Experts x, hipStream_t st) {
   const auto in = [](bool wanted, uint32_t n) { return static_cast<int32_t>(wanted ? n : 0); };
   const Shares n{in(x.dx, product_grid<kBackwardIn>(x)), in(x.dw1, product_grid<kWeightsIn>(x)),
                  in(x.dw2, product_grid<kWeightsOut>(x))};
-  const uint32_t threads = x.side == kTileRows ? kLargeThreads : kSmallThreads;
+  const uint32_t threads = x.side == kTileRows ? kLargeThreads : kLooseThreads;
   const uint32_t grid = n.in_x + n.in_w1 + n.in_w2 + (x.dweights ? blocks_of(x.pairs, threads) : 0);
   if (grid == 0) return;
   if constexpr (sizeof(T) == 2) {
@@ -1406,8 +1436,12 @@ void gradients(Experts x, hipStream_t st) {
       return;
     }
   }
-  if (tiny<T>(x)) ex_small_gradients<T, true><<<grid, threads, 0, st>>>(x, n);
-  else ex_small_gradients<T, false><<<grid, threads, 0, st>>>(x, n);
+  if (x.side == kMiddleRows)
+    ex_loose_gradients<T, kMiddleRows, false><<<grid, threads, 0, st>>>(x, n);
+  else if (tiny<T>(x))
+    ex_loose_gradients<T, kSmallRows, true><<<grid, threads, 0, st>>>(x, n);
+  else
+    ex_loose_gradients<T, kSmallRows, false><<<grid, threads, 0, st>>>(x, n);
 }
 
 }  // namespace

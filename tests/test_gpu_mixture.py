@@ -596,6 +596,66 @@ def test_a_recorded_graph_of_many_rows_replays(mix):
         assert all(torch.equal(p, q) for p, q in zip(got, step()))
 
 
+# The same of rows that begin anywhere: tiles of 128 x 128.
+LOOSE = [(3000, 4, 2, 515, 701), (2600, 5, 2, 1023, 520), (9000, 3, 1, 130, 1307),
+         (4100, 8, 3, 1001, 259), (6000, 2, 1, 9, 700)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", LOOSE)
+def test_experts_many_loose_rows(mix, dtype, tokens, experts, k, dim, hidden):
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 55)]
+    x, ids, weights, w1, w2, dout = a
+    ids[5], ids[6, 0], ids[7, 0] = -1, experts, -9
+    ids[8] = int(ids[8, 0])
+    want = experts_in_float64(*a)
+    out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+    got = mix.experts_backward(dout, x, ids, weights, w1, w2, saved)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    near(mix.experts(x, ids, weights, w1, w2), want[0].detach().cpu(), rel, "out alone")
+    for g, v, name in zip((out, *got), want, ("out", "dx", "dweights", "dw1", "dw2")):
+        near(g, v.detach().cpu(), rel, name)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_experts_many_loose_rows_uneven_strided_and_repeated(mix, dtype):
+    """Aligned sizes, but rows of x that begin anywhere, and one expert with nearly all pairs."""
+    tokens, experts, k, dim, hidden = 3000, 4, 2, 520, 704
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, tokens, experts, k, dim, hidden, 56)
+    ids[:] = 0
+    ids[:300, 1] = -1
+    ids[77, 1] = 3
+    wide = torch.full((tokens, dim + 13), float("nan"), dtype=dtype)
+    wide[:, 3:dim + 3] = x
+    a = [t.cuda() for t in (x, ids, weights, w1, w2, dout)]
+    strided = [wide.cuda()[:, 3:dim + 3], *a[1:5]]
+    want = experts_in_float64(*a)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    first = None
+    for _ in range(2):
+        out, saved = mix.experts_forward(*strided)
+        got = (out, *mix.experts_backward(a[5], *strided, saved))
+        for g, v, name in zip(got, want, ("out", "dx", "dweights", "dw1", "dw2")):
+            near(g, v.detach().cpu(), rel, name)
+        assert not got[3][1].any() and not got[4][2].any()
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_experts_gradients_one_by_one(mix, dtype):
+    """Each gradient alone is the one of all four together."""
+    for size in ((3000, 4, 2, 1032, 1544), (3000, 4, 2, 515, 701), (90, 5, 2, 72, 40)):
+        a = [t.cuda() for t in expert_inputs(dtype, *size, 57)]
+        x, ids, weights, w1, w2, dout = a
+        _, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        whole = mix.experts_backward(dout, x, ids, weights, w1, w2, saved)
+        for i in range(4):
+            need = [j == i for j in range(4)]
+            got = mix.experts_backward(dout, x, ids, weights, w1, w2, saved, need)
+            assert torch.equal(got[i], whole[i]) and sum(g is not None for g in got) == 1
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
     (64, 4, 1, 136, 72), (150, 16, 1, 264, 200), (40, 9, 3, 1000, 96), (200, 33, 2, 65, 129),
