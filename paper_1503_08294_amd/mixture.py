@@ -45,8 +45,8 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     """(y, stats): the norm of every row of x (rows, dim) and what its backward pass takes."""
     _rows(x, "x")
     _same_device(x, weight, bias)
-    y = x.new_empty(x.shape)
-    stats = x.new_empty((2, x.shape[0]), dtype=torch.float32)
+    y = torch.empty_like(x)
+    stats = x.new_empty(2, x.shape[0], dtype=torch.float32)
     gsn.gsn_layer_norm(x, weight, bias, eps, y, stats)
     return y, stats
 
@@ -56,7 +56,7 @@ def layer_norm_backward(dy, x, weight, bias, stats, need=(True, True, True)):
     _rows(x, "x")
     _same_device(x, dy, weight, bias, stats)
     rows, dim = x.shape
-    dx = x.new_empty(x.shape) if need[0] else None
+    dx = torch.empty_like(x) if need[0] else None
     dweight = torch.empty_like(weight) if need[1] and weight is not None else None
     dbias = torch.empty_like(bias) if need[2] and bias is not None else None
     ws = None
@@ -89,7 +89,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
         return _LayerNorm.apply(x, weight, bias, eps)
     _rows(x, "x")
     _same_device(x, weight, bias)
-    y = x.new_empty(x.shape)
+    y = torch.empty_like(x)
     gsn.gsn_layer_norm(x, weight, bias, eps, y)
     return y
 
@@ -102,15 +102,15 @@ _route_params = functools.lru_cache(maxsize=256)(gsn.make_route)  # (never writt
 def _route(logits, params, balance, valid):
     _same_device(logits, balance, valid)
     tokens = logits.shape[0]
-    ids = logits.new_empty((tokens, params.top), dtype=torch.int32)
-    weights = logits.new_empty((tokens, params.top), dtype=torch.float32)
+    ids = logits.new_empty(tokens, params.top, dtype=torch.int32)
+    weights = logits.new_empty(tokens, params.top, dtype=torch.float32)
     gsn.gsn_route(params, logits, balance, valid, ids, weights)
     return ids, weights
 
 
 def _route_backward(dweights, logits, ids, params):
     _same_device(logits, dweights, ids)
-    dlogits = logits.new_empty(logits.shape)
+    dlogits = torch.empty_like(logits)
     gsn.gsn_route_backward(params, dweights, logits, ids, dlogits)
     return dlogits
 
@@ -174,7 +174,7 @@ def _experts_forward(x, ids, weights, w1, w2, save):
     size = gsn.gsn_experts_workspace_bytes(p, False)
     if size == 0:
         raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
-    out = x.new_empty(x.shape)
+    out = torch.empty_like(x, memory_format=torch.contiguous_format)
     saved = _bytes(gsn.gsn_experts_saved_bytes(p), x) if save else None
     gsn.gsn_experts(p, x, ids, weights, w1, w2, out, saved, _bytes(size, x))
     return out, saved
@@ -194,7 +194,7 @@ def experts_backward(dout, x, ids, weights, w1, w2, saved, need=(True, True, Tru
     if size == 0:
         raise gsn.GsnError(gsn.GSN_E_INVAL, "gsn_experts_workspace_bytes")
     dx, dweights, dw1, dw2 = (
-        t.new_empty(t.shape) if n else None
+        torch.empty_like(t, memory_format=torch.contiguous_format) if n else None
         for t, n in zip((x, weights, w1, w2), need))
     gsn.gsn_experts_backward(p, dout, x, weights, w1, w2, saved, dx, dweights, dw1, dw2,
                              _bytes(size, x))
