@@ -8,8 +8,7 @@ library.  Flags:
                          no packed fp32 instructions are generated;
   -mllvm -amdgpu-mfma-vgpr-form
                          matrix-core results are written to ordinary VGPRs, so the vector
-                         unit reads them without accumulator-register copies (not for the
-                         experts' products, see flags());
+                         unit reads them without accumulator-register copies;
   no fast-math, IEEE denormals (default for gfx950 fp32).
 """
 import os
@@ -30,15 +29,8 @@ ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",
          "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+         "-mllvm", "-amdgpu-mfma-vgpr-form",
          "-Wall", "-Wno-unused-result"]
-
-VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-
-
-def flags(source: str):
-    """The experts' products hold up to 256 sums a lane besides their operands: those go to the
-    accumulation registers, which are as many again as the ordinary ones."""
-    return FLAGS if source.startswith("experts_") else FLAGS + VGPR_FORM
 
 
 def hipcc() -> str:
@@ -58,7 +50,7 @@ def build(verbose: bool = False, extra=()) -> str:
     for s in SOURCES:
         obj = os.path.join(OBJ_DIR, os.path.splitext(s)[0] + ".o")
         objs.append(obj)
-        cmds.append([hipcc(), *flags(s), *extra, "-c", os.path.join(CSRC, s), "-o", obj])
+        cmds.append([hipcc(), *FLAGS, *extra, "-c", os.path.join(CSRC, s), "-o", obj])
     if verbose:
         for c in cmds:
             print(" ".join(c), flush=True)

@@ -26,9 +26,9 @@ typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int64_t kFewTokens = 2;    // tokens up to which one launch makes the second product and the sum
+constexpr int64_t kFewTokens = 2;    // for which one launch makes the second product and the sum
 constexpr int64_t kFewPairs = 2048;  // pairs that a workgroup lists at most
-constexpr int kRowBytes = 128;  // bytes of k (contiguous operands) in a stage
+constexpr int kRowBytes = 128;       // bytes of k (contiguous operands) in a stage
 
 // 16 bytes of an operand in a lane: 8 or 4 values of k of row (lane & 15)
 union Frag {
@@ -277,9 +277,9 @@ __device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t 
 }
 // Runs of the large tiles, one a CU, and of the middle ones, two a CU; small ones go round in order
 // (runs of 128 in blocks of 8 x 16 gained 2% on 32,768 pairs and lost up to 50% on small products).
-// Middle tiles in order, in runs of 16 and of 64, us: 16,384 tokens, 2 of 32 experts, 2,047 x 2,047:
-// 5,353, 5,252, 5,318; forward of 8,192, 4 of 32, 777 x 1,501: 609, 556, 550; 4,096, 2 of 16, 1,023
-// x 1,023: 535, 533, 594.
+// Middle tiles in order, in runs of 16 and of 64, us: 16,384 tokens, 2 of 32 experts, 2,047 x
+// 2,047: 5,353, 5,252, 5,318; forward of 8,192, 4 of 32, 777 x 1,501: 609, 556, 550; 4,096, 2 of
+// 16, 1,023 x 1,023: 535, 533, 594.
 template <int SIDE>
 constexpr int32_t kTall = SIDE == kSmallRows ? 1 : 4;
 template <int SIDE>
@@ -301,11 +301,18 @@ struct Shares {
   int32_t in_x, in_w1, in_w2;
 };
 
-// One tile of BM x BN by WM x WN waves, for any sizes and alignment: a stage's 16-byte chunks are
-// loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk that
-// a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so that every
-// load is one instruction without a branch (one with a branch has to be awaited at once); TINY:
-// rows may be shorter than that, and are loaded element by element.
+// One tile of SIDE x SIDE by four waves, for any sizes and alignment: a stage's 16-byte chunks are
+// loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk
+// that a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so
+// that every load is one instruction without a branch (one with a branch has to be awaited at
+// once); TINY: rows may be shorter than that, and are loaded element by element.
+// Several workgroups share a CU, so that one's loads, barriers and results hide behind another's
+// products.  In binary32 bound by the matrix cores (0.153 PFLOP/s in a large library product):
+// 4,096 tokens, 2 of 16 experts, 1,024 x 1,024, forward and backward 1.55 ms, 0.10 PFLOP/s with
+// the rows that fill up tiles left out.  2-byte elements, tiles of 128: bound by what moves the
+// operands through registers and LDS, 16,384, 2 of 32, 2,047 x 2,047: 5.3 ms, 0.47 PFLOP/s.  Small
+// calls are bound by the latency of a tile (the list, the tokens, the rows: three loads that wait
+// for each other) and of a launch: 777, 3 of 7, 501 x 333, binary32 150 us in 8 launches.
 template <int SIDE>
 constexpr int kLooseLds = 2 * 2 * SIDE * kRowBytes;
 template <typename T, Kind KIND, int SIDE, bool TINY>
@@ -562,13 +569,20 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
 }
 
 constexpr int kLooseThreads = 256;
+// Waves of a SIMD that registers have to last for.  Five in place of four, steps in us: binary32,
+// 4,096 tokens, 2 of 16 experts, 1,024 x 1,024: 1,556 and 1,625; bfloat16, 465, 3 of 32, 343 x
+// 1,343: 195 and 179.  Middle tiles, two in place of one: 16,384, 2 of 32, 2,047 x 2,047: 5,350 and
+// 8,216.
+template <typename T, int SIDE>
+constexpr int kLooseWaves = SIDE == kMiddleRows ? 2 : sizeof(T) == 4 ? 5 : 4;
 template <typename T, Kind KIND, int SIDE, bool TINY>
-__global__ __launch_bounds__(kLooseThreads, 2) void ex_loose(Experts x) {
+__global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loose(Experts x) {
   __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
   loose_tile<T, KIND, SIDE, TINY>(x, blockIdx.x, smem);
 }
 template <typename T, int SIDE, bool TINY>
-__global__ __launch_bounds__(kLooseThreads, 2) void ex_loose_gradients(Experts x, Shares n) {
+__global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loose_gradients(
+    Experts x, Shares n) {
   __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
   int32_t id = blockIdx.x;
   if (id < n.in_x) return loose_tile<T, kBackwardIn, SIDE, TINY>(x, id, smem);
@@ -649,7 +663,8 @@ struct Turn {
 #pragma unroll
     for (int i = 0; i < kStores; ++i) {
       const int row = i * (kWave / kLanes) + lane / kLanes, col = lane % kLanes * kW;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(at + row * kRow + col * static_cast<int>(sizeof(U)));
+      const u32x4 v = *reinterpret_cast<const u32x4*>(at + row * kRow +
+                                                      col * static_cast<int>(sizeof(U)));
       if (row < rows && col < cols) *reinterpret_cast<u32x4*>(to + row * ld + col) = v;
     }
   }
@@ -711,13 +726,10 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
     // The gates and ups of 16 rows come to LDS while the rows before are worked on.
     using Narrow = Turn<T, kW>;
     constexpr int kPre = 16 * kW * 4;  // bytes of 16 rows of gates, or of ups
-    // three results turned at once, or (4-byte ones) one after another in the same place
-    constexpr int kTurns = sizeof(T) == 2 ? 3 : 1;
-    static_assert(2 * kPre + kTurns * Narrow::kBytes <= kRoom && kPre % 1024 == 0);
+    static_assert(2 * kPre + 3 * Narrow::kBytes <= kRoom && kPre % 1024 == 0);
     const char* const pre = room;
     char* const turns = room + 2 * kPre;
-    const Narrow dgate{turns}, dup{turns + (kTurns > 1 ? 1 : 0) * Narrow::kBytes},
-        wact{turns + (kTurns > 1 ? 2 : 0) * Narrow::kBytes};
+    const Narrow dgate{turns}, dup{turns + Narrow::kBytes}, wact{turns + 2 * Narrow::kBytes};
     const uint32_t pre_at = lds + wave * kRoom;
     constexpr int kLanes = kW / 4;  // of a row of 4-byte elements
     const auto fetch = [&](int i) {
@@ -742,48 +754,37 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
       const float w = m + li < mrows ? x.weights[x.plan.rows[row0 + m + li]] : 0.0f;
       // (the stores since then count too)
       if (i == 0) await_own<0>();
-      else await_own<kTurns * Narrow::kStores>();
+      else await_own<3 * Narrow::kStores>();
       const int64_t row = row0 + m;
-      T* const to_dg = static_cast<T*>(x.dpre) + row * 2 * F + n;
-      T* const to_wa = static_cast<T*>(x.wact) + row * F + n;
       float part = 0.0f;
 #pragma unroll
-      for (int turn = 0; turn < 4 - kTurns; ++turn) {  // 0: all at once, or the gate's gradient
-        if (turn > 0) {
-          (turn == 1 ? dgate.out(to_dg, 2 * F, mrows - m, cols, lane)
-                     : dup.out(to_dg + F, 2 * F, mrows - m, cols, lane));
-          wave_fence();
-        }
+      for (int j = 0; j < NT; ++j) {
+        const int at = (li * kW + j * 16 + lg) * 4;
+        const f32x4 g = *reinterpret_cast<const f32x4*>(pre + at);
+        const f32x4 u = *reinterpret_cast<const f32x4*>(pre + kPre + at);
+        float dg[4], du[4], wa[4];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int at = (li * kW + j * 16 + lg) * 4;
-          const f32x4 g = *reinterpret_cast<const f32x4*>(pre + at);
-          const f32x4 u = *reinterpret_cast<const f32x4*>(pre + kPre + at);
-          float dg[4], du[4], wa[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const Gated r = gated(acc[i][j][q], g[q], u[q], w);
-            if (turn == 0) part += j * 16 + lg < cols ? r.dot : 0.0f;
-            dg[q] = r.dg;
-            du[q] = r.du;
-            wa[q] = r.wa;
-          }
-          if (turn == 0) dgate.put(li, j * 16 + lg, dg);
-          if (kTurns > 1 || turn == 1) dup.put(li, j * 16 + lg, du);
-          if (kTurns > 1 || turn == 2) wact.put(li, j * 16 + lg, wa);
+        for (int q = 0; q < 4; ++q) {
+          const Gated r = gated(acc[i][j][q], g[q], u[q], w);
+          part += j * 16 + lg < cols ? r.dot : 0.0f;
+          dg[q] = r.dg;
+          du[q] = r.du;
+          wa[q] = r.wa;
         }
-        wave_fence();
+        dgate.put(li, j * 16 + lg, dg);
+        dup.put(li, j * 16 + lg, du);
+        wact.put(li, j * 16 + lg, wa);
       }
+      wave_fence();
       parts[i] = part;
       if (i + 1 < MT) {
         await_reads();
         fetch(i + 1);
       }
-      if constexpr (kTurns > 1) {
-        dgate.out(to_dg, 2 * F, mrows - m, cols, lane);
-        dup.out(to_dg + F, 2 * F, mrows - m, cols, lane);
-      }
-      wact.out(to_wa, F, mrows - m, cols, lane);
+      T* const to = static_cast<T*>(x.dpre) + row * 2 * F + n;
+      dgate.out(to, 2 * F, mrows - m, cols, lane);
+      dup.out(to + F, 2 * F, mrows - m, cols, lane);
+      wact.out(static_cast<T*>(x.wact) + row * F + n, F, mrows - m, cols, lane);
       wave_fence();
     }
     __syncthreads();
@@ -828,8 +829,16 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
   }
 }
 
-// One tile of BM x BN by WM x WN waves.  Rows of every operand start at a multiple of 16 bytes
-// and hold a multiple of 16 bytes.
+// One tile of 256 x 256 of 2-byte elements by eight waves.  Rows of every operand start at a
+// multiple of 16 bytes and hold a multiple of 16 bytes.
+// So large a tile moves the fewest bytes per product into LDS: 64 KB a stage of 64 k, which the
+// card's L2 caches bring in 1.19 us when all CUs load (14 TB/s), while the products alone take 1.0
+// us at the clock that they leave; together 1.2 to 1.3.  Besides its stages a tile takes 7 us to
+// start (list, tokens, first stages) and 12 for its results, which nothing hides, as LDS holds one
+// workgroup a CU; the gates' gradients, with 0.9 MB a tile to read and write, some 50.
+// 16,384 tokens, 2 of 32 experts, 2,048 x 2,048, bfloat16 (a large library product reaches 1.28
+// PFLOP/s): first product 592 us (0.93 PFLOP/s), second 295 (0.93), gates' gradients 503 (0.55),
+// the other three together 1,600 (0.86).
 constexpr int kLargeThreads = 512;
 constexpr int kLargeLds = 5 * kTileRows * kRowBytes;
 template <typename T, Kind KIND>
@@ -897,12 +906,10 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
   constexpr bool kGatherA = KIND == kForwardGate || KIND == kBackwardGate || KIND == kWeightsOut;
   constexpr bool kGatherB = KIND == kWeightsIn;
   const int ra = kTrA ? tid / kCA : tid >> 3, rb = kTrB ? tid / kCB : tid >> 3;
-  const auto col_a = [&](int j) { return chunk_n<T>(ra + j * kStepA, tid % kCA); };
-  const auto col_b = [&](int j) { return chunk_n<T>(rb + j * kStepB, tid % kCB); };
-  // (2-byte types: kStep is a multiple of 16, which leaves the chunk's place alone)
-  constexpr bool kSame = sizeof(T) == 2;
-  const int ca = kTrA ? col_a(0) : chunk_k(ra, tid & 7);
-  const int cb = kTrB ? col_b(0) : chunk_k(rb, tid & 7);
+  // (kStep is a multiple of 16, which leaves the chunk's place alone)
+  static_assert(sizeof(T) == 2 && kStepA % 16 == 0 && kStepB % 16 == 0);
+  const int ca = kTrA ? chunk_n<T>(ra, tid % kCA) : chunk_k(ra, tid & 7);
+  const int cb = kTrB ? chunk_n<T>(rb, tid % kCB) : chunk_k(rb, tid & 7);
   const int32_t ka = kTrA ? ra : ca * kE, kb = kTrB ? rb : cb * kE;  // k of j = 0 in stage 0
   int64_t lda, ldb;  // bytes from row to row
   const T *a0, *b0;
@@ -981,11 +988,7 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
       if constexpr (kGatherA) p += token[j] * lda;
       else p += j * (kStepA * lda);
       bool in = h * kBK + ka + (kTrA ? j * kStepA : 0) < K;
-      if constexpr (kTrA) {
-        const int c = kSame ? ca : col_a(j);
-        if constexpr (!kSame) p += (c - ca) * 16;
-        in = in && c * kE < mrows;
-      }
+      if constexpr (kTrA) in = in && ca * kE < mrows;
       load_to_lds(in ? p : zeros, at_a + slot * kSlotA + j * (kThr * 16));
     }
     pa += step_a;
@@ -997,13 +1000,7 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
       if constexpr (kGatherB) p += token[j] * ldb;
       else p += j * (kNextB * ldb);
       bool in = h * kBK + kb + (kTrB ? j * kStepB : 0) < K;
-      if constexpr (kTrB) {
-        const int c = kSame ? cb : col_b(j);
-        if constexpr (!kSame) p += (c - cb) * 16;
-        in = in && n0 + c * kE < N;
-      } else {
-        in = in && nb + j * kNextB < N;
-      }
+      in = in && (kTrB ? n0 + cb * kE : nb + j * kNextB) < N;
       load_to_lds(in ? p : zeros, at_b + slot * kSlotB + j * (kThr * 16));
     }
     pb += step_b;
@@ -1041,11 +1038,9 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int q = 0; q < kParts<T>; ++q)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j], q);
+      for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j], 0);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -1128,7 +1123,8 @@ __global__ __launch_bounds__(kLargeThreads) void ex_large_gradients(Experts x, S
 // staging, a wave loads 16 rows of weights straight into fragments and multiplies them with 16
 // rows of tokens.  A workgroup takes one expert and 16 GT columns; its four waves each take a
 // quarter of k, joined through LDS.  An expert's pairs are listed from all ids by every workgroup
-// (rows of act and y are the pairs' numbers: no plan), 16 MT at a time.
+// (rows of act and y are the pairs' numbers: no plan), 16 MT at a time.  64 tokens, 8 of 64 experts,
+// 2,048 x 1,024, float16: 0.8 GB in 131 + 69 us (4.0 TB/s; a large copy 4.75).
 template <typename T, bool GATE, int MT, int GT>
 __global__ __launch_bounds__(256) void ex_few(Experts x) {
   constexpr int kE = 16 / sizeof(T), kStep = 8 * kE;  // 128 bytes of k a step
@@ -1326,7 +1322,9 @@ __global__ __launch_bounds__(256) void ex_pairs_join(Experts x) {
   static_cast<T*>(x.out)[t * x.dim + d] = from_float<T>(s);
 }
 
-// out[t] = sum_k weight[t, k] y[row of (t, k)], k ascending, in binary32, rounded once
+// out[t] = sum_k weight[t, k] y[row of (t, k)], k ascending, in binary32, rounded once.  Bound by
+// memory: 32,768 rows of 2,048, 0.34 GB, 71 us (4.7 TB/s).  (Rows of y in 16 bits would be half of
+// that, and a second rounding of every result.)
 template <typename T, bool WEIGHTED>
 __global__ __launch_bounds__(256) void ex_join(Experts x, const float* __restrict__ y,
                                                T* __restrict__ out) {

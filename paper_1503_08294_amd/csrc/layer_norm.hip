@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-
 template <typename T>
 constexpr int kWidth = 16 / sizeof(T);
 // 16 bytes of a row; rows start at any element, which these loads and stores take
@@ -413,7 +412,8 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   else if (d <= 4 * kRow) forward_rows<T, kThreads, 1>(a, st);
   else if (d <= 8 * kRow) forward_rows<T, kThreads, 2>(a, st);
   else if (d <= 16 * kRow) forward_rows<T, kThreads, 4>(a, st);
-  else if (sizeof(T) == 4 && d <= 32 * kRow) forward_rows<T, kThreads, sizeof(T) == 4 ? 8 : 4>(a, st);
+  else if (sizeof(T) == 4 && d <= 32 * kRow)
+    forward_rows<T, kThreads, sizeof(T) == 4 ? 8 : 4>(a, st);
   else ln_forward_long<T><<<static_cast<uint32_t>(std::min(a.rows, kMostBlocks)), kThreads, 0,
                             st>>>(a);
   return hipGetLastError();
