@@ -245,17 +245,16 @@ Experts experts_of(const gsn_experts_params& p) {
 }
 
 // Sides of the products' tiles: of 2-byte elements the larger ones, from 128 pairs an expert on and
-// where the first product has enough of them to fill the chip; the largest need rows, and starts of
-// rows, at multiples of 16 bytes.  Forward and backward pass in us,
-// 256 and 64 (128 tiles of 256): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 280 and 286; 495, 3 of 7,
-//   1,984 x 320: 214 and 145; 1,920, 1 of 7, 3,456 x 448: 320 and 280; 465, 3 of 32, 344 x 1,344: 244
-//   and 194; forward of 5,100, 1 of 8, 448 x 992: 60 and 64.
-// 128 and 64 (256 tiles of 128): 16,384, 2 of 32, 2,047 x 2,047: 5,252 and 7,935; 1,500, 2 of 8, 999 x
-//   701 (297 tiles): 177 and 191; 1,500, 1 of 8, 511 x 1,023 (240 tiles): 141 and 110; with fewer pairs
-//   an expert, 2,048, 2 of 64, 511 x 701: 307 and 281.
-// In binary32, where the matrix cores are 16 times slower, small tiles waste less at the edges: 128
-// and 64: 4,096, 2 of 16, 1,024 x 1,024: 1,938 and 1,647; forward of 7,706, 8 of 32, 576 x 704: 1,494
-// and 1,434.
+// where the first product has enough of them to fill the chip; the largest need rows, and starts
+// of rows, at multiples of 16 bytes.  Forward and backward pass in us, with sides of
+// 256 and 64 (from 128 tiles of 256 on): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 218 and 251;
+//   16,384, 2 of 32, 2,048 x 2,048: 2,989 and 5,282; 1,024, 2 of 4, 1,024 x 512 (40 tiles): 141 and
+//   94; 495, 3 of 7, 1,984 x 320: 175 and 116; forward of 5,100, 1 of 8, 448 x 992: 55 and 66;
+// 128 and 64 (from 256 tiles of 128 on): 16,384, 2 of 32, 2,047 x 2,047: 5,243 and 7,782; 1,500, 2
+//   of 8, 999 x 701 (297 tiles): 174 and 190; 1,500, 1 of 8, 511 x 1,023 (240 tiles): 141 and 109;
+//   with fewer pairs an expert, 2,048, 2 of 64, 511 x 701: 307 and 281.
+// In binary32, where the matrix cores are 16 times slower, small tiles waste less at the edges:
+// 128 and 64: 4,096, 2 of 16, 1,024 x 1,024: 1,981 and 1,558.
 int32_t tile_side(const Experts& x, int32_t dtype) {
   const auto tiles = [&](int32_t side) {
     return (x.pairs / side + x.experts / 2) *

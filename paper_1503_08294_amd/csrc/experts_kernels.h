@@ -27,8 +27,10 @@ typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int64_t kFewTokens = 2;    // for which one launch makes the second product and the sum
-constexpr int64_t kFewPairs = 2048;  // pairs that a workgroup lists at most
-constexpr int kRowBytes = 128;       // bytes of k (contiguous operands) in a stage
+// pairs up to which weights go straight into fragments; a workgroup lists that many at most
+template <typename T>
+constexpr int64_t kFewPairs = sizeof(T) == 4 ? 768 : 256;
+constexpr int kRowBytes = 128;  // bytes of k (contiguous operands) in a stage
 
 // 16 bytes of an operand in a lane: 8 or 4 values of k of row (lane & 15)
 union Frag {
@@ -1123,16 +1125,16 @@ __global__ __launch_bounds__(kLargeThreads) void ex_large_gradients(Experts x, S
 // staging, a wave loads 16 rows of weights straight into fragments and multiplies them with 16
 // rows of tokens.  A workgroup takes one expert and 16 GT columns; its four waves each take a
 // quarter of k, joined through LDS.  An expert's pairs are listed from all ids by every workgroup
-// (rows of act and y are the pairs' numbers: no plan), 16 MT at a time.  64 tokens, 8 of 64 experts,
-// 2,048 x 1,024, float16: 0.8 GB in 131 + 69 us (4.0 TB/s; a large copy 4.75).
-template <typename T, bool GATE, int MT, int GT>
+// (rows of act and y are the pairs' numbers: no plan), 16 at a time.  32 tokens, 8 of 64 experts,
+// 2,048 x 1,024, bfloat16: 0.6 GB in 158 us (3.9 TB/s; a large copy 4.75).
+template <typename T, bool GATE, int GT>
 __global__ __launch_bounds__(256) void ex_few(Experts x) {
   constexpr int kE = 16 / sizeof(T), kStep = 8 * kE;  // 128 bytes of k a step
   constexpr int NT = GATE ? 2 * GT : GT;
-  constexpr int kCols = 16 * GT, kRows = 16 * MT;
-  __shared__ int32_t list[kFewPairs];
+  constexpr int kCols = 16 * GT, kRows = 16;
+  __shared__ int32_t list[kFewPairs<T>];
   __shared__ int32_t found[5];
-  __shared__ float part[4][MT * NT][64][4];
+  __shared__ float part[4][NT][64][4];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int g = lane >> 4, i = lane & 15;
   const int32_t D = x.dim, F = x.hidden, pairs = static_cast<int32_t>(x.pairs);
@@ -1177,64 +1179,48 @@ __global__ __launch_bounds__(256) void ex_few(Experts x) {
   const int32_t k_end = (wave + 1) * per * kStep < K ? (wave + 1) * per * kStep : K;
 
   for (int32_t r0 = 0; r0 < count; r0 += kRows) {
-    const T* a[MT];
-    bool live[MT];
+    const bool live = r0 + i < count;
+    const int32_t mine = list[live ? r0 + i : 0];
+    const T* const a = GATE ? static_cast<const T*>(x.x) +
+                                  static_cast<int64_t>(mine / x.top) * x.x_stride
+                            : static_cast<const T*>(x.act) + static_cast<int64_t>(mine) * F;
+    f32x4 acc[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const int32_t r = r0 + t * 16 + i;
-      live[t] = r < count;
-      const int32_t j = list[live[t] ? r : 0];
-      a[t] = GATE ? static_cast<const T*>(x.x) + static_cast<int64_t>(j / x.top) * x.x_stride
-                  : static_cast<const T*>(x.act) + static_cast<int64_t>(j) * F;
-    }
-    f32x4 acc[MT][NT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) acc[t][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const auto step = [&](auto inside, int32_t k0) {
       constexpr bool kIn = decltype(inside)::value;
-      Frag fw[2][NT], fa[2][MT];
+      Frag fw[2][NT], fa[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int32_t k = k0 + (4 * h + g) * kE;
 #pragma unroll
         for (int n = 0; n < NT; ++n) fw[h][n] = row_chunk<kIn>(w[n], k, K);
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          fa[h][t].u = u32x4{0, 0, 0, 0};
-          if (live[t]) fa[h][t] = row_chunk<kIn>(a[t], k, K);
-        }
+        fa[h].u = u32x4{0, 0, 0, 0};
+        if (live) fa[h] = row_chunk<kIn>(a, k, K);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int q = 0; q < kParts<T>; ++q)
-              acc[t][n] = multiply<T>(fw[h][n], fa[h][t], acc[t][n], q);
+          for (int q = 0; q < kParts<T>; ++q) acc[n] = multiply<T>(fw[h][n], fa[h], acc[n], q);
     };
     int32_t k0 = k_begin;
     for (; k0 + kStep <= k_end; k0 += kStep) step(std::true_type(), k0);
     if (k0 < k_end) step(std::false_type(), k0);
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-        *reinterpret_cast<f32x4*>(part[wave][t * NT + n][lane]) = acc[t][n];
+    for (int n = 0; n < NT; ++n) *reinterpret_cast<f32x4*>(part[wave][n][lane]) = acc[n];
     __syncthreads();
     const int32_t rows = count - r0 < kRows ? count - r0 : kRows;
     for (int o = tid; o < rows * kCols; o += 256) {
       const int m = o / kCols, c = o % kCols, n = n0 + c;
       if (n >= N) continue;
       const int32_t j = list[r0 + m];
-      const int at = ((c & 15) >> 2) * 16 + (m & 15);
+      const int at = ((c & 15) >> 2) * 16 + m;
       const auto sum = [&](int t) {
         float s = 0.0f;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) s += part[v][(m >> 4) * NT + t][at][c & 3];
+        for (int v = 0; v < 4; ++v) s += part[v][t][at][c & 3];
         return s;
       };
       if constexpr (GATE) {
@@ -1444,31 +1430,33 @@ void gradients(Experts x, hipStream_t st) {
 
 }  // namespace
 
-template <typename T, int MT, int GT>
+template <typename T, int GT>
 void few(const Experts& x, hipStream_t st) {
   const uint32_t y = static_cast<uint32_t>(x.pairs < x.experts ? x.pairs : x.experts);
-  ex_few<T, true, MT, GT><<<dim3(blocks_of(x.hidden, 16 * GT), y), 256, 0, st>>>(x);
+  ex_few<T, true, GT><<<dim3(blocks_of(x.hidden, 16 * GT), y), 256, 0, st>>>(x);
   if (x.tokens <= kFewTokens) {
     const uint32_t waves = 2 * static_cast<uint32_t>(x.top < 8 ? x.top : 8);
     ex_few_join<T><<<dim3(blocks_of(x.dim, 16), static_cast<uint32_t>(x.tokens)),
                      waves * kWave, 0, st>>>(x);
     return;
   }
-  ex_few<T, false, MT, GT><<<dim3(blocks_of(x.dim, 16 * GT), y), 256, 0, st>>>(x);
+  ex_few<T, false, GT><<<dim3(blocks_of(x.dim, 16 * GT), y), 256, 0, st>>>(x);
   ex_pairs_join<T><<<dim3(blocks_of(x.dim, 256), static_cast<uint32_t>(x.tokens)), 256, 0, st>>>(
       x);
 }
 
 template <typename T>
 hipError_t launch_experts(const Experts& x, hipStream_t st) {
-  // Few pairs an expert, and no backward pass that needs the rows in the experts' order.  At 64
-  // experts of 2,048 x 1,024 (bfloat16, 8 of them a token) this takes 26, 101, 197, 224 us for 1,
-  // 8, 64, 128 tokens, the tiles below 113, 204, 230, 231 us; for 192 tokens it is 278 to 235.
-  // Two rows of 16 from 8 pairs an expert on: 96 tokens 198 us, 245 us with one.
-  if (!x.pre && x.pairs <= kFewPairs && x.pairs <= int64_t{16} * x.experts) {
-    if (x.pairs <= x.experts) few<T, 1, 1>(x, st);
-    else if (x.pairs <= int64_t{8} * x.experts) few<T, 1, 2>(x, st);
-    else few<T, 2, 2>(x, st);
+  // Few pairs, in all and an expert, and no backward pass that needs the rows in the experts'
+  // order.  This and the tiles below, us, experts of 2,048 x 1,024, bfloat16: 8 of 64, 1 token 26
+  // and 43, 8 tokens 100 and 125, 32 tokens 158 and 170, 48 tokens 180 and 176, 64 tokens 196 and
+  // 179; 2 of 16, 64 tokens 60 and 59, 96 tokens 76 and 59.  1,024 x 1,024, binary32: 4 of 128, 128
+  // tokens 289 and 391, 192 tokens 345 and 425, 384 tokens 470 and 465; 2 of 16, 128 tokens 86 and
+  // 88.
+  constexpr int64_t kEach = sizeof(T) == 4 ? 16 : 8;
+  if (!x.pre && x.pairs <= kFewPairs<T> && x.pairs <= kEach * x.experts) {
+    if (x.pairs <= x.experts) few<T, 1>(x, st);
+    else few<T, 2>(x, st);
     return hipGetLastError();
   }
   const hipError_t e = launch_plan(x, st);

@@ -671,6 +671,21 @@ def test_experts_few_rows_an_expert(mix, dtype, tokens, experts, k, dim, hidden)
     assert torch.equal(got, mix.experts(x, ids, weights, w1, w2))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (100, 16, 1, 136, 72), (60, 16, 2, 65, 129), (31, 64, 8, 264, 200), (3, 4, 4, 33, 1)])
+def test_experts_a_crowded_expert_among_few_pairs(mix, dtype, tokens, experts, k, dim, hidden):
+    """Half of the tokens have expert 0 first: more rows than are taken at a time."""
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 58)]
+    x, ids, weights, w1, w2, _ = a
+    ids[:tokens // 2, 0] = 0
+    ids[-1] = -1
+    want = experts_in_float64(*a)[0].detach().cpu()
+    got = mix.experts(x, ids, weights, w1, w2)
+    near(got, want, expert_tolerance(dtype, dim, hidden, tokens * k), "out")
+    assert not got[-1].any()
+
+
 def test_experts_gradient_against_differences(mix):
     x, ids, weights, w1, w2, dout = expert_inputs(F32, 6, 3, 2, 7, 5, 36, empty=False)
     a = [x, weights, w1, w2]
