@@ -18,6 +18,7 @@ int32_t plan_chunks(int64_t pairs) {
 // A stable counting sort of the pairs by expert: a first launch counts every chunk's pairs of each
 // expert, a second one adds up what comes before a chunk and places its pairs.  32,764 pairs of
 // 64 experts: 12 us in all, 31 us in one launch in which a workgroup an expert reads all ids twice.
+// The pairs of a single chunk are counted where they are placed, without the first launch.
 __global__ __launch_bounds__(kPlanThreads) void ex_count(int32_t pairs, int32_t experts,
                                                          const int32_t* __restrict__ ids,
                                                          int32_t* __restrict__ counts) {
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_place(int32_t pairs, int32_t 
   // of every expert, the pairs of all chunks and of those before this one; and this chunk's by wave
   int span = 1;
   while (span < experts && span < kPlanThreads) span *= 2;
-  for (int e = tid % span; e < experts; e += span) {
+  for (int e = tid % span; chunks > 1 && e < experts; e += span) {
     int32_t all = 0, less = 0;
 #pragma unroll 8
     for (int32_t c = tid / span; c < chunks; c += kPlanThreads / span) {
@@ -77,6 +78,7 @@ __global__ __launch_bounds__(kPlanThreads) void ex_place(int32_t pairs, int32_t 
       id[k] = -1;
     } else {
       atomicAdd(&next[wave][id[k]], 1);
+      if (chunks == 1) atomicAdd(&total[id[k]], 1);
     }
   }
   __syncthreads();
@@ -287,7 +289,8 @@ bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 
 hipError_t launch_plan(const Experts& x, hipStream_t st) {
   const int32_t pairs = static_cast<int32_t>(x.pairs);
   const uint32_t chunks = static_cast<uint32_t>(plan_chunks(x.pairs));
-  ex_count<<<chunks, kPlanThreads, 0, st>>>(pairs, x.experts, x.ids, x.plan.counts);
+  if (chunks > 1)
+    ex_count<<<chunks, kPlanThreads, 0, st>>>(pairs, x.experts, x.ids, x.plan.counts);
   ex_place<<<chunks, kPlanThreads, 0, st>>>(pairs, x.experts, x.top, x.ids, x.plan.counts,
                                             x.plan);
   return hipGetLastError();
