@@ -298,9 +298,14 @@ __device__ __forceinline__ void sum_dots(const Experts& x, int64_t j) {
   x.dweights[j] = s;
 }
 
-// Workgroups of the backward pass's second launch: for dxr, then dw1, dw2 and dweights.
+// Workgroups of the backward pass's second launch: for dxr, dw1, dw2 and dweights.  The launch
+// begins with those from `begin` on and ends with those before.
 struct Shares {
-  int32_t in_x, in_w1, in_w2;
+  int32_t in_x, in_w1, in_w2, begin;
+  __device__ __forceinline__ int32_t mine() const {
+    const int32_t all = gridDim.x, id = blockIdx.x + begin;
+    return id < all ? id : id - all;
+  }
 };
 
 // One tile of SIDE x SIDE by four waves, for any sizes and alignment: a stage's 16-byte chunks are
@@ -586,7 +591,7 @@ template <typename T, int SIDE, bool TINY>
 __global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loose_gradients(
     Experts x, Shares n) {
   __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
-  int32_t id = blockIdx.x;
+  int32_t id = n.mine();
   if (id < n.in_x) return loose_tile<T, kBackwardIn, SIDE, TINY>(x, id, smem);
   id -= n.in_x;
   if (id < n.in_w1) return loose_tile<T, kWeightsIn, SIDE, TINY>(x, id, smem);
@@ -1110,7 +1115,7 @@ __global__ __launch_bounds__(kLargeThreads) void ex_large(Experts x) {
 template <typename T>
 __global__ __launch_bounds__(kLargeThreads) void ex_large_gradients(Experts x, Shares n) {
   __shared__ __attribute__((aligned(1024))) char smem[kLargeLds];
-  int32_t block = blockIdx.x;
+  int32_t block = n.mine();
   if (block < n.in_x) return large_tile<T, kBackwardIn>(x, block, smem);
   block -= n.in_x;
   if (block < n.in_w1) return large_tile<T, kWeightsIn>(x, block, smem);
@@ -1409,11 +1414,13 @@ template <typename T>
 void gradients(Experts x, hipStream_t st) {
   x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
   const auto in = [](bool wanted, uint32_t n) { return static_cast<int32_t>(wanted ? n : 0); };
-  const Shares n{in(x.dx, product_grid<kBackwardIn>(x)), in(x.dw1, product_grid<kWeightsIn>(x)),
-                 in(x.dw2, product_grid<kWeightsOut>(x))};
+  Shares n{in(x.dx, product_grid<kBackwardIn>(x)), in(x.dw1, product_grid<kWeightsIn>(x)),
+           in(x.dw2, product_grid<kWeightsOut>(x)), 0};
+  if (x.pairs > int64_t{2} * x.hidden * x.experts) n.begin = n.in_x;
   const uint32_t threads = x.side == kTileRows ? kLargeThreads : kLooseThreads;
   const uint32_t grid = n.in_x + n.in_w1 + n.in_w2 + (x.dweights ? blocks_of(x.pairs, threads) : 0);
   if (grid == 0) return;
+  if (n.begin == static_cast<int32_t>(grid)) n.begin = 0;
   if constexpr (sizeof(T) == 2) {
     if (x.side == kTileRows) {
       ex_large_gradients<T><<<grid, threads, 0, st>>>(x, n);

@@ -703,6 +703,75 @@ def test_experts_gradient_against_differences(mix):
             assert abs(got[j] - d) < 1e-5 * (1 + abs(d)), (i, j)
 
 
+# --------------------------------------------------------- offsets that pass 32 bits ----
+
+def far_apart(x, first=0):
+    """The rows of x on the GPU, 2^20 elements apart (their end passes 2^32 elements)."""
+    rows, dim = x.shape
+    assert rows << 20 > 1 << 32
+    wide = torch.empty((rows, 1 << 20), dtype=x.dtype, device="cuda")
+    wide[:, first:first + dim] = x.cuda()
+    return wide[:, first:first + dim]
+
+
+def test_norm_and_route_of_rows_beyond_32_bits(mix):
+    rows = 4200
+    x = randn(rows, 70, seed=90, dtype=torch.bfloat16)
+    w, b = (randn(70, seed=91 + i) for i in range(2))
+    dy = randn(rows, 70, seed=93, dtype=torch.bfloat16)
+    y, stats = mix.layer_norm_forward(x.cuda(), w.cuda(), b.cuda())
+    grads = mix.layer_norm_backward(dy.cuda(), x.cuda(), w.cuda(), b.cuda(), stats)
+    far = far_apart(x, 5)
+    far_y, far_stats = mix.layer_norm_forward(far, w.cuda(), b.cuda())
+    assert torch.equal(far_y, y) and torch.equal(far_stats, stats)
+    far_grads = mix.layer_norm_backward(far_apart(dy), far, w.cuda(), b.cuda(), stats)
+    assert all(torch.equal(p, q) for p, q in zip(far_grads, grads))
+    ids, weights = mix.route(x.cuda(), 4)
+    far_ids, far_weights = mix.route(far, 4)
+    assert torch.equal(far_ids, ids) and torch.equal(far_weights, weights)
+    dw = randn(rows, 4, seed=94).cuda()
+    assert torch.equal(mix.route_backward(dw, far, ids), mix.route_backward(dw, x.cuda(), ids))
+
+
+@pytest.mark.parametrize("dim", [64, 70])  # tiles of 256 (4,300 pairs an expert) and of 128
+def test_experts_of_tokens_beyond_32_bits(mix, dim):
+    x, ids, weights, w1, w2, dout = expert_inputs(torch.bfloat16, 4300, 2, 2, dim, 900, 95)
+    a = [t.cuda() for t in (x, ids, weights, w1, w2)]
+    out, saved = mix.experts_forward(*a)
+    grads = mix.experts_backward(dout.cuda(), *a, saved)
+    far = [far_apart(x), *a[1:]]
+    far_out, far_saved = mix.experts_forward(*far)
+    assert torch.equal(far_out, out)
+    far_grads = mix.experts_backward(dout.cuda(), *far, far_saved)
+    assert all(torch.equal(p, q) for p, q in zip(far_grads, grads))
+
+
+@pytest.mark.parametrize("tokens,dim,hidden", [(20, 4096, 4200), (2500, 4096, 4200),
+                                               (20, 4097, 4200), (2500, 4097, 4200),
+                                               (17000, 4096, 4200), (17000, 4097, 4200)])
+def test_experts_of_weights_beyond_32_bits(mix, tokens, dim, hidden):
+    """The last of 126 experts, whose weights begin past 2^32 elements, as the only one."""
+    experts, dtype = 126, torch.bfloat16
+    x, _, weights, w1, w2, dout = expert_inputs(dtype, tokens, 1, 1, dim, hidden, 96)
+    many1 = torch.zeros((experts, 2 * hidden, dim), dtype=dtype, device="cuda")
+    many2 = torch.zeros((experts, dim, hidden), dtype=dtype, device="cuda")
+    many1[-1:], many2[-1:] = w1.cuda(), w2.cuda()
+    assert (experts - 1) * 2 * hidden * dim > 1 << 32
+    ids = torch.zeros(tokens, 1, dtype=torch.int32, device="cuda")
+    x, weights, dout = x.cuda(), weights.cuda(), dout.cuda()
+    out, saved = mix.experts_forward(x, ids, weights, w1.cuda(), w2.cuda())
+    want = (out, *mix.experts_backward(dout, x, ids, weights, w1.cuda(), w2.cuda(), saved))
+    ids += experts - 1
+    alone = mix.experts(x, ids, weights, many1, many2)
+    out, saved = mix.experts_forward(x, ids, weights, many1, many2)
+    got = mix.experts_backward(dout, x, ids, weights, many1, many2, saved)
+    rel = 2 * expert_tolerance(dtype, dim, hidden, tokens)  # (both are rounded)
+    near(alone, want[0].double().cpu(), rel, "out alone")
+    got = (out, *got[:2], got[2][-1:], got[3][-1:])
+    for g, v, name in zip(got, want, ("out", "dx", "dweights", "dw1", "dw2")):
+        near(g, v.double().cpu(), rel, name)
+
+
 # ------------------------------------------------------------------------ use of the GPU ----
 
 def everything(mix, x, logits, w, b, w1, w2, dout):
