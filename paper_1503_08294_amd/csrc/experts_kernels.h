@@ -782,6 +782,8 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
         dup.put(li, j * 16 + lg, du);
         wact.put(li, j * 16 + lg, wa);
       }
+      // (summed here: left to the compiler, the terms of all rows wait in memory for the end)
+      asm volatile("" : "+v"(part));
       wave_fence();
       parts[i] = part;
       if (i + 1 < MT) {
@@ -842,10 +844,10 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
 // card's L2 caches bring in 1.19 us when all CUs load (14 TB/s), while the products alone take 1.0
 // us at the clock that they leave; together 1.2 to 1.3.  Besides its stages a tile takes 7 us to
 // start (list, tokens, first stages) and 12 for its results, which nothing hides, as LDS holds one
-// workgroup a CU; the gates' gradients, with 0.9 MB a tile to read and write, some 50.
+// workgroup a CU; the gates' gradients, with 0.9 MB a tile to read and write, some 40.
 // 16,384 tokens, 2 of 32 experts, 2,048 x 2,048, bfloat16 (a large library product reaches 1.28
-// PFLOP/s): first product 592 us (0.93 PFLOP/s), second 295 (0.93), gates' gradients 503 (0.55),
-// the other three together 1,600 (0.86).
+// PFLOP/s): first product 592 us (0.93 PFLOP/s), second 296 (0.93), gates' gradients
+// 442 (0.62), the other three together 1,600 (0.86).
 constexpr int kLargeThreads = 512;
 constexpr int kLargeLds = 5 * kTileRows * kRowBytes;
 template <typename T, Kind KIND>
