@@ -204,12 +204,11 @@ size_t carve_saved(void* base, Experts* x) {
   return c.used;
 }
 
-// (rows past the last one may be read, for results that are not stored)
 size_t carve_forward(void* base, int32_t dtype, bool saved, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs);
   Carver c{static_cast<char*>(base)};
   if (!saved) carve_plan(&c, x);
-  x->act = c.take(size_of(dtype) * (n + kPlanRows) * x->hidden);
+  x->act = c.take(size_of(dtype) * n * x->hidden);
   x->y = static_cast<float*>(c.take(4 * n * x->dim));
   return c.used;
 }
@@ -218,7 +217,7 @@ size_t carve_backward(void* base, int32_t dtype, Experts* x) {
   const size_t n = static_cast<size_t>(x->pairs), s = size_of(dtype);
   Carver c{static_cast<char*>(base)};
   x->dot_tiles = (x->hidden + kSmallRows - 1) / kSmallRows;
-  x->dpre = c.take(2 * s * (n + kPlanRows) * x->hidden);
+  x->dpre = c.take(2 * s * n * x->hidden);
   x->wact = c.take(s * n * x->hidden);
   x->dots = static_cast<float*>(c.take(4 * n * x->dot_tiles));
   x->dxr = static_cast<float*>(c.take(4 * n * x->dim));
