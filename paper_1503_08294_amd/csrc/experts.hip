@@ -277,7 +277,8 @@ bool grids_ok(const Experts& x) {
   const auto tiles = [&](int64_t n) { return (n + side - 1) / side; };
   const int64_t rows = x.pairs / side + x.experts;
   const int64_t wide = tiles(2 * static_cast<int64_t>(x.hidden)) + 1, deep = tiles(x.dim);
-  const int64_t most = std::max(rows * wide, rows * deep + 2 * x.experts * wide * deep);
+  const int64_t most = std::max(
+      rows * wide, rows * deep + 2 * x.experts * wide * deep + x.pairs / threads);
   return most + 4096 < (int64_t{1} << 32) / threads;
 }
 

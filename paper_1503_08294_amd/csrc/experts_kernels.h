@@ -1406,10 +1406,12 @@ void product(Experts x, hipStream_t st) {
       ex_large<T, KIND><<<grid, kLargeThreads, 0, st>>>(x);
       return;
     }
+    if (x.side == kMiddleRows) {
+      ex_loose<T, KIND, kMiddleRows, false><<<grid, kLooseThreads, 0, st>>>(x);
+      return;
+    }
   }
-  if (x.side == kMiddleRows)
-    ex_loose<T, KIND, kMiddleRows, false><<<grid, kLooseThreads, 0, st>>>(x);
-  else if (tiny<T>(x))
+  if (tiny<T>(x))
     ex_loose<T, KIND, kSmallRows, true><<<grid, kLooseThreads, 0, st>>>(x);
   else
     ex_loose<T, KIND, kSmallRows, false><<<grid, kLooseThreads, 0, st>>>(x);
@@ -1435,10 +1437,12 @@ void gradients(Experts x, hipStream_t st) {
       ex_large_gradients<T><<<grid, threads, 0, st>>>(x, n);
       return;
     }
+    if (x.side == kMiddleRows) {
+      ex_loose_gradients<T, kMiddleRows, false><<<grid, threads, 0, st>>>(x, n);
+      return;
+    }
   }
-  if (x.side == kMiddleRows)
-    ex_loose_gradients<T, kMiddleRows, false><<<grid, threads, 0, st>>>(x, n);
-  else if (tiny<T>(x))
+  if (tiny<T>(x))
     ex_loose_gradients<T, kSmallRows, true><<<grid, threads, 0, st>>>(x, n);
   else
     ex_loose_gradients<T, kSmallRows, false><<<grid, threads, 0, st>>>(x, n);
