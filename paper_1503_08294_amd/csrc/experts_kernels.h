@@ -308,11 +308,12 @@ struct Shares {
   }
 };
 
-// One tile of SIDE x SIDE by four waves, for any sizes and alignment: a stage's 16-byte chunks are
-// loaded into registers two stages ahead, and from there to one of two places in LDS.  A chunk
-// that a row's end cuts is loaded as the row's last 16 bytes and shifted on its way to LDS, so
-// that every load is one instruction without a branch (one with a branch has to be awaited at
-// once); TINY: rows may be shorter than that, and are loaded element by element.
+// One tile of SIDE x SIDE by four waves, or GROUPS times four that share k, for any sizes and
+// alignment: a stage's 16-byte chunks are loaded into registers two stages ahead, and from there to
+// one of two places in LDS.  A chunk that a row's end cuts is loaded as the row's last 16 bytes and
+// shifted on its way to LDS, so that every load is one instruction without a branch (one with a
+// branch has to be awaited at once); TINY: rows may be shorter than that, and are loaded element by
+// element.
 // Several workgroups share a CU, so that one's loads, barriers and results hide behind another's
 // products.  In binary32 bound by the matrix cores (0.153 PFLOP/s in a large library product):
 // 4,096 tokens, 2 of 16 experts, 1,024 x 1,024, forward and backward 1.55 ms, 0.10 PFLOP/s with
@@ -322,7 +323,7 @@ struct Shares {
 // for each other) and of a launch: 777, 3 of 7, 501 x 333, binary32 150 us in 8 launches.
 template <int SIDE>
 constexpr int kLooseLds = 2 * 2 * SIDE * kRowBytes;
-template <typename T, Kind KIND, int SIDE, bool TINY>
+template <typename T, Kind KIND, int SIDE, bool TINY, int GROUPS = 1>
 __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* smem) {
   constexpr int BM = SIDE, BN = SIDE, WM = 2, WN = 2;
   constexpr int kThr = WM * WN * kWave;
@@ -335,7 +336,9 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
   constexpr int LA = BM * 8 / kThr, LB = BN * 8 / kThr;
   constexpr int kStage = kLooseLds<SIDE> / 2;
 
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThr);
+  const int tid = threadIdx.x - group * kThr, lane = tid % kWave, wave = tid / kWave;
+  smem += group * kLooseLds<SIDE>;
   const int wm = wave / WN, wn = wave % WN;
   const int32_t D = x.dim, F = x.hidden;
   const int32_t N = KIND == kForwardGate || KIND == kBackwardGate || KIND == kWeightsOut ? F : D;
@@ -384,6 +387,9 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
     K = KIND == kForwardGate || KIND == kBackwardGate ? D : KIND == kForwardOut ? F : 2 * F;
   }
 
+  // this group's part of k (what of it is past the end loads zeros)
+  const int32_t part = GROUPS == 1 ? K : (K + GROUPS * kBK - 1) / (GROUPS * kBK) * kBK;
+  const int32_t k_begin = group * part, k_end = k_begin + part;
   // With k contiguous: this lane's LA (LB) rows, null outside.
   const auto token = [&](int64_t r) { return static_cast<int64_t>(x.plan.token[r]); };
   const T* rows_a[LA];
@@ -477,9 +483,10 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
     first[j] = i / ((is_a ? BM : BN) / kE);
     end[j] = at < len ? K : 0;
     walk[j] = (is_a ? base_a : base_b) + (TINY || at + kE <= len ? at : len - kE);
-    if (!(is_a ? kGatherA : kGatherB)) walk[j] += first[j] * (is_a ? step_a : step_b);
+    if (!(is_a ? kGatherA : kGatherB))
+      walk[j] += (k_begin + first[j]) * (is_a ? step_a : step_b);
   }
-  if (K > 0) load_tokens(0);
+  if (K > 0) load_tokens(k_begin);
   Frag ahead[2][LA + LB];
   const auto load = [&](int32_t k0, Frag (&to)[LA + LB]) {
     const T* from[LA + LB];
@@ -546,7 +553,7 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
       *reinterpret_cast<u32x4*>(sb + (j * kThr + tid) * 16) =
           shifted(chunks[LA + j], false, j, k0).u;
     __syncthreads();
-    if (k0 + 2 * kBK < K) load(k0 + 2 * kBK, chunks);
+    if (k0 + 2 * kBK < k_end) load(k0 + 2 * kBK, chunks);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Frag fa[MT], fb[NT];
@@ -564,13 +571,32 @@ __device__ __forceinline__ void loose_tile(const Experts& x, int32_t id, char* s
           for (int j = 0; j < NT; ++j) acc[i][j] = multiply<T>(fb[j], fa[i], acc[i][j], q);
     }
   };
-  if (K > 0) load(0, ahead[0]);
-  if (K > kBK) load(kBK, ahead[1]);
-  for (int32_t k0 = 0; k0 < K; k0 += 2 * kBK) {
+  if (part > 0) load(k_begin, ahead[0]);
+  if (part > kBK) load(k_begin + kBK, ahead[1]);
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += 2 * kBK) {
     stage(k0, ahead[0], smem);
-    if (k0 + kBK < K) stage(k0 + kBK, ahead[1], smem + kStage);
+    if (k0 + kBK < k_end) stage(k0 + kBK, ahead[1], smem + kStage);
   }
   __syncthreads();
+  if constexpr (GROUPS > 1) {
+    static_assert(kThr * MT * NT * 16 <= kLooseLds<SIDE>);
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem);
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < MT * NT; ++i) sums[i * kThr + tid] = acc[i / NT][i % NT];
+    }
+    __syncthreads();
+    if (group > 0) {
+      if constexpr (KIND == kBackwardGate) __syncthreads();  // (the one in finish)
+      return;
+    }
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+      for (int i = 0; i < MT * NT; ++i)
+        acc[i / NT][i % NT] +=
+            *reinterpret_cast<const f32x4*>(smem + g * kLooseLds<SIDE> + (i * kThr + tid) * 16);
+  }
 
   finish<T, KIND, BM, BN, WM, WN>(x, acc, reinterpret_cast<float*>(smem), e, m0, mrows, n0, row0);
 }
@@ -586,6 +612,12 @@ template <typename T, Kind KIND, int SIDE, bool TINY>
 __global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loose(Experts x) {
   __shared__ __attribute__((aligned(16))) char smem[kLooseLds<SIDE>];
   loose_tile<T, KIND, SIDE, TINY>(x, blockIdx.x, smem);
+}
+// The groups of four waves each take a part of k, and add their sums up in the groups' order.
+template <typename T, Kind KIND, int GROUPS>
+__global__ __launch_bounds__(GROUPS* kLooseThreads) void ex_split(Experts x) {
+  __shared__ __attribute__((aligned(16))) char smem[GROUPS * kLooseLds<kSmallRows>];
+  loose_tile<T, KIND, kSmallRows, false, GROUPS>(x, blockIdx.x, smem);
 }
 template <typename T, int SIDE, bool TINY>
 __global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loose_gradients(
@@ -1411,8 +1443,22 @@ void product(Experts x, hipStream_t st) {
       return;
     }
   }
-  if (tiny<T>(x))
+  if (tiny<T>(x)) {
     ex_loose<T, KIND, kSmallRows, true><<<grid, kLooseThreads, 0, st>>>(x);
+    return;
+  }
+  // Few tiles of many stages leave a CU's SIMDs one wave each, which waits for its own loads: as
+  // many groups as fill the CU take parts of k.  Forward and backward pass with one, two and four
+  // groups, us: 78 tokens, 1 of 16 experts, 3,636 x 320, bfloat16: 160, 146, 135; 64, 2 of 8, 2,048
+  // x 512: 91, 79, 73; forward of 100, 4 of 8, 2,048 x 1,024 (some 320 tiles): 44, 41, 48.
+  const int64_t depth = KIND == kForwardOut ? x.hidden : x.dim;
+  const int64_t blocks = x.pairs / kSmallRows + (x.pairs < x.experts ? x.pairs : x.experts) / 2;
+  const int64_t tiles = blocks * (grid / static_cast<uint32_t>(x.plan.most_small));
+  const bool deep = depth * static_cast<int64_t>(sizeof(T)) >= 16 * kRowBytes;
+  if (deep && tiles <= 192)
+    ex_split<T, KIND, 4><<<grid, 4 * kLooseThreads, 0, st>>>(x);
+  else if (deep && tiles <= 448)
+    ex_split<T, KIND, 2><<<grid, 2 * kLooseThreads, 0, st>>>(x);
   else
     ex_loose<T, KIND, kSmallRows, false><<<grid, kLooseThreads, 0, st>>>(x);
 }

@@ -673,6 +673,27 @@ def test_experts_few_rows_an_expert(mix, dtype, tokens, experts, k, dim, hidden)
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (60, 4, 2, 1500, 1030), (5, 3, 1, 2047, 40), (300, 4, 2, 1024, 1024), (90, 3, 2, 1111, 2050),
+    (150, 2, 2, 1025, 1100), (1, 2, 1, 4000, 16)])
+def test_experts_few_rows_of_long_products(mix, dtype, tokens, experts, k, dim, hidden):
+    """Products whose sums are long and whose tiles are few: several parts of k a workgroup."""
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 59)]
+    x, ids, weights, w1, w2, dout = a
+    ids[tokens // 2] = -1 if tokens > 1 else 0
+    want = experts_in_float64(*a)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    first = None
+    for _ in range(2):
+        out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        got = (out, *mix.experts_backward(dout, x, ids, weights, w1, w2, saved))
+        for g, v, name in zip(got, want, ("out", "dx", "dweights", "dw1", "dw2")):
+            near(g, v.detach().cpu(), rel, name)
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
     (100, 16, 1, 136, 72), (60, 16, 2, 65, 129), (31, 64, 8, 264, 200), (3, 4, 4, 33, 1)])
 def test_experts_a_crowded_expert_among_few_pairs(mix, dtype, tokens, experts, k, dim, hidden):
     """Half of the tokens have expert 0 first: more rows than are taken at a time."""
