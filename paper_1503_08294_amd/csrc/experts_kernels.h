@@ -1515,11 +1515,10 @@ template <typename T>
 hipError_t launch_experts(const Experts& x, hipStream_t st) {
   // Few pairs, in all and an expert, and no backward pass that needs the rows in the experts'
   // order.  This and the tiles below, us, experts of 2,048 x 1,024, bfloat16: 8 of 64, 1 token 26
-  // and 43, 8 tokens 100 and 125, 32 tokens 158 and 170, 48 tokens 180 and 176, 64 tokens 196 and
-  // 179; 2 of 16, 64 tokens 60 and 59, 96 tokens 76 and 59.  1,024 x 1,024, binary32: 4 of 128, 128
-  // tokens 289 and 391, 192 tokens 345 and 425, 384 tokens 470 and 465; 2 of 16, 128 tokens 86 and
-  // 88.
-  constexpr int64_t kEach = sizeof(T) == 4 ? 16 : 8;
+  // and 43, 8 tokens 100 and 123, 32 tokens 158 and 168, 64 tokens 196 and 178; 2 of 16, 32 tokens
+  // 47 and 46, 64 tokens 60 and 50.  1,024 x 1,024, binary32: 4 of 128, 128 tokens 290 and 392, 192
+  // tokens 347 and 425, 384 tokens 470 and 466; 2 of 16, 64 tokens 65 and 81, 128 tokens 86 and 83.
+  constexpr int64_t kEach = sizeof(T) == 4 ? 16 : 4;
   if (!x.pre && x.pairs <= kFewPairs<T> && x.pairs <= kEach * x.experts) {
     if (x.pairs <= x.experts) few<T, 1>(x, st);
     else few<T, 2>(x, st);

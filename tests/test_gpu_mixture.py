@@ -694,7 +694,8 @@ def test_experts_few_rows_of_long_products(mix, dtype, tokens, experts, k, dim, 
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
-    (100, 16, 1, 136, 72), (60, 16, 2, 65, 129), (31, 64, 8, 264, 200), (3, 4, 4, 33, 1)])
+    (100, 16, 1, 136, 72), (60, 16, 2, 65, 129), (31, 64, 8, 264, 200), (3, 4, 4, 33, 1),
+    (60, 16, 1, 136, 72), (120, 40, 1, 65, 129)])
 def test_experts_a_crowded_expert_among_few_pairs(mix, dtype, tokens, experts, k, dim, hidden):
     """Half of the tokens have expert 0 first: more rows than are taken at a time."""
     a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 58)]
