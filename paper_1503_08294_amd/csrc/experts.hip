@@ -249,7 +249,7 @@ Experts experts_of(const gsn_experts_params& p) {
 // where the first product has enough of them to fill the chip; the largest need rows, and starts
 // of rows, at multiples of 16 bytes.  Forward and backward pass in us, with sides of
 // 256 and 64 (from 128 tiles of 256 on): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 218 and 251;
-//   16,384, 2 of 32, 2,048 x 2,048: 2,989 and 5,282; 1,024, 2 of 4, 1,024 x 512 (40 tiles): 141 and
+//   16,384, 2 of 32, 2,048 x 2,048: 2,900 and 5,282; 1,024, 2 of 4, 1,024 x 512 (40 tiles): 141 and
 //   94; 495, 3 of 7, 1,984 x 320: 175 and 116; forward of 5,100, 1 of 8, 448 x 992: 55 and 66;
 // 128 and 64 (from 256 tiles of 128 on): 16,384, 2 of 32, 2,047 x 2,047: 5,243 and 7,782; 1,500, 2
 //   of 8, 999 x 701 (297 tiles): 174 and 190; 1,500, 1 of 8, 511 x 1,023 (240 tiles): 141 and 109;
