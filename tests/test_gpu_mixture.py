@@ -102,6 +102,13 @@ def test_norm_forward_and_backward(mix, dtype, rows, dim):
               + 2.0 ** -25 * (w_type == F16), "dbias")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,dim", [(512, 300), (513, 1), (513, 300), (600, 65), (700, 2100),
+                                      (520, 4100), (515, 9000)])
+def test_norm_around_the_rows_of_one_launch(mix, dtype, rows, dim):
+    test_norm_forward_and_backward(mix, dtype, rows, dim)
+
+
 @pytest.mark.parametrize("rows,dim", [(3000, 96), (70_001, 8), (1025, 1000)])
 def test_norm_many_rows(mix, rows, dim):
     x, dy = randn(rows, dim, seed=5) + 1.0, randn(rows, dim, seed=6)
