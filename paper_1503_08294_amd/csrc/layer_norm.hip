@@ -425,6 +425,17 @@ int32_t norm_parts(int64_t rows) {
 
 constexpr int64_t kMostBlocks = 1 << 20;
 
+// Whether the memory from the first to the last element of two matrices with these strides meets.
+template <typename T>
+bool overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows,
+             int32_t dim) {
+  const auto bytes = [&](int64_t stride) {
+    return (static_cast<uint64_t>(rows - 1) * static_cast<uint64_t>(stride) + dim) * sizeof(T);
+  };
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  return a && b && rows > 0 && p < q + bytes(b_stride) && q < p + bytes(a_stride);
+}
+
 // Rows up to which the columns' sums have workgroups of their own beside the rows', in one launch.
 // A backward pass with a join and without, us: 27 rows of 704 16.9 and 14.0, 512 of 4,000 bfloat16
 // 19.7 and 13.8, 1,024 of 2,048 binary32 16.7 and 20.3.
@@ -468,8 +479,11 @@ hipError_t backward(NormBackArgs a, void* dw, void* db, hipStream_t st) {
   const uint32_t nb = sums ? a.parts
                            : static_cast<uint32_t>(std::min(std::max<int64_t>(a.rows, 1),
                                                             kMostBlocks));
-  // few rows: the columns' sums by workgroups of their own in the same launch, without a join
-  const bool few = sums && a.rows <= kFewRows && d <= 16 * kRow;
+  // few rows: the columns' sums by workgroups of their own in the same launch, without a join; not
+  // where dx goes over the dy that they read (else a workgroup reads all of a row before it writes
+  // any of it, and takes its part of the sums from what it read)
+  const bool few = sums && a.rows <= kFewRows && d <= 16 * kRow &&
+                   !overlap<T>(a.dx, a.dx_stride, a.dy, a.dy_stride, a.rows, d);
   a.row_blocks = nb;
   uint32_t grid = nb;
   if (few) {
@@ -484,11 +498,11 @@ hipError_t backward(NormBackArgs a, void* dw, void* db, hipStream_t st) {
   else if (d <= 8 * kRow) ln_backward<T, kThreads, 2><<<grid, kThreads, 0, st>>>(a);
   else if (d <= 16 * kRow) ln_backward<T, kThreads, 4><<<grid, kThreads, 0, st>>>(a);
   else {
+    if (sums)  // (first: dx may go over dy)
+      ln_columns<T><<<dim3((d + kThreads - 1) / kThreads, a.parts), kThreads, 0, st>>>(a);
     if (a.dx && a.rows > 0)
       ln_backward_long<T><<<static_cast<uint32_t>(std::min(a.rows, kMostBlocks)), kThreads, 0,
                             st>>>(a);
-    if (sums)
-      ln_columns<T><<<dim3((d + kThreads - 1) / kThreads, a.parts), kThreads, 0, st>>>(a);
   }
   if (sums && !few)
     ln_join<T><<<dim3((d + kJoinColumns - 1) / kJoinColumns, 2), kThreads, 0, st>>>(
