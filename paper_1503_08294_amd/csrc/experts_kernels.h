@@ -1131,9 +1131,13 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
     }
     load_a(0, 0);
     load_b(0, 0);
-    if constexpr (SA == 3) load_a(1, 1);
     if constexpr (kWeightsKind) read_tokens(1);
-    meet_loaded<SA == 3 ? LA : 0>();
+    if (SA == 3 && stages > 1) {
+      load_a(1, 1);
+      meet_loaded<LA>();
+    } else {  // (of one stage no later meet waits for loads, and the results take over their places)
+      meet_loaded<0>();
+    }
     if (late) meet();
     int32_t h = 0;
     for (; h + SA - 1 < stages; ++h) stage(yes, yes, h);

@@ -1,0 +1,38 @@
+"""The experts' products in tiles of 256 x 256 at sizes where a sum ends early: of one stage of k,
+of two, and of less than one."""
+import pytest
+import torch
+
+from test_gpu_mixture import BF16, F16, expert_inputs, expert_tolerance, experts_in_float64, near
+
+pytestmark = pytest.mark.gpu
+
+NAMES = ("out", "dx", "dweights", "dw1", "dw2")
+
+
+@pytest.fixture(scope="module")
+def mix():
+    from paper_1503_08294_amd import mixture
+    return mixture
+
+
+# (a stage is 64 of k; 128 tiles of the first product and more take sides of 256)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("tokens,experts,k,dim,hidden", [
+    (16_384, 8, 2, 64, 512), (16_384, 8, 2, 512, 64), (17_001, 4, 2, 520, 32),
+    (17_001, 4, 2, 56, 264), (17_001, 4, 2, 8, 8), (9_001, 4, 2, 72, 520), (17_001, 4, 2, 264, 72)])
+def test_sums_of_few_stages(mix, dtype, tokens, experts, k, dim, hidden):
+    a = [t.cuda() for t in expert_inputs(dtype, tokens, experts, k, dim, hidden, 61)]
+    x, ids, weights, w1, w2, dout = a
+    ids[5], ids[6, 0] = -1, experts
+    want = experts_in_float64(*a)
+    rel = expert_tolerance(dtype, dim, hidden, tokens * k)
+    first = None
+    for _ in range(3):
+        out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        got = (out, *mix.experts_backward(dout, x, ids, weights, w1, w2, saved))
+        for g, v, name in zip(got, want, NAMES):
+            near(g, v.detach().cpu(), rel, name)
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
+    near(mix.experts(x, ids, weights, w1, w2), want[0].detach().cpu(), rel, "out alone")
