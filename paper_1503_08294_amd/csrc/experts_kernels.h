@@ -792,8 +792,10 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
     for (int i = 0; i < MT; ++i) {
       const int32_t m = wm * (BM / WM) + i * 16;
       const float w = m + li < mrows ? x.weights[x.plan.rows[row0 + m + li]] : 0.0f;
-      // (the stores since then count too)
-      if (i == 0) await_own<0>();
+      // (The stores since then count too.  A wave whose rows or columns have ended sends none and
+      // may read what is not there yet, of which it uses nothing; but its loads may not outlast the
+      // loop, after which others write the dots to their place.)
+      if (i == 0 || i + 1 == MT) await_own<0>();
       else await_own<3 * Narrow::kStores>();
       const int64_t row = row0 + m;
       float part = 0.0f;

@@ -36,3 +36,26 @@ def test_sums_of_few_stages(mix, dtype, tokens, experts, k, dim, hidden):
         first = first or got
         assert all(torch.equal(p, q) for p, q in zip(got, first))
     near(mix.experts(x, ids, weights, w1, w2), want[0].detach().cpu(), rel, "out alone")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rest", [1, 17, 40, 129])
+def test_blocks_that_end_early(mix, dtype, rest):
+    """Every expert's last block holds a few rows, hidden ends inside a tile: waves without rows or
+    columns leave the sums of the others alone."""
+    experts, dim, hidden = 3, 520, 1304
+    each = 256 * 12 + rest
+    tokens = experts * each
+    x, _, weights, w1, w2, dout = (t.cuda() for t in expert_inputs(dtype, tokens, experts, 1, dim,
+                                                                   hidden, 62))
+    ids = (torch.arange(tokens, dtype=torch.int32, device="cuda") % experts)[:, None].contiguous()
+    want = experts_in_float64(x, ids, weights, w1, w2, dout)
+    rel = expert_tolerance(dtype, dim, hidden, tokens)
+    first = None
+    for _ in range(3):
+        out, saved = mix.experts_forward(x, ids, weights, w1, w2)
+        got = (out, *mix.experts_backward(dout, x, ids, weights, w1, w2, saved))
+        for g, v, name in zip(got, want, NAMES):
+            near(g, v.detach().cpu(), rel, name)
+        first = first or got
+        assert all(torch.equal(p, q) for p, q in zip(got, first))
