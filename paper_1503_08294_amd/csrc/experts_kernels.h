@@ -262,8 +262,10 @@ __device__ __forceinline__ Frag row_chunk(const T* row, int32_t k, int32_t K) {
 
 // Workgroups go round the 8 XCDs.  Runs of `run` tiles go to one XCD, where the tiles that its CUs
 // work on at a time share operands through its L2; the next run goes to the next XCD.
-// Fewer tiles than 8 runs are dealt out evenly.
+// Fewer tiles than 8 runs are dealt out evenly.  -1: no tile for this workgroup (for any of them,
+// where no pair has an expert and there are no tiles).
 __device__ __forceinline__ int32_t spread(int32_t block, int32_t total, int32_t run) {
+  if (total <= 0) return -1;
   if (total < 8 * run) run = (total + 7) / 8;
   const int32_t in = block >> 3;
   const int32_t id = (in / run * 8 + (block & 7)) * run + in % run;
