@@ -5,8 +5,9 @@ A network of units answers with the nearest units of a signal; a mixture of loca
 answers with what the models of its best units say about it.  ``route`` picks every token's
 experts (of the negative squared distances to the units with ``top=2``: the winner and the
 second of ``Network.find_winners``), ``experts`` runs their products, ``layer_norm`` goes before
-them.  ``layer_norm``, ``route`` and ``experts`` take part in autograd; the ``_forward`` and
-``_backward`` calls are their two halves for programs that keep their own order.
+them.  ``layer_norm``, ``route`` and ``experts`` take part in autograd, once: derivatives of their
+gradients raise ``RuntimeError``, and tensors that carry a forward-mode tangent are refused.  The
+``_forward`` and ``_backward`` calls are their two halves for programs that keep their own order.
 
 Tensors are on one HIP device; work goes to torch's current stream, where the outputs and
 workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
@@ -16,6 +17,7 @@ from __future__ import annotations
 import functools
 
 import torch
+from torch.autograd import forward_ad
 
 from . import gsn
 
@@ -26,6 +28,38 @@ def _same_device(x, *others):
     for t in others:
         if t is not None and t.get_device() != d:
             raise ValueError(f"a tensor of {tuple(t.shape)} is on {t.device}, not on {x.device}")
+
+
+def _no_tangent(*tensors):
+    """Refuses tensors with a forward-mode tangent, which the kernels would drop."""
+    if getattr(forward_ad, "_current_level", 0) < 0:  # outside of any dual_level: the usual case
+        return
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"a tensor of {tuple(t.shape)} carries a forward-mode tangent; "
+                             "there is no forward-mode derivative")
+
+
+class _Once(torch.autograd.Function):
+    """The first ``count`` tensors, gradients computed from the others; raises where they are
+    differentiated."""
+
+    @staticmethod
+    def forward(ctx, what, count, *tensors):
+        ctx.what = what
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"the gradients of {ctx.what} cannot be differentiated a second time")
+
+
+def _once(what, grads, *of):
+    """The gradients that a backward method returns, made of the tensors ``of``.  In a backward
+    pass that is itself recorded (create_graph=True) they would else count as constants."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in of):
+        return _Once.apply(what, len(grads), *grads, *of)
+    return grads
 
 
 def _rows(x: torch.Tensor, what: str) -> torch.Tensor:
@@ -78,12 +112,14 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, bias, stats = ctx.saved_tensors
         if dy.stride(-1) != 1 or (dy.shape[0] > 1 and dy.stride(0) < dy.shape[1]):
             dy = dy.contiguous()  # (an expanded gradient, as that of a sum)
-        return (*layer_norm_backward(dy, x, weight, bias, stats, ctx.needs_input_grad), None)
+        grads = layer_norm_backward(dy, x, weight, bias, stats, ctx.needs_input_grad)
+        return (*_once("layer_norm", grads, dy, x, weight), None)
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """Layer norm over the last dimension of x (rows, dim).  weight and bias: (dim,), float32 or
     of x's type, or None.  Rows may be those of a wider tensor (any row stride)."""
+    _no_tangent(x, weight, bias)
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad
                                        for t in (x, weight, bias)):
         return _LayerNorm.apply(x, weight, bias, eps)
@@ -127,7 +163,8 @@ class _Route(torch.autograd.Function):
     @staticmethod
     def backward(ctx, _, dweights):
         logits, ids = ctx.saved_tensors
-        return _route_backward(dweights.contiguous(), logits, ids, ctx.params), None, None, None
+        dlogits = _route_backward(dweights.contiguous(), logits, ids, ctx.params)
+        return *_once("route", (dlogits,), dweights, logits), None, None, None
 
 
 def route(logits, top, *, score="softmax", balance=None, groups=1, top_groups=1, best=1,
@@ -136,6 +173,7 @@ def route(logits, top, *, score="softmax", balance=None, groups=1, top_groups=1,
     and their weights; see gsn_route in include/gsn.h for the order, masks and ties.  The weights
     are differentiable with respect to the logits."""
     _rows(logits, "logits")
+    _no_tangent(logits, balance)
     params = _route_params(logits.shape[1], top, score, groups, top_groups, best, renormalise,
                            scale)
     if torch.is_grad_enabled() and logits.requires_grad:
@@ -212,9 +250,10 @@ class _Experts(torch.autograd.Function):
     def backward(ctx, dout):
         x, ids, weights, w1, w2, saved = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dweights, dw1, dw2 = experts_backward(dout.contiguous(), x, ids, weights, w1, w2,
-                                                  saved, (need[0], *need[2:5]))
-        return dx, None, dweights, dw1, dw2
+        grads = experts_backward(dout.contiguous(), x, ids, weights, w1, w2, saved,
+                                 (need[0], *need[2:5]))
+        dx, *rest = _once("experts", grads, dout, x, weights, w1, w2)
+        return dx, None, *rest
 
 
 def experts(x, ids, weights, w1, w2):
@@ -222,6 +261,7 @@ def experts(x, ids, weights, w1, w2):
     e = ids[t, k].  x (tokens, dim), ids int32 and weights float32 (tokens, top), w1 (experts,
     2 * hidden, dim) with the gate's rows first, w2 (experts, dim, hidden).  A pair whose id is
     not an expert's adds nothing."""
+    _no_tangent(x, weights, w1, w2)
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, weights, w1, w2)):
         return _Experts.apply(x, ids, weights, w1, w2)
     return _experts_forward(x, ids, weights, w1, w2, False)[0]
