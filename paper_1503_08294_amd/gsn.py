@@ -488,6 +488,7 @@ def _flat(t: torch.Tensor | None, dtype, shape, what: str):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _on(t: torch.Tensor, stream) -> int | ctypes.c_void_p:
@@ -495,6 +496,15 @@ def _on(t: torch.Tensor, stream) -> int | ctypes.c_void_p:
     if stream is None and _raw_stream is not None:
         return _raw_stream(t.device.index)
     return _stream(stream)
+
+
+def _run(f, t: torch.Tensor, stream, *args) -> int:
+    """f(*args, stream's handle) with t's device as the current one, where the kernels go to."""
+    device = t.get_device()
+    if device == _current_device():
+        return _check(f(*args, _on(t, stream)), f.__name__)
+    with torch.cuda.device(device):
+        return _check(f(*args, _on(t, stream)), f.__name__)
 
 
 def _params_type(x_dtype, weight, bias) -> torch.dtype:
@@ -510,10 +520,10 @@ def gsn_layer_norm(x, weight, bias, eps: float, y, stats=None, stream=None):
     xp, xs = _matrix(x, x.dtype, rows, dim, "x")
     yp, ys = _matrix(y, x.dtype, rows, dim, "y")
     pt = _params_type(x.dtype, weight, bias)
-    return _check(_lib.gsn_layer_norm(
-        code, _DTYPES.get(pt, -1), rows, dim, xp, xs, _flat(weight, pt, (dim,), "weight"),
-        _flat(bias, pt, (dim,), "bias"), eps, yp, ys,
-        _flat(stats, torch.float32, (2, rows), "stats"), _on(x, stream)), "gsn_layer_norm")
+    return _run(
+        _lib.gsn_layer_norm, x, stream, code, _DTYPES.get(pt, -1), rows, dim, xp, xs,
+        _flat(weight, pt, (dim,), "weight"), _flat(bias, pt, (dim,), "bias"), eps, yp, ys,
+        _flat(stats, torch.float32, (2, rows), "stats"))
 
 
 def gsn_layer_norm_workspace_bytes(rows: int, dim: int) -> int:
@@ -528,12 +538,12 @@ def gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, workspace,
     xp, xs = _matrix(x, x.dtype, rows, dim, "x")
     dxp, dxs = (None, dim) if dx is None else _matrix(dx, x.dtype, rows, dim, "dx")
     pt = _params_type(x.dtype, weight if weight is not None else dweight, dbias)
-    return _check(_lib.gsn_layer_norm_backward(
-        code, _DTYPES.get(pt, -1), rows, dim, dyp, dys, xp, xs,
-        _flat(weight, pt, (dim,), "weight"), _flat(stats, torch.float32, (2, rows), "stats"),
+    return _run(
+        _lib.gsn_layer_norm_backward, x, stream, code, _DTYPES.get(pt, -1), rows, dim, dyp, dys,
+        xp, xs, _flat(weight, pt, (dim,), "weight"),
+        _flat(stats, torch.float32, (2, rows), "stats"),
         dxp, dxs, _flat(dweight, pt, (dim,), "dweight"), _flat(dbias, pt, (dim,), "dbias"),
-        _dev(workspace, torch.uint8), 0 if workspace is None else workspace.numel(),
-        _on(x, stream)), "gsn_layer_norm_backward")
+        _dev(workspace, torch.uint8), 0 if workspace is None else workspace.numel())
 
 
 def make_route(experts: int, top: int, score="softmax", groups=1, top_groups=1, best=1,
@@ -550,37 +560,35 @@ def gsn_route(params: gsn_route_params, logits, balance, valid, ids, weights, st
     None; ids, weights: (tokens, top)."""
     tokens = logits.shape[0]
     lp, ls = _matrix(logits, logits.dtype, tokens, params.experts, "logits")
-    return _check(_lib.gsn_route(
-        params, _type(logits, "logits"), tokens, lp, ls,
+    return _run(
+        _lib.gsn_route, logits, stream, params, _type(logits, "logits"), tokens, lp, ls,
         _flat(balance, torch.float32, (params.experts,), "balance"),
         _flat(valid, torch.uint8, (tokens,), "valid"),
         _flat(ids, torch.int32, (tokens, params.top), "ids"),
-        _flat(weights, torch.float32, (tokens, params.top), "weights"), _on(logits, stream)),
-        "gsn_route")
+        _flat(weights, torch.float32, (tokens, params.top), "weights"))
 
 
 def gsn_route_backward(params: gsn_route_params, dweights, logits, ids, dlogits, stream=None):
     tokens = logits.shape[0]
     lp, ls = _matrix(logits, logits.dtype, tokens, params.experts, "logits")
     dp, ds = _matrix(dlogits, logits.dtype, tokens, params.experts, "dlogits")
-    return _check(_lib.gsn_route_backward(
-        params, _type(logits, "logits"), tokens,
+    return _run(
+        _lib.gsn_route_backward, logits, stream, params, _type(logits, "logits"), tokens,
         _flat(dweights, torch.float32, (tokens, params.top), "dweights"), lp, ls,
-        _flat(ids, torch.int32, (tokens, params.top), "ids"), dp, ds, _on(logits, stream)),
-        "gsn_route_backward")
+        _flat(ids, torch.int32, (tokens, params.top), "ids"), dp, ds)
 
 
 def gsn_route_counts(ids, counts, stream=None):
-    return _check(_lib.gsn_route_counts(
-        ids.numel(), counts.numel(), _dev(ids, torch.int32, what="ids"),
-        _dev(counts, torch.int32, what="counts"), _on(ids, stream)), "gsn_route_counts")
+    return _run(
+        _lib.gsn_route_counts, ids, stream, ids.numel(), counts.numel(),
+        _dev(ids, torch.int32, what="ids"), _dev(counts, torch.int32, what="counts"))
 
 
 def gsn_route_balance(counts, rate: float, balance, stream=None):
-    return _check(_lib.gsn_route_balance(
-        counts.numel(), _dev(counts, torch.int32, what="counts"), rate,
-        _dev(balance, torch.float32, counts.numel(), "balance"), _on(counts, stream)),
-        "gsn_route_balance")
+    return _run(
+        _lib.gsn_route_balance, counts, stream, counts.numel(),
+        _dev(counts, torch.int32, what="counts"), rate,
+        _dev(balance, torch.float32, counts.numel(), "balance"))
 
 
 def make_experts(x, ids, w1, w2) -> gsn_experts_params:
@@ -605,14 +613,14 @@ def gsn_experts(params: gsn_experts_params, x, ids, weights, w1, w2, out, saved,
     p = params
     xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
     pairs = (p.tokens, p.top)
-    return _check(_lib.gsn_experts(
-        p, xp, xs, _flat(ids, torch.int32, pairs, "ids"),
+    return _run(
+        _lib.gsn_experts, x, stream, p, xp, xs, _flat(ids, torch.int32, pairs, "ids"),
         _flat(weights, torch.float32, pairs, "weights"),
         _flat(w1, x.dtype, (p.experts, 2 * p.hidden, p.dim), "w1"),
         _flat(w2, x.dtype, (p.experts, p.dim, p.hidden), "w2"),
         _flat(out, x.dtype, (p.tokens, p.dim), "out"), _dev(saved, torch.uint8, what="saved"),
         0 if saved is None else saved.numel(), _dev(workspace, torch.uint8, what="workspace"),
-        workspace.numel(), _on(x, stream)), "gsn_experts")
+        workspace.numel())
 
 
 def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, saved, dx,
@@ -621,14 +629,15 @@ def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, s
     xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
     pairs = (p.tokens, p.top)
     s1, s2 = (p.experts, 2 * p.hidden, p.dim), (p.experts, p.dim, p.hidden)
-    return _check(_lib.gsn_experts_backward(
-        p, _flat(dout, x.dtype, (p.tokens, p.dim), "dout"), xp, xs,
+    return _run(
+        _lib.gsn_experts_backward, x, stream, p,
+        _flat(dout, x.dtype, (p.tokens, p.dim), "dout"), xp, xs,
         _flat(weights, torch.float32, pairs, "weights"), _flat(w1, x.dtype, s1, "w1"),
         _flat(w2, x.dtype, s2, "w2"), _dev(saved, torch.uint8, what="saved"), saved.numel(),
         _flat(dx, x.dtype, (p.tokens, p.dim), "dx"),
         _flat(dweights, torch.float32, pairs, "dweights"), _flat(dw1, x.dtype, s1, "dw1"),
         _flat(dw2, x.dtype, s2, "dw2"), _dev(workspace, torch.uint8, what="workspace"),
-        workspace.numel(), _on(x, stream)), "gsn_experts_backward")
+        workspace.numel())
 
 
 # ------------------------------------------------------------------ convenience ----

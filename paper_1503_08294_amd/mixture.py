@@ -9,8 +9,8 @@ them.  ``layer_norm``, ``route`` and ``experts`` take part in autograd, once: de
 gradients raise ``RuntimeError``, and tensors that carry a forward-mode tangent are refused.  The
 ``_forward`` and ``_backward`` calls are their two halves for programs that keep their own order.
 
-Tensors are on one HIP device; work goes to torch's current stream, where the outputs and
-workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
+Tensors are on one HIP device; work goes to torch's current stream of that device, where the
+outputs and workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
 """
 from __future__ import annotations
 
@@ -199,6 +199,7 @@ def route_counts(ids, experts):
 
 def route_balance(counts, balance, rate=1e-3):
     """Moves balance in place by rate towards the experts with fewer pairs than the mean."""
+    _same_device(counts, balance)
     gsn.gsn_route_balance(counts, rate, balance)
     return balance
 
