@@ -526,7 +526,9 @@ typedef struct gsn_experts_params {
 size_t gsn_experts_workspace_bytes(const gsn_experts_params* params, int32_t backward);
 size_t gsn_experts_saved_bytes(const gsn_experts_params* params);
 
-/* saved may be NULL (no backward pass will follow). */
+/* saved may be NULL (no backward pass will follow).  GSN_E_CAPACITY if a grid has no room for a
+ * product's tiles (64, 128 or 256 a side): some 2^24 of the forward pass or of the gates'
+ * gradients, or of those of dx, dw1 and dw2 together, as far as they are wanted. */
 int gsn_experts(const gsn_experts_params* params, const void* x, int64_t x_stride,
                 const int32_t* ids, const float* weights, const void* w1, const void* w2,
                 void* out, void* saved, size_t saved_bytes, void* workspace,

@@ -64,8 +64,35 @@ hipError_t launch_experts(const Experts& x, hipStream_t st);
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
 
-// Side of the products' large tiles (kSmallRows: the small ones).
+// Side of the products' large tiles (kSmallRows: the small ones), and the run of them that goes to
+// one XCD.
 constexpr int32_t kTileRows = kPlanRows;
 constexpr int32_t kMiddleRows = 128;
+constexpr int32_t tile_run(int32_t side) {
+  return side == kTileRows ? 32 : side == kMiddleRows ? 16 : 1;
+}
+
+enum Kind {
+  kForwardGate,   // act (and pre) from x, w1
+  kForwardOut,    // y from act, w2
+  kBackwardGate,  // dpre, wact, dots from dout, w2
+  kBackwardIn,    // dxr from dpre, w1
+  kWeightsIn,     // dw1 from dpre, x
+  kWeightsOut     // dw2 from dout, wact
+};
+
+// Workgroups for every tile of a product.
+inline int64_t product_blocks(Kind kind, const Experts& x) {
+  const auto up = [](int64_t n, int64_t per) { return (n + per - 1) / per; };
+  const bool of_hidden = kind == kForwardGate || kind == kBackwardGate || kind == kWeightsOut;
+  const int64_t n = up(of_hidden ? x.hidden : x.dim, kind == kForwardGate ? x.side / 2 : x.side);
+  const int64_t m = kind == kWeightsIn    ? x.experts * up(2 * int64_t{x.hidden}, x.side)
+                    : kind == kWeightsOut ? x.experts * up(x.dim, x.side)
+                    : x.side == kSmallRows
+                        ? x.plan.most_small
+                        : int64_t{x.plan.most_tiles} * (kPlanRows / x.side);
+  const int64_t round = x.side == kSmallRows ? 1 : 8 * tile_run(x.side);
+  return up(n * m, round) * round;
+}
 
 }  // namespace gsn

@@ -271,15 +271,24 @@ int32_t tile_side(const Experts& x, int32_t dtype) {
   return x.dim >= 8 && x.hidden >= 8 && tiles(kMiddleRows) >= 256 ? kMiddleRows : kSmallRows;
 }
 
-// Whether every launch's grid stays below 2^32 threads.
-bool grids_ok(const Experts& x) {
-  const int64_t side = x.side, threads = side == kTileRows ? 512 : 256;
-  const auto tiles = [&](int64_t n) { return (n + side - 1) / side; };
-  const int64_t rows = x.pairs / side + x.experts;
-  const int64_t wide = tiles(2 * static_cast<int64_t>(x.hidden)) + 1, deep = tiles(x.dim);
-  const int64_t most = std::max(
-      rows * wide, rows * deep + 2 * x.experts * wide * deep + x.pairs / threads);
-  return most + 4096 < (int64_t{1} << 32) / threads;
+// Whether the grids of a call's products stay below 2^32 threads: of the backward pass one for the
+// gates' gradients and one for what is wanted of the others.
+bool grids_ok(const Experts& x, bool backward) {
+  const int64_t threads = x.side == kTileRows ? 512 : 256;
+  const auto in = [&](Kind kind) { return product_blocks(kind, x); };
+  const int64_t most =
+      backward ? std::max(in(kBackwardGate), (x.dx ? in(kBackwardIn) : 0) +
+                                                 (x.dw1 ? in(kWeightsIn) : 0) +
+                                                 (x.dw2 ? in(kWeightsOut) : 0) +
+                                                 (x.dweights ? x.pairs / threads + 1 : 0))
+               : std::max(in(kForwardGate), in(kForwardOut));
+  return most < (int64_t{1} << 32) / threads;
+}
+
+// Weights beyond the addresses of a process are no weights.
+bool weights_ok(const gsn_experts_params& p) {
+  const int64_t bytes = p.experts * static_cast<int64_t>(size_of(p.dtype));
+  return int64_t{2} * p.hidden * p.dim <= (int64_t{1} << 47) / bytes;
 }
 
 bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256 == 0; }
@@ -341,9 +350,9 @@ int gsn_experts(const gsn_experts_params* p, const void* x, int64_t x_stride,
   a.w2 = w2;
   a.out = out;
   a.side = gsn::tile_side(a, p->dtype);
-  if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   if (saved) gsn::carve_saved(saved, &a);
   gsn::carve_forward(workspace, p->dtype, saved != nullptr, &a);
+  if (!gsn::weights_ok(*p) || !gsn::grids_ok(a, false)) return GSN_E_CAPACITY;
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (a.tokens == 0) e = gsn::launch_plan(a, st);
@@ -377,9 +386,9 @@ int gsn_experts_backward(const gsn_experts_params* p, const void* dout, const vo
   a.dw1 = dw1;
   a.dw2 = dw2;
   a.side = gsn::tile_side(a, p->dtype);
-  if (!gsn::grids_ok(a)) return GSN_E_CAPACITY;
   gsn::carve_saved(const_cast<void*>(saved), &a);
   gsn::carve_backward(workspace, p->dtype, &a);
+  if (!gsn::weights_ok(*p) || !gsn::grids_ok(a, true)) return GSN_E_CAPACITY;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32 ? gsn::launch_experts_backward<float>(a, st)
                        : p->dtype == GSN_BF16

@@ -98,15 +98,6 @@ __device__ __forceinline__ Frag fragment(const char* tile, int r0, int s, int la
   return f;
 }
 
-enum Kind {
-  kForwardGate,   // act (and pre) from x, w1
-  kForwardOut,    // y from act, w2
-  kBackwardGate,  // dpre, wact, dots from dout, w2
-  kBackwardIn,    // dxr from dpre, w1
-  kWeightsIn,     // dw1 from dpre, x
-  kWeightsOut     // dw2 from dout, wact
-};
-
 // Four results of a row at column n, N columns in all.  Rows start at any element.
 template <typename T>
 struct LooseOf {
@@ -287,7 +278,7 @@ __device__ __forceinline__ int2 tile_place(int32_t id, int32_t tiles_m, int32_t 
 template <int SIDE>
 constexpr int32_t kTall = SIDE == kSmallRows ? 1 : 4;
 template <int SIDE>
-constexpr int32_t kRun = SIDE == kTileRows ? 32 : SIDE == kMiddleRows ? 16 : 1;
+constexpr int32_t kRun = tile_run(SIDE);
 
 // Gradients of the weights of the pairs from j on, one a thread: the sums of their parts.
 __device__ __forceinline__ void sum_dots(const Experts& x, int64_t j) {
@@ -1139,7 +1130,7 @@ __device__ __forceinline__ void large_tile(const Experts& x, int32_t block, char
     if (SA == 3 && stages > 1) {
       load_a(1, 1);
       meet_loaded<LA>();
-    } else {  // (of one stage no later meet waits for loads, and the results take over their places)
+    } else {  // (of one stage no later meet waits for loads, and the results take their places)
       meet_loaded<0>();
     }
     if (late) meet();
@@ -1414,22 +1405,6 @@ inline uint32_t join_blocks(const Experts& x) {
   return static_cast<uint32_t>(n < (1 << 20) ? n : 1 << 20);
 }
 
-// Workgroups for every tile of a product.
-template <Kind KIND>
-uint32_t product_grid(const Experts& x) {
-  const uint32_t n = blocks_of(KIND == kForwardGate || KIND == kBackwardGate ||
-                               KIND == kWeightsOut ? x.hidden : x.dim,
-                               KIND == kForwardGate ? x.side / 2 : x.side);
-  const uint32_t tiles =
-      n * (KIND == kWeightsIn    ? x.experts * blocks_of(2 * x.hidden, x.side)
-           : KIND == kWeightsOut ? x.experts * blocks_of(x.dim, x.side)
-           : x.side == kSmallRows ? x.plan.most_small
-                                  : x.plan.most_tiles * (kPlanRows / x.side));
-  const uint32_t round = x.side == kTileRows     ? 8 * kRun<kTileRows>
-                         : x.side == kMiddleRows ? 8 * kRun<kMiddleRows> : 1;
-  return blocks_of(tiles, round) * round;
-}
-
 template <typename T>
 bool tiny(const Experts& x) {
   constexpr int kE = 16 / sizeof(T);
@@ -1439,7 +1414,7 @@ bool tiny(const Experts& x) {
 template <typename T, Kind KIND>
 void product(Experts x, hipStream_t st) {
   x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
-  const uint32_t grid = product_grid<KIND>(x);
+  const uint32_t grid = static_cast<uint32_t>(product_blocks(KIND, x));
   if (grid == 0) return;
   if constexpr (sizeof(T) == 2) {
     if (x.side == kTileRows) {
@@ -1478,9 +1453,10 @@ void product(Experts x, hipStream_t st) {
 template <typename T>
 void gradients(Experts x, hipStream_t st) {
   x.dot_tiles = static_cast<int32_t>(blocks_of(x.hidden, x.side));
-  const auto in = [](bool wanted, uint32_t n) { return static_cast<int32_t>(wanted ? n : 0); };
-  Shares n{in(x.dx, product_grid<kBackwardIn>(x)), in(x.dw1, product_grid<kWeightsIn>(x)),
-           in(x.dw2, product_grid<kWeightsOut>(x)), 0};
+  const auto in = [&](const void* wanted, Kind kind) {
+    return static_cast<int32_t>(wanted ? product_blocks(kind, x) : 0);
+  };
+  Shares n{in(x.dx, kBackwardIn), in(x.dw1, kWeightsIn), in(x.dw2, kWeightsOut), 0};
   if (x.pairs > int64_t{2} * x.hidden * x.experts) n.begin = n.in_x;
   const uint32_t threads = x.side == kTileRows ? kLargeThreads : kLooseThreads;
   const uint32_t grid = n.in_x + n.in_w1 + n.in_w2 + (x.dweights ? blocks_of(x.pairs, threads) : 0);
