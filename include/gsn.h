@@ -445,7 +445,7 @@ enum { GSN_F32 = 0, GSN_BF16 = 1, GSN_F16 = 2 };
  * dtype: the type of x and y; param_dtype: that of weight and bias, GSN_F32 or dtype.  weight
  * and bias may be NULL (1 and 0).  stats (device float [2][rows], or NULL) receives the means,
  * then the r's, which the backward pass takes.  x and y may be the same memory.  rows >= 0,
- * dim >= 1, eps >= 0. */
+ * dim 1 to 2^27, eps >= 0. */
 int gsn_layer_norm(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim, const void* x,
                    int64_t x_stride, const void* weight, const void* bias, float eps, void* y,
                    int64_t y_stride, float* stats, void* stream);

@@ -516,6 +516,8 @@ bool types_ok(int32_t dtype, int32_t param_dtype) {
 }
 
 constexpr int64_t kMostRows = int64_t{1} << 40;
+// (32-bit places in a row, with a step past its end; 16 threads a column in the columns' join)
+constexpr int32_t kMostDim = 1 << 27;
 
 }  // namespace
 }  // namespace gsn
@@ -526,7 +528,7 @@ int gsn_layer_norm(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim
                    int64_t x_stride, const void* weight, const void* bias, float eps, void* y,
                    int64_t y_stride, float* stats, void* stream) {
   if (!gsn::types_ok(dtype, param_dtype) || rows < 0 || rows > gsn::kMostRows || dim < 1 ||
-      !(eps >= 0.0f))
+      dim > gsn::kMostDim || !(eps >= 0.0f))
     return GSN_E_INVAL;
   if (rows == 0) return GSN_OK;
   if (!x || !y || x_stride < dim || y_stride < dim) return GSN_E_INVAL;
@@ -540,7 +542,7 @@ int gsn_layer_norm(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim
 }
 
 size_t gsn_layer_norm_workspace_bytes(int64_t rows, int32_t dim) {
-  if (rows < 0 || rows > gsn::kMostRows || dim < 1) return 0;
+  if (rows < 0 || rows > gsn::kMostRows || dim < 1 || dim > gsn::kMostDim) return 0;
   return sizeof(float) * 2 * static_cast<size_t>(gsn::norm_parts(rows)) * dim;
 }
 
@@ -549,7 +551,8 @@ int gsn_layer_norm_backward(int32_t dtype, int32_t param_dtype, int64_t rows, in
                             const void* weight, const float* stats, void* dx, int64_t dx_stride,
                             void* dweight, void* dbias, void* workspace,
                             size_t workspace_bytes, void* stream) {
-  if (!gsn::types_ok(dtype, param_dtype) || rows < 0 || rows > gsn::kMostRows || dim < 1)
+  if (!gsn::types_ok(dtype, param_dtype) || rows < 0 || rows > gsn::kMostRows || dim < 1 ||
+      dim > gsn::kMostDim)
     return GSN_E_INVAL;
   if (rows > 0 && (!dy || !x || !stats || dy_stride < dim || x_stride < dim ||
                    (dx && dx_stride < dim)))
