@@ -1,13 +1,13 @@
 // The experts' products: what the host passes to the kernels of one type of element.
 #pragma once
 
+#include "experts_rule.h"
 #include "mixture.h"
 
 namespace gsn {
 
-constexpr int kPlanExperts = 1024;  // experts at most
-constexpr int kPlanRows = 256;      // rows of a listed block
-constexpr int kSmallRows = 64;      // of a small one
+constexpr int kPlanExperts = 1024;    // experts at most
+constexpr int kPlanRows = kTileRows;  // rows of a listed block
 
 // Pairs (token, place k), number token * top + k, sorted by expert and then by number: row r of
 // the products is pair rows[r], pair j is row pos[j] (-1 for a pair without an expert), expert
@@ -63,14 +63,6 @@ template <typename T>
 hipError_t launch_experts(const Experts& x, hipStream_t st);
 template <typename T>
 hipError_t launch_experts_backward(const Experts& x, hipStream_t st);
-
-// Side of the products' large tiles (kSmallRows: the small ones), and the run of them that goes to
-// one XCD.
-constexpr int32_t kTileRows = kPlanRows;
-constexpr int32_t kMiddleRows = 128;
-constexpr int32_t tile_run(int32_t side) {
-  return side == kTileRows ? 32 : side == kMiddleRows ? 16 : 1;
-}
 
 enum Kind {
   kForwardGate,   // act (and pre) from x, w1

@@ -245,30 +245,11 @@ Experts experts_of(const gsn_experts_params& p) {
   return x;
 }
 
-// Sides of the products' tiles: of 2-byte elements the larger ones, from 128 pairs an expert on and
-// where the first product has enough of them to fill the chip; the largest need rows, and starts
-// of rows, at multiples of 16 bytes.  Forward and backward pass in us, with sides of
-// 256 and 64 (from 128 tiles of 256 on): 2,000 tokens, 2 of 8 experts, 1,024 x 1,024: 218 and 251;
-//   16,384, 2 of 32, 2,048 x 2,048: 2,900 and 5,282; 1,024, 2 of 4, 1,024 x 512 (40 tiles): 141 and
-//   94; 495, 3 of 7, 1,984 x 320: 175 and 116; forward of 5,100, 1 of 8, 448 x 992: 55 and 66;
-// 128 and 64 (from 256 tiles of 128 on): 16,384, 2 of 32, 2,047 x 2,047: 5,243 and 7,782; 1,500, 2
-//   of 8, 999 x 701 (297 tiles): 174 and 190; 1,500, 1 of 8, 511 x 1,023 (240 tiles): 141 and 109;
-//   with fewer pairs an expert, 2,048, 2 of 64, 511 x 701: 307 and 281.
-// In binary32, where the matrix cores are 16 times slower, small tiles waste less at the edges:
-// 128 and 64: 4,096, 2 of 16, 1,024 x 1,024: 1,981 and 1,558.
-int32_t tile_side(const Experts& x, int32_t dtype) {
-  const auto tiles = [&](int32_t side) {
-    return (x.pairs / side + x.experts / 2) *
-           ((2 * static_cast<int64_t>(x.hidden) + side - 1) / side);
-  };
-  if (dtype == GSN_F32 || x.pairs < int64_t{128} * x.experts) return kSmallRows;
-  const bool aligned = x.dim % 8 == 0 && x.hidden % 8 == 0 && x.x_stride % 8 == 0 &&
-                       aligned16(x.x) && aligned16(x.w1) && aligned16(x.w2) &&
-                       aligned16(x.out) && aligned16(x.dout) && aligned16(x.dx) &&
-                       aligned16(x.dw1) && aligned16(x.dw2);
-  if (aligned && tiles(kTileRows) >= 128) return kTileRows;
-  // (a row shorter than 16 bytes is loaded by the small tiles alone)
-  return x.dim >= 8 && x.hidden >= 8 && tiles(kMiddleRows) >= 256 ? kMiddleRows : kSmallRows;
+int32_t side_of(const Experts& x, int32_t dtype) {
+  const bool aligned = x.x_stride % 8 == 0 && aligned16(x.x) && aligned16(x.w1) &&
+                       aligned16(x.w2) && aligned16(x.out) && aligned16(x.dout) &&
+                       aligned16(x.dx) && aligned16(x.dw1) && aligned16(x.dw2);
+  return tile_side(dtype == GSN_F32, x.pairs, x.experts, x.dim, x.hidden, aligned);
 }
 
 // Whether the grids of a call's products stay below 2^32 threads: of the backward pass one for the
@@ -349,7 +330,7 @@ int gsn_experts(const gsn_experts_params* p, const void* x, int64_t x_stride,
   a.w1 = w1;
   a.w2 = w2;
   a.out = out;
-  a.side = gsn::tile_side(a, p->dtype);
+  a.side = gsn::side_of(a, p->dtype);
   if (saved) gsn::carve_saved(saved, &a);
   gsn::carve_forward(workspace, p->dtype, saved != nullptr, &a);
   if (!gsn::weights_ok(*p) || !gsn::grids_ok(a, false)) return GSN_E_CAPACITY;
@@ -385,7 +366,7 @@ int gsn_experts_backward(const gsn_experts_params* p, const void* dout, const vo
   a.dweights = dweights;
   a.dw1 = dw1;
   a.dw2 = dw2;
-  a.side = gsn::tile_side(a, p->dtype);
+  a.side = gsn::side_of(a, p->dtype);
   gsn::carve_saved(const_cast<void*>(saved), &a);
   gsn::carve_backward(workspace, p->dtype, &a);
   if (!gsn::weights_ok(*p) || !gsn::grids_ok(a, true)) return GSN_E_CAPACITY;

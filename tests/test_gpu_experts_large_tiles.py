@@ -1,9 +1,10 @@
 """The experts' products in tiles of 256 x 256 at sizes where a sum ends early: of one stage of k,
-of two, and of less than one."""
+of two, and of less than one; where blocks end early; and with tokens past 2^32 elements."""
 import pytest
 import torch
 
-from test_gpu_mixture import BF16, F16, expert_inputs, expert_tolerance, experts_in_float64, near
+from test_gpu_mixture import (BF16, F16, expert_inputs, expert_tolerance, experts_in_float64,
+                              far_apart, near)
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,21 @@ def test_blocks_that_end_early(mix, dtype, rest):
             near(g, v.detach().cpu(), rel, name)
         first = first or got
         assert all(torch.equal(p, q) for p, q in zip(got, first))
+
+
+FAR = [(64, 904), (136, 904)]  # dim, hidden
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim,hidden", FAR)
+def test_tokens_beyond_32_bits(mix, dtype, dim, hidden):
+    """Rows of x as rows of the first product, and as k of the gradient of w1."""
+    x, ids, weights, w1, w2, dout = expert_inputs(dtype, 4300, 2, 2, dim, hidden, 64)
+    a = [t.cuda() for t in (x, ids, weights, w1, w2)]
+    out, saved = mix.experts_forward(*a)
+    grads = mix.experts_backward(dout.cuda(), *a, saved)
+    far = [far_apart(x), *a[1:]]
+    far_out, far_saved = mix.experts_forward(*far)
+    assert torch.equal(far_out, out)
+    far_grads = mix.experts_backward(dout.cuda(), *far, far_saved)
+    assert all(torch.equal(p, q) for p, q in zip(far_grads, grads))
