@@ -513,8 +513,10 @@ int gsn_route_balance(int32_t experts, const int32_t* counts, float rate, float*
  * with e = ids[t][k], silu(v) = v / (1 + exp(-v)); a pair whose id is out of range adds nothing.
  * x [tokens][dim] with a row stride, w1 [experts][2 * hidden][dim] (the gate's rows first),
  * w2 [experts][dim][hidden] and out [tokens][dim] are of type dtype; silu(gate) * up is rounded
- * to dtype between the two products, the sum over k is in binary32.  tokens up to 2^23,
- * tokens * top up to 2^26, experts 1 to 1024, top 1 to 64, dim and hidden 1 to 2^20. */
+ * to dtype between the two products, the sum over k is in binary32.  In GSN_F16 that rounding has
+ * the type's range too: a token with |silu(gate) * up| of 65,520 or more has a result that is not
+ * finite.  tokens up to 2^23, tokens * top up to 2^26, experts 1 to 1024, top 1 to 64, dim and
+ * hidden 1 to 2^20. */
 typedef struct gsn_experts_params {
   int32_t dtype;
   int32_t experts, top, dim, hidden;
@@ -536,7 +538,10 @@ int gsn_experts(const gsn_experts_params* params, const void* x, int64_t x_strid
 
 /* Gradients from dout [tokens][dim], with the arguments and the saved buffer of the forward
  * call: dx [tokens][dim], dweights float [tokens][top], dw1, dw2 (every element written; 0 for
- * an expert without tokens).  Each may be NULL (not computed). */
+ * an expert without tokens).  Each may be NULL (not computed).  A pair's gradients of gate and up
+ * (for dx and dw1) and its weight times silu(gate) * up (for dw2) are rounded to dtype before they
+ * are summed.  In GSN_F16 gradients of gate and up of 2^-25 or less are thus 0, below 2^-14 they
+ * have fewer bits, and at 65,520 they are infinite: scale dout so that they lie between. */
 int gsn_experts_backward(const gsn_experts_params* params, const void* dout, const void* x,
                          int64_t x_stride, const float* weights, const void* w1, const void* w2,
                          const void* saved, size_t saved_bytes, void* dx, float* dweights,

@@ -9,6 +9,10 @@
 //   da = dout w2     dout gathered; pre                       -> dpre, wact, parts of dweights
 //   dx = dpre w1                                              -> dxr, then joined by token
 //   dw1 = dpre^T x,  dw2 = dout^T wact       k: an expert's pairs
+// act, dpre and wact are rounded to the type of the elements, as the matrix cores take operands of
+// one type and binary32 ones at an eighth of the rate (0.153 to 1.28 PFLOP/s in large products): a
+// result has the error of one more rounding, and in f16 the range of that type.  Sums, the first
+// product's results for the backward pass, and the rows that are joined by token are binary32.
 #pragma once
 
 #include "experts.h"

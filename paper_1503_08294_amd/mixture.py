@@ -261,7 +261,9 @@ def experts(x, ids, weights, w1, w2):
     """out[t] = sum_k weights[t, k] * w2[e] (silu(gate) * up), (gate, up) = w1[e] x[t] and
     e = ids[t, k].  x (tokens, dim), ids int32 and weights float32 (tokens, top), w1 (experts,
     2 * hidden, dim) with the gate's rows first, w2 (experts, dim, hidden).  A pair whose id is
-    not an expert's adds nothing."""
+    not an expert's adds nothing.  silu(gate) * up, and the gradients of gate and up, are rounded
+    to x's type between the products: in float16 they have its range (include/gsn.h), and a loss
+    is scaled as usual there."""
     _no_tangent(x, weights, w1, w2)
     if torch.is_grad_enabled() and any(t.requires_grad for t in (x, weights, w1, w2)):
         return _Experts.apply(x, ids, weights, w1, w2)
