@@ -473,6 +473,8 @@ int gsn_layer_norm_backward(int32_t dtype, int32_t param_dtype, int64_t rows, in
  *   - ids receives the top best of what is left, -1 where nothing is left; weights their s
  *     (without the balance), over the sum of the chosen s if renormalise is not 0, times
  *     scale; 0 where the id is -1.
+ * Exponentials are binary32: a score far below the largest (softmax) or below 1 (sigmoid) has a
+ * relative error of some (v + 3) 2^-24 at a difference, or a negative logit, of size v.
  * A token whose valid byte is 0 has no experts, whatever its logits (valid may be NULL).
  * experts 1 to 1024, top 1 to 64 and at most top_groups * experts / groups, groups a divisor
  * of experts, 1 to 64. */
