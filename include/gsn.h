@@ -455,7 +455,7 @@ size_t gsn_layer_norm_workspace_bytes(int64_t rows, int32_t dim);
 
 /* Gradients of gsn_layer_norm from dy: dx, and the sums over the rows dweight = sum dy n,
  * dbias = sum dy with n = (x - mean) * r.  Each output may be NULL (not computed); dx may be
- * the memory of dy.  workspace: 256-byte aligned, needed for dweight or dbias. */
+ * the memory of dy or of x.  workspace: 256-byte aligned, needed for dweight or dbias. */
 int gsn_layer_norm_backward(int32_t dtype, int32_t param_dtype, int64_t rows, int32_t dim,
                             const void* dy, int64_t dy_stride, const void* x, int64_t x_stride,
                             const void* weight, const float* stats, void* dx, int64_t dx_stride,

@@ -635,8 +635,8 @@ __global__ __launch_bounds__(kLooseThreads, (kLooseWaves<T, SIDE>)) void ex_loos
 // The compiler does not count these loads: meet() does (with the builtin of this load the
 // compiler waits for all of them before every read of LDS, as it cannot tell the buffers apart).
 // m0 is a reserved register, which asm cannot declare as written; no other instruction of these
-// kernels reads it (tests/test_experts_assembly.py; putting its old value back after every load took
-// up to 3% of a training step's time).
+// kernels reads it (tests/test_experts_assembly.py; putting its old value back after every load
+// took up to 3% of a training step's time).
 __device__ __forceinline__ void load_to_lds(const void* p, uint32_t at) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :

@@ -480,10 +480,11 @@ hipError_t backward(NormBackArgs a, void* dw, void* db, hipStream_t st) {
                            : static_cast<uint32_t>(std::min(std::max<int64_t>(a.rows, 1),
                                                             kMostBlocks));
   // few rows: the columns' sums by workgroups of their own in the same launch, without a join; not
-  // where dx goes over the dy that they read (else a workgroup reads all of a row before it writes
-  // any of it, and takes its part of the sums from what it read)
+  // where dx goes over the dy or x that they read (else a workgroup reads all of a row before it
+  // writes any of it, and takes its part of the sums from what it read)
   const bool few = sums && a.rows <= kFewRows && d <= 16 * kRow &&
-                   !overlap<T>(a.dx, a.dx_stride, a.dy, a.dy_stride, a.rows, d);
+                   !overlap<T>(a.dx, a.dx_stride, a.dy, a.dy_stride, a.rows, d) &&
+                   !overlap<T>(a.dx, a.dx_stride, a.x, a.x_stride, a.rows, d);
   a.row_blocks = nb;
   uint32_t grid = nb;
   if (few) {
@@ -498,7 +499,7 @@ hipError_t backward(NormBackArgs a, void* dw, void* db, hipStream_t st) {
   else if (d <= 8 * kRow) ln_backward<T, kThreads, 2><<<grid, kThreads, 0, st>>>(a);
   else if (d <= 16 * kRow) ln_backward<T, kThreads, 4><<<grid, kThreads, 0, st>>>(a);
   else {
-    if (sums)  // (first: dx may go over dy)
+    if (sums)  // (first: dx may go over dy or x)
       ln_columns<T><<<dim3((d + kThreads - 1) / kThreads, a.parts), kThreads, 0, st>>>(a);
     if (a.dx && a.rows > 0)
       ln_backward_long<T><<<static_cast<uint32_t>(std::min(a.rows, kMostBlocks)), kThreads, 0,

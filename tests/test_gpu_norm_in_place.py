@@ -1,5 +1,5 @@
-"""The layer norm's backward pass where dx is the memory of dy: the sums over the rows are those of
-dy, whatever order dx is written in."""
+"""The layer norm's backward pass where dx is the memory of dy or of x: the sums over the rows are
+those of what was there, whatever order dx is written in."""
 import pytest
 import torch
 
@@ -9,7 +9,7 @@ from test_gpu_mixture import BF16, F16, F32, TYPES, close, randn
 pytestmark = pytest.mark.gpu
 
 
-def check_in_place(dtype, rows, dim, pad, wanted):
+def check_in_place(dtype, rows, dim, pad, wanted, over="dy"):
     from paper_1503_08294_amd import gsn, mixture
     x = randn(rows, dim, seed=1, dtype=dtype, scale=2.0) + 0.5
     w = 1 + 0.2 * randn(dim, seed=2)
@@ -18,12 +18,13 @@ def check_in_place(dtype, rows, dim, pad, wanted):
     _, want, dw, db = ref.layer_norm(x, w, None, 1e-5, dy)
     wide = torch.full((rows, dim + pad), 7.0, dtype=dtype, device="cuda")
     both = wide[:, :dim]
-    both.copy_(dy)
+    both.copy_(dy if over == "dy" else x)
     dweight, dbias = (torch.empty(dim, device="cuda") if n in wanted else None
                       for n in ("dweight", "dbias"))
     ws = torch.empty(gsn.gsn_layer_norm_workspace_bytes(rows, dim), dtype=torch.uint8,
                      device="cuda")
-    gsn.gsn_layer_norm_backward(both, x.cuda(), w.cuda(), stats, both, dweight, dbias, ws)
+    a = (both, x.cuda()) if over == "dy" else (dy.cuda(), both)
+    gsn.gsn_layer_norm_backward(*a, w.cuda(), stats, both, dweight, dbias, ws)
     # one rounding of dx; binary32 sums of D terms, D / 64 at a time by a lane and joined in a few
     # steps, in the mean, in r and in the two means of the gradient; over the rows, sums of as many
     # terms.  An error of f mean|x| in the mean shifts every n by r times that.
@@ -58,3 +59,10 @@ def test_dx_over_dy(dtype, rows, dim):
 @pytest.mark.parametrize("wanted", [("dweight",), ("dbias",), ()])
 def test_dx_over_dy_in_rows_of_a_wider_tensor(dtype, rows, dim, wanted):
     check_in_place(dtype, rows, dim, 9, wanted)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,dim,pad", [(1, 64, 0), (27, 704, 0), (512, 2048, 0), (513, 300, 0),
+                                          (27, 704, 9), (3, 20_003, 0), (300, 9000, 9)])
+def test_dx_over_x(dtype, rows, dim, pad):
+    check_in_place(dtype, rows, dim, pad, ("dweight", "dbias"), over="x")
