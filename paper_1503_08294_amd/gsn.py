@@ -491,20 +491,16 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _on(t: torch.Tensor, stream) -> int | ctypes.c_void_p:
-    """The stream's handle; without one, torch's current stream of t's device."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(t.device.index)
-    return _stream(stream)
-
-
 def _run(f, t: torch.Tensor, stream, *args) -> int:
-    """f(*args, stream's handle) with t's device as the current one, where the kernels go to."""
+    """f(*args, stream's handle; without one, of the current stream of t's device) with t's device
+    as the current one, where the kernels go to."""
     device = t.get_device()
-    if device == _current_device():
-        return _check(f(*args, _on(t, stream)), f.__name__)
-    with torch.cuda.device(device):
-        return _check(f(*args, _on(t, stream)), f.__name__)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return _run(f, t, stream, *args)
+    if stream is None and _raw_stream is not None:
+        return _check(f(*args, _raw_stream(device)), f.__name__)
+    return _check(f(*args, _stream(stream)), f.__name__)
 
 
 def _params_type(x_dtype, weight, bias) -> torch.dtype:
