@@ -517,8 +517,9 @@ int gsn_route_balance(int32_t experts, const int32_t* counts, float rate, float*
  * w2 [experts][dim][hidden] and out [tokens][dim] are of type dtype; silu(gate) * up is rounded
  * to dtype between the two products, the sum over k is in binary32.  In GSN_F16 that rounding has
  * the type's range too: a token with |silu(gate) * up| of 65,520 or more has a result that is not
- * finite.  tokens up to 2^23, tokens * top up to 2^26, experts 1 to 1024, top 1 to 64, dim and
- * hidden 1 to 2^20. */
+ * finite.  tokens up to 2^23, tokens * top up to 2^26 (beyond 2^21 better in several calls: the
+ * order of the pairs takes a time that grows with their square), experts 1 to 1024, top 1 to 64,
+ * dim and hidden 1 to 2^20. */
 typedef struct gsn_experts_params {
   int32_t dtype;
   int32_t experts, top, dim, hidden;

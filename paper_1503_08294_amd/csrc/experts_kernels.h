@@ -880,8 +880,9 @@ __device__ __forceinline__ void finish_rows(const Experts& x,
 // start (list, tokens, first stages) and 12 for its results, which nothing hides, as LDS holds one
 // workgroup a CU; the gates' gradients, with 0.9 MB a tile to read and write, some 40.
 // 16,384 tokens, 2 of 32 experts, 2,048 x 2,048, bfloat16 (a large library product reaches 1.28
-// PFLOP/s): first product 592 us (0.93 PFLOP/s), second 296 (0.93), gates' gradients
-// 442 (0.62), the other three together 1,600 (0.86).
+// PFLOP/s): first product 564 us (0.97 PFLOP/s), second 282 (0.97), gates' gradients
+// 424 (0.65), the other three together 1,500 (0.92); the matrix cores are busy 47, 46, 29 and 42%
+// of the cycles.
 constexpr int kLargeThreads = 512;
 constexpr int kLargeLds = 5 * kTileRows * kRowBytes;
 template <typename T, Kind KIND>

@@ -9,9 +9,13 @@
 // results are rounded to their type once.
 //
 // Both passes are bound by memory (a large copy runs at 4.75 TB/s): 16,384 x 4,096 bfloat16
-// forward in 63 us (4.2 TB/s); 16,384 x 2,048 backward in 39 us (5.2 TB/s: some of it is still in
+// forward in 63 us (4.2 TB/s); 16,384 x 2,048 backward in 38 us (5.3 TB/s: some of it is still in
 // the last cache) and 7 us for the join of the columns' sums; 8,191 x 1,001 binary32, whose rows
-// start at no multiple of 16 bytes, 16 us forward, 22 + 5 us backward.
+// start at no multiple of 16 bytes, 15 us forward, 22 + 5 us backward.  Rows that a workgroup's
+// registers do not hold are read again, an element at a time: forward beyond 8,192 elements,
+// backward beyond 4,096 of binary32 and 8,192 of 2-byte types.  4,096 rows of binary32, us forward
+// and backward: of 4,096 24 and 40, of 5,120 42 and 95, of 8,192 48 and 178, of 10,240 138 and 238;
+// of bfloat16: of 8,192 41 and 49, of 16,384 192 and 278.
 #include "mixture.h"
 
 #include <algorithm>

@@ -44,8 +44,8 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// 1 / (1 + exp(-v)).  __expf multiplies by log2 e in binary32 before it takes the power of two, so its
-// relative error grows with its argument, to some (|v| + 3) 2^-24; where the exponential is the
+// 1 / (1 + exp(-v)).  __expf multiplies by log2 e in binary32 before it takes the power of two, so
+// its relative error grows with its argument, to some (|v| + 3) 2^-24; where the exponential is the
 // smaller term of the sum (v > 0) little of that is left.  exp(-v) past the largest float gives
 // 1 / inf = 0, as it should.
 __device__ __forceinline__ float sigmoid(float v) {

@@ -10,7 +10,8 @@ gradients raise ``RuntimeError``, and tensors that carry a forward-mode tangent 
 ``_forward`` and ``_backward`` calls are their two halves for programs that keep their own order.
 
 Tensors are on one HIP device; work goes to torch's current stream of that device, where the
-outputs and workspaces are allocated too.  Arguments that do not fit raise ``ValueError``.
+outputs and workspaces are allocated too.  Tensors that do not fit raise ``ValueError``, sizes and
+options out of the kernels' range ``gsn.GsnError``.
 """
 from __future__ import annotations
 
