@@ -551,6 +551,106 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
                          void* dw1, void* dw2, void* workspace, size_t workspace_bytes,
                          void* stream);
 
+/* ------------------------------------------- models over the units: training, serving --
+ *
+ * A model that answers with a unit (the winner of a signal, say) has the units as its classes;
+ * these calls are its loss, the updates of its matrices, and its products in 8 bits.  They keep
+ * the rules of the mixture's calls above: no handle, async, may be captured, allocate nothing,
+ * the same bits on every run, sums in binary32 (products of 8 bits: in 32-bit integers), a
+ * result rounded once to nearest even.  Workspaces are 256-byte aligned; two calls that may run
+ * at a time need one each. */
+
+/* Softmax cross entropy of every token, the logits never kept as a whole:
+ *     l[c] = x[t] . w[c],  loss[t] = log(sum over the valid classes of exp(l[c])) - l[targets[t]]
+ * x [tokens][dim], w [classes][dim] of type dtype with row strides; targets int32 [tokens];
+ * valid: uint8 [classes] or NULL, 0 for a class that is not there: it is in no sum and its row of
+ * w means nothing.  A token whose target is out of range or not valid has none: its loss is 0
+ * and its x means nothing.  tokens 0 to 2^24, dim 1 to 2^16, classes 1 to 2^28.
+ * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128. */
+typedef struct gsn_entropy_params {
+  int32_t dtype;
+  int32_t dim, classes;
+  int64_t tokens;
+} gsn_entropy_params;
+
+/* Device bytes of a call's workspace (backward: 0 or 1); 0 if the parameters are invalid. */
+size_t gsn_cross_entropy_workspace_bytes(const gsn_entropy_params* params, int32_t backward);
+
+/* loss: float [tokens].  stats (float [2][tokens], or NULL) receives the largest logit and the sum
+ * of exp(l - largest) of every token, which the backward pass takes. */
+int gsn_cross_entropy(const gsn_entropy_params* params, const void* x, int64_t x_stride,
+                      const void* w, int64_t w_stride, const int32_t* targets,
+                      const uint8_t* valid, float* loss, float* stats, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* Gradients from dloss float [tokens]: dx [tokens][dim] and dw [classes][dim] of type dtype,
+ * every element written, 0 for tokens without a target and classes that are not valid; each may
+ * be NULL (not computed).  The logits' gradients dloss (exp(l) / sum - [c = target]) are rounded
+ * to dtype before they are multiplied with w and x; in GSN_F16 as multiples of the largest
+ * |dloss|, so that a small dloss loses no digits there. */
+int gsn_cross_entropy_backward(const gsn_entropy_params* params, const float* dloss,
+                               const void* x, int64_t x_stride, const void* w, int64_t w_stride,
+                               const int32_t* targets, const uint8_t* valid, const float* stats,
+                               void* dx, void* dw, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/* Orthogonalised matrices: with X = x / (norm(x) + eps), norm the root of the sum of squares, and
+ * `steps` times
+ *     A = X X^T,  X <- a X + (b A + c A A) X
+ * (X^T in place of X where a matrix has more rows than columns).  x: [batch][rows][cols] of type
+ * dtype, contiguous.  A, b A + c A A and X are kept between the products as one or two float16
+ * values, a rounding to 11 or 22 bits: one for an update of weights of 2 bytes, two otherwise.
+ * batch 0 to 2^20, rows and cols 1 to 2^15, steps 1 to 64, eps >= 0.  Coefficients that let a
+ * singular value that starts at 1 or less grow past 5, or a + b s^2 + c s^4 past 28 for a value s
+ * on its way, are refused (GSN_E_INVAL).  A matrix of zeros stays one (eps = 0 too); one that holds
+ * a NaN or an infinity becomes NaN. */
+typedef struct gsn_orthogonal_params {
+  int32_t dtype;
+  int32_t rows, cols;
+  int32_t steps;
+  int64_t batch;
+  float a, b, c, eps;
+} gsn_orthogonal_params;
+
+/* update: 0 for gsn_orthogonalise, 1 for gsn_orthogonal_step. */
+size_t gsn_orthogonal_workspace_bytes(const gsn_orthogonal_params* params, int32_t update);
+
+/* out may be the memory of x. */
+int gsn_orthogonalise(const gsn_orthogonal_params* params, const void* x, void* out,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* One update of weights [batch][rows][cols] of type dtype:
+ *     new_momentum = beta momentum + gradient
+ *     u = gradient + beta new_momentum (nesterov != 0) or new_momentum
+ *     new_weights = (1 - decay) weights - rate orthogonal(u)
+ * gradient of type dtype, momentum float.  new_weights may be the memory of weights, new_momentum
+ * that of momentum. */
+int gsn_orthogonal_step(const gsn_orthogonal_params* params, const void* weights,
+                        const void* gradient, const float* momentum, float rate, float beta,
+                        float decay, int32_t nesterov, void* new_weights, float* new_momentum,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* 8-bit integers of the rows of x [rows][dim] of type dtype, with a row stride:
+ *     scales[r] = max(max |x[r]| / 127, 2^-126),  q[r][k] = x[r][k] / scales[r] to the nearest
+ * integer, ties to even.  q: int8 [rows][dim] with a row stride; scales: float [rows].  A row
+ * that holds a NaN or an infinity has a NaN as its scale and zeros.  rows >= 0, dim 1 to 2^27. */
+int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_t x_stride,
+                 int8_t* q, int64_t q_stride, float* scales, void* stream);
+
+/* y[t][n] = (sum over k of q[t][k] w[n][k]) scale[t] scales[n], with q and scale those of
+ * gsn_quantise of x.  x [tokens][dim] and y [tokens][out] of type dtype; w int8 [out][dim], scales
+ * float [out]; row strides.  The sum is exact.  tokens 0 to 2^24, dim 1 to 2^17 - 1, out 1 to
+ * 2^28.  GSN_E_CAPACITY if the product has more than some 2^23 tiles of 128 x 128. */
+typedef struct gsn_linear_params {
+  int32_t dtype;
+  int32_t dim, out;
+  int64_t tokens;
+} gsn_linear_params;
+size_t gsn_linear_quantised_workspace_bytes(const gsn_linear_params* params);
+int gsn_linear_quantised(const gsn_linear_params* params, const void* x, int64_t x_stride,
+                const int8_t* w, int64_t w_stride, const float* scales, void* y,
+                int64_t y_stride, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

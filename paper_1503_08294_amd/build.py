@@ -23,7 +23,9 @@ SOURCES = ["gsn_host.hip", "find_winners.hip", "staging.hip", "find_screened.hip
            "find_mfma.hip", "find_f16.hip", "update.hip", "update_winner.hip", "grow.hip",
            "schedule.hip", "find_grid.hip", "resolve_greedy.hip", "find_small.hip",
            "find_pruned.hip", "export.hip", "layer_norm.hip", "route.hip", "experts.hip",
-           "experts_bf16.hip", "experts_f16.hip", "experts_f32.hip"]
+           "experts_bf16.hip", "experts_f16.hip", "experts_f32.hip", "entropy.hip",
+           "entropy_bf16.hip", "entropy_f16.hip", "entropy_f32.hip", "orthogonal.hip",
+           "linear8.hip"]
 ARCH = "gfx950"
 
 FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",

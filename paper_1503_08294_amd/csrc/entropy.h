@@ -1,0 +1,44 @@
+// Softmax cross entropy over many classes: what the host passes to the kernels of one type.
+#pragma once
+
+#include "mixture.h"
+
+namespace gsn {
+
+struct Entropy {
+  int64_t tokens;
+  int32_t classes, dim;
+  int32_t pitch;     // elements of a row of the copies of x and w
+  const void* x;
+  int64_t x_stride;
+  const void* w;
+  int64_t w_stride;
+  const int32_t* targets;
+  const uint8_t* valid;  // of the classes, or null
+  // pieces of the classes: of a forward and of a backward pass
+  int32_t piece, parts;  // classes of a piece; tiles of its columns, at most
+  bool copy_x, copy_w;
+  void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the ends
+  void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
+  // forward
+  float* loss;
+  float* stats;   // [2][tokens]: the largest logit, and the sum of exp(logit - largest)
+  float2* part;   // [parts][tokens] the same of every tile's columns
+  float* chosen;  // [tokens] logit of the target
+  // backward
+  const float* dloss;
+  float* factor;  // 2: what dloss is multiplied by where the logits' gradients are kept, and back
+  void* d;        // [tokens][piece] gradients of the logits
+  int32_t splits_x, splits_w;
+  float* dxp;     // [splits_x][tokens][pitch]
+  float* dwp;     // [splits_w][piece][pitch], where splits_w > 1
+  void* dx;
+  void* dw;
+};
+
+template <typename T>
+hipError_t launch_entropy(const Entropy& x, hipStream_t st);
+template <typename T>
+hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st);
+
+}  // namespace gsn

@@ -1,0 +1,412 @@
+// Kernels of the softmax cross entropy for one type of element, included by one source a type.
+//
+//   l(t, c) = x[t] . w[c] over the valid classes c,  loss = log sum exp(l) - l(target)
+//   d = dloss (exp(l) / sum exp(l) - [c = target]),  dx = d w,  dw = d^T x
+// The logits are not kept: a tile of them is reduced to its rows' largest value and sum of
+// exponentials, and the backward pass makes them again, a piece of the classes at a time, as d.
+#pragma once
+
+#include "entropy.h"
+#include "product.h"
+
+namespace gsn {
+namespace {
+
+// A token's target, -1 where there is none: out of range, or a class that is not valid.
+__device__ __forceinline__ int32_t target_of(const Entropy& x, int64_t t) {
+  const int32_t c = x.targets[t];
+  if (c < 0 || c >= x.classes) return -1;
+  return x.valid && !x.valid[c] ? -1 : c;
+}
+
+// e^v of a difference to the largest logit (or to the sum's logarithm).
+template <typename T>
+__device__ __forceinline__ float power(float v) {
+  // (__expf's error grows with -v, to some (|v| + 3) 2^-24: too much for results of 32 bits)
+  if constexpr (sizeof(T) == 4) return expf(v);
+  else return __expf(v);
+}
+
+// Of a lane's columns n + 16 j + q: bit 4 j + q for one that is no valid class.
+template <int NT>
+__device__ __forceinline__ uint32_t shut_columns(const uint8_t* valid, int32_t classes, int32_t n) {
+  uint32_t shut = 0;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int32_t c = n + 16 * j + q;
+      const bool out = c >= classes || (valid && !valid[c]);
+      shut |= out ? 1u << (4 * j + q) : 0u;
+    }
+  return shut;
+}
+
+// (largest, sum of exp(. - largest)) of two sets of logits.
+__device__ __forceinline__ float2 merged(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x);
+  const float base = m == -INFINITY ? 0.0f : m;
+  return float2{m, a.y * expf(a.x - base) + b.y * expf(b.x - base)};
+}
+
+// A tile of the logits -> (largest, sum) of each row, and the target's logit.
+template <typename T>
+struct Reduce {
+  Entropy x;
+  int32_t first;  // the piece's first class
+
+  template <int SIDE, int WN, int MT, int NT>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
+                                       int lane, char* smem) const {
+    const int li = lane & 15, lg = (lane >> 4) * 4;
+    float2* const rows = reinterpret_cast<float2*>(smem);  // [WN][SIDE]
+    const int32_t n = first + at.n0 + nw + lg;
+    const uint32_t shut = shut_columns<NT>(x.valid, x.classes, n);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t t = at.m0 + mw + 16 * i + li;
+      const int32_t target = t < x.tokens ? x.targets[t] : -1;
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float l = shut >> (4 * j + q) & 1 ? -INFINITY : acc[i][j][q];
+          acc[i][j][q] = l;
+          top = fmaxf(top, l);
+          if (n + 16 * j + q == target && l != -INFINITY) x.chosen[t] = l;
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += power<T>(acc[i][j][q] - base);
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (lane < 16) rows[nw / (SIDE / WN) * SIDE + mw + 16 * i + li] = float2{top, sum};
+    }
+    __syncthreads();
+    for (int m = threadIdx.x; m < SIDE; m += blockDim.x) {
+      const int64_t t = int64_t{at.m0} + m;
+      if (t >= x.tokens) break;
+      float2 v = rows[m];
+#pragma unroll
+      for (int w = 1; w < WN; ++w) v = merged(v, rows[w * SIDE + m]);
+      x.part[at.n0 / SIDE * x.tokens + t] = v;
+    }
+  }
+};
+
+// The parts of a piece, and of the pieces before it, joined; after the last piece the losses.
+constexpr int kJoinTokens = 64, kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinTokens* kJoinWaves) void ce_join(Entropy x, int32_t parts,
+                                                                  int32_t begin, int32_t last) {
+  __shared__ float2 some[kJoinWaves][kJoinTokens];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kJoinTokens + lane;
+  float2 v{-INFINITY, 0.0f};
+  if (t < x.tokens) {
+#pragma unroll 4
+    for (int32_t i = wave; i < parts; i += kJoinWaves) v = merged(v, x.part[i * x.tokens + t]);
+  }
+  some[wave][lane] = v;
+  __syncthreads();
+  if (wave > 0 || t >= x.tokens) return;
+  if (!begin) v = merged(float2{x.stats[t], x.stats[x.tokens + t]}, v);
+  for (int w = 1; w < kJoinWaves; ++w) v = merged(v, some[w][lane]);
+  const int32_t target = target_of(x, t);
+  if (last) {
+    // (the logarithm of the sum and the difference to the largest are each small: their difference
+    // keeps the digits that one to the logarithm of all would lose)
+    x.loss[t] = target < 0 ? 0.0f : logf(v.y) - (x.chosen[t] - v.x);
+    if (target < 0) v = float2{0.0f, 1.0f};
+  }
+  x.stats[t] = v.x;
+  x.stats[x.tokens + t] = v.y;
+}
+
+// A tile of the logits -> their gradients, rounded to the type of the operands of the two products
+// that take them.
+template <typename T>
+struct Gradient {
+  Entropy x;
+  int32_t first, count;  // the piece's classes
+
+  template <int SIDE, int WN, int MT, int NT>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
+                                       int lane, char*) const {
+    const int li = lane & 15, lg = (lane >> 4) * 4;
+    const int32_t n = at.n0 + nw + lg;
+    const uint32_t shut = shut_columns<NT>(x.valid, x.classes, first + n);
+    const float factor = sizeof(T) == 2 && __is_same(T, f16_t) ? x.factor[0] : 1.0f;
+    // (columns up to a multiple of 16 bytes are written, zeros past the last class)
+    const int32_t cols = (count + 7) / 8 * 8;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t t = at.m0 + mw + 16 * i + li;
+      if (t >= x.tokens) break;
+      const int32_t target = target_of(x, t) - first;
+      const bool live = target + first >= 0;
+      const float top = x.stats[t], each = 1.0f / x.stats[x.tokens + t];
+      const float g = x.dloss[t] * factor;
+      T* const row = static_cast<T*>(x.d) + t * x.piece;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float p = power<T>(acc[i][j][q] - top) * each;
+          const float d = (p - (n + 16 * j + q == target ? 1.0f : 0.0f)) * g;
+          v[q] = live && !(shut >> (4 * j + q) & 1) ? d : 0.0f;
+        }
+        store4(row, n + 16 * j, cols, v);
+      }
+    }
+  }
+};
+
+// A tile of sums of 32 bits in memory, added to what is there or not.
+struct Partial {
+  float* to;
+  int64_t split;  // elements from a split to the next
+  int32_t rows, pitch;
+  int32_t add;
+
+  template <int SIDE, int WN, int MT, int NT>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
+                                       int lane, char*) const {
+    const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
+      if (m >= rows) break;
+      float* const row = to + at.split * split + static_cast<int64_t>(m) * pitch;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (n + 16 * j >= pitch) break;
+        f32x4* const p = reinterpret_cast<f32x4*>(row + n + 16 * j);
+        *p = add ? acc[i][j] + *p : acc[i][j];
+      }
+    }
+  }
+};
+
+// A tile of dw, rounded to its type.
+template <typename T>
+struct Weights {
+  Entropy x;
+  int32_t first, count;
+
+  template <int SIDE, int WN, int MT, int NT>
+  __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
+                                       int lane, char*) const {
+    const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+    const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
+      if (m >= count) break;
+      const bool shut = x.valid && !x.valid[first + m];
+      T* const row = static_cast<T*>(x.dw) + static_cast<int64_t>(first + m) * x.dim;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = shut ? 0.0f : acc[i][j][q] * factor;
+        if (n + 16 * j < x.dim) store4(row, n + 16 * j, x.dim, v);
+      }
+    }
+  }
+};
+
+// The splits' sums, and their one rounding.  Rows without a target, or that are no valid class, are
+// zeros.
+template <typename T, bool OF_TOKENS>
+__global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict__ part,
+                                              int32_t splits, int64_t rows, int32_t first,
+                                              int64_t split, T* __restrict__ out) {
+  const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
+  const int32_t each = (x.dim + 3) / 4;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < rows * each;
+       at += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t r = at / each;
+    const int32_t d = static_cast<int32_t>(at - r * each) * 4;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    const bool live = OF_TOKENS ? target_of(x, r) >= 0 : !(x.valid && !x.valid[first + r]);
+    if (live)
+      for (int32_t i = 0; i < splits; ++i)
+        s += *reinterpret_cast<const f32x4*>(part + i * split + r * x.pitch + d);
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = s[q] * factor;
+    store4(out + (first + r) * x.dim, d, x.dim, v);
+  }
+}
+
+// Rows of x (OF_TOKENS) or of w from `first` on, in rows of `pitch`, with zeros at their ends.
+// DEAD: rows of zeros where a token has no target or a class is not valid.
+template <typename T, bool OF_TOKENS, bool DEAD>
+__global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t first,
+                                               T* __restrict__ out) {
+  constexpr int kE = 16 / sizeof(T);
+  const T* const from = static_cast<const T*>(OF_TOKENS ? x.x : x.w);
+  const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
+  const int32_t each = x.pitch / kE;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < rows * each;
+       at += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t r = at / each;
+    const int32_t k = static_cast<int32_t>(at - r * each) * kE;
+    const bool live =
+        !DEAD || (OF_TOKENS ? target_of(x, r) >= 0 : !(x.valid && !x.valid[first + r]));
+    Frag f;
+    f.u = u32x4{0, 0, 0, 0};
+    if (live) f = row_chunk<false>(from + (first + r) * stride, k, x.dim);
+    *reinterpret_cast<u32x4*>(out + r * x.pitch + k) = f.u;
+  }
+}
+
+// Gradients of the logits in float16 are kept times 2^11 / max |dloss|: at most 2^11, and those of
+// small probabilities are not lost (2^-25 of the largest dloss still has all of its 11 bits).
+__global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
+  __shared__ float some[16];
+  float m = 0.0f;
+  for (int64_t t = threadIdx.x; t < x.tokens; t += 1024) {
+    if (target_of(x, t) < 0) continue;
+    const float v = fabsf(x.dloss[t]);
+    m = v > m || v != v ? v : m;  // (NaN stays)
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float v = __shfl_xor(m, o);
+    m = v > m || v != v ? v : m;
+  }
+  if (threadIdx.x % kWave == 0) some[threadIdx.x / kWave] = m;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  for (int w = 1; w < 16; ++w) m = some[w] > m || some[w] != some[w] ? some[w] : m;
+  const float base = m < 0x1p-100f ? 0x1p-100f : m;
+  x.factor[0] = 2048.0f / base;
+  x.factor[1] = base / 2048.0f;
+}
+
+inline uint32_t some_blocks(int64_t threads) {
+  const int64_t n = (threads + 255) / 256;
+  return static_cast<uint32_t>(n < 1 ? 1 : n < (1 << 16) ? n : 1 << 16);
+}
+
+template <typename T>
+Operand operand_of(const void* p, int64_t ld, int64_t rows) {
+  constexpr int64_t kSize = sizeof(T);
+  return Operand{static_cast<const char*>(p), {0, 0}, ld * kSize, 0, static_cast<int32_t>(rows)};
+}
+
+// A product's parts of k: `splits` of them, whole stages.
+template <typename T>
+void split(Product* p, int32_t splits) {
+  constexpr int32_t kBK = kRowBytes / sizeof(T);
+  p->splits = splits;
+  p->part = ((p->k + splits - 1) / splits + kBK - 1) / kBK * kBK;
+}
+
+template <typename T, bool TRA, bool TRB, class EPI>
+void entropy_product(const Product& p, const EPI& epi, hipStream_t st) {
+  // (tiles of 128 from one a CU on)
+  if (int64_t{tiles_of(p.a.rows, kMiddleRows)} * tiles_of(p.b.rows, kMiddleRows) * p.splits >= 256)
+    run_product<T, TRA, TRB, kMiddleRows>(p, epi, st);
+  else
+    run_product<T, TRA, TRB, kSmallRows>(p, epi, st);
+}
+
+// x or its copy, w from class `first` on or its copy.
+template <typename T>
+Product logits_of(const Entropy& x, int32_t first, int32_t count) {
+  Product p{};
+  p.a = x.copy_x ? operand_of<T>(x.xc, x.pitch, x.tokens)
+                 : operand_of<T>(x.x, x.x_stride, x.tokens);
+  p.b = x.copy_w ? operand_of<T>(x.wc, x.pitch, count)
+                 : operand_of<T>(static_cast<const T*>(x.w) + first * x.w_stride, x.w_stride,
+                                 count);
+  p.terms = p.batch = 1;
+  p.k = x.dim;
+  split<T>(&p, 1);
+  return p;
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
+  const int64_t row = x.pitch / (16 / sizeof(T));
+  if (x.copy_x)
+    ce_rows<T, true, false><<<some_blocks(x.tokens * row), 256, 0, st>>>(
+        x, x.tokens, 0, static_cast<T*>(x.xc));
+  for (int32_t first = 0; first < x.classes; first += x.piece) {
+    const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
+    if (x.copy_w)
+      ce_rows<T, false, false><<<some_blocks(count * row), 256, 0, st>>>(
+          x, count, first, static_cast<T*>(x.wc));
+    const Product p = logits_of<T>(x, first, count);
+    const int32_t side =
+        int64_t{tiles_of(x.tokens, kMiddleRows)} * tiles_of(count, kMiddleRows) >= 256
+            ? kMiddleRows
+            : kSmallRows;
+    entropy_product<T, false, false>(p, Reduce<T>{x, first}, st);
+    ce_join<<<static_cast<uint32_t>((x.tokens + kJoinTokens - 1) / kJoinTokens),
+              kJoinTokens * kJoinWaves, 0, st>>>(x, tiles_of(count, side), first == 0,
+                                                 first + count == x.classes);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st) {
+  const int64_t row = x.pitch / (16 / sizeof(T));
+  if (__is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
+  ce_rows<T, true, true><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
+                                                                      static_cast<T*>(x.xc));
+  for (int32_t first = 0; first < x.classes; first += x.piece) {
+    const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
+    if (x.copy_w)
+      ce_rows<T, false, true><<<some_blocks(count * row), 256, 0, st>>>(
+          x, count, first, static_cast<T*>(x.wc));
+    const Product l = logits_of<T>(x, first, count);
+    entropy_product<T, false, false>(l, Gradient<T>{x, first, count}, st);
+    Operand d = operand_of<T>(x.d, x.piece, x.tokens);
+    if (x.dx) {
+      Product p = l;
+      p.a = d;
+      p.b.rows = x.dim;
+      p.k = count;
+      split<T>(&p, x.splits_x);
+      const int64_t each = x.tokens * x.pitch;
+      entropy_product<T, false, true>(
+          p, Partial{x.dxp, each, static_cast<int32_t>(x.tokens), x.pitch, first > 0}, st);
+    }
+    if (x.dw) {
+      Product p{};
+      p.a = d;
+      p.a.rows = count;
+      p.b = operand_of<T>(x.xc, x.pitch, x.dim);
+      p.terms = p.batch = 1;
+      p.k = static_cast<int32_t>(x.tokens);
+      split<T>(&p, x.splits_w);
+      if (x.splits_w > 1) {
+        const int64_t each = int64_t{x.piece} * x.pitch;
+        entropy_product<T, true, true>(p, Partial{x.dwp, each, count, x.pitch, 0}, st);
+        ce_sum<T, false><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
+            x, x.dwp, x.splits_w, count, first, each, static_cast<T*>(x.dw));
+      } else {
+        entropy_product<T, true, true>(p, Weights<T>{x, first, count}, st);
+      }
+    }
+  }
+  if (x.dx)
+    ce_sum<T, true><<<some_blocks(x.tokens * ((x.dim + 3) / 4)), 256, 0, st>>>(
+        x, x.dxp, x.splits_x, x.tokens, 0, x.tokens * x.pitch, static_cast<T*>(x.dx));
+  return hipGetLastError();
+}
+
+}  // namespace gsn

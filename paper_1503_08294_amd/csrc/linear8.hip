@@ -1,0 +1,228 @@
+// Products of 8-bit integers: rows quantised to 8 bits, multiplied with weights of 8 bits in sums
+// of 32-bit integers, which are exact.
+#include <algorithm>
+
+#include "product.h"
+
+namespace gsn {
+namespace {
+
+struct Linear8 {
+  int64_t tokens;
+  int32_t dim, out, pitch;  // pitch: bytes of a row of q and of the copy of w
+  const void* x;
+  int64_t x_stride;
+  const int8_t* w;
+  int64_t w_stride;
+  const float* scales;
+  void* y;
+  int64_t y_stride;
+  int8_t* q;        // [tokens][pitch], zeros at the rows' ends
+  float* x_scales;  // [tokens]
+  int8_t* wc;       // [out][pitch] w, where its rows are not at multiples of 16 bytes
+};
+
+// v / s to the nearest integer, ties to even, as of the exact quotient: the product with 1 / s may
+// be one off beside a border, and the fma's sign tells on which side of it v is, or that it is on
+// it.  |v / s| <= 127 but for rounding.
+__device__ __forceinline__ int quantised(float v, float s, float inverse) {
+  float q = rintf(v * inverse);
+  const float above = fmaf(-(q + 0.5f), s, v);  // > 0: v / s > q + 0.5
+  const float below = fmaf(-(q - 0.5f), s, v);  // < 0: v / s < q - 0.5
+  const bool odd = (static_cast<int>(q) & 1) != 0;
+  if (above > 0.0f || (above == 0.0f && odd)) q += 1.0f;
+  else if (below < 0.0f || (below == 0.0f && odd)) q -= 1.0f;
+  return static_cast<int>(fminf(fmaxf(q, -127.0f), 127.0f));
+}
+
+// Rows in 8 bits, a workgroup a row: the largest value, then the quotients.  `pitch` bytes of q are
+// written, zeros past the end.  Bound by memory.
+template <typename T>
+__global__ __launch_bounds__(256) void q8_rows(const T* __restrict__ x, int64_t stride,
+                                               int64_t rows, int32_t dim, int8_t* __restrict__ q,
+                                               int64_t q_stride, int32_t pitch,
+                                               float* __restrict__ scales) {
+  __shared__ float some[4];
+  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    const T* const row = x + r * stride;
+    float top = 0.0f;
+    for (int32_t k = threadIdx.x; k < dim; k += 256) {
+      const float v = fabsf(to_float(row[k]));
+      top = v > top || v != v ? v : top;  // (NaN stays)
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float v = __shfl_xor(top, o);
+      top = v > top || v != v ? v : top;
+    }
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) some[threadIdx.x / kWave] = top;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) top = some[w] > top || some[w] != some[w] ? some[w] : top;
+    const bool bad = !(top < INFINITY);
+    const float s = top / 127.0f > 0x1p-126f ? top / 127.0f : 0x1p-126f, inverse = 1.0f / s;
+    for (int32_t k = threadIdx.x; k < pitch; k += 256)
+      q[r * q_stride + k] =
+          k < dim && !bad ? static_cast<int8_t>(quantised(to_float(row[k]), s, inverse)) : 0;
+    if (threadIdx.x == 0) scales[r] = bad ? NAN : s;
+  }
+}
+
+// w in rows of `pitch` bytes.
+__global__ __launch_bounds__(256) void q8_copy(Linear8 x) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+       i < static_cast<int64_t>(x.out) * x.pitch; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t r = i / x.pitch;
+    const int32_t k = static_cast<int32_t>(i - r * x.pitch);
+    x.wc[i] = k < x.dim ? x.w[r * x.w_stride + k] : 0;
+  }
+}
+
+template <typename T>
+struct Scaled {
+  Linear8 x;
+
+  template <int SIDE, int WN, int MT, int NT>
+  __device__ __forceinline__ void tile(i32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
+                                       int lane, char*) const {
+    const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t t = at.m0 + mw + 16 * i + (lane & 15);
+      if (t >= x.tokens) break;
+      const float s = x.x_scales[t];
+      T* const row = static_cast<T*>(x.y) + t * x.y_stride;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (n + 16 * j >= x.out) break;
+        float v[4];
+        load4(x.scales, n + 16 * j, x.out, v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = static_cast<float>(acc[i][j][q]) * s * v[q];
+        store4(row, n + 16 * j, x.out, v);
+      }
+    }
+  }
+};
+
+uint32_t row_blocks(int64_t rows) {
+  return static_cast<uint32_t>(std::min<int64_t>(rows, 1 << 16));
+}
+
+template <typename T>
+hipError_t launch(const Linear8& x, hipStream_t st) {
+  q8_rows<T><<<row_blocks(x.tokens), 256, 0, st>>>(static_cast<const T*>(x.x), x.x_stride,
+                                                   x.tokens, x.dim, x.q, x.pitch, x.pitch,
+                                                   x.x_scales);
+  const bool copy = !aligned16(x.w) || x.w_stride % 16 != 0 || x.dim % 16 != 0;
+  if (copy) {
+    const int64_t n = (static_cast<int64_t>(x.out) * x.pitch + 255) / 256;
+    q8_copy<<<static_cast<uint32_t>(std::min<int64_t>(n, 1 << 16)), 256, 0, st>>>(x);
+  }
+  Product p{};
+  p.a = Operand{reinterpret_cast<const char*>(x.q), {0, 0}, x.pitch, 0,
+                static_cast<int32_t>(x.tokens)};
+  p.b = Operand{reinterpret_cast<const char*>(copy ? x.wc : x.w), {0, 0},
+                copy ? x.pitch : x.w_stride, 0, x.out};
+  p.terms = p.batch = p.splits = 1;
+  p.k = p.part = x.dim;
+  // (tiles of 128 from one a CU on)
+  if (int64_t{tiles_of(x.tokens, kMiddleRows)} * tiles_of(x.out, kMiddleRows) >= 256)
+    run_product<int8_t, false, false, kMiddleRows>(p, Scaled<T>{x}, st);
+  else
+    run_product<int8_t, false, false, kSmallRows>(p, Scaled<T>{x}, st);
+  return hipGetLastError();
+}
+
+bool params_ok(const gsn_linear_params* p) {
+  // (a sum of 2^17 - 1 products of -128 and -128 is the last below 2^31)
+  return p && p->dtype >= GSN_F32 && p->dtype <= GSN_F16 && p->tokens >= 0 &&
+         p->tokens <= (1 << 24) && p->dim >= 1 && p->dim < (1 << 17) && p->out >= 1 &&
+         p->out <= (1 << 28);
+}
+
+Linear8 linear8_of(const gsn_linear_params& p) {
+  Linear8 x{};
+  x.tokens = p.tokens;
+  x.dim = p.dim;
+  x.out = p.out;
+  x.pitch = (p.dim + 15) / 16 * 16;
+  return x;
+}
+
+size_t carve(void* base, Linear8* x) {
+  size_t used = 0;
+  const auto take = [&](size_t n) {
+    char* const p = base ? static_cast<char*>(base) + used : nullptr;
+    used += (n + 255) / 256 * 256;
+    return static_cast<void*>(p);
+  };
+  const size_t pitch = static_cast<size_t>(x->pitch);
+  x->q = static_cast<int8_t*>(take(static_cast<size_t>(x->tokens) * pitch));
+  x->x_scales = static_cast<float*>(take(4 * static_cast<size_t>(x->tokens)));
+  x->wc = static_cast<int8_t*>(take(static_cast<size_t>(x->out) * pitch));
+  return used;
+}
+
+}  // namespace
+}  // namespace gsn
+
+extern "C" {
+
+int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_t x_stride,
+                 int8_t* q, int64_t q_stride, float* scales, void* stream) {
+  if (dtype < GSN_F32 || dtype > GSN_F16 || rows < 0 || dim < 1 || dim > (1 << 27))
+    return GSN_E_INVAL;
+  if (rows == 0) return GSN_OK;
+  if (!x || !q || !scales || x_stride < dim || q_stride < dim) return GSN_E_INVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const uint32_t blocks = gsn::row_blocks(rows);
+  if (dtype == GSN_F32)
+    gsn::q8_rows<float><<<blocks, 256, 0, st>>>(static_cast<const float*>(x), x_stride, rows, dim,
+                                                q, q_stride, dim, scales);
+  else if (dtype == GSN_BF16)
+    gsn::q8_rows<gsn::bf16_t><<<blocks, 256, 0, st>>>(static_cast<const gsn::bf16_t*>(x),
+                                                      x_stride, rows, dim, q, q_stride, dim,
+                                                      scales);
+  else
+    gsn::q8_rows<gsn::f16_t><<<blocks, 256, 0, st>>>(static_cast<const gsn::f16_t*>(x), x_stride,
+                                                     rows, dim, q, q_stride, dim, scales);
+  return hipGetLastError() == hipSuccess ? GSN_OK : GSN_E_HIP;
+}
+
+size_t gsn_linear_quantised_workspace_bytes(const gsn_linear_params* p) {
+  if (!gsn::params_ok(p)) return 0;
+  gsn::Linear8 x = gsn::linear8_of(*p);
+  return gsn::carve(nullptr, &x) + 256;
+}
+
+int gsn_linear_quantised(const gsn_linear_params* p, const void* x, int64_t x_stride,
+                         const int8_t* w, int64_t w_stride, const float* scales, void* y,
+                         int64_t y_stride, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (!gsn::params_ok(p)) return GSN_E_INVAL;
+  if (p->tokens == 0) return GSN_OK;
+  if (!x || !w || !scales || !y || x_stride < p->dim || w_stride < p->dim || y_stride < p->out ||
+      !workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+    return GSN_E_INVAL;
+  if (workspace_bytes < gsn_linear_quantised_workspace_bytes(p)) return GSN_E_CAPACITY;
+  if (int64_t{gsn::tiles_of(p->tokens, gsn::kMiddleRows)} *
+          gsn::tiles_of(p->out, gsn::kMiddleRows) >= (1 << 23))
+    return GSN_E_CAPACITY;
+  gsn::Linear8 a = gsn::linear8_of(*p);
+  a.x = x;
+  a.x_stride = x_stride;
+  a.w = w;
+  a.w_stride = w_stride;
+  a.scales = scales;
+  a.y = y;
+  a.y_stride = y_stride;
+  gsn::carve(workspace, &a);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const hipError_t e = p->dtype == GSN_F32    ? gsn::launch<float>(a, st)
+                       : p->dtype == GSN_BF16 ? gsn::launch<gsn::bf16_t>(a, st)
+                                              : gsn::launch<gsn::f16_t>(a, st);
+  return e == hipSuccess ? GSN_OK : GSN_E_HIP;
+}
+
+}  // extern "C"

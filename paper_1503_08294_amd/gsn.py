@@ -150,6 +150,38 @@ class gsn_experts_params(ctypes.Structure):
     ]
 
 
+class gsn_entropy_params(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("classes", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+    ]
+
+
+class gsn_orthogonal_params(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("rows", ctypes.c_int32),
+        ("cols", ctypes.c_int32),
+        ("steps", ctypes.c_int32),
+        ("batch", ctypes.c_int64),
+        ("a", ctypes.c_float),
+        ("b", ctypes.c_float),
+        ("c", ctypes.c_float),
+        ("eps", ctypes.c_float),
+    ]
+
+
+class gsn_linear_params(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("out", ctypes.c_int32),
+        ("tokens", ctypes.c_int64),
+    ]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _L = ctypes.c_int64
@@ -201,6 +233,21 @@ _sig = {
                                    _P, _P, _Z, _P, _Z, _P]),
     "gsn_experts_backward": (ctypes.c_int, [ctypes.POINTER(gsn_experts_params), _P, _P, _L, _P,
                                             _P, _P, _P, _Z, _P, _P, _P, _P, _P, _Z, _P]),
+    "gsn_cross_entropy_workspace_bytes": (_Z, [ctypes.POINTER(gsn_entropy_params), _I]),
+    "gsn_cross_entropy": (ctypes.c_int, [ctypes.POINTER(gsn_entropy_params), _P, _L, _P, _L, _P,
+                                         _P, _P, _P, _P, _Z, _P]),
+    "gsn_cross_entropy_backward": (ctypes.c_int, [ctypes.POINTER(gsn_entropy_params), _P, _P, _L,
+                                                  _P, _L, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "gsn_orthogonal_workspace_bytes": (_Z, [ctypes.POINTER(gsn_orthogonal_params), _I]),
+    "gsn_orthogonalise": (ctypes.c_int, [ctypes.POINTER(gsn_orthogonal_params), _P, _P, _P, _Z,
+                                         _P]),
+    "gsn_orthogonal_step": (ctypes.c_int, [ctypes.POINTER(gsn_orthogonal_params), _P, _P, _P,
+                                           ctypes.c_float, ctypes.c_float, ctypes.c_float, _I, _P,
+                                           _P, _P, _Z, _P]),
+    "gsn_quantise": (ctypes.c_int, [_I, _L, _I, _P, _L, _P, _L, _P, _P]),
+    "gsn_linear_quantised_workspace_bytes": (_Z, [ctypes.POINTER(gsn_linear_params)]),
+    "gsn_linear_quantised": (ctypes.c_int, [ctypes.POINTER(gsn_linear_params), _P, _L, _P, _L, _P,
+                                            _P, _L, _P, _Z, _P]),
 }
 for _name, (_res, _args) in _sig.items():
     _f = getattr(_lib, _name)
@@ -634,6 +681,119 @@ def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, s
         _flat(dweights, torch.float32, pairs, "dweights"), _flat(dw1, x.dtype, s1, "dw1"),
         _flat(dw2, x.dtype, s2, "dw2"), _dev(workspace, torch.uint8, what="workspace"),
         workspace.numel())
+
+
+# ------------------------------ C-named calls: training and serving over the units ----
+# (paper_1503_08294_amd.learning holds the calls on torch tensors that allocate their outputs.)
+
+def make_entropy(x, w) -> gsn_entropy_params:
+    """Parameters of the cross entropy of these tensors."""
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be 2-dimensional")
+    return gsn_entropy_params(_type(x, "x"), x.shape[1], w.shape[0], x.shape[0])
+
+
+def gsn_cross_entropy_workspace_bytes(params: gsn_entropy_params, backward: bool) -> int:
+    return int(_lib.gsn_cross_entropy_workspace_bytes(params, 1 if backward else 0))
+
+
+def gsn_cross_entropy(params: gsn_entropy_params, x, w, targets, valid, loss, stats, workspace,
+                      stream=None):
+    """x: (tokens, dim); w: (classes, dim); targets: (tokens,) int32; valid: (classes,) uint8 or
+    None; loss: (tokens,) float32; stats: (2, tokens) float32 or None."""
+    p = params
+    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    wp, ws = _matrix(w, x.dtype, p.classes, p.dim, "w")
+    return _run(
+        _lib.gsn_cross_entropy, x, stream, p, xp, xs, wp, ws,
+        _flat(targets, torch.int32, (p.tokens,), "targets"),
+        _flat(valid, torch.uint8, (p.classes,), "valid"),
+        _flat(loss, torch.float32, (p.tokens,), "loss"),
+        _flat(stats, torch.float32, (2, p.tokens), "stats"),
+        _dev(workspace, torch.uint8, what="workspace"), workspace.numel())
+
+
+def gsn_cross_entropy_backward(params: gsn_entropy_params, dloss, x, w, targets, valid, stats, dx,
+                               dw, workspace, stream=None):
+    """Gradients of gsn_cross_entropy; dx and dw may be None."""
+    p = params
+    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    wp, ws = _matrix(w, x.dtype, p.classes, p.dim, "w")
+    return _run(
+        _lib.gsn_cross_entropy_backward, x, stream, p,
+        _flat(dloss, torch.float32, (p.tokens,), "dloss"), xp, xs, wp, ws,
+        _flat(targets, torch.int32, (p.tokens,), "targets"),
+        _flat(valid, torch.uint8, (p.classes,), "valid"),
+        _flat(stats, torch.float32, (2, p.tokens), "stats"),
+        _flat(dx, x.dtype, (p.tokens, p.dim), "dx"), _flat(dw, x.dtype, (p.classes, p.dim), "dw"),
+        _dev(workspace, torch.uint8, what="workspace"), workspace.numel())
+
+
+def make_orthogonal(x, steps: int, coefficients, eps: float) -> gsn_orthogonal_params:
+    """Parameters of the orthogonalised matrices of x (..., rows, cols)."""
+    if x.dim() < 2:
+        raise ValueError(f"a matrix or a batch of them is needed, got {tuple(x.shape)}")
+    rows, cols = x.shape[-2:]
+    batch = x.numel() // (rows * cols) if rows * cols > 0 else 0
+    return gsn_orthogonal_params(_type(x, "x"), rows, cols, steps, batch, *coefficients, eps)
+
+
+def gsn_orthogonal_workspace_bytes(params: gsn_orthogonal_params, update: bool) -> int:
+    return int(_lib.gsn_orthogonal_workspace_bytes(params, 1 if update else 0))
+
+
+def gsn_orthogonalise(params: gsn_orthogonal_params, x, out, workspace, stream=None):
+    """x, out: (..., rows, cols), contiguous."""
+    return _run(
+        _lib.gsn_orthogonalise, x, stream, params, _flat(x, x.dtype, x.shape, "x"),
+        _flat(out, x.dtype, x.shape, "out"), _dev(workspace, torch.uint8, what="workspace"),
+        workspace.numel())
+
+
+def gsn_orthogonal_step(params: gsn_orthogonal_params, weights, gradient, momentum, rate: float,
+                        beta: float, decay: float, nesterov: bool, new_weights, new_momentum,
+                        workspace, stream=None):
+    """weights, gradient: (..., rows, cols) of one type; momentum: float32 of that shape."""
+    w, shape = weights, weights.shape
+    return _run(
+        _lib.gsn_orthogonal_step, w, stream, params, _flat(w, w.dtype, shape, "weights"),
+        _flat(gradient, w.dtype, shape, "gradient"),
+        _flat(momentum, torch.float32, shape, "momentum"), rate, beta, decay,
+        1 if nesterov else 0, _flat(new_weights, w.dtype, shape, "new_weights"),
+        _flat(new_momentum, torch.float32, shape, "new_momentum"),
+        _dev(workspace, torch.uint8, what="workspace"), workspace.numel())
+
+
+def gsn_quantise(x, q, scales, stream=None):
+    """x: (rows, dim); q: (rows, dim) int8; scales: (rows,) float32."""
+    rows, dim = x.shape
+    xp, xs = _matrix(x, x.dtype, rows, dim, "x")
+    qp, qs = _matrix(q, torch.int8, rows, dim, "q")
+    return _run(_lib.gsn_quantise, x, stream, _type(x, "x"), rows, dim, xp, xs, qp, qs,
+                _flat(scales, torch.float32, (rows,), "scales"))
+
+
+def make_linear8(x, w) -> gsn_linear_params:
+    """Parameters of the 8-bit product of these tensors."""
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must be 2-dimensional")
+    return gsn_linear_params(_type(x, "x"), x.shape[1], w.shape[0], x.shape[0])
+
+
+def gsn_linear_quantised_workspace_bytes(params: gsn_linear_params) -> int:
+    return int(_lib.gsn_linear_quantised_workspace_bytes(params))
+
+
+def gsn_linear_quantised(params: gsn_linear_params, x, w, scales, y, workspace, stream=None):
+    """x: (tokens, dim); w: (out, dim) int8; scales: (out,) float32; y: (tokens, out)."""
+    p = params
+    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    wp, ws = _matrix(w, torch.int8, p.out, p.dim, "w")
+    yp, ys = _matrix(y, x.dtype, p.tokens, p.out, "y")
+    return _run(
+        _lib.gsn_linear_quantised, x, stream, p, xp, xs, wp, ws,
+        _flat(scales, torch.float32, (p.out,), "scales"), yp, ys,
+        _dev(workspace, torch.uint8, what="workspace"), workspace.numel())
 
 
 # ------------------------------------------------------------------ convenience ----

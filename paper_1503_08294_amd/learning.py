@@ -1,0 +1,177 @@
+"""Training and serving models over the units of a network, on torch tensors, through the C calls of
+``include/gsn.h``.
+
+A network of units is a vocabulary: what a signal is to it is its winner.  A model that answers with
+a unit has its units as classes: ``cross_entropy`` is that model's loss, without keeping the logits
+of all units.  ``orthogonal_step`` updates its matrices and those of the local experts of
+``mixture`` by the orthogonalised momentum of their gradients, ``linear_8bit`` serves a layer in 8
+bits.  ``cross_entropy`` takes part in autograd, once: derivatives of its gradients raise
+``RuntimeError``.  The other calls have no derivatives and refuse tensors that want them, and all
+refuse tensors that carry a forward-mode tangent.
+
+Tensors are on one HIP device; work goes to torch's current stream of that device, where the
+outputs and workspaces are allocated too.  Tensors that do not fit raise ``ValueError``, sizes and
+options out of the kernels' range ``gsn.GsnError``.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import gsn
+from .mixture import _bytes, _no_tangent, _once, _rows, _same_device
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # five steps take singular values of 0.002 to 1 near 1
+
+
+def _workspace(size: int, x: torch.Tensor, what: str) -> torch.Tensor:
+    if size == 0:
+        raise gsn.GsnError(gsn.GSN_E_INVAL, what)
+    return _bytes(size, x)
+
+
+def _no_gradient(what: str, *tensors):
+    """Refuses tensors that want a gradient, which would not get one."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{what} has no derivative: call it under torch.no_grad(), or with "
+                         "detached tensors")
+
+
+# -------------------------------------------------------------------- cross entropy ----
+
+def _cross_entropy(x, w, targets, valid, save):
+    _rows(x, "x")
+    _same_device(x, w, targets, valid)
+    p = gsn.make_entropy(x, w)
+    ws = _workspace(gsn.gsn_cross_entropy_workspace_bytes(p, False), x,
+                    "gsn_cross_entropy_workspace_bytes")
+    loss = x.new_empty(x.shape[0], dtype=torch.float32)
+    stats = x.new_empty(2, x.shape[0], dtype=torch.float32) if save else None
+    gsn.gsn_cross_entropy(p, x, w, targets, valid, loss, stats, ws)
+    return loss, stats
+
+
+def cross_entropy_forward(x, w, targets, valid=None):
+    """(loss, stats): the loss of every token and what the backward pass takes."""
+    return _cross_entropy(x, w, targets, valid, True)
+
+
+def cross_entropy_backward(dloss, x, w, targets, valid, stats, need=(True, True)):
+    """(dx, dw) from dloss (tokens,) float32; None for what is not needed."""
+    _rows(x, "x")
+    _same_device(x, dloss, w, targets, valid, stats)
+    p = gsn.make_entropy(x, w)
+    ws = _workspace(gsn.gsn_cross_entropy_workspace_bytes(p, True), x,
+                    "gsn_cross_entropy_workspace_bytes")
+    dx, dw = (torch.empty_like(t, memory_format=torch.contiguous_format) if n else None
+              for t, n in zip((x, w), need))
+    gsn.gsn_cross_entropy_backward(p, dloss, x, w, targets, valid, stats, dx, dw, ws)
+    return dx, dw
+
+
+class _CrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, targets, valid):
+        loss, stats = cross_entropy_forward(x, w, targets, valid)
+        ctx.save_for_backward(x, w, targets, valid, stats)
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x, w, targets, valid, stats = ctx.saved_tensors
+        grads = cross_entropy_backward(dloss.contiguous(), x, w, targets, valid, stats,
+                                       ctx.needs_input_grad[:2])
+        return (*_once("cross_entropy", grads, dloss, x, w), None, None)
+
+
+def cross_entropy(x, w, targets, valid=None):
+    """loss[t] = log(sum_c exp(x[t] . w[c])) - x[t] . w[targets[t]], float32 (tokens,), over the
+    valid classes c.  x (tokens, dim) and w (classes, dim), rows of wider tensors as they may be;
+    targets int32 (tokens,); valid uint8 (classes,) or None.  A token whose target is out of range
+    or not valid has the loss 0 and no gradient, whatever its x; a class that is not valid is in no
+    sum, whatever its row of w.  The logits are never kept as a whole; the backward pass makes
+    them again."""
+    _no_tangent(x, w)
+    if torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
+        return _CrossEntropy.apply(x, w, targets, valid)
+    return _cross_entropy(x, w, targets, valid, False)[0]
+
+
+# -------------------------------------------------------------- orthogonalised updates ----
+
+def orthogonalise(x, *, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
+    """The orthogonalised matrices of x (..., rows, cols): their singular vectors with singular
+    values near 1 (0.7 to 1.2 with the usual coefficients and steps, where a value is above some
+    0.002 of the matrix's norm).  See gsn_orthogonalise in include/gsn.h for the products."""
+    _no_tangent(x)
+    _no_gradient("orthogonalise", x)
+    p = gsn.make_orthogonal(x, steps, coefficients, eps)
+    x = x.contiguous()
+    out = torch.empty_like(x)
+    if x.numel() == 0:
+        return out
+    ws = _workspace(gsn.gsn_orthogonal_workspace_bytes(p, False), x,
+                    "gsn_orthogonal_workspace_bytes")
+    gsn.gsn_orthogonalise(p, x, out, ws)
+    return out
+
+
+def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=True, decay=0.0,
+                    scale=None, steps=5, coefficients=COEFFICIENTS, eps=1e-7, out=None):
+    """(weights, momentum) after one update of matrices (..., rows, cols):
+
+        momentum = beta * momentum + gradient
+        weights = (1 - rate * decay) * weights
+                  - rate * scale * orthogonalise(gradient + beta * momentum)
+
+    (of the momentum alone without nesterov).  scale: sqrt(max(1, rows / cols)) if None, so that
+    the update moves outputs as far whatever the shape.  momentum is float32, gradient of the type
+    of weights.  out: the two tensors that take the results, (weights, momentum) for an update in
+    place; new ones if None."""
+    _no_tangent(weights, gradient, momentum)
+    _no_gradient("orthogonal_step", weights, gradient, momentum)
+    p = gsn.make_orthogonal(weights, steps, coefficients, eps)
+    new_weights, new_momentum = out if out is not None else (
+        torch.empty_like(weights, memory_format=torch.contiguous_format),
+        torch.empty_like(momentum, memory_format=torch.contiguous_format))
+    _same_device(weights, gradient, momentum, new_weights, new_momentum)
+    if weights.numel() == 0:
+        return new_weights, new_momentum
+    if scale is None:
+        scale = max(1.0, p.rows / p.cols) ** 0.5
+    ws = _workspace(gsn.gsn_orthogonal_workspace_bytes(p, True), weights,
+                    "gsn_orthogonal_workspace_bytes")
+    gsn.gsn_orthogonal_step(p, weights, gradient, momentum, rate * scale, beta, rate * decay,
+                            nesterov, new_weights, new_momentum, ws)
+    return new_weights, new_momentum
+
+
+# -------------------------------------------------------------------- products in 8 bits ----
+
+def quantise(x):
+    """(q, scales) of the rows of x (rows, dim): q int8 with x near q * scales[:, None], scales
+    float32 (rows,), the largest |x| of a row over 127.  The rows of q start at multiples of 16
+    bytes, as linear_8bit reads them fastest."""
+    _rows(x, "x")
+    _no_tangent(x)
+    _no_gradient("quantise", x)
+    rows, dim = x.shape
+    q = x.new_empty(rows, (dim + 15) // 16 * 16, dtype=torch.int8)[:, :dim]
+    scales = x.new_empty(rows, dtype=torch.float32)
+    gsn.gsn_quantise(x, q, scales)
+    return q, scales
+
+
+def linear_8bit(x, w, scales):
+    """y = (q w^T) * s[:, None] * scales, (q, s) = quantise(x): x (tokens, dim) through a layer
+    whose weights w int8 (out, dim) and scales float32 (out,) quantise() made.  Sums are exact;
+    y is of x's type."""
+    _rows(x, "x")
+    _no_tangent(x)
+    _no_gradient("linear_8bit", x, scales)
+    _same_device(x, w, scales)
+    p = gsn.make_linear8(x, w)
+    y = x.new_empty(x.shape[0], w.shape[0])
+    ws = _workspace(gsn.gsn_linear_quantised_workspace_bytes(p), x,
+                    "gsn_linear_quantised_workspace_bytes")
+    gsn.gsn_linear_quantised(p, x, w, scales, y, ws)
+    return y
