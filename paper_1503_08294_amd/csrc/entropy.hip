@@ -39,7 +39,8 @@ int32_t split_of(int64_t rows, int64_t cols, int64_t k, int32_t dtype) {
   const int64_t tiles =
       up_to(rows, kSmallRows) / kSmallRows * (up_to(cols, kSmallRows) / kSmallRows);
   const int64_t bytes = k * static_cast<int64_t>(size_of(dtype));
-  return static_cast<int32_t>(std::max<int64_t>(1, std::min(kFill / tiles, bytes / 1024)));
+  const int64_t fill = dtype == GSN_F32 ? 3 * kFill : kFill;
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min(fill / tiles, bytes / 1024)));
 }
 
 Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
@@ -49,12 +50,14 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   x.tokens = p.tokens;
   x.classes = p.classes;
   x.dim = p.dim;
-  x.pitch = static_cast<int32_t>(up_to(p.dim, 16 / size));
+  // (rows of the copies and of d are whole lines of 128 bytes: products read rows that begin inside
+  // a line up to a fifth slower)
+  x.pitch = static_cast<int32_t>(up_to(p.dim, 128 / size));
   int64_t piece = kPieceBytes / (size * x.pitch);
   if (backward) piece = std::min(piece, kPieceBytes / (size * tokens));
   else piece = std::min(piece, kPartBytes / (8 * tokens) * kSmallRows);
   piece = std::max<int64_t>(piece / 256 * 256, 256);
-  x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 8)));
+  x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 128 / size)));
   x.parts = static_cast<int32_t>(up_to(x.piece, kSmallRows) / kSmallRows);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
   x.splits_w = split_of(x.piece, x.pitch, tokens, p.dtype);

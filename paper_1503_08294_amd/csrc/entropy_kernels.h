@@ -55,27 +55,38 @@ struct Reduce {
   Entropy x;
   int32_t first;  // the piece's first class
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char* smem) const {
+    constexpr int BM = TILE::BM, BN = TILE::BN;
     const int li = lane & 15, lg = (lane >> 4) * 4;
-    float2* const rows = reinterpret_cast<float2*>(smem);  // [WN][SIDE]
+    float2* const rows = reinterpret_cast<float2*>(smem);  // [2][BM]
     const int32_t n = first + at.n0 + nw + lg;
     const uint32_t shut = shut_columns<NT>(x.valid, x.classes, n);
+    if (__any(shut != 0))
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (shut >> (4 * j + q) & 1) acc[i][j][q] = -INFINITY;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int64_t t = at.m0 + mw + 16 * i + li;
-      const int32_t target = t < x.tokens ? x.targets[t] : -1;
-      float top = -INFINITY;
+      const int32_t place = (t < x.tokens ? x.targets[t] : -1) - n;
+      if (__any(place >= 0 && place < 16 * NT)) {  // (few tiles hold a target)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (place == 16 * j + q && acc[i][j][q] != -INFINITY) x.chosen[t] = acc[i][j][q];
+      }
+      float top = acc[i][0][0];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float l = shut >> (4 * j + q) & 1 ? -INFINITY : acc[i][j][q];
-          acc[i][j][q] = l;
-          top = fmaxf(top, l);
-          if (n + 16 * j + q == target && l != -INFINITY) x.chosen[t] = l;
-        }
+        for (int q = 0; q < 4; ++q) top = fmaxf(top, acc[i][j][q]);
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
       const float base = top == -INFINITY ? 0.0f : top;
@@ -86,16 +97,13 @@ struct Reduce {
         for (int q = 0; q < 4; ++q) sum += power<T>(acc[i][j][q] - base);
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
-      if (lane < 16) rows[nw / (SIDE / WN) * SIDE + mw + 16 * i + li] = float2{top, sum};
+      if (lane < 16) rows[nw / (BN / 2) * BM + mw + 16 * i + li] = float2{top, sum};
     }
     __syncthreads();
-    for (int m = threadIdx.x; m < SIDE; m += blockDim.x) {
+    for (int m = threadIdx.x; m < BM; m += kProductThreads) {
       const int64_t t = int64_t{at.m0} + m;
       if (t >= x.tokens) break;
-      float2 v = rows[m];
-#pragma unroll
-      for (int w = 1; w < WN; ++w) v = merged(v, rows[w * SIDE + m]);
-      x.part[at.n0 / SIDE * x.tokens + t] = v;
+      x.part[at.n0 / BN * x.tokens + t] = merged(rows[m], rows[BM + m]);
     }
   }
 };
@@ -135,35 +143,56 @@ struct Gradient {
   Entropy x;
   int32_t first, count;  // the piece's classes
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
-                                       int lane, char*) const {
+                                       int lane, char* smem) const {
     const int li = lane & 15, lg = (lane >> 4) * 4;
     const int32_t n = at.n0 + nw + lg;
     const uint32_t shut = shut_columns<NT>(x.valid, x.classes, first + n);
-    const float factor = sizeof(T) == 2 && __is_same(T, f16_t) ? x.factor[0] : 1.0f;
-    // (columns up to a multiple of 16 bytes are written, zeros past the last class)
-    const int32_t cols = (count + 7) / 8 * 8;
+    const float factor = __is_same(T, f16_t) ? x.factor[0] : 1.0f;
+    // (columns up to the rows' pitch are written, zeros past the last class)
+    const int32_t cols = x.piece;
+    const bool masked = __any(shut != 0);
+    Turn<T, 16 * NT> turn{smem + threadIdx.x / kWave * Turn<T, 16 * NT>::kBytes};
+    static_assert(4 * Turn<T, 16 * NT>::kBytes <= TILE::kLds);
+    T* const to = static_cast<T*>(x.d) + at.n0 + nw;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int64_t t = at.m0 + mw + 16 * i + li;
-      if (t >= x.tokens) break;
-      const int32_t target = target_of(x, t) - first;
-      const bool live = target + first >= 0;
-      const float top = x.stats[t], each = 1.0f / x.stats[x.tokens + t];
-      const float g = x.dloss[t] * factor;
-      T* const row = static_cast<T*>(x.d) + t * x.piece;
+      const int64_t t0 = at.m0 + mw + 16 * i, t = t0 + li;
+      if (t0 >= x.tokens) break;
+      const int64_t tt = t < x.tokens ? t : x.tokens - 1;
+      const int32_t target = target_of(x, tt);
+      const int32_t place = target - first - n;
+      const float top = x.stats[tt], g = x.dloss[tt] * factor;
+      const float each = g / x.stats[x.tokens + tt];
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[i][j][q] = power<T>(acc[i][j][q] - top) * each;
+      if (__any(place >= 0 && place < 16 * NT)) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (place == 16 * j + q) acc[i][j][q] -= g;
+      }
+      if (masked || __any(target < 0)) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (target < 0 || (shut >> (4 * j + q) & 1)) acc[i][j][q] = 0.0f;
+      }
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        float v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float p = power<T>(acc[i][j][q] - top) * each;
-          const float d = (p - (n + 16 * j + q == target ? 1.0f : 0.0f)) * g;
-          v[q] = live && !(shut >> (4 * j + q) & 1) ? d : 0.0f;
-        }
-        store4(row, n + 16 * j, cols, v);
+        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        turn.put(li, 16 * j + lg, v);
       }
+      wave_fence();
+      const int64_t left = x.tokens - t0;
+      turn.out(to + t0 * x.piece, x.piece, static_cast<int32_t>(left < 16 ? left : 16),
+               cols - at.n0 - nw, lane);
+      wave_fence();
     }
   }
 };
@@ -175,7 +204,7 @@ struct Partial {
   int32_t rows, pitch;
   int32_t add;
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
@@ -200,7 +229,7 @@ struct Weights {
   Entropy x;
   int32_t first, count;
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
@@ -311,15 +340,6 @@ void split(Product* p, int32_t splits) {
   p->part = ((p->k + splits - 1) / splits + kBK - 1) / kBK * kBK;
 }
 
-template <typename T, bool TRA, bool TRB, class EPI>
-void entropy_product(const Product& p, const EPI& epi, hipStream_t st) {
-  // (tiles of 128 from one a CU on)
-  if (int64_t{tiles_of(p.a.rows, kMiddleRows)} * tiles_of(p.b.rows, kMiddleRows) * p.splits >= 256)
-    run_product<T, TRA, TRB, kMiddleRows>(p, epi, st);
-  else
-    run_product<T, TRA, TRB, kSmallRows>(p, epi, st);
-}
-
 // x or its copy, w from class `first` on or its copy.
 template <typename T>
 Product logits_of(const Entropy& x, int32_t first, int32_t count) {
@@ -349,13 +369,11 @@ hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
       ce_rows<T, false, false><<<some_blocks(count * row), 256, 0, st>>>(
           x, count, first, static_cast<T*>(x.wc));
     const Product p = logits_of<T>(x, first, count);
-    const int32_t side =
-        int64_t{tiles_of(x.tokens, kMiddleRows)} * tiles_of(count, kMiddleRows) >= 256
-            ? kMiddleRows
-            : kSmallRows;
-    entropy_product<T, false, false>(p, Reduce<T>{x, first}, st);
+    int32_t parts = 0;
+    with_tile<T, false, false>(p, [&](auto tile) { parts = tiles_of(count, tile.BN); });
+    run_product<T, false, false>(p, Reduce<T>{x, first}, st);
     ce_join<<<static_cast<uint32_t>((x.tokens + kJoinTokens - 1) / kJoinTokens),
-              kJoinTokens * kJoinWaves, 0, st>>>(x, tiles_of(count, side), first == 0,
+              kJoinTokens * kJoinWaves, 0, st>>>(x, parts, first == 0,
                                                  first + count == x.classes);
   }
   return hipGetLastError();
@@ -373,7 +391,7 @@ hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st) {
       ce_rows<T, false, true><<<some_blocks(count * row), 256, 0, st>>>(
           x, count, first, static_cast<T*>(x.wc));
     const Product l = logits_of<T>(x, first, count);
-    entropy_product<T, false, false>(l, Gradient<T>{x, first, count}, st);
+    run_product<T, false, false>(l, Gradient<T>{x, first, count}, st);
     Operand d = operand_of<T>(x.d, x.piece, x.tokens);
     if (x.dx) {
       Product p = l;
@@ -382,7 +400,7 @@ hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st) {
       p.k = count;
       split<T>(&p, x.splits_x);
       const int64_t each = x.tokens * x.pitch;
-      entropy_product<T, false, true>(
+      run_product<T, false, true>(
           p, Partial{x.dxp, each, static_cast<int32_t>(x.tokens), x.pitch, first > 0}, st);
     }
     if (x.dw) {
@@ -395,11 +413,11 @@ hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st) {
       split<T>(&p, x.splits_w);
       if (x.splits_w > 1) {
         const int64_t each = int64_t{x.piece} * x.pitch;
-        entropy_product<T, true, true>(p, Partial{x.dwp, each, count, x.pitch, 0}, st);
+        run_product<T, true, true>(p, Partial{x.dwp, each, count, x.pitch, 0}, st);
         ce_sum<T, false><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
             x, x.dwp, x.splits_w, count, first, each, static_cast<T*>(x.dw));
       } else {
-        entropy_product<T, true, true>(p, Weights<T>{x, first, count}, st);
+        run_product<T, true, true>(p, Weights<T>{x, first, count}, st);
       }
     }
   }

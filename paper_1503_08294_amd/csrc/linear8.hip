@@ -82,7 +82,7 @@ template <typename T>
 struct Scaled {
   Linear8 x;
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(i32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
@@ -126,11 +126,7 @@ hipError_t launch(const Linear8& x, hipStream_t st) {
                 copy ? x.pitch : x.w_stride, 0, x.out};
   p.terms = p.batch = p.splits = 1;
   p.k = p.part = x.dim;
-  // (tiles of 128 from one a CU on)
-  if (int64_t{tiles_of(x.tokens, kMiddleRows)} * tiles_of(x.out, kMiddleRows) >= 256)
-    run_product<int8_t, false, false, kMiddleRows>(p, Scaled<T>{x}, st);
-  else
-    run_product<int8_t, false, false, kSmallRows>(p, Scaled<T>{x}, st);
+  run_product<int8_t, false, false>(p, Scaled<T>{x}, st);
   return hipGetLastError();
 }
 

@@ -45,13 +45,32 @@ struct Orthogonal {
   f16_t* poly;     // B
 };
 
-// What is orthogonalised, at element i of all matrices.  The momentum is new_momentum by then.
+// v as a binary32 value: what is made of it is made of the same one.  (Left to the compiler, a
+// product may be fused with its rounding to float16, and a second value that is made of the product
+// as rounded to binary32 does not belong to the first where that is a tie.)
+__device__ __forceinline__ float settled(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
+
+// Eight elements of a row from column c on, of which those inside are used.
+template <typename T>
+__device__ __forceinline__ void load8(const T* row, int32_t c, int32_t cols, float* v) {
+  load4(row, c, cols, v);
+  load4(row, c + 4, cols, v + 4);
+}
+
+// What is orthogonalised, at eight elements of a row of all matrices.  The momentum is new_momentum
+// by then.
 template <typename T, bool UPDATE>
-__device__ __forceinline__ float input(const Orthogonal& x, int64_t i) {
-  const float g = to_float(static_cast<const T*>(x.x)[i]);
-  if constexpr (!UPDATE) return g;
-  const float m = x.new_momentum[i];
-  return x.nesterov ? g + x.beta * m : m;
+__device__ __forceinline__ void input8(const Orthogonal& x, int64_t row, int32_t c, float* v) {
+  load8(static_cast<const T*>(x.x) + row * x.cols, c, x.cols, v);
+  if constexpr (UPDATE) {
+    float m[8];
+    load8(x.new_momentum + row * x.cols, c, x.cols, m);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = x.nesterov ? v[q] + x.beta * m[q] : m[q];
+  }
 }
 
 // Sums of squares in 64 bits (squares of binary32 leave its range), a part of a matrix a workgroup;
@@ -61,17 +80,30 @@ template <typename T, bool UPDATE>
 __global__ __launch_bounds__(kNormThreads) void or_norm(Orthogonal x) {
   __shared__ double some[kNormThreads / kWave];
   const int64_t pair = blockIdx.x / x.blocks;
-  const int32_t part = static_cast<int32_t>(blockIdx.x - pair * x.blocks);
-  const int64_t n = static_cast<int64_t>(x.rows) * x.cols;
+  const uint32_t part = static_cast<uint32_t>(blockIdx.x - pair * x.blocks);
+  const uint32_t each = static_cast<uint32_t>(x.cols8) / 8, n = each * x.rows;
   double s = 0.0;
-  for (int64_t i = static_cast<int64_t>(part) * kNormThreads + threadIdx.x; i < n;
-       i += static_cast<int64_t>(x.blocks) * kNormThreads) {
-    const int64_t at = pair * n + i;
-    if constexpr (UPDATE)
-      x.new_momentum[at] =
-          x.beta * x.momentum[at] + to_float(static_cast<const T*>(x.x)[at]);
-    const double v = input<T, UPDATE>(x, at);
-    s += v * v;
+  for (uint32_t i = part * kNormThreads + threadIdx.x; i < n; i += x.blocks * kNormThreads) {
+    const uint32_t r = i / each;
+    const int32_t c = static_cast<int32_t>(i - r * each) * 8;
+    const int64_t row = pair * x.rows + r;
+    float v[8];
+    if constexpr (UPDATE) {
+      float m[8];
+      load8(static_cast<const T*>(x.x) + row * x.cols, c, x.cols, v);
+      load8(x.momentum + row * x.cols, c, x.cols, m);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        m[q] = x.beta * m[q] + v[q];
+        v[q] = x.nesterov ? v[q] + x.beta * m[q] : m[q];
+      }
+      store4(x.new_momentum + row * x.cols, c, x.cols, m);
+      store4(x.new_momentum + row * x.cols, c + 4, x.cols, m + 4);
+    } else {
+      input8<T, false>(x, row, c, v);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) s += static_cast<double>(v[q]) * v[q];
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
@@ -82,55 +114,45 @@ __global__ __launch_bounds__(kNormThreads) void or_norm(Orthogonal x) {
   x.norms[blockIdx.x] = s;
 }
 
-// v (times 2^11) as one or two float16 values at element i.
-__device__ __forceinline__ void keep2(f16_t* to, int64_t other, int32_t values, int64_t i,
-                                      float v) {
-  const f16_t hi = from_float<f16_t>(v);
-  to[i] = hi;
-  if (values > 1) to[other + i] = from_float<f16_t>(v - to_float(hi));
-}
-
-// X of the first step.
+// X of the first step, times 2^11, as one or two float16 values a number.
 template <typename T, bool UPDATE>
 __global__ __launch_bounds__(256) void or_begin(Orthogonal x) {
-  __shared__ float factor;
+  __shared__ double some[4];
   const int64_t pair = blockIdx.x / x.blocks;
-  const int32_t part = static_cast<int32_t>(blockIdx.x - pair * x.blocks);
-  if (threadIdx.x == 0) {
-    double s = 0.0;
-    for (int32_t i = 0; i < x.blocks; ++i) s += x.norms[pair * x.blocks + i];
-    const double norm = sqrt(s) + static_cast<double>(x.eps);
-    // (a matrix of zeros without an eps; infinities become NaN below)
-    factor = norm > 0.0 ? static_cast<float>(kScale / norm) : s != s ? NAN : 0.0f;
-  }
-  __syncthreads();
-  const int64_t n = static_cast<int64_t>(x.rows) * x.cols;
-  const int64_t all = static_cast<int64_t>(x.rows8) * x.cols8;
-  for (int64_t i = static_cast<int64_t>(part) * 256 + threadIdx.x; i < all;
-       i += static_cast<int64_t>(x.blocks) * 256) {
-    const int32_t r = static_cast<int32_t>(i / x.cols8);
-    const int32_t c = static_cast<int32_t>(i - static_cast<int64_t>(r) * x.cols8);
-    float v = 0.0f;
-    if (r < x.rows && c < x.cols)
-      v = input<T, UPDATE>(x, pair * n + static_cast<int64_t>(r) * x.cols + c) * factor;
-    keep2(x.now[0], x.batch * all, x.values, pair * all + i, v);
-  }
-}
-
-// Four values of a row as one or two float16 values each.
-__device__ __forceinline__ void keep4(f16_t* to, int64_t other, int32_t values, int64_t i,
-                                      const float* v) {
-  Vec<f16_t, 4> hi, lo;
+  const uint32_t part = static_cast<uint32_t>(blockIdx.x - pair * x.blocks);
+  const int tid = threadIdx.x;
+  double s = tid < x.blocks ? x.norms[pair * x.blocks + tid] : 0.0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    hi.v[q] = from_float<f16_t>(v[q]);
-    lo.v[q] = from_float<f16_t>(v[q] - to_float(hi.v[q]));
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (tid % kWave == 0) some[tid / kWave] = s;
+  __syncthreads();
+  s = some[0] + some[1] + some[2] + some[3];
+  const double norm = sqrt(s) + static_cast<double>(x.eps);
+  // (a matrix of zeros without an eps; infinities become NaN)
+  const float factor = norm > 0.0 ? static_cast<float>(kScale / norm) : s != s ? NAN : 0.0f;
+  const uint32_t each = static_cast<uint32_t>(x.cols8) / 8, n = each * x.rows8;
+  const int64_t other = x.batch * (int64_t{8} * n);
+  for (uint32_t i = part * 256 + tid; i < n; i += x.blocks * 256) {
+    const uint32_t r = i / each;
+    const int32_t c = static_cast<int32_t>(i - r * each) * 8;
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (static_cast<int32_t>(r) < x.rows) input8<T, UPDATE>(x, pair * x.rows + r, c, v);
+    Vec<f16_t, 8> hi, lo;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float w = settled(v[q] * factor);
+      hi.v[q] = from_float<f16_t>(w);
+      lo.v[q] = from_float<f16_t>(w - to_float(hi.v[q]));
+    }
+    f16_t* const to = x.now[0] + (pair * n + i) * 8;
+    *reinterpret_cast<Vec<f16_t, 8>*>(to) = hi;
+    if (x.values > 1) *reinterpret_cast<Vec<f16_t, 8>*>(to + other) = lo;
   }
-  *reinterpret_cast<Vec<f16_t, 4>*>(to + i) = hi;
-  if (values > 1) *reinterpret_cast<Vec<f16_t, 4>*>(to + other + i) = lo;
 }
 
-// Tiles of A, of B and of X.
+// Tiles of A, of B and of X, as one or two float16 values a number, by way of LDS to whole lines of
+// memory (a lane's own results would go out in pieces of 8 bytes, and those of the transposed half
+// of A and of B in pieces of 2).
 enum Made { kGram, kPoly, kNext };
 template <Made MADE>
 struct Keep {
@@ -140,40 +162,100 @@ struct Keep {
   int32_t rows, cols, values;
   float a, b, c;
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
-                                       int lane, char*) const {
-    const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+                                       int lane, char* smem) const {
+    constexpr int BM = 16 * MT, BN = 16 * NT;  // of a wave
+    const int li = lane & 15, lg = (lane >> 4) * 4;
+    const int32_t m0 = at.m0 + mw, n0 = at.n0 + nw;
     const int64_t first = at.pair * (static_cast<int64_t>(rows) * cols);
+    char* const room = smem + threadIdx.x / kWave * (TILE::kLds / 4);
+    static_assert(Turn<f16_t, BN>::kBytes <= TILE::kLds / 4 &&
+                  Turn<f16_t, BM>::kBytes <= TILE::kLds / 4);
+    if (m0 >= rows || n0 >= cols) return;
+    // a wave's part is above the diagonal, or below it and left to its mirror image, or on it
+    const bool above = MADE == kNext || n0 >= m0 + BM - 1;
+    if (MADE != kNext && n0 + BN <= m0) return;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
-      if (m >= rows) break;
-      const int64_t row = first + static_cast<int64_t>(m) * cols;
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        const int32_t n1 = n + 16 * j;
-        if (n1 >= cols) break;
-        float v[4];
+        const int32_t m = m0 + 16 * i + li, n = n0 + 16 * j + lg;
         if constexpr (MADE == kPoly) {
-          const Vec<f16_t, 4> hi = *reinterpret_cast<const Vec<f16_t, 4>*>(gram + row + n1);
-          Vec<f16_t, 4> lo{};
-          if (values > 1) lo = *reinterpret_cast<const Vec<f16_t, 4>*>(gram + other + row + n1);
+          Vec<f16_t, 4> hi{}, lo{};
+          const f16_t* const p = gram + first + static_cast<int64_t>(m) * cols + n;
+          if (m < rows && n < cols) {
+            hi = *reinterpret_cast<const Vec<f16_t, 4>*>(p);
+            if (values > 1) lo = *reinterpret_cast<const Vec<f16_t, 4>*>(p + other);
+          }
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            v[q] = c * (acc[i][j][q] * (1.0f / kScale)) +
-                   (b * (to_float(hi.v[q]) + to_float(lo.v[q])) +
-                    (m == n1 + q ? a * kScale : 0.0f));
+            acc[i][j][q] = c * (acc[i][j][q] * (1.0f / kScale)) +
+                           (b * (to_float(hi.v[q]) + to_float(lo.v[q])) +
+                            (m == n + q ? a * kScale : 0.0f));
         } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] = acc[i][j][q] * (1.0f / kScale);
+          for (int q = 0; q < 4; ++q) acc[i][j][q] *= 1.0f / kScale;
         }
-        keep4(to, other, values, row + n1, v);
-        if (MADE != kNext && at.n0 > at.m0)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[i][j][q] = settled(acc[i][j][q]);
+      }
+    for (int part = 0; part < values; ++part) {
+      f16_t* const out = to + first + (part ? other : 0);
+      if (above) {
+        const Turn<f16_t, BN> turn{room};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            turn.put(li, 16 * j + lg, v);
+          }
+          wave_fence();
+          const int32_t m = m0 + 16 * i;
+          turn.out(out + static_cast<int64_t>(m) * cols + n0, cols, rows - m, cols - n0, lane);
+          wave_fence();
+        }
+        if constexpr (MADE != kNext) {
+          // rows n of the transposed tile: columns m, 16 rows at a time
+          using Mirror = Turn<f16_t, BM>;
+          const Mirror turned{room};
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f16_t*>(room + (lg + q) * Mirror::kRow + (16 * i + li) * 2) =
+                    from_float<f16_t>(acc[i][j][q]);
+            wave_fence();
+            const int32_t n = n0 + 16 * j;
+            turned.out(out + static_cast<int64_t>(n) * cols + m0, cols, rows - n, cols - m0, lane);
+            wave_fence();
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int32_t m = m0 + 16 * i + li, n = n0 + 16 * j + lg + q;
+              if (m >= rows || n >= cols || n < m) continue;
+              const f16_t v = from_float<f16_t>(acc[i][j][q]);
+              out[static_cast<int64_t>(m) * cols + n] = v;
+              out[static_cast<int64_t>(n) * cols + m] = v;
+            }
+      }
+      // what the first value leaves
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            keep2(to, other, values, first + static_cast<int64_t>(n1 + q) * cols + m, v[q]);
-      }
+            acc[i][j][q] = settled(acc[i][j][q] - to_float(from_float<f16_t>(acc[i][j][q])));
     }
   }
 };
@@ -186,7 +268,7 @@ struct Finish {
   int32_t rows, cols;
   float rate, keep;
 
-  template <int SIDE, int WN, int MT, int NT>
+  template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
@@ -213,18 +295,6 @@ struct Finish {
   }
 };
 
-template <bool TRA, bool TRB, class EPI>
-void product(Product p, const EPI& epi, hipStream_t st) {
-  p.splits = 1;
-  p.part = p.k;
-  const int64_t m = tiles_of(p.a.rows, kMiddleRows), n = tiles_of(p.b.rows, kMiddleRows);
-  // (tiles of 128 from one a CU on)
-  if ((p.symmetric ? m * (m + 1) / 2 : m * n) * p.batch >= 256)
-    run_product<f16_t, TRA, TRB, kMiddleRows>(p, epi, st);
-  else
-    run_product<f16_t, TRA, TRB, kSmallRows>(p, epi, st);
-}
-
 template <typename T, bool UPDATE>
 hipError_t launch(const Orthogonal& x, hipStream_t st) {
   const uint32_t blocks = static_cast<uint32_t>(x.batch * x.blocks);
@@ -243,20 +313,21 @@ hipError_t launch(const Orthogonal& x, hipStream_t st) {
   Product p{};
   p.terms = x.values == 2 ? 3 : 1;
   p.batch = static_cast<int32_t>(x.batch);
+  p.splits = 1;
   for (int32_t s = 0; s < x.steps; ++s) {
     const f16_t* const now = x.now[s & 1];
     p.symmetric = 1;
     p.a = operand(now, true, x.cols8, all, side);
     p.b = operand(now, false, x.cols8, all, side);
-    p.k = wide ? x.cols8 : x.rows8;
+    p.k = p.part = wide ? x.cols8 : x.rows8;
     const Keep<kGram> gram{x.gram, nullptr, x.batch * square, side, side, x.values, x.a, x.b, x.c};
-    if (wide) product<false, false>(p, gram, st);
-    else product<true, true>(p, gram, st);
+    if (wide) run_product<f16_t, false, false>(p, gram, st);
+    else run_product<f16_t, true, true>(p, gram, st);
     p.a = operand(x.gram, true, side, square, side);
     p.b = operand(x.gram, false, side, square, side);
-    p.k = side;
-    product<false, false>(p, Keep<kPoly>{x.poly, x.gram, x.batch * square, side, side, x.values,
-                                         x.a, x.b, x.c}, st);
+    p.k = p.part = side;
+    run_product<f16_t, false, false>(p, Keep<kPoly>{x.poly, x.gram, x.batch * square, side, side,
+                                                    x.values, x.a, x.b, x.c}, st);
     p.symmetric = 0;
     if (wide) {
       p.a = operand(x.poly, true, side, square, side);
@@ -266,8 +337,8 @@ hipError_t launch(const Orthogonal& x, hipStream_t st) {
       p.b = operand(x.poly, false, side, square, side);
     }
     const auto last = [&](const auto& epi) {
-      if (wide) product<false, true>(p, epi, st);
-      else product<false, false>(p, epi, st);
+      if (wide) run_product<f16_t, false, true>(p, epi, st);
+      else run_product<f16_t, false, false>(p, epi, st);
     };
     if (s + 1 < x.steps)
       last(Keep<kNext>{x.now[~s & 1], nullptr, x.batch * all, x.rows8, x.cols8, x.values, x.a,
@@ -311,7 +382,7 @@ Orthogonal orthogonal_of(const gsn_orthogonal_params& p, bool update) {
   x.rows8 = (p.rows + 7) / 8 * 8;
   x.cols8 = (p.cols + 7) / 8 * 8;
   const int64_t n = int64_t{p.rows} * p.cols;
-  x.blocks = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(256, n / 4096)));
+  x.blocks = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(256, n / 8192)));
   x.steps = p.steps;
   // An update is a small part of the weights: in 2-byte weights its error of 3e-3 at most is below
   // their own rounding.

@@ -41,12 +41,6 @@ struct Place {
 inline int32_t tiles_of(int64_t n, int32_t side) {
   return static_cast<int32_t>((n + side - 1) / side);
 }
-inline int64_t tiles_of(const Product& p) {
-  const int64_t t = p.symmetric ? int64_t{p.tiles_m} * (p.tiles_m + 1) / 2
-                                : int64_t{p.tiles_m} * p.tiles_n;
-  return t * p.batch * p.splits;
-}
-
 namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
@@ -64,28 +58,52 @@ __device__ __forceinline__ AccOf<T> multiply_any(const Frag& n, const Frag& m, A
     return multiply<T>(n, m, acc, q);
 }
 
-// Fragments of an operand of 8-bit elements: the bytes lie as those of wider elements with k
-// contiguous do.
-template <typename T, bool TR, int R>
+// Tiles of BM x BN by four waves, 2 x 2 of them: stages of KB bytes of k, SLOTS of them in LDS, and
+// WAVES of a SIMD (workgroups of a CU) that registers and LDS have to last for.  RUN of them at a
+// time are an XCD's, in blocks TALL tiles high.
+template <int BM_, int BN_, int KB_, int SLOTS_, int WAVES_, int RUN_, int TALL_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, KB = KB_, SLOTS = SLOTS_, WAVES = WAVES_;
+  static constexpr int RUN = RUN_, TALL = TALL_;
+  static constexpr int kSlot = (BM + BN) * KB;
+  static constexpr int kLds = SLOTS * kSlot;
+  static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024);
+};
+
+// Place of 16-byte chunk c in row r of a staged operand with k contiguous: the 16 rows that a
+// quarter wave reads at one k fall on different banks.
+template <int KB>
+__device__ __forceinline__ int chunk_row(int r, int c) {
+  static_assert(KB == 128 || KB == 64);
+  if constexpr (KB == 128) return chunk_k(r, c);
+  else return c ^ ((r >> 2) & 3);
+}
+
+// Fragment of 16 rows at r0 and the s-th 64 bytes of a stage's k; R rows, or columns, in all.
+template <typename T, bool TR, int R, int KB>
 __device__ __forceinline__ Frag fragment_any(const char* tile, int r0, int s, int lane) {
-  if constexpr (sizeof(T) == 1) {
-    static_assert(!TR);
-    return fragment<float, false, R>(tile, r0, s, lane);
+  if constexpr (TR) {
+    static_assert(sizeof(T) > 1);
+    return fragment<T, true, R>(tile, r0, s, lane);
   } else {
-    return fragment<T, TR, R>(tile, r0, s, lane);
+    const int r = r0 + (lane & 15);
+    Frag f;
+    f.u = *reinterpret_cast<const u32x4*>(tile + r * KB +
+                                          chunk_row<KB>(r, 4 * s + (lane >> 4)) * 16);
+    return f;
   }
 }
 
 // What this lane loads of one operand's stages: of stage h the chunks j THR + thread for j = 0, 1,
-// ..., SIDE rows (or columns) of 128 bytes of k in all.
-template <typename T, bool TR, int SIDE, int THR>
+// ..., SIDE rows (or columns) of KB bytes of k in all.
+template <typename T, bool TR, int SIDE, int KB, int THR>
 struct Feed {
   static constexpr int kE = 16 / static_cast<int>(sizeof(T));
-  static constexpr int kBK = kRowBytes / static_cast<int>(sizeof(T));
-  static constexpr int kC = TR ? SIDE / kE : 8;  // chunks of a row
-  static constexpr int kLoads = SIDE * 8 / THR;
+  static constexpr int kBK = KB / static_cast<int>(sizeof(T));
+  static constexpr int kC = TR ? SIDE / kE : KB / 16;  // chunks of a row
+  static constexpr int kLoads = SIDE * KB / 16 / THR;
   static constexpr int kStep = THR / kC;  // rows from one j to the next
-  static_assert(THR % kC == 0 && SIDE * 8 % THR == 0);
+  static_assert(THR % kC == 0 && SIDE * KB / 16 % THR == 0);
 
   const char* p;   // the chunk j = 0 of the next stage
   int64_t ld, step;
@@ -95,7 +113,7 @@ struct Feed {
 
   __device__ __forceinline__ static int chunk(int row, int c) {
     if constexpr (TR) return chunk_n<T, kC>(row, c);
-    else return chunk_k(row, c);
+    else return chunk_row<KB>(row, c);
   }
   __device__ __forceinline__ void begin(const Operand& o, int32_t pair, int32_t row0, int32_t k0,
                                         int32_t k_end, int tid) {
@@ -112,7 +130,7 @@ struct Feed {
     } else {
       p = base + static_cast<int64_t>(row0 + r) * ld +
           (static_cast<int64_t>(k0) + c * kE) * static_cast<int>(sizeof(T));
-      step = kRowBytes;
+      step = KB;
       k = k0 + c * kE;
       left = o.rows - row0 - r;
     }
@@ -147,65 +165,75 @@ struct Feed {
   }
 };
 
-// Number of the tile in its pair -> its row and column of tiles.
-__device__ __forceinline__ int2 symmetric_place(int32_t id) {
-  // column c holds the tiles (0, c) .. (c, c), c (c + 1) / 2 before it
-  int32_t c = static_cast<int32_t>((sqrtf(8.0f * static_cast<float>(id) + 1.0f) - 1.0f) * 0.5f);
-  while (c * (c + 1) / 2 > id) --c;
-  while ((c + 1) * (c + 2) / 2 <= id) ++c;
-  return int2{id - c * (c + 1) / 2, c};
+// Number of a tile in its pair -> its row and column of tiles, of a symmetric product those that
+// hold something on or above the diagonal, a column of tiles after the other.
+template <class TILE>
+__device__ __forceinline__ int2 symmetric_place(int32_t id, int32_t tiles_m) {
+  constexpr int32_t R = TILE::BN / TILE::BM;  // column c has the tiles 0 .. R (c + 1) - 1
+  const float f = sqrtf(8.0f / R * static_cast<float>(id) + 1.0f);
+  int32_t c = static_cast<int32_t>((f - 1.0f) * 0.5f);
+  while (R * c * (c + 1) / 2 > id) --c;
+  while (R * (c + 1) * (c + 2) / 2 <= id) ++c;
+  return int2{id - R * c * (c + 1) / 2, c};
 }
 
-// false: no tile for this workgroup.
-template <int SIDE>
-__device__ __forceinline__ bool place_of(const Product& p, Place* at) {
-  const int32_t each =
-      p.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
-  const int32_t id = spread(blockIdx.x, each * p.batch * p.splits, tile_run(SIDE));
+// Tiles of a pair.  (The last column of a symmetric product may have fewer tiles than R (c + 1):
+// its number of rows.)
+template <class TILE>
+__host__ __device__ inline int32_t tiles_of_pair(const Product& p) {
+  constexpr int32_t R = TILE::BN / TILE::BM;
+  return p.symmetric ? R * (p.tiles_n - 1) * p.tiles_n / 2 + p.tiles_m : p.tiles_m * p.tiles_n;
+}
+
+// Workgroups of a product: those of a round of 8 runs are dealt out to the XCDs a run each
+// (spread()), where the tiles that are worked on at a time share operands.
+template <class TILE>
+__host__ __device__ inline int32_t numbers_of(const Product& p) {
+  constexpr int32_t round = 8 * TILE::RUN;
+  const int32_t tiles = tiles_of_pair<TILE>(p) * p.batch * p.splits;
+  return tiles < round ? (tiles + 7) / 8 * 8 : (tiles + round - 1) / round * round;
+}
+
+// false: there is no tile of this number.
+template <class TILE>
+__device__ __forceinline__ bool place_of(const Product& p, int32_t number, Place* at) {
+  const int32_t each = tiles_of_pair<TILE>(p);
+  const int32_t id = spread(number, each * p.batch * p.splits, TILE::RUN);
   if (id < 0) return false;
   const int32_t outer = id / each, in = id - outer * each;
-  const int2 t = p.symmetric ? symmetric_place(in) : tile_place<4>(in, p.tiles_m, p.tiles_n);
+  const int2 t = p.symmetric ? symmetric_place<TILE>(in, p.tiles_m)
+                             : tile_place<TILE::TALL>(in, p.tiles_m, p.tiles_n);
   at->split = outer / p.batch;
   at->pair = outer - at->split * p.batch;
-  at->m0 = t.x * SIDE;
-  at->n0 = t.y * SIDE;
+  at->m0 = t.x * TILE::BM;
+  at->n0 = t.y * TILE::BN;
   return true;
 }
 
-// Workgroups of a product's grid.
-template <int SIDE>
-int64_t grid_of(const Product& p) {
-  constexpr int64_t round = 8 * tile_run(SIDE);
-  return (tiles_of(p) + round - 1) / round * round;
-}
-
-// Tiles of 128 or 64 a side by four waves, 2 x 2 of them.  Stages go from memory straight to LDS;
-// a stage is awaited by all waves together, then a later one is sent out and this one multiplied.
-template <int SIDE>
-constexpr int kSlots = SIDE == kMiddleRows ? 2 : 3;
-template <int SIDE>
-constexpr int kProductLds = kSlots<SIDE> * 2 * SIDE * kRowBytes;
 constexpr int kProductThreads = 256;
 
-// What becomes of a tile's results is the functor's:
-//   EPI::tile<SIDE, WN, MT, NT>(acc, place, mw, nw, lane, smem)
+// A tile by four waves.  Stages go from memory straight to LDS; a stage is awaited by all waves
+// together, then a later one is sent out and this one multiplied.  Two or three workgroups share a
+// CU: one's waits, start and results hide behind another's products.  What becomes of the results
+// is the functor's:
+//   EPI::tile<TILE, MT, NT>(acc, place, mw, nw, lane, room)
 // acc[i][j][q] is C(m0 + mw + 16 i + (lane & 15), n0 + nw + 16 j + 4 (lane >> 4) + q); mw and nw
-// are the wave's first row and column in the tile, of WN waves a row.  All threads of the workgroup
-// come, LDS is free.
-template <typename T, bool TRA, bool TRB, int SIDE, class EPI>
-__global__ __launch_bounds__(kProductThreads, SIDE == kMiddleRows ? 2 : 3) void mt_product(
-    Product p, EPI epi) {
-  constexpr int kThr = kProductThreads, MT = SIDE / 32, NT = SIDE / 32;
-  constexpr int kSlot = 2 * SIDE * kRowBytes, SLOTS = kSlots<SIDE>;
-  __shared__ __attribute__((aligned(1024))) char smem[kProductLds<SIDE>];
+// are the wave's first row and column in the tile.  All threads of the workgroup come; room is LDS
+// that no other wave reads any more.
+template <typename T, bool TRA, bool TRB, class TILE, class EPI>
+__global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Product p, EPI epi) {
+  constexpr int kThr = kProductThreads, BM = TILE::BM, BN = TILE::BN, KB = TILE::KB;
+  constexpr int MT = BM / 32, NT = BN / 32, kSlot = TILE::kSlot, SLOTS = TILE::SLOTS;
+  static_assert(SLOTS == 2 || SLOTS == 3);
+  __shared__ __attribute__((aligned(1024))) char smem[TILE::kLds];
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int wm = wave >> 1, wn = wave & 1;
+  const int mw = (wave >> 1) * (BM / 2), nw = (wave & 1) * (BN / 2);
   Place at;
-  if (!place_of<SIDE>(p, &at)) return;
+  if (!place_of<TILE>(p, blockIdx.x, &at)) return;
 
-  using FeedA = Feed<T, TRA, SIDE, kThr>;
-  using FeedB = Feed<T, TRB, SIDE, kThr>;
+  using FeedA = Feed<T, TRA, BM, KB, kThr>;
+  using FeedB = Feed<T, TRB, BN, KB, kThr>;
   constexpr int kBK = FeedA::kBK, kLoads = FeedA::kLoads + FeedB::kLoads;
   const int32_t k0 = at.split * p.part;
   const int32_t k_end = k0 + p.part < p.k ? k0 + p.part : p.k;
@@ -221,7 +249,7 @@ __global__ __launch_bounds__(kProductThreads, SIDE == kMiddleRows ? 2 : 3) void 
   int32_t in_term = 0, term = 0;
   const auto load = [&](int slot) {
     fa.load(lds + slot * kSlot);
-    fb.load(lds + slot * kSlot + SIDE * kRowBytes);
+    fb.load(lds + slot * kSlot + BM * KB);
     if (++in_term == each) {
       in_term = 0;
       fa.turn(term == 0 ? p.a.next[0] : p.a.next[1], each);
@@ -244,16 +272,14 @@ __global__ __launch_bounds__(kProductThreads, SIDE == kMiddleRows ? 2 : 3) void 
     else meet_loaded<0>();
     if (h + SLOTS - 1 < stages) load(slot == 0 ? SLOTS - 1 : slot - 1);
     const char* const sa = smem + slot * kSlot;
-    const char* const sb = sa + SIDE * kRowBytes;
+    const char* const sb = sa + BM * KB;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < KB / 64; ++s) {
       Frag ra[MT], rb[NT];
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
-        ra[i] = fragment_any<T, TRA, SIDE>(sa, wm * (SIDE / 2) + i * 16, s, lane);
+      for (int j = 0; j < NT; ++j) rb[j] = fragment_any<T, TRB, BN, KB>(sb, nw + j * 16, s, lane);
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        rb[j] = fragment_any<T, TRB, SIDE>(sb, wn * (SIDE / 2) + j * 16, s, lane);
+      for (int i = 0; i < MT; ++i) ra[i] = fragment_any<T, TRA, BM, KB>(sa, mw + i * 16, s, lane);
 #pragma unroll
       for (int q = 0; q < kParts<T>; ++q)
 #pragma unroll
@@ -264,17 +290,53 @@ __global__ __launch_bounds__(kProductThreads, SIDE == kMiddleRows ? 2 : 3) void 
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   }
   meet_read();
-  epi.template tile<SIDE, 2, MT, NT>(acc, at, wm * (SIDE / 2), wn * (SIDE / 2), lane, smem);
+  epi.template tile<TILE, MT, NT>(acc, at, mw, nw, lane, smem);
 }
 
-template <typename T, bool TRA, bool TRB, int SIDE, class EPI>
-void run_product(Product p, const EPI& epi, hipStream_t st) {
-  p.tiles_m = tiles_of(p.a.rows, SIDE);
-  p.tiles_n = tiles_of(p.b.rows, SIDE);
-  const int64_t grid = grid_of<SIDE>(p);
+template <typename T, bool TRA, bool TRB, class TILE, class EPI>
+void run_tiles(Product p, const EPI& epi, hipStream_t st) {
+  p.tiles_m = tiles_of(p.a.rows, TILE::BM);
+  p.tiles_n = tiles_of(p.b.rows, TILE::BN);
+  const int32_t grid = numbers_of<TILE>(p);
   if (grid > 0)
-    mt_product<T, TRA, TRB, SIDE, EPI>
+    mt_product<T, TRA, TRB, TILE, EPI>
         <<<static_cast<uint32_t>(grid), kProductThreads, 0, st>>>(p, epi);
+}
+
+// Which tiles a product takes.  Of 2-byte elements, us, C of bfloat16, tiles of 128 x 256, 128 x
+// 128 and 64 x 64 (two workgroups a CU of the first two, three of the last):
+//   k contiguous: 8,192 x 8,192 x 2,048: 280, 277, 613; 4,096 x 4,096 x 1,024: 42, 41, 63;
+//     2,048 x 2,048 x 1,024 (256 tiles of 128): 25, 16, 18; 1,536 x 1,536 x 1,024: 25, 15, 13
+//   n contiguous in B: 257, 283, 655; 40, 42, 68; 27, 17, 20; 26, 16, 14
+//   m and n contiguous: 256, 300, 671; 40, 45, 69; 27, 18, 21; 27, 17, 15
+//     (4,096 x 2,048 x 1,024, 256 tiles of 128 x 256: 30, 25, 35)
+// With k contiguous a stage of 64 bytes reads half lines of memory, and the middle tiles' 128 bytes
+// make up for their size.  Binary32 products are bound by the matrix cores, and small tiles fill
+// the CUs more evenly.
+using LargeTile = Tile<128, 256, 64, 2, 2, 32, 8>;
+using MiddleTile = Tile<128, 128, 128, 2, 2, 16, 4>;
+using SmallTile = Tile<64, 64, 128, 3, 3, 1, 4>;
+
+// f(a tile's type) for the tiles of a product.
+template <typename T, bool TRA, bool TRB, class F>
+void with_tile(Product p, const F& f) {
+  const auto tiles = [&](int32_t bm, int32_t bn) {
+    p.tiles_m = tiles_of(p.a.rows, bm);
+    p.tiles_n = tiles_of(p.b.rows, bn);
+    const int64_t all = int64_t{p.tiles_m} * p.tiles_n * p.batch * p.splits;
+    return p.symmetric ? all / 2 : all;
+  };
+  if constexpr (sizeof(T) < 4) {
+    if constexpr (TRA || TRB)
+      if (tiles(LargeTile::BM, LargeTile::BN) >= 512) return f(LargeTile());
+    if (tiles(MiddleTile::BM, MiddleTile::BN) >= 256) return f(MiddleTile());
+  }
+  f(SmallTile());
+}
+
+template <typename T, bool TRA, bool TRB, class EPI>
+void run_product(const Product& p, const EPI& epi, hipStream_t st) {
+  with_tile<T, TRA, TRB>(p, [&](auto tile) { run_tiles<T, TRA, TRB, decltype(tile)>(p, epi, st); });
 }
 
 }  // namespace

@@ -249,6 +249,19 @@ def test_orthogonalise_other_polynomials(learn, steps, coefficients, batch, rows
     check_orthogonal(got, x, F32, 2, f"{steps}", steps=steps, coefficients=coefficients)
 
 
+@pytest.mark.parametrize("rows,cols", [(300, 700), (700, 300), (64, 64), (1_000, 1_100)])
+def test_orthogonalise_keeps_every_element(learn, rows, cols):
+    """X <- X, three times: every element keeps its 22 bits, those beside a tie of float16 too."""
+    x = randn(rows, cols, seed=28)
+    got = learn.orthogonalise(x.cuda(), steps=3, coefficients=(1.0, 0.0, 0.0)).double().cpu()
+    want = x.double() / (x.double().norm() + 1e-7)
+    # 1 / norm and its product are rounded to binary32; what is kept three times is off by half a
+    # step of the second value, 2^-23 of the number or 2^-36 of the norm; the sums are exact but for
+    # a rounding each, as is the result
+    tol = want.abs() * (3 * 2.0 ** -23 + 6 * ref.U) + 3 * 2.0 ** -36
+    assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).max()
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_orthogonalise_extreme_sizes_and_zeros(learn, dtype):
     big, small = {F32: (1e30, 1e-30), BF16: (1e30, 1e-30), F16: (1e4, 1e-4)}[dtype]
