@@ -566,7 +566,7 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
  * valid: uint8 [classes] or NULL, 0 for a class that is not there: it is in no sum and its row of
  * w means nothing.  A token whose target is out of range or not valid has none: its loss is 0
  * and its x means nothing.  tokens 0 to 2^24, dim 1 to 2^16, classes 1 to 2^28.
- * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128. */
+ * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128 (GSN_F32: 64 x 64). */
 typedef struct gsn_entropy_params {
   int32_t dtype;
   int32_t dim, classes;

@@ -17,7 +17,7 @@ struct Entropy {
   const uint8_t* valid;  // of the classes, or null
   // pieces of the classes: of a forward and of a backward pass
   int32_t piece, parts;  // classes of a piece; tiles of its columns, at most
-  bool copy_x, copy_w;
+  bool copy_x, copy_w, few;
   void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the ends
   void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
   // forward

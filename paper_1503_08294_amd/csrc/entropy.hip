@@ -18,6 +18,8 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 // Workgroups that a product of few tiles is split up into, along k, where a part keeps 1,024 bytes
 // of k at least.
 constexpr int64_t kFill = 512;
+constexpr int64_t kFewTokens = 32;  // that few_rows() takes
+constexpr int64_t kPartCols = 32;   // columns of a part, at least
 
 bool params_ok(const gsn_entropy_params* p) {
   return p && p->dtype >= GSN_F32 && p->dtype <= GSN_F16 && p->tokens >= 0 &&
@@ -57,8 +59,11 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   if (backward) piece = std::min(piece, kPieceBytes / (size * tokens));
   else piece = std::min(piece, kPartBytes / (8 * tokens) * kSmallRows);
   piece = std::max<int64_t>(piece / 256 * 256, 256);
+  // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
+  x.few = !backward && p.tokens <= kFewTokens;
+  if (x.few) piece = up_to(p.classes, 256);
   x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 128 / size)));
-  x.parts = static_cast<int32_t>(up_to(x.piece, kSmallRows) / kSmallRows);
+  x.parts = static_cast<int32_t>(up_to(x.piece, kPartCols) / kPartCols);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
   x.splits_w = split_of(x.piece, x.pitch, tokens, p.dtype);
   return x;
@@ -67,8 +72,10 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
 size_t carve_forward(void* base, int32_t dtype, Entropy* x) {
   Carver c{static_cast<char*>(base)};
   const size_t s = size_of(dtype), t = static_cast<size_t>(x->tokens);
-  x->xc = c.take(s * t * x->pitch);
-  x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
+  if (!x->few) {
+    x->xc = c.take(s * t * x->pitch);
+    x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
+  }
   x->part = static_cast<float2*>(c.take(8 * t * x->parts));
   x->chosen = static_cast<float*>(c.take(4 * t));
   float* const stats = static_cast<float*>(c.take(8 * t));
@@ -92,9 +99,10 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
 }
 
 // Whether the grids of a call's products stay below 2^32 threads of 256.
-bool grids_ok(const Entropy& x, bool backward) {
-  const auto tiles = [](int64_t m, int64_t n) {
-    return up_to(m, kMiddleRows) / kMiddleRows * (up_to(n, kMiddleRows) / kMiddleRows);
+bool grids_ok(const Entropy& x, int32_t dtype, bool backward) {
+  const int64_t side = dtype == GSN_F32 ? kSmallRows : kMiddleRows;
+  const auto tiles = [&](int64_t m, int64_t n) {
+    return up_to(m, side) / side * (up_to(n, side) / side);
   };
   int64_t most = tiles(x.tokens, x.piece);
   if (backward) most = std::max({most, tiles(x.tokens, x.pitch), tiles(x.piece, x.pitch)});
@@ -139,7 +147,7 @@ int gsn_cross_entropy(const gsn_entropy_params* p, const void* x, int64_t x_stri
     return GSN_E_INVAL;
   if (workspace_bytes < gsn_cross_entropy_workspace_bytes(p, 0)) return GSN_E_CAPACITY;
   gsn::Entropy a = gsn::entropy_of(*p, false);
-  if (!gsn::grids_ok(a, false)) return GSN_E_CAPACITY;
+  if (!gsn::grids_ok(a, p->dtype, false)) return GSN_E_CAPACITY;
   a.x = x;
   a.x_stride = x_stride;
   a.w = w;
@@ -171,7 +179,7 @@ int gsn_cross_entropy_backward(const gsn_entropy_params* p, const float* dloss, 
     return GSN_E_INVAL;
   if (workspace_bytes < gsn_cross_entropy_workspace_bytes(p, 1)) return GSN_E_CAPACITY;
   gsn::Entropy a = gsn::entropy_of(*p, true);
-  if (!gsn::grids_ok(a, true)) return GSN_E_CAPACITY;
+  if (!gsn::grids_ok(a, p->dtype, true)) return GSN_E_CAPACITY;
   a.dloss = dloss;
   a.x = x;
   a.x_stride = x_stride;

@@ -2,6 +2,7 @@
 // of 32-bit integers, which are exact.
 #include <algorithm>
 
+#include "few.h"
 #include "product.h"
 
 namespace gsn {
@@ -35,20 +36,41 @@ __device__ __forceinline__ int quantised(float v, float s, float inverse) {
   return static_cast<int>(fminf(fmaxf(q, -127.0f), 127.0f));
 }
 
-// Rows in 8 bits, a workgroup a row: the largest value, then the quotients.  `pitch` bytes of q are
-// written, zeros past the end.  Bound by memory.
+// Rows in 8 bits, a workgroup a row: the largest value, then the quotients, the row kept in
+// registers in between where it has up to 8,192 elements.  `pitch` bytes of q are written (at most
+// up to the next multiple of 16 bytes), zeros past the end.  Bound by memory.
 template <typename T>
 __global__ __launch_bounds__(256) void q8_rows(const T* __restrict__ x, int64_t stride,
                                                int64_t rows, int32_t dim, int8_t* __restrict__ q,
                                                int64_t q_stride, int32_t pitch,
                                                float* __restrict__ scales) {
+  constexpr int kKept = 4, kEach = 8 * 256;
   __shared__ float some[4];
+  const int tid = threadIdx.x;
+  const auto load = [&](const T* row, int32_t k, float* v) {
+    load4(row, k, dim, v);
+    load4(row, k + 4, dim, v + 4);
+  };
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* const row = x + r * stride;
-    float top = 0.0f;
-    for (int32_t k = threadIdx.x; k < dim; k += 256) {
-      const float v = fabsf(to_float(row[k]));
-      top = v > top || v != v ? v : top;  // (NaN stays)
+    float kept[kKept][8], top = 0.0f;
+    const auto largest = [&](const float* v) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = fabsf(v[i]);
+        top = a > top || a != a ? a : top;  // (NaN stays)
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+      if (i * kEach < dim) load(row, i * kEach + tid * 8, kept[i]);
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+      if (i * kEach < dim) largest(kept[i]);
+    for (int32_t k = kKept * kEach + tid * 8; k < dim; k += kEach) {
+      float v[8];
+      load(row, k, v);
+      largest(v);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -56,15 +78,35 @@ __global__ __launch_bounds__(256) void q8_rows(const T* __restrict__ x, int64_t 
       top = v > top || v != v ? v : top;
     }
     __syncthreads();
-    if (threadIdx.x % kWave == 0) some[threadIdx.x / kWave] = top;
+    if (tid % kWave == 0) some[tid / kWave] = top;
     __syncthreads();
+#pragma unroll
     for (int w = 0; w < 4; ++w) top = some[w] > top || some[w] != some[w] ? some[w] : top;
     const bool bad = !(top < INFINITY);
     const float s = top / 127.0f > 0x1p-126f ? top / 127.0f : 0x1p-126f, inverse = 1.0f / s;
-    for (int32_t k = threadIdx.x; k < pitch; k += 256)
-      q[r * q_stride + k] =
-          k < dim && !bad ? static_cast<int8_t>(quantised(to_float(row[k]), s, inverse)) : 0;
-    if (threadIdx.x == 0) scales[r] = bad ? NAN : s;
+    int8_t* const to = q + r * q_stride;
+    const auto store = [&](int32_t k, const float* v) {
+      Vec<int8_t, 8> o;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        o.v[i] = bad ? 0 : static_cast<int8_t>(quantised(v[i], s, inverse));
+      if (k + 8 <= pitch) {
+        typedef uint8_t Loose __attribute__((ext_vector_type(8), aligned(1)));
+        *reinterpret_cast<Loose*>(to + k) = __builtin_bit_cast(Loose, o);
+      } else {
+        for (int i = 0; i < 8; ++i)
+          if (k + i < pitch) to[k + i] = o.v[i];
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kKept; ++i)
+      if (i * kEach + tid * 8 < pitch) store(i * kEach + tid * 8, kept[i]);
+    for (int32_t k = kKept * kEach + tid * 8; k < pitch; k += kEach) {
+      float v[8];
+      load(row, k, v);
+      store(k, v);
+    }
+    if (tid == 0) scales[r] = bad ? NAN : s;
   }
 }
 
@@ -81,6 +123,16 @@ __global__ __launch_bounds__(256) void q8_copy(Linear8 x) {
 template <typename T>
 struct Scaled {
   Linear8 x;
+
+  __device__ __forceinline__ void few(int32_t m, int32_t n, i32x4 sums) const {
+    if (n >= x.out) return;
+    float v[4];
+    load4(x.scales, n, x.out, v);
+    const float s = x.x_scales[m];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = static_cast<float>(sums[q]) * s * v[q];
+    store4(static_cast<T*>(x.y) + m * x.y_stride, n, x.out, v);
+  }
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(i32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
@@ -114,6 +166,11 @@ hipError_t launch(const Linear8& x, hipStream_t st) {
   q8_rows<T><<<row_blocks(x.tokens), 256, 0, st>>>(static_cast<const T*>(x.x), x.x_stride,
                                                    x.tokens, x.dim, x.q, x.pitch, x.pitch,
                                                    x.x_scales);
+  if (x.tokens <= kFewRows) {
+    run_few<int8_t>(Few{x.q, x.pitch, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.out,
+                        x.dim}, Scaled<T>{x}, st);
+    return hipGetLastError();
+  }
   const bool copy = !aligned16(x.w) || x.w_stride % 16 != 0 || x.dim % 16 != 0;
   if (copy) {
     const int64_t n = (static_cast<int64_t>(x.out) * x.pitch + 255) / 256;

@@ -314,6 +314,7 @@ hipError_t launch(const Orthogonal& x, hipStream_t st) {
   p.terms = x.values == 2 ? 3 : 1;
   p.batch = static_cast<int32_t>(x.batch);
   p.splits = 1;
+  p.eighths = 1;
   for (int32_t s = 0; s < x.steps; ++s) {
     const f16_t* const now = x.now[s & 1];
     p.symmetric = 1;
@@ -337,8 +338,7 @@ hipError_t launch(const Orthogonal& x, hipStream_t st) {
       p.b = operand(x.poly, false, side, square, side);
     }
     const auto last = [&](const auto& epi) {
-      if (wide) run_product<f16_t, false, true>(p, epi, st);
-      else run_product<f16_t, false, false>(p, epi, st);
+      run_product<f16_t, false, true>(p, epi, st);  // (B = B^T)
     };
     if (s + 1 < x.steps)
       last(Keep<kNext>{x.now[~s & 1], nullptr, x.batch * all, x.rows8, x.cols8, x.values, x.a,

@@ -30,6 +30,13 @@ struct Product {
   int32_t splits;  // parts of k, each summed by a workgroup of its own
   int32_t part;    // k of a part, a multiple of a stage's
   int32_t tiles_m, tiles_n;
+  // An XCD takes an eighth of all tiles, not runs of them in turn.  With many pairs, each stays
+  // with one XCD: 64 pairs, 2,048 x 1,024 by 1,024 x 1,024 of float16, 310 us in eighths and 342 in
+  // runs; 4 pairs, 2,048 x 4,096 by its transposed self, three products, 315 and 356; 7 of 666 x
+  // 501, 20 and 27.  One pair with few rows and very many columns: 8,192 x 131,072 x 2,048, nothing
+  // written, 4.5 and 4.9 ms; but with its results written a piece of 32,768 columns takes 1.23 and
+  // 1.18, and 8,192 x 2,048 x 32,768 1.10 and 0.96.
+  int32_t eighths;
   int32_t symmetric;  // C = C^T: tiles with n0 >= m0 alone
 };
 
@@ -191,14 +198,15 @@ template <class TILE>
 __host__ __device__ inline int32_t numbers_of(const Product& p) {
   constexpr int32_t round = 8 * TILE::RUN;
   const int32_t tiles = tiles_of_pair<TILE>(p) * p.batch * p.splits;
-  return tiles < round ? (tiles + 7) / 8 * 8 : (tiles + round - 1) / round * round;
+  return p.eighths || tiles < round ? (tiles + 7) / 8 * 8 : (tiles + round - 1) / round * round;
 }
 
 // false: there is no tile of this number.
 template <class TILE>
 __device__ __forceinline__ bool place_of(const Product& p, int32_t number, Place* at) {
   const int32_t each = tiles_of_pair<TILE>(p);
-  const int32_t id = spread(number, each * p.batch * p.splits, TILE::RUN);
+  const int32_t all = each * p.batch * p.splits;
+  const int32_t id = spread(number, all, p.eighths ? (all + 7) / 8 : TILE::RUN);
   if (id < 0) return false;
   const int32_t outer = id / each, in = id - outer * each;
   const int2 t = p.symmetric ? symmetric_place<TILE>(in, p.tiles_m)
@@ -328,8 +336,11 @@ void with_tile(Product p, const F& f) {
   };
   if constexpr (sizeof(T) < 4) {
     if constexpr (TRA || TRB)
-      if (tiles(LargeTile::BM, LargeTile::BN) >= 512) return f(LargeTile());
-    if (tiles(MiddleTile::BM, MiddleTile::BN) >= 256) return f(MiddleTile());
+      if (!p.symmetric && tiles(LargeTile::BM, LargeTile::BN) >= 512) return f(LargeTile());
+    // (few rows: bound by reading the other operand, of which small tiles have more on its way: 64
+    // rows by 16,384 of 4,096, 26 us and 43)
+    if (p.a.rows > SmallTile::BM && tiles(MiddleTile::BM, MiddleTile::BN) >= 256)
+      return f(MiddleTile());
   }
   f(SmallTile());
 }
