@@ -17,9 +17,15 @@ struct Entropy {
   const uint8_t* valid;  // of the classes, or null
   // pieces of the classes: of a forward and of a backward pass
   int32_t piece, parts;  // classes of a piece; tiles of its columns, at most
-  bool copy_x, copy_w, few;
+  bool copy_x, copy_w;
+  bool few;       // tokens that read w once, as it is
+  bool two;       // binary32 operands in two float16 values, copies always
   void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the ends
   void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
+  float* fx;      // of operands in two values: the powers of two of the rows of xc,
+  float* fw;      // and of wc
+  int32_t pieces;
+  uint32_t* most;  // [1 + pieces] bits of the largest of fx, of each piece's fw; backward
   // forward
   float* loss;
   float* stats;   // [2][tokens]: the largest logit, and the sum of exp(logit - largest)
@@ -29,6 +35,7 @@ struct Entropy {
   const float* dloss;
   float* factor;  // 2: what dloss is multiplied by where the logits' gradients are kept, and back
   void* d;        // [tokens][piece] gradients of the logits
+  void* dt;       // of operands in two values those for the product with x
   int32_t splits_x, splits_w;
   float* dxp;     // [splits_x][tokens][pitch]
   float* dwp;     // [splits_w][piece][pitch], where splits_w > 1

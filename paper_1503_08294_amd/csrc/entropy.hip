@@ -20,6 +20,8 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 constexpr int64_t kFill = 512;
 constexpr int64_t kFewTokens = 32;  // that few_rows() takes
 constexpr int64_t kPartCols = 32;   // columns of a part, at least
+// Tokens from which on binary32 operands are split up into two float16 values.
+constexpr int64_t kTwoTokens = 192;
 
 bool params_ok(const gsn_entropy_params* p) {
   return p && p->dtype >= GSN_F32 && p->dtype <= GSN_F16 && p->tokens >= 0 &&
@@ -39,10 +41,9 @@ struct Carver {
 
 int32_t split_of(int64_t rows, int64_t cols, int64_t k, int32_t dtype) {
   const int64_t tiles =
-      up_to(rows, kSmallRows) / kSmallRows * (up_to(cols, kSmallRows) / kSmallRows);
+      up_to(rows, kMiddleRows) / kMiddleRows * (up_to(cols, kMiddleRows) / kMiddleRows);
   const int64_t bytes = k * static_cast<int64_t>(size_of(dtype));
-  const int64_t fill = dtype == GSN_F32 ? 3 * kFill : kFill;
-  return static_cast<int32_t>(std::max<int64_t>(1, std::min(fill / tiles, bytes / 1024)));
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min(kFill / tiles, bytes / 1024)));
 }
 
 Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
@@ -54,7 +55,8 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   x.dim = p.dim;
   // (rows of the copies and of d are whole lines of 128 bytes: products read rows that begin inside
   // a line up to a fifth slower)
-  x.pitch = static_cast<int32_t>(up_to(p.dim, 128 / size));
+  x.two = p.dtype == GSN_F32 && p.tokens >= kTwoTokens;
+  x.pitch = static_cast<int32_t>(up_to(p.dim, 64));
   int64_t piece = kPieceBytes / (size * x.pitch);
   if (backward) piece = std::min(piece, kPieceBytes / (size * tokens));
   else piece = std::min(piece, kPartBytes / (8 * tokens) * kSmallRows);
@@ -62,11 +64,22 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
   x.few = !backward && p.tokens <= kFewTokens;
   if (x.few) piece = up_to(p.classes, 256);
-  x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 128 / size)));
+  x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 64)));
+  x.pieces = (p.classes - 1) / x.piece + 1;
   x.parts = static_cast<int32_t>(up_to(x.piece, kPartCols) / kPartCols);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
   x.splits_w = split_of(x.piece, x.pitch, tokens, p.dtype);
   return x;
+}
+
+// What operands in two values need besides (a tile reads the powers of two of whole tiles).
+void carve_two(Carver* c, Entropy* x, bool backward) {
+  if (!x->two) return;
+  x->fx = static_cast<float*>(c->take(4 * static_cast<size_t>(x->tokens)));
+  x->fw = static_cast<float*>(c->take(4 * (static_cast<size_t>(x->piece) + kTileRows)));
+  if (!backward) return;
+  x->most = static_cast<uint32_t*>(c->take(4 * (1 + static_cast<size_t>(x->pieces))));
+  x->dt = c->take(4 * static_cast<size_t>(x->tokens) * x->piece);
 }
 
 size_t carve_forward(void* base, int32_t dtype, Entropy* x) {
@@ -76,6 +89,7 @@ size_t carve_forward(void* base, int32_t dtype, Entropy* x) {
     x->xc = c.take(s * t * x->pitch);
     x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
   }
+  carve_two(&c, x, false);
   x->part = static_cast<float2*>(c.take(8 * t * x->parts));
   x->chosen = static_cast<float*>(c.take(4 * t));
   float* const stats = static_cast<float*>(c.take(8 * t));
@@ -90,6 +104,7 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
   x->xc = c.take(s * t * x->pitch);
   x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
   x->d = c.take(s * t * x->piece);
+  carve_two(&c, x, true);
   x->dxp = static_cast<float*>(c.take(4 * t * x->pitch * static_cast<size_t>(x->splits_x)));
   x->dwp = x->splits_w > 1
                ? static_cast<float*>(c.take(4 * static_cast<size_t>(x->piece) * x->pitch *
@@ -100,7 +115,7 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
 
 // Whether the grids of a call's products stay below 2^32 threads of 256.
 bool grids_ok(const Entropy& x, int32_t dtype, bool backward) {
-  const int64_t side = dtype == GSN_F32 ? kSmallRows : kMiddleRows;
+  const int64_t side = dtype == GSN_F32 && !x.two ? kSmallRows : kMiddleRows;
   const auto tiles = [&](int64_t m, int64_t n) {
     return up_to(m, side) / side * (up_to(n, side) / side);
   };
@@ -156,8 +171,8 @@ int gsn_cross_entropy(const gsn_entropy_params* p, const void* x, int64_t x_stri
   a.valid = valid;
   a.loss = loss;
   a.stats = stats;
-  a.copy_x = !gsn::in_place(x, x_stride, p->dim, p->dtype);
-  a.copy_w = !gsn::in_place(w, w_stride, p->dim, p->dtype);
+  a.copy_x = a.two || !gsn::in_place(x, x_stride, p->dim, p->dtype);
+  a.copy_w = a.two || !gsn::in_place(w, w_stride, p->dim, p->dtype);
   gsn::carve_forward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32    ? gsn::launch_entropy<float>(a, st)
@@ -190,9 +205,9 @@ int gsn_cross_entropy_backward(const gsn_entropy_params* p, const float* dloss, 
   a.stats = const_cast<float*>(stats);
   a.dx = p->tokens > 0 ? dx : nullptr;
   a.dw = dw;
-  a.copy_x = !gsn::in_place(x, x_stride, p->dim, p->dtype);
+  a.copy_x = a.two || !gsn::in_place(x, x_stride, p->dim, p->dtype);
   // (the product with w meets its classes that are not valid as zeros)
-  a.copy_w = valid || !gsn::in_place(w, w_stride, p->dim, p->dtype);
+  a.copy_w = a.two || valid || !gsn::in_place(w, w_stride, p->dim, p->dtype);
   gsn::carve_backward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32 ? gsn::launch_entropy_backward<float>(a, st)

@@ -4,6 +4,12 @@
 //   d = dloss (exp(l) / sum exp(l) - [c = target]),  dx = d w,  dw = d^T x
 // The logits are not kept: a tile of them is reduced to its rows' largest value and sum of
 // exponentials, and the backward pass makes them again, a piece of the classes at a time, as d.
+//
+// Binary32 operands in two values (TWO): the matrix cores multiply float16 at 9 times the rate that
+// they multiply binary32 at (1.43 and 0.153 PFLOP/s in large library products).  A row of x or w is
+// kept times a power of two, which takes its largest element to 2^14 to 2^15, as hi = float16(v)
+// and lo = float16(v - hi): 22 bits of every element down to 2^-18 of the largest, 2^-40 of it
+// below.  A product is hi lo + lo hi + hi hi, three products of one binary32 sum.
 #pragma once
 
 #include "entropy.h"
@@ -50,8 +56,28 @@ __device__ __forceinline__ float2 merged(float2 a, float2 b) {
   return float2{m, a.y * expf(a.x - base) + b.y * expf(b.x - base)};
 }
 
+// The logits of rows and columns that were kept times a power of two.
+template <int MT, int NT>
+__device__ __forceinline__ void unscale(const Entropy& x, f32x4 (&acc)[MT][NT], int64_t m,
+                                        int32_t n, int lane) {
+  f32x4 cols[NT];
+  // (columns past the last class are not used, but read: fw has room for them)
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+    cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j + (lane >> 4) * 4);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t t = m + 16 * i + (lane & 15);
+    const float row = x.fx[t < x.tokens ? t : x.tokens - 1];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[i][j][q] *= row * cols[j][q];
+  }
+}
+
 // A tile of the logits -> (largest, sum) of each row, and the target's logit.
-template <typename T>
+template <typename T, bool TWO>
 struct Reduce {
   Entropy x;
   int32_t first;  // the piece's first class
@@ -64,6 +90,7 @@ struct Reduce {
     float2* const rows = reinterpret_cast<float2*>(smem);  // [2][BM]
     const int32_t n = first + at.n0 + nw + lg;
     const uint32_t shut = shut_columns<NT>(x.valid, x.classes, n);
+    if constexpr (TWO) unscale(x, acc, int64_t{at.m0} + mw, at.n0 + nw, lane);
     if (__any(shut != 0))
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -186,12 +213,48 @@ __global__ __launch_bounds__(kJoinTokens* kJoinWaves) void ce_join(Entropy x, in
   finish_token(x, t, v, last);
 }
 
-// A tile of the logits -> their gradients, rounded to the type of the operands of the two products
-// that take them.
-template <typename T>
+// 16 rows from t0 on of the logits' gradients, columns n0 on, in 2- or 4-byte elements.
+template <typename E, int NT>
+__device__ __forceinline__ void store_rows(const Entropy& x, void* d, const f32x4 (&v)[NT],
+                                           int64_t t0, int32_t n0, int lane, char* room) {
+  using Lines = Turn<E, 16 * NT>;
+  const Lines turn{room};
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const float some[4] = {v[j][0], v[j][1], v[j][2], v[j][3]};
+    turn.put(lane & 15, 16 * j + (lane >> 4) * 4, some);
+  }
+  wave_fence();
+  const int64_t left = x.tokens - t0;
+  turn.out(static_cast<E*>(d) + t0 * x.piece + n0, x.piece,
+           static_cast<int32_t>(left < 16 ? left : 16), x.piece - n0, lane);
+  wave_fence();
+}
+
+// The same as two float16 values each, of which the second comes `other` elements later.
+template <int NT>
+__device__ __forceinline__ void store_two(const Entropy& x, void* d, f32x4 (&v)[NT], int64_t t0,
+                                          int32_t n0, int lane, char* room) {
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[j][q] = settled(v[j][q]);
+  store_rows<f16_t>(x, d, v, t0, n0, lane, room);
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[j][q] -= to_float(from_float<f16_t>(v[j][q]));
+  store_rows<f16_t>(x, static_cast<f16_t*>(d) + x.tokens * x.piece, v, t0, n0, lane, room);
+}
+
+// A tile of the logits -> their gradients, as the operands of the two products that take them: of
+// one type rounded to it; of binary32 in two values as d for the product with w, times the class's
+// power of two (at most 2^11) and without dloss, and as dt for the product with x, times the
+// token's power of two and dloss (at most 2^11).
+template <typename T, bool TWO>
 struct Gradient {
   Entropy x;
-  int32_t first, count;  // the piece's classes
+  int32_t first, index;  // the piece's first class, and its number
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
@@ -199,13 +262,21 @@ struct Gradient {
     const int li = lane & 15, lg = (lane >> 4) * 4;
     const int32_t n = at.n0 + nw + lg;
     const uint32_t shut = shut_columns<NT>(x.valid, x.classes, first + n);
-    const float factor = __is_same(T, f16_t) ? x.factor[0] : 1.0f;
-    // (columns up to the rows' pitch are written, zeros past the last class)
-    const int32_t cols = x.piece;
+    constexpr bool kScaled = TWO || __is_same(T, f16_t);
+    const float factor = kScaled ? x.factor[0] : 1.0f;
     const bool masked = __any(shut != 0);
-    Turn<T, 16 * NT> turn{smem + threadIdx.x / kWave * Turn<T, 16 * NT>::kBytes};
-    static_assert(4 * Turn<T, 16 * NT>::kBytes <= TILE::kLds);
-    T* const to = static_cast<T*>(x.d) + at.n0 + nw;
+    char* const room = smem + threadIdx.x / kWave * (TILE::kLds / 4);
+    static_assert(Turn<std::conditional_t<TWO, f16_t, T>, 16 * NT>::kBytes <= TILE::kLds / 4);
+    f32x4 cols[TWO ? NT : 1];
+    float most_x = 1.0f;
+    if constexpr (TWO) {
+      unscale(x, acc, int64_t{at.m0} + mw, at.n0 + nw, lane);
+      most_x = 1.0f / __uint_as_float(x.most[0]);
+      const float most_w = 1.0f / __uint_as_float(x.most[1 + index]);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j) * most_w * 2048.0f;
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int64_t t0 = at.m0 + mw + 16 * i, t = t0 + li;
@@ -213,7 +284,7 @@ struct Gradient {
       const int64_t tt = t < x.tokens ? t : x.tokens - 1;
       const int32_t target = target_of(x, tt);
       const int32_t place = target - first - n;
-      const float top = x.stats[tt], g = x.dloss[tt] * factor;
+      const float top = x.stats[tt], g = TWO ? 1.0f : x.dloss[tt] * factor;
       const float each = g / x.stats[x.tokens + tt];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
@@ -233,16 +304,26 @@ struct Gradient {
           for (int q = 0; q < 4; ++q)
             if (target < 0 || (shut >> (4 * j + q) & 1)) acc[i][j][q] = 0.0f;
       }
+      if constexpr (TWO) {
+        f32x4 v[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-        turn.put(li, 16 * j + lg, v);
+        for (int j = 0; j < NT; ++j) v[j] = acc[i][j] * cols[j];
+        // (columns past the last class have no power of two: their zeros are made again)
+        if (masked)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (shut >> (4 * j + q) & 1) v[j][q] = 0.0f;
+        store_two(x, x.d, v, t0, at.n0 + nw, lane, room);
+        // (a token without a target may have any dloss)
+        const float h = target < 0 ? 0.0f : x.dloss[tt] * factor * (x.fx[tt] * most_x);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) v[j] = acc[i][j] * h;
+        store_two(x, x.dt, v, t0, at.n0 + nw, lane, room);
+      } else {
+        store_rows<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
       }
-      wave_fence();
-      const int64_t left = x.tokens - t0;
-      turn.out(to + t0 * x.piece, x.piece, static_cast<int32_t>(left < 16 ? left : 16),
-               cols - at.n0 - nw, lane);
-      wave_fence();
     }
   }
 };
@@ -253,11 +334,18 @@ struct Partial {
   int64_t split;  // elements from a split to the next
   int32_t rows, pitch;
   int32_t add;
+  // of operands in two values: what the sums are multiplied by, bits of a power of two, a number
+  // (or null) and a constant
+  const uint32_t* power;
+  const float* number;
+  float constant;
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+    const float factor =
+        power ? __uint_as_float(*power) * constant * (number ? *number : 1.0f) : 1.0f;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
@@ -267,14 +355,15 @@ struct Partial {
       for (int j = 0; j < NT; ++j) {
         if (n + 16 * j >= pitch) break;
         f32x4* const p = reinterpret_cast<f32x4*>(row + n + 16 * j);
-        *p = add ? acc[i][j] + *p : acc[i][j];
+        const f32x4 v = acc[i][j] * factor;
+        *p = add ? v + *p : v;
       }
     }
   }
 };
 
 // A tile of dw, rounded to its type.
-template <typename T>
+template <typename T, bool TWO>
 struct Weights {
   Entropy x;
   int32_t first, count;
@@ -283,7 +372,9 @@ struct Weights {
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
-    const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
+    const float factor = TWO                    ? x.factor[1] * __uint_as_float(x.most[0])
+                         : __is_same(T, f16_t) ? x.factor[1]
+                                               : 1.0f;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
@@ -303,11 +394,11 @@ struct Weights {
 
 // The splits' sums, and their one rounding.  Rows without a target, or that are no valid class, are
 // zeros.
-template <typename T, bool OF_TOKENS>
+template <typename T, bool OF_TOKENS, bool TWO>
 __global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict__ part,
                                               int32_t splits, int64_t rows, int32_t first,
                                               int64_t split, T* __restrict__ out) {
-  const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
+  const float all = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
   const int32_t each = (x.dim + 3) / 4;
   for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < rows * each;
        at += static_cast<int64_t>(gridDim.x) * 256) {
@@ -318,6 +409,7 @@ __global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict
     if (live)
       for (int32_t i = 0; i < splits; ++i)
         s += *reinterpret_cast<const f32x4*>(part + i * split + r * x.pitch + d);
+    const float factor = TWO && OF_TOKENS && live ? x.dloss[r] : all;
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = s[q] * factor;
@@ -347,10 +439,79 @@ __global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t 
   }
 }
 
+// Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends; the power of
+// two that gives the row back, and the largest of them (as bits of positive numbers, whose largest
+// is the same in any order).
+template <bool OF_TOKENS, bool DEAD>
+__global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t first,
+                                                f16_t* __restrict__ out, float* __restrict__ power,
+                                                uint32_t* __restrict__ most) {
+  const float* const from = static_cast<const float*>(OF_TOKENS ? x.x : x.w);
+  const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
+  const int lane = threadIdx.x % kWave;
+  const int64_t other = (OF_TOKENS ? x.tokens : int64_t{x.piece}) * x.pitch;
+  __shared__ uint32_t some[4];
+  uint32_t largest = 0;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; r < rows;
+       r += static_cast<int64_t>(gridDim.x) * 4) {
+    const bool live =
+        !DEAD || (OF_TOKENS ? target_of(x, r) >= 0 : !(x.valid && !x.valid[first + r]));
+    const float* const row = from + (first + r) * stride;
+    float top = 0.0f;
+    if (live)
+      for (int32_t k = lane * 4; k < x.dim; k += kWave * 4) {
+        float v[4];
+        load4(row, k, x.dim, v);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) top = fmaxf(top, fabsf(v[q]));
+      }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    // (rows below 2^-86 keep fewer bits, so that the power and its inverse are normal numbers; what
+    // is not finite stays so)
+    int up = 0;
+    if (top > 0.0f && top < INFINITY) {
+      frexpf(top, &up);
+      up = 15 - up < 100 ? 15 - up : 100;
+    }
+    const float back = top > 0.0f ? ldexpf(1.0f, -up) : 0x1p-126f;  // (zeros: the smallest)
+    for (int32_t k = lane * 8; k < x.pitch; k += kWave * 8) {
+      float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (live) {
+        load4(row, k, x.dim, v);
+        load4(row, k + 4, x.dim, v + 4);
+      }
+      Vec<f16_t, 8> hi, lo;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float w = settled(ldexpf(v[q], up));
+        hi.v[q] = from_float<f16_t>(w);
+        lo.v[q] = from_float<f16_t>(w - to_float(hi.v[q]));
+      }
+      f16_t* const to = out + r * x.pitch + k;
+      *reinterpret_cast<Vec<f16_t, 8>*>(to) = hi;
+      *reinterpret_cast<Vec<f16_t, 8>*>(to + other) = lo;
+    }
+    if (lane == 0) power[r] = back;
+    largest = max(largest, __float_as_uint(back));
+  }
+  if (!most) return;
+  if (lane == 0) some[threadIdx.x / kWave] = largest;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  largest = max(max(some[0], some[1]), max(some[2], some[3]));
+  // (most workgroups have nothing larger to tell: 10,007 rows took 118 us when all did)
+  if (largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+    atomicMax(most, largest);
+}
+
 // Gradients of the logits in float16 are kept times 2^11 / max |dloss|: at most 2^11, and those of
-// small probabilities are not lost (2^-25 of the largest dloss still has all of its 11 bits).
+// small probabilities are not lost (2^-25 of the largest dloss still has all of its 11 bits).  And
+// the largest powers of two of the rows in two values begin (2^-126, were all rows zeros).
 __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   __shared__ float some[16];
+  for (int32_t i = threadIdx.x; i <= x.pieces; i += 1024)
+    if (x.most) x.most[i] = 0x00800000u;
   float m = 0.0f;
   for (int64_t t = threadIdx.x; t < x.tokens; t += 1024) {
     if (target_of(x, t) < 0) continue;
@@ -382,54 +543,79 @@ Operand operand_of(const void* p, int64_t ld, int64_t rows) {
   return Operand{static_cast<const char*>(p), {0, 0}, ld * kSize, 0, static_cast<int32_t>(rows)};
 }
 
-// A product's parts of k: `splits` of them, whole stages.
-template <typename T>
+// An operand in two values: of the terms hi lo, lo hi, hi hi (the small ones first: fewer roundings
+// of a large sum), where `lo` is `other` elements behind hi.
+Operand pair_of(const void* p, int64_t ld, int64_t rows, int64_t other, bool first) {
+  const int64_t lo = 2 * other;
+  return Operand{static_cast<const char*>(p) + (first ? 0 : lo),
+                 {first ? lo : -lo, first ? -lo : 0}, 2 * ld, 0, static_cast<int32_t>(rows)};
+}
+
+// A product's parts of k: `splits` of them, whole stages (of any tile).
+template <typename E>
 void split(Product* p, int32_t splits) {
-  constexpr int32_t kBK = kRowBytes / sizeof(T);
+  constexpr int32_t kBK = kRowBytes / sizeof(E);
   p->splits = splits;
   p->part = ((p->k + splits - 1) / splits + kBK - 1) / kBK * kBK;
 }
 
-// x or its copy, w from class `first` on or its copy.
-template <typename T>
+// x or its copy by w from class `first` on or its copy.
+template <typename T, bool TWO>
 Product logits_of(const Entropy& x, int32_t first, int32_t count) {
   Product p{};
-  p.a = x.copy_x ? operand_of<T>(x.xc, x.pitch, x.tokens)
-                 : operand_of<T>(x.x, x.x_stride, x.tokens);
-  p.b = x.copy_w ? operand_of<T>(x.wc, x.pitch, count)
-                 : operand_of<T>(static_cast<const T*>(x.w) + first * x.w_stride, x.w_stride,
-                                 count);
-  p.terms = p.batch = 1;
+  if constexpr (TWO) {
+    p.a = pair_of(x.xc, x.pitch, x.tokens, x.tokens * x.pitch, true);
+    p.b = pair_of(x.wc, x.pitch, count, int64_t{x.piece} * x.pitch, false);
+    p.terms = 3;
+  } else {
+    p.a = x.copy_x ? operand_of<T>(x.xc, x.pitch, x.tokens)
+                   : operand_of<T>(x.x, x.x_stride, x.tokens);
+    p.b = x.copy_w ? operand_of<T>(x.wc, x.pitch, count)
+                   : operand_of<T>(static_cast<const T*>(x.w) + first * x.w_stride, x.w_stride,
+                                   count);
+    p.terms = 1;
+  }
+  p.batch = 1;
   p.k = x.dim;
   split<T>(&p, 1);
   return p;
 }
 
-}  // namespace
-
-template <typename T>
-hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
+// The copies of x and of a piece of w.
+template <typename T, bool TWO, bool DEAD>
+void copy_tokens(const Entropy& x, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
-  if (x.few) {
-    run_few<T>(Few{x.x, x.x_stride, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.classes,
-                   x.dim}, ReduceFew{x}, st);
-    ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(
-        x, (x.classes + kFewCols - 1) / kFewCols, 1, 1);
-    return hipGetLastError();
-  }
-  if (x.copy_x)
-    ce_rows<T, true, false><<<some_blocks(x.tokens * row), 256, 0, st>>>(
-        x, x.tokens, 0, static_cast<T*>(x.xc));
+  if constexpr (TWO)
+    ce_pairs<true, DEAD><<<some_blocks(x.tokens * kWave), 256, 0, st>>>(
+        x, x.tokens, 0, static_cast<f16_t*>(x.xc), x.fx, x.most);
+  else
+    ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
+                                                                        static_cast<T*>(x.xc));
+}
+template <typename T, bool TWO, bool DEAD>
+void copy_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
+  const int64_t row = x.pitch / (16 / sizeof(T));
+  if constexpr (TWO)
+    ce_pairs<false, DEAD><<<some_blocks(int64_t{count} * kWave), 256, 0, st>>>(
+        x, count, first, static_cast<f16_t*>(x.wc), x.fw,
+        x.most ? x.most + 1 + first / x.piece : nullptr);
+  else
+    ce_rows<T, false, DEAD><<<some_blocks(count * row), 256, 0, st>>>(x, count, first,
+                                                                      static_cast<T*>(x.wc));
+}
+
+template <typename T, bool TWO>
+void forward(const Entropy& x, hipStream_t st) {
+  using E = std::conditional_t<TWO, f16_t, T>;
+  if (x.copy_x) copy_tokens<T, TWO, false>(x, st);
   for (int32_t first = 0; first < x.classes; first += x.piece) {
     const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    if (x.copy_w)
-      ce_rows<T, false, false><<<some_blocks(count * row), 256, 0, st>>>(
-          x, count, first, static_cast<T*>(x.wc));
-    Product p = logits_of<T>(x, first, count);
+    if (x.copy_w) copy_classes<T, TWO, false>(x, first, count, st);
+    Product p = logits_of<T, TWO>(x, first, count);
     p.eighths = 1;
     int32_t parts = 0;
-    with_tile<T, false, false>(p, [&](auto tile) { parts = tiles_of(count, tile.BN); });
-    run_product<T, false, false>(p, Reduce<T>{x, first}, st);
+    with_tile<E, false, false>(p, [&](auto tile) { parts = tiles_of(count, tile.BN); });
+    run_product<E, false, false>(p, Reduce<T, TWO>{x, first}, st);
     // (of 64 tokens, 782 parts: 10.5 us by lanes)
     if (x.tokens <= 1024)
       ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(
@@ -439,54 +625,87 @@ hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
                 kJoinTokens * kJoinWaves, 0, st>>>(x, parts, first == 0,
                                                    first + count == x.classes);
   }
+}
+
+template <typename T, bool TWO>
+void backward(const Entropy& x, hipStream_t st) {
+  using E = std::conditional_t<TWO, f16_t, T>;
+  if (TWO || __is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
+  copy_tokens<T, TWO, true>(x, st);
+  for (int32_t first = 0; first < x.classes; first += x.piece) {
+    const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
+    const int32_t index = first / x.piece;
+    if (x.copy_w) copy_classes<T, TWO, true>(x, first, count, st);
+    const Product l = logits_of<T, TWO>(x, first, count);
+    run_product<E, false, false>(l, Gradient<T, TWO>{x, first, index}, st);
+    const int64_t other_d = x.tokens * x.piece;
+    if (x.dx) {
+      Product p = l;
+      p.a = TWO ? pair_of(x.d, x.piece, x.tokens, other_d, true)
+                : operand_of<E>(x.d, x.piece, x.tokens);
+      p.b.rows = x.dim;
+      p.k = count;
+      split<E>(&p, x.splits_x);
+      const int64_t each = x.tokens * x.pitch;
+      run_product<E, false, true>(
+          p, Partial{x.dxp, each, static_cast<int32_t>(x.tokens), x.pitch, first > 0,
+                     TWO ? x.most + 1 + index : nullptr, nullptr, 1.0f / 2048.0f}, st);
+    }
+    if (x.dw) {
+      Product p{};
+      p.a = TWO ? pair_of(x.dt, x.piece, count, other_d, true)
+                : operand_of<E>(x.d, x.piece, count);
+      p.b = TWO ? pair_of(x.xc, x.pitch, x.dim, x.tokens * x.pitch, false)
+                : operand_of<E>(x.xc, x.pitch, x.dim);
+      p.terms = l.terms;
+      p.batch = 1;
+      p.k = static_cast<int32_t>(x.tokens);
+      split<E>(&p, x.splits_w);
+      if (x.splits_w > 1) {
+        const int64_t each = int64_t{x.piece} * x.pitch;
+        run_product<E, true, true>(
+            p, Partial{x.dwp, each, count, x.pitch, 0, TWO ? x.most : nullptr,
+                       TWO ? x.factor + 1 : nullptr, 1.0f}, st);
+        ce_sum<T, false, TWO><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
+            x, x.dwp, x.splits_w, count, first, each, static_cast<T*>(x.dw));
+      } else {
+        run_product<E, true, true>(p, Weights<T, TWO>{x, first, count}, st);
+      }
+    }
+  }
+  if (x.dx)
+    ce_sum<T, true, TWO><<<some_blocks(x.tokens * ((x.dim + 3) / 4)), 256, 0, st>>>(
+        x, x.dxp, x.splits_x, x.tokens, 0, x.tokens * x.pitch, static_cast<T*>(x.dx));
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
+  if (x.few) {
+    run_few<T>(Few{x.x, x.x_stride, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.classes,
+                   x.dim}, ReduceFew{x}, st);
+    ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(
+        x, (x.classes + kFewCols - 1) / kFewCols, 1, 1);
+    return hipGetLastError();
+  }
+  if constexpr (sizeof(T) == 4)
+    if (x.two) {
+      forward<T, true>(x, st);
+      return hipGetLastError();
+    }
+  forward<T, false>(x, st);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_entropy_backward(const Entropy& x, hipStream_t st) {
-  const int64_t row = x.pitch / (16 / sizeof(T));
-  if (__is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
-  ce_rows<T, true, true><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
-                                                                      static_cast<T*>(x.xc));
-  for (int32_t first = 0; first < x.classes; first += x.piece) {
-    const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    if (x.copy_w)
-      ce_rows<T, false, true><<<some_blocks(count * row), 256, 0, st>>>(
-          x, count, first, static_cast<T*>(x.wc));
-    const Product l = logits_of<T>(x, first, count);
-    run_product<T, false, false>(l, Gradient<T>{x, first, count}, st);
-    Operand d = operand_of<T>(x.d, x.piece, x.tokens);
-    if (x.dx) {
-      Product p = l;
-      p.a = d;
-      p.b.rows = x.dim;
-      p.k = count;
-      split<T>(&p, x.splits_x);
-      const int64_t each = x.tokens * x.pitch;
-      run_product<T, false, true>(
-          p, Partial{x.dxp, each, static_cast<int32_t>(x.tokens), x.pitch, first > 0}, st);
+  if constexpr (sizeof(T) == 4)
+    if (x.two) {
+      backward<T, true>(x, st);
+      return hipGetLastError();
     }
-    if (x.dw) {
-      Product p{};
-      p.a = d;
-      p.a.rows = count;
-      p.b = operand_of<T>(x.xc, x.pitch, x.dim);
-      p.terms = p.batch = 1;
-      p.k = static_cast<int32_t>(x.tokens);
-      split<T>(&p, x.splits_w);
-      if (x.splits_w > 1) {
-        const int64_t each = int64_t{x.piece} * x.pitch;
-        run_product<T, true, true>(p, Partial{x.dwp, each, count, x.pitch, 0}, st);
-        ce_sum<T, false><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
-            x, x.dwp, x.splits_w, count, first, each, static_cast<T*>(x.dw));
-      } else {
-        run_product<T, true, true>(p, Weights<T>{x, first, count}, st);
-      }
-    }
-  }
-  if (x.dx)
-    ce_sum<T, true><<<some_blocks(x.tokens * ((x.dim + 3) / 4)), 256, 0, st>>>(
-        x, x.dxp, x.splits_x, x.tokens, 0, x.tokens * x.pitch, static_cast<T*>(x.dx));
+  backward<T, false>(x, st);
   return hipGetLastError();
 }
 

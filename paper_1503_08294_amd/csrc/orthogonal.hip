@@ -45,14 +45,6 @@ struct Orthogonal {
   f16_t* poly;     // B
 };
 
-// v as a binary32 value: what is made of it is made of the same one.  (Left to the compiler, a
-// product may be fused with its rounding to float16, and a second value that is made of the product
-// as rounded to binary32 does not belong to the first where that is a tie.)
-__device__ __forceinline__ float settled(float v) {
-  asm("" : "+v"(v));
-  return v;
-}
-
 // Eight elements of a row from column c on, of which those inside are used.
 template <typename T>
 __device__ __forceinline__ void load8(const T* row, int32_t c, int32_t cols, float* v) {

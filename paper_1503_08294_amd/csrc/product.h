@@ -101,6 +101,14 @@ __device__ __forceinline__ Frag fragment_any(const char* tile, int r0, int s, in
   }
 }
 
+// v as a binary32 value: what is made of it is made of the same one.  (Left to the compiler, a
+// product may be fused with its rounding to float16, and a second value that is made of the product
+// as rounded to binary32 does not belong to the first where that is a tie.)
+__device__ __forceinline__ float settled(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
+
 // What this lane loads of one operand's stages: of stage h the chunks j THR + thread for j = 0, 1,
 // ..., SIDE rows (or columns) of KB bytes of k in all.
 template <typename T, bool TR, int SIDE, int KB, int THR>

@@ -16,10 +16,13 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
     """A dict with loss, dx, dw and, for each, how far a result of the kernels may be off: *_tol.
 
     A logit is a sum of dim products in binary32, off by at most dim U sum |x w| (U = 2^-24): E at
-    most for a token.  exp(l - largest) is off by that twice, by (|l - largest| + 3) 2 U of the
+    most for a token.  Binary32 operands may be kept in two float16 values: each element to 2^-23 of
+    itself (and 2^-40 of its row's largest), the product of the two last ones, 2^-22 at most, left
+    out: 8 U more.  exp(l - largest) is off by that twice, by (|l - largest| + 3) 2 U of the
     exponential (its argument and itself), and the sum of the exponentials by one U for each of the
     additions that a term goes through, 64 + classes / 64 at most.  The gradients of the logits are
-    rounded to the operands' type, those of float16 as multiples of 2^-11 of the largest dloss.
+    rounded to the operands' type, those of float16 as multiples of 2^-11 of the largest dloss; in
+    two values to 2^-23, and to 2^-36 of the largest that one could be beside w's, or x's, largest.
     Their products with w and x are sums of binary32, the results are rounded once."""
     dtype = x.dtype
     classes, dim = w.shape
@@ -32,7 +35,9 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
     w = torch.where(there[:, None], w.double(), 0.0)
     l = (x @ w.t()).masked_fill(~there, -torch.inf)
     size = (x.abs() @ w.abs().t()).masked_fill(~there, 0.0)
-    err = dim * U * size.max(1, keepdim=True)[0]
+    two = dtype == torch.float32
+    err = (dim + 8 * two) * U * size.max(1, keepdim=True)[0] \
+        + two * dim * 2.0 ** -39 * x.abs().max() * w.abs().max()
     top = l.max(1, keepdim=True)[0]
     top = torch.where(top == -torch.inf, 0.0, top)
     e = torch.exp(l - top)
@@ -53,7 +58,7 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
     d.scatter_add_(1, at[:, None], torch.full_like(chosen, -1.0))
     d = d * g
     rel_p = rel_sum + 2 * err + (torch.where(p > 0, (l - top).abs(), 0.0) + 3) * 2 * U
-    ulp = HALF_ULP[dtype]
+    ulp = 2.0 ** -23 if two else HALF_ULP[dtype]
     step = HALF_STEP[dtype]
     if dtype == torch.float16:
         step = step * 2.0 ** -11 * g.abs().max()
@@ -63,8 +68,11 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
         tol = d_tol if name == "dx" else d_tol.t()
         v = a @ b
         out[name] = v
-        out[name + "_tol"] = (tol + (a.shape[1] + 4) * U * (a.abs() + tol)) @ b.abs() * (1 + ulp) \
+        out[name + "_tol"] = (tol + (a.shape[1] + 12) * U * (a.abs() + tol)) @ b.abs() * (1 + ulp) \
             + ulp * v.abs() + HALF_STEP[dtype]
+        if two:
+            out[name + "_tol"] += a.shape[1] * 2.0 ** -34 * b.abs().max() * (
+                g.abs() if name == "dx" else g.abs().max())
     return out
 
 

@@ -69,7 +69,9 @@ def check_entropy(learn, x, w, t, valid, dloss, what, view=lambda v: v.cuda()):
     return dx, dw
 
 
-SIZES = [(1, 1, 1), (1, 64, 100), (2, 8, 7), (3, 5, 129), (17, 33, 65), (64, 64, 64),
+# (from 192 tokens on binary32 operands are kept in two float16 values)
+SIZES = [(191, 40, 90), (192, 40, 90), (193, 1, 3), (1, 1, 1), (1, 64, 100), (2, 8, 7),
+         (3, 5, 129), (17, 33, 65), (64, 64, 64),
          (65, 128, 257), (130, 72, 513), (129, 501, 333), (257, 256, 1000)]
 
 
@@ -134,11 +136,34 @@ def test_entropy_large_and_small_logits(learn, dtype):
 
 @pytest.mark.parametrize("dtype,tokens,dim,classes", [
     (BF16, 300, 128, 33_000), (F16, 2_100, 64, 9_000), (F32, 1_100, 72, 5_000),
-    (BF16, 5_000, 264, 130), (F32, 40, 16, 40_000)])
+    (BF16, 5_000, 264, 130), (F32, 40, 16, 40_000), (F32, 5_000, 264, 130),
+    (F32, 300, 1_100, 900)])
 def test_entropy_many_classes_or_tokens(learn, dtype, tokens, dim, classes):
     """Tiles of 128, sums split up along the classes and along the tokens."""
     check_entropy(learn, *entropy_inputs(tokens, dim, classes, dtype, 6, shut=0.02, lost=0.02),
                   f"{dtype}")
+
+
+def test_entropy_rows_of_very_different_size(learn):
+    """Binary32 in two values: tokens and classes 2^-30 to 2^30 times the others' size, zeros."""
+    x, w, t, _, dloss = entropy_inputs(260, 48, 200, F32, 13)
+    t[t < 10] += 20
+    x[3] *= 2.0 ** -30
+    x[4] = 0
+    x[5] *= 2.0 ** -100
+    w[2] *= 2.0 ** -40
+    w[3] = 0
+    w[4] *= 2.0 ** -120
+    x[6] *= 2.0 ** 9
+    dloss[7] *= 2.0 ** -40
+    dx, dw = check_entropy(learn, x, w, t, None, dloss, "sizes")
+    want = ref.cross_entropy(x, w, t, None, dloss)["dx"][3]
+    # (a token's gradient does not depend on how small it is itself)
+    assert (dx[3].double().cpu() - want).norm() <= 1e-5 * want.norm()
+    z, v = torch.zeros_like(x), torch.zeros_like(w)
+    check_entropy(learn, z, w, t, None, dloss, "tokens of zeros")
+    check_entropy(learn, x, v, t, None, dloss, "classes of zeros")
+    check_entropy(learn, x * 2.0 ** 100, w * 2.0 ** -100, t, None, dloss, "far from 1")
 
 
 def test_entropy_in_pieces(learn):

@@ -1,6 +1,6 @@
-"""The loads to LDS of the learning operators' products set m0 in inline assembly, which cannot say so
-to the compiler: nothing else in these kernels may use it.  Checked in the assembly that the build's
-flags give (no GPU needed)."""
+"""The loads to LDS of the learning operators' products set m0 in inline assembly, which cannot say
+so to the compiler: nothing else in these kernels may use it.  Checked in the assembly that the
+build's flags give (no GPU needed)."""
 import os
 import re
 import subprocess
