@@ -532,6 +532,10 @@ __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   x.factor[1] = base / 2048.0f;
 }
 
+// A wave a row; few enough workgroups that they have little to tell each other (ce_pairs).
+inline uint32_t row_blocks(int64_t rows) {
+  return static_cast<uint32_t>(rows < 4 ? 1 : rows < 4096 ? rows / 4 : 1024);
+}
 inline uint32_t some_blocks(int64_t threads) {
   const int64_t n = (threads + 255) / 256;
   return static_cast<uint32_t>(n < 1 ? 1 : n < (1 << 16) ? n : 1 << 16);
@@ -586,7 +590,7 @@ template <typename T, bool TWO, bool DEAD>
 void copy_tokens(const Entropy& x, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
   if constexpr (TWO)
-    ce_pairs<true, DEAD><<<some_blocks(x.tokens * kWave), 256, 0, st>>>(
+    ce_pairs<true, DEAD><<<row_blocks(x.tokens), 256, 0, st>>>(
         x, x.tokens, 0, static_cast<f16_t*>(x.xc), x.fx, x.most);
   else
     ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
@@ -596,7 +600,7 @@ template <typename T, bool TWO, bool DEAD>
 void copy_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
   if constexpr (TWO)
-    ce_pairs<false, DEAD><<<some_blocks(int64_t{count} * kWave), 256, 0, st>>>(
+    ce_pairs<false, DEAD><<<row_blocks(count), 256, 0, st>>>(
         x, count, first, static_cast<f16_t*>(x.wc), x.fw,
         x.most ? x.most + 1 + first / x.piece : nullptr);
   else

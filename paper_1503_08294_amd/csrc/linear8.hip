@@ -21,75 +21,93 @@ struct Linear8 {
   int8_t* q;        // [tokens][pitch], zeros at the rows' ends
   float* x_scales;  // [tokens]
   int8_t* wc;       // [out][pitch] w, where its rows are not at multiples of 16 bytes
+  bool lines;       // rows of y begin and end at multiples of 16 bytes
 };
 
-// v / s to the nearest integer, ties to even, as of the exact quotient: the product with 1 / s may
-// be one off beside a border, and the fma's sign tells on which side of it v is, or that it is on
-// it.  |v / s| <= 127 but for rounding.
-__device__ __forceinline__ int quantised(float v, float s, float inverse) {
-  float q = rintf(v * inverse);
+// v / s to the nearest integer, ties to even, as of the exact quotient, where `q` is the product
+// with 1 / s rounded so: it may be one off beside a border, and an fma's sign tells on which side of
+// the border v is, or that it is on it.
+__device__ __forceinline__ float beside_border(float q, float v, float s) {
   const float above = fmaf(-(q + 0.5f), s, v);  // > 0: v / s > q + 0.5
   const float below = fmaf(-(q - 0.5f), s, v);  // < 0: v / s < q - 0.5
   const bool odd = (static_cast<int>(q) & 1) != 0;
-  if (above > 0.0f || (above == 0.0f && odd)) q += 1.0f;
-  else if (below < 0.0f || (below == 0.0f && odd)) q -= 1.0f;
-  return static_cast<int>(fminf(fmaxf(q, -127.0f), 127.0f));
+  if (above > 0.0f || (above == 0.0f && odd)) return q + 1.0f;
+  if (below < 0.0f || (below == 0.0f && odd)) return q - 1.0f;
+  return q;
+}
+// Eight of them (|v / s| <= 127 but for rounding).  What is left of v after q s has an error of
+// 2^-24 of itself: up to 0.4999 s no other integer is nearer, and few values are looked at again.
+__device__ __forceinline__ Vec<int8_t, 8> quantised(const float* v, float s, float inverse) {
+  float q[8];
+  bool again = false;
+  const float sure = 0.4999f * s;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    q[i] = rintf(v[i] * inverse);
+    again |= !(fabsf(fmaf(-q[i], s, v[i])) < sure);
+  }
+  if (__any(again)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = beside_border(q[i], v[i], s);
+  }
+  Vec<int8_t, 8> o;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o.v[i] = static_cast<int8_t>(static_cast<int>(q[i]));
+  return o;
 }
 
 // Rows in 8 bits, a workgroup a row: the largest value, then the quotients, the row kept in
 // registers in between where it has up to 8,192 elements.  `pitch` bytes of q are written (at most
 // up to the next multiple of 16 bytes), zeros past the end.  Bound by memory.
+constexpr int kRowThreads = 256;
 template <typename T>
-__global__ __launch_bounds__(256) void q8_rows(const T* __restrict__ x, int64_t stride,
-                                               int64_t rows, int32_t dim, int8_t* __restrict__ q,
-                                               int64_t q_stride, int32_t pitch,
-                                               float* __restrict__ scales) {
-  constexpr int kKept = 4, kEach = 8 * 256;
-  __shared__ float some[4];
+__device__ __forceinline__ void quantise_rows(const T* __restrict__ x, int64_t stride,
+                                              int64_t rows, int32_t dim, int8_t* __restrict__ q,
+                                              int64_t q_stride, int32_t pitch,
+                                              float* __restrict__ scales, int64_t block,
+                                              int64_t blocks) {
+  constexpr int kKept = 4, kEach = 8 * kRowThreads;
+  typedef T Eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  __shared__ uint32_t some[kRowThreads / kWave];
   const int tid = threadIdx.x;
-  const auto load = [&](const T* row, int32_t k, float* v) {
-    load4(row, k, dim, v);
-    load4(row, k + 4, dim, v + 4);
-  };
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+  for (int64_t r = block; r < rows; r += blocks) {
     const T* const row = x + r * stride;
-    float kept[kKept][8], top = 0.0f;
-    const auto largest = [&](const float* v) {
+    Eight kept[kKept];
+    uint32_t top = 0;  // bits without the sign: larger for larger numbers, largest for NaN
+    const auto load = [&](int32_t k, bool inside) {
+      Eight v;
+      if (inside || k + 8 <= dim) return *reinterpret_cast<const Eight*>(row + k);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = fabsf(v[i]);
-        top = a > top || a != a ? a : top;  // (NaN stays)
-      }
+      for (int i = 0; i < 8; ++i) v[i] = k + i < dim ? row[k + i] : from_float<T>(0.0f);
+      return v;
     };
+    const auto largest = [&](const Eight& v) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(to_float(v[i])) & 0x7fffffffu);
+    };
+    // (whole parts without a branch a lane: the loads of all of them are under way together)
 #pragma unroll
     for (int i = 0; i < kKept; ++i)
-      if (i * kEach < dim) load(row, i * kEach + tid * 8, kept[i]);
+      if (i * kEach < dim) kept[i] = load(i * kEach + tid * 8, (i + 1) * kEach <= dim);
 #pragma unroll
     for (int i = 0; i < kKept; ++i)
       if (i * kEach < dim) largest(kept[i]);
-    for (int32_t k = kKept * kEach + tid * 8; k < dim; k += kEach) {
-      float v[8];
-      load(row, k, v);
-      largest(v);
-    }
+    for (int32_t k = kKept * kEach + tid * 8; k < dim; k += kEach) largest(load(k, false));
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float v = __shfl_xor(top, o);
-      top = v > top || v != v ? v : top;
-    }
+    for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
     __syncthreads();
     if (tid % kWave == 0) some[tid / kWave] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = some[w] > top || some[w] != some[w] ? some[w] : top;
-    const bool bad = !(top < INFINITY);
-    const float s = top / 127.0f > 0x1p-126f ? top / 127.0f : 0x1p-126f, inverse = 1.0f / s;
+    for (int w = 0; w < kRowThreads / kWave; ++w) top = max(top, some[w]);
+    const bool bad = top >= 0x7f800000u;
+    const float s = fmaxf(__uint_as_float(bad ? 0 : top) / 127.0f, 0x1p-126f), inverse = 1.0f / s;
     int8_t* const to = q + r * q_stride;
-    const auto store = [&](int32_t k, const float* v) {
-      Vec<int8_t, 8> o;
+    const auto store = [&](int32_t k, const Eight& v) {
+      float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        o.v[i] = bad ? 0 : static_cast<int8_t>(quantised(v[i], s, inverse));
+      for (int i = 0; i < 8; ++i) f[i] = bad ? 0.0f : to_float(v[i]);
+      const Vec<int8_t, 8> o = quantised(f, s, inverse);
       if (k + 8 <= pitch) {
         typedef uint8_t Loose __attribute__((ext_vector_type(8), aligned(1)));
         *reinterpret_cast<Loose*>(to + k) = __builtin_bit_cast(Loose, o);
@@ -101,22 +119,33 @@ __global__ __launch_bounds__(256) void q8_rows(const T* __restrict__ x, int64_t 
 #pragma unroll
     for (int i = 0; i < kKept; ++i)
       if (i * kEach + tid * 8 < pitch) store(i * kEach + tid * 8, kept[i]);
-    for (int32_t k = kKept * kEach + tid * 8; k < pitch; k += kEach) {
-      float v[8];
-      load(row, k, v);
-      store(k, v);
-    }
+    for (int32_t k = kKept * kEach + tid * 8; k < pitch; k += kEach) store(k, load(k, false));
     if (tid == 0) scales[r] = bad ? NAN : s;
   }
 }
 
-// w in rows of `pitch` bytes.
-__global__ __launch_bounds__(256) void q8_copy(Linear8 x) {
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-       i < static_cast<int64_t>(x.out) * x.pitch; i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t r = i / x.pitch;
-    const int32_t k = static_cast<int32_t>(i - r * x.pitch);
-    x.wc[i] = k < x.dim ? x.w[r * x.w_stride + k] : 0;
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void q8_rows(const T* x, int64_t stride, int64_t rows,
+                                                       int32_t dim, int8_t* q, int64_t q_stride,
+                                                       float* scales) {
+  quantise_rows(x, stride, rows, dim, q, q_stride, dim, scales, blockIdx.x, gridDim.x);
+}
+
+// x in 8 bits by the first `blocks` workgroups, and by the others w in rows of `pitch` bytes with
+// zeros at their ends.
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void q8_begin(Linear8 x, uint32_t blocks) {
+  if (blockIdx.x < blocks)
+    return quantise_rows(static_cast<const T*>(x.x), x.x_stride, x.tokens, x.dim, x.q, x.pitch,
+                         x.pitch, x.x_scales, blockIdx.x, blocks);
+  const int32_t each = x.pitch / 16;
+  const int64_t all = static_cast<int64_t>(x.out) * each;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x - blocks) * kRowThreads + threadIdx.x; i < all;
+       i += static_cast<int64_t>(gridDim.x - blocks) * kRowThreads) {
+    const int64_t r = i / each;
+    const int32_t k = static_cast<int32_t>(i - r * each) * 16;
+    *reinterpret_cast<u32x4*>(x.wc + i * 16) =
+        row_chunk<false>(x.w + r * x.w_stride, k, x.dim).u;
   }
 }
 
@@ -136,23 +165,34 @@ struct Scaled {
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(i32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
-                                       int lane, char*) const {
-    const int32_t n = at.n0 + nw + (lane >> 4) * 4;
+                                       int lane, char* smem) const {
+    const int32_t n0 = at.n0 + nw, n = n0 + (lane >> 4) * 4;
+    using Lines = Turn<T, 16 * NT>;
+    static_assert(Lines::kBytes <= TILE::kLds / 4);
+    const Lines turn{smem + threadIdx.x / kWave * (TILE::kLds / 4)};
+    float cols[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) load4(x.scales, n + 16 * j, x.out, cols[j]);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int64_t t = at.m0 + mw + 16 * i + (lane & 15);
-      if (t >= x.tokens) break;
-      const float s = x.x_scales[t];
+      const int64_t t0 = at.m0 + mw + 16 * i, t = t0 + (lane & 15);
+      if (t0 >= x.tokens) break;
+      const float s = x.x_scales[t < x.tokens ? t : x.tokens - 1];
       T* const row = static_cast<T*>(x.y) + t * x.y_stride;
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        if (n + 16 * j >= x.out) break;
         float v[4];
-        load4(x.scales, n + 16 * j, x.out, v);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = static_cast<float>(acc[i][j][q]) * s * v[q];
-        store4(row, n + 16 * j, x.out, v);
+        for (int q = 0; q < 4; ++q) v[q] = static_cast<float>(acc[i][j][q]) * s * cols[j][q];
+        if (x.lines) turn.put(lane & 15, 16 * j + (lane >> 4) * 4, v);
+        else if (t < x.tokens && n + 16 * j < x.out) store4(row, n + 16 * j, x.out, v);
       }
+      if (!x.lines) continue;
+      wave_fence();
+      const int64_t left = x.tokens - t0;
+      turn.out(static_cast<T*>(x.y) + t0 * x.y_stride + n0, x.y_stride,
+               static_cast<int32_t>(left < 16 ? left : 16), x.out - n0, lane);
+      wave_fence();
     }
   }
 };
@@ -163,18 +203,19 @@ uint32_t row_blocks(int64_t rows) {
 
 template <typename T>
 hipError_t launch(const Linear8& x, hipStream_t st) {
-  q8_rows<T><<<row_blocks(x.tokens), 256, 0, st>>>(static_cast<const T*>(x.x), x.x_stride,
-                                                   x.tokens, x.dim, x.q, x.pitch, x.pitch,
-                                                   x.x_scales);
-  if (x.tokens <= kFewRows) {
+  // A few tokens: w is read once, as it is.  Otherwise its rows have to begin and end at multiples
+  // of 16 bytes.
+  const bool few = x.tokens <= kFewRows;
+  const bool copy = !few && (!aligned16(x.w) || x.w_stride % 16 != 0 || x.dim % 16 != 0);
+  const uint32_t blocks = row_blocks(x.tokens);
+  const int64_t copies =
+      (static_cast<int64_t>(x.out) * (x.pitch / 16) + kRowThreads - 1) / kRowThreads;
+  q8_begin<T><<<blocks + (copy ? static_cast<uint32_t>(std::min<int64_t>(copies, 1 << 14)) : 0),
+                kRowThreads, 0, st>>>(x, blocks);
+  if (few) {
     run_few<int8_t>(Few{x.q, x.pitch, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.out,
                         x.dim}, Scaled<T>{x}, st);
     return hipGetLastError();
-  }
-  const bool copy = !aligned16(x.w) || x.w_stride % 16 != 0 || x.dim % 16 != 0;
-  if (copy) {
-    const int64_t n = (static_cast<int64_t>(x.out) * x.pitch + 255) / 256;
-    q8_copy<<<static_cast<uint32_t>(std::min<int64_t>(n, 1 << 16)), 256, 0, st>>>(x);
   }
   Product p{};
   p.a = Operand{reinterpret_cast<const char*>(x.q), {0, 0}, x.pitch, 0,
@@ -230,16 +271,12 @@ int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_
   if (!x || !q || !scales || x_stride < dim || q_stride < dim) return GSN_E_INVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const uint32_t blocks = gsn::row_blocks(rows);
-  if (dtype == GSN_F32)
-    gsn::q8_rows<float><<<blocks, 256, 0, st>>>(static_cast<const float*>(x), x_stride, rows, dim,
-                                                q, q_stride, dim, scales);
-  else if (dtype == GSN_BF16)
-    gsn::q8_rows<gsn::bf16_t><<<blocks, 256, 0, st>>>(static_cast<const gsn::bf16_t*>(x),
-                                                      x_stride, rows, dim, q, q_stride, dim,
-                                                      scales);
-  else
-    gsn::q8_rows<gsn::f16_t><<<blocks, 256, 0, st>>>(static_cast<const gsn::f16_t*>(x), x_stride,
-                                                     rows, dim, q, q_stride, dim, scales);
+  const auto run = [&](auto* p) {
+    gsn::q8_rows<<<blocks, gsn::kRowThreads, 0, st>>>(p, x_stride, rows, dim, q, q_stride, scales);
+  };
+  if (dtype == GSN_F32) run(static_cast<const float*>(x));
+  else if (dtype == GSN_BF16) run(static_cast<const gsn::bf16_t*>(x));
+  else run(static_cast<const gsn::f16_t*>(x));
   return hipGetLastError() == hipSuccess ? GSN_OK : GSN_E_HIP;
 }
 
@@ -270,6 +307,8 @@ int gsn_linear_quantised(const gsn_linear_params* p, const void* x, int64_t x_st
   a.scales = scales;
   a.y = y;
   a.y_stride = y_stride;
+  const int64_t elements = 16 / static_cast<int64_t>(gsn::size_of(p->dtype));
+  a.lines = gsn::aligned16(y) && y_stride % elements == 0 && p->out % elements == 0;
   gsn::carve(workspace, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32    ? gsn::launch<float>(a, st)
