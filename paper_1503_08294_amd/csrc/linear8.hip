@@ -25,8 +25,8 @@ struct Linear8 {
 };
 
 // v / s to the nearest integer, ties to even, as of the exact quotient, where `q` is the product
-// with 1 / s rounded so: it may be one off beside a border, and an fma's sign tells on which side of
-// the border v is, or that it is on it.
+// with 1 / s rounded so: it may be one off beside a border, and an fma's sign tells on which side
+// of the border v is, or that it is on it.
 __device__ __forceinline__ float beside_border(float q, float v, float s) {
   const float above = fmaf(-(q + 0.5f), s, v);  // > 0: v / s > q + 0.5
   const float below = fmaf(-(q - 0.5f), s, v);  // < 0: v / s < q - 0.5

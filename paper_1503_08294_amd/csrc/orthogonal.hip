@@ -287,8 +287,230 @@ struct Finish {
   }
 };
 
+// A small matrix by one workgroup, all steps in LDS: X, A and B as above, with S (the short side)
+// rows and L columns.  A wave takes tiles of 16 x 16 of A and of B, and columns of 16 of X, which it
+// alone reads and writes.
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallLds = 152 * 1024;
+constexpr int kSmallSide = 128;  // of S at most
+struct SmallSizes {
+  int32_t s, l;        // sides
+  int32_t rows_x;      // S up to a multiple of 32
+  int32_t x, a;        // elements of a row of X, and of A and B: up to a multiple of 32, and 8
+  int32_t many_x, many_a;  // elements of X, of A
+  __host__ __device__ SmallSizes(int32_t rows, int32_t cols) {
+    s = rows < cols ? rows : cols;
+    l = rows < cols ? cols : rows;
+    rows_x = (s + 31) / 32 * 32;
+    x = (l + 31) / 32 * 32 + 8;
+    a = rows_x + 8;
+    many_x = rows_x * x;
+    many_a = rows_x * a;
+  }
+  __host__ __device__ int64_t bytes(int32_t values) const {
+    return int64_t{2} * values * (many_x + 2 * many_a);
+  }
+};
+
+template <typename T, bool UPDATE, int VALUES>
+__global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
+  constexpr int kWaves = kSmallThreads / kWave;
+  __shared__ __attribute__((aligned(16))) char smem[kSmallLds];
+  __shared__ double some[kWaves];
+  const SmallSizes z(x.rows, x.cols);
+  const bool wide = x.rows <= x.cols;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int g = lane >> 4, li = lane & 15, lg = g * 4;
+  f16_t* const xs = reinterpret_cast<f16_t*>(smem);
+  f16_t* const as = xs + VALUES * z.many_x;
+  f16_t* const bs = as + VALUES * z.many_a;
+  const int64_t pair = blockIdx.x;
+  const int32_t n = x.rows * x.cols;
+  const int64_t first = pair * n;
+
+  for (int32_t i = tid; i < VALUES * (z.many_x + 2 * z.many_a) / 8; i += kSmallThreads)
+    reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
+  // four elements at a time, whatever rows they belong to
+  const T* const from = static_cast<const T*>(x.x) + first;
+  double sum = 0.0;
+#pragma unroll 4
+  for (int32_t i = 4 * tid; i < n; i += 4 * kSmallThreads) {
+    float v[4];
+    load4(from, i, n, v);
+    if constexpr (UPDATE) {
+      float m[4];
+      load4(x.momentum + first, i, n, m);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        m[q] = x.beta * m[q] + v[q];
+        v[q] = x.nesterov ? v[q] + x.beta * m[q] : m[q];
+      }
+      store4(x.new_momentum + first, i, n, m);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += static_cast<double>(v[q]) * v[q];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) some[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) sum += some[w];
+  const double norm = sqrt(sum) + static_cast<double>(x.eps);
+  const float factor = norm > 0.0 ? static_cast<float>(kScale / norm) : sum != sum ? NAN : 0.0f;
+  // one or two float16 values of v at element i of X, A or B
+  const auto keep = [&](f16_t* to, int32_t other, int32_t i, float v) {
+    v = settled(v);
+    const f16_t hi = from_float<f16_t>(v);
+    to[i] = hi;
+    if constexpr (VALUES > 1) to[i + other] = from_float<f16_t>(v - to_float(hi));
+  };
+#pragma unroll 4
+  for (int32_t i = 4 * tid; i < n; i += 4 * kSmallThreads) {
+    float v[4];
+    load4(from, i, n, v);
+    if constexpr (UPDATE) {
+      float m[4];
+      load4(x.new_momentum + first, i, n, m);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = x.nesterov ? v[q] + x.beta * m[q] : m[q];
+    }
+    int32_t r = i / x.cols, c = i - r * x.cols;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (i + q < n) keep(xs, z.many_x, wide ? r * z.x + c : c * z.x + r, v[q] * factor);
+      if (++c == x.cols) {
+        c = 0;
+        ++r;
+      }
+    }
+  }
+  __syncthreads();
+
+  // products of 16 rows of p (from row r0) and of q (from row r1), k contiguous in both
+  const auto rows = [&](const f16_t* p, const f16_t* q, int32_t r0, int32_t r1, int32_t ld,
+                        int32_t other, int32_t k_end) {
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f16_t* const a = p + (r0 + li) * ld + 8 * g;
+    const f16_t* const b = q + (r1 + li) * ld + 8 * g;
+    const auto term = [&](int32_t u, int32_t v) {
+#pragma unroll 4
+      for (int32_t k = 0; k < k_end; k += 32) {
+        Frag fa, fb;
+        fa.u = *reinterpret_cast<const u32x4*>(a + u + k);
+        fb.u = *reinterpret_cast<const u32x4*>(b + v + k);
+        acc = multiply<f16_t>(fb, fa, acc, 0);
+      }
+    };
+    if constexpr (VALUES > 1) {
+      term(0, other);
+      term(other, 0);
+    }
+    term(0, 0);
+    return acc;
+  };
+  const int32_t tiles = (z.s + 15) / 16, columns = (z.l + 15) / 16;
+  const auto symmetric = [&](const auto& make, f16_t* to) {
+    for (int32_t t = wave; t < tiles * (tiles + 1) / 2; t += kWaves) {
+      int32_t c = 0;
+      while ((c + 1) * (c + 2) / 2 <= t) ++c;
+      const int32_t m0 = 16 * (t - c * (c + 1) / 2), n0 = 16 * c;
+      const f32x4 v = make(m0, n0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int32_t m = m0 + li, nn = n0 + lg + q;
+        if (nn < m) continue;
+        keep(to, z.many_a, m * z.a + nn, v[q]);
+        keep(to, z.many_a, nn * z.a + m, v[q]);
+      }
+    }
+    __syncthreads();
+  };
+  for (int32_t step = 0; step < x.steps; ++step) {
+    symmetric([&](int32_t m0, int32_t n0) {
+      return rows(xs, xs, m0, n0, z.x, z.many_x, z.x - 8) * (1.0f / kScale);
+    }, as);
+    symmetric([&](int32_t m0, int32_t n0) {
+      f32x4 v = rows(as, as, m0, n0, z.a, z.many_a, z.rows_x) * (1.0f / kScale);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int32_t i = (m0 + li) * z.a + n0 + lg + q;
+        float a = to_float(as[i]);
+        if constexpr (VALUES > 1) a += to_float(as[i + z.many_a]);
+        v[q] = x.c * v[q] + (x.b * a + (m0 + li == n0 + lg + q ? x.a * kScale : 0.0f));
+      }
+      return v;
+    }, bs);
+    const bool last = step + 1 == x.steps;
+    for (int32_t c = wave; c < columns; c += kWaves) {
+      constexpr int kMost = kSmallSide / 16;
+      f32x4 acc[kMost];
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      const auto term = [&](int32_t u, int32_t v) {
+        for (int32_t k = 0; k < z.rows_x; k += 32) {
+          // rows of k, 16 columns wide, transposed on the way
+          Frag fx;
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            fx.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(
+                    xs + v + (k + 8 * g + 4 * j + (li >> 2)) * z.x + 16 * c + (li & 3) * 4));
+#pragma unroll
+          for (int i = 0; i < kMost; ++i) {
+            if (i >= tiles) break;
+            Frag fb;
+            fb.u = *reinterpret_cast<const u32x4*>(bs + u + (16 * i + li) * z.a + k + 8 * g);
+            acc[i] = multiply<f16_t>(fx, fb, acc[i], 0);
+          }
+        }
+      };
+      if constexpr (VALUES > 1) {
+        term(0, z.many_x);
+        term(z.many_a, 0);
+      }
+      term(0, 0);
+      wave_fence();
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        if (i >= tiles) break;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int32_t m = 16 * i + li, l = 16 * c + lg + q;
+          if (m >= z.s || l >= z.l) continue;
+          if (last) {
+            const int64_t at = first + (wide ? m * x.cols + l : l * x.cols + m);
+            const float o = acc[i][q] * (1.0f / (kScale * kScale));
+            T* const out = static_cast<T*>(x.out);
+            if constexpr (UPDATE)
+              out[at] = from_float<T>(x.keep * to_float(static_cast<const T*>(x.weights)[at]) -
+                                      x.rate * o);
+            else
+              out[at] = from_float<T>(o);
+          } else {
+            keep(xs, z.many_x, m * z.x + l, acc[i][q] * (1.0f / kScale));
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+bool small_matrix(const Orthogonal& x) {
+  const SmallSizes z(x.rows, x.cols);
+  return z.s <= kSmallSide && z.bytes(x.values) <= kSmallLds;
+}
+
 template <typename T, bool UPDATE>
 hipError_t launch(const Orthogonal& x, hipStream_t st) {
+  if (small_matrix(x)) {
+    const uint32_t grid = static_cast<uint32_t>(x.batch);
+    if (x.values == 2) or_small<T, UPDATE, 2><<<grid, kSmallThreads, 0, st>>>(x);
+    else or_small<T, UPDATE, 1><<<grid, kSmallThreads, 0, st>>>(x);
+    return hipGetLastError();
+  }
   const uint32_t blocks = static_cast<uint32_t>(x.batch * x.blocks);
   or_norm<T, UPDATE><<<blocks, kNormThreads, 0, st>>>(x);
   or_begin<T, UPDATE><<<blocks, 256, 0, st>>>(x);
