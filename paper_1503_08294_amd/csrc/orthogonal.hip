@@ -292,7 +292,7 @@ struct Finish {
 // alone reads and writes.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallLds = 152 * 1024;
-constexpr int kSmallSide = 128;  // of S at most
+constexpr int small_side(int values) { return values == 1 ? 128 : 96; }  // of S at most
 struct SmallSizes {
   int32_t s, l;        // sides
   int32_t rows_x;      // S up to a multiple of 32
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
   // four elements at a time, whatever rows they belong to
   const T* const from = static_cast<const T*>(x.x) + first;
   double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 2
   for (int32_t i = 4 * tid; i < n; i += 4 * kSmallThreads) {
     float v[4];
     load4(from, i, n, v);
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
     to[i] = hi;
     if constexpr (VALUES > 1) to[i + other] = from_float<f16_t>(v - to_float(hi));
   };
-#pragma unroll 4
+#pragma unroll 2
   for (int32_t i = 4 * tid; i < n; i += 4 * kSmallThreads) {
     float v[4];
     load4(from, i, n, v);
@@ -391,24 +391,26 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
   // products of 16 rows of p (from row r0) and of q (from row r1), k contiguous in both
   const auto rows = [&](const f16_t* p, const f16_t* q, int32_t r0, int32_t r1, int32_t ld,
                         int32_t other, int32_t k_end) {
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    // (the small products in sums of their own, which do not wait for each other)
+    f32x4 acc[VALUES > 1 ? 3 : 1] = {};
     const f16_t* const a = p + (r0 + li) * ld + 8 * g;
     const f16_t* const b = q + (r1 + li) * ld + 8 * g;
-    const auto term = [&](int32_t u, int32_t v) {
-#pragma unroll 4
-      for (int32_t k = 0; k < k_end; k += 32) {
-        Frag fa, fb;
-        fa.u = *reinterpret_cast<const u32x4*>(a + u + k);
-        fb.u = *reinterpret_cast<const u32x4*>(b + v + k);
-        acc = multiply<f16_t>(fb, fa, acc, 0);
+#pragma unroll 2
+    for (int32_t k = 0; k < k_end; k += 32) {
+      Frag fa[VALUES], fb[VALUES];
+#pragma unroll
+      for (int u = 0; u < VALUES; ++u) {
+        fa[u].u = *reinterpret_cast<const u32x4*>(a + u * other + k);
+        fb[u].u = *reinterpret_cast<const u32x4*>(b + u * other + k);
       }
-    };
-    if constexpr (VALUES > 1) {
-      term(0, other);
-      term(other, 0);
+      acc[0] = multiply<f16_t>(fb[0], fa[0], acc[0], 0);
+      if constexpr (VALUES > 1) {
+        acc[1] = multiply<f16_t>(fb[1], fa[0], acc[1], 0);
+        acc[2] = multiply<f16_t>(fb[0], fa[1], acc[2], 0);
+      }
     }
-    term(0, 0);
-    return acc;
+    if constexpr (VALUES > 1) return acc[0] + (acc[1] + acc[2]);
+    else return acc[0];
   };
   const int32_t tiles = (z.s + 15) / 16, columns = (z.l + 15) / 16;
   const auto symmetric = [&](const auto& make, f16_t* to) {
@@ -444,33 +446,37 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
     }, bs);
     const bool last = step + 1 == x.steps;
     for (int32_t c = wave; c < columns; c += kWaves) {
-      constexpr int kMost = kSmallSide / 16;
-      f32x4 acc[kMost];
+      constexpr int kMost = small_side(VALUES) / 16;
+      f32x4 acc[kMost] = {}, small[kMost] = {};
+      for (int32_t k = 0; k < z.rows_x; k += 32) {
+        // rows of k, 16 columns wide, transposed on the way
+        Frag fx[VALUES];
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      const auto term = [&](int32_t u, int32_t v) {
-        for (int32_t k = 0; k < z.rows_x; k += 32) {
-          // rows of k, 16 columns wide, transposed on the way
-          Frag fx;
+        for (int u = 0; u < VALUES; ++u)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
-            fx.s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            fx[u].s[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) s16x4*)(
-                    xs + v + (k + 8 * g + 4 * j + (li >> 2)) * z.x + 16 * c + (li & 3) * 4));
+                    xs + u * z.many_x + (k + 8 * g + 4 * j + (li >> 2)) * z.x + 16 * c +
+                    (li & 3) * 4));
 #pragma unroll
-          for (int i = 0; i < kMost; ++i) {
-            if (i >= tiles) break;
-            Frag fb;
-            fb.u = *reinterpret_cast<const u32x4*>(bs + u + (16 * i + li) * z.a + k + 8 * g);
-            acc[i] = multiply<f16_t>(fx, fb, acc[i], 0);
+        for (int i = 0; i < kMost; ++i) {
+          if (i >= tiles) break;
+          Frag fb[VALUES];
+#pragma unroll
+          for (int u = 0; u < VALUES; ++u)
+            fb[u].u = *reinterpret_cast<const u32x4*>(bs + u * z.many_a + (16 * i + li) * z.a + k +
+                                                      8 * g);
+          acc[i] = multiply<f16_t>(fx[0], fb[0], acc[i], 0);
+          if constexpr (VALUES > 1) {
+            small[i] = multiply<f16_t>(fx[1], fb[0], small[i], 0);
+            small[i] = multiply<f16_t>(fx[0], fb[1], small[i], 0);
           }
         }
-      };
-      if constexpr (VALUES > 1) {
-        term(0, z.many_x);
-        term(z.many_a, 0);
       }
-      term(0, 0);
+      if constexpr (VALUES > 1)
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) acc[i] += small[i];
       wave_fence();
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
@@ -500,7 +506,7 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
 
 bool small_matrix(const Orthogonal& x) {
   const SmallSizes z(x.rows, x.cols);
-  return z.s <= kSmallSide && z.bytes(x.values) <= kSmallLds;
+  return z.s <= small_side(x.values) && z.bytes(x.values) <= kSmallLds;
 }
 
 template <typename T, bool UPDATE>
