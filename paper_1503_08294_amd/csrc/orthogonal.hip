@@ -288,8 +288,8 @@ struct Finish {
 };
 
 // A small matrix by one workgroup, all steps in LDS: X, A and B as above, with S (the short side)
-// rows and L columns.  A wave takes tiles of 16 x 16 of A and of B, and columns of 16 of X, which it
-// alone reads and writes.
+// rows and L columns.  A wave takes tiles of 16 x 16 of A and of B, and columns of 16 of X, which
+// it alone reads and writes.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallLds = 152 * 1024;
 constexpr int small_side(int values) { return values == 1 ? 128 : 96; }  // of S at most

@@ -66,15 +66,17 @@ __device__ __forceinline__ AccOf<T> multiply_any(const Frag& n, const Frag& m, A
 }
 
 // Tiles of BM x BN by four waves, 2 x 2 of them: stages of KB bytes of k, SLOTS of them in LDS, and
-// WAVES of a SIMD (workgroups of a CU) that registers and LDS have to last for.  RUN of them at a
-// time are an XCD's, in blocks TALL tiles high.
-template <int BM_, int BN_, int KB_, int SLOTS_, int WAVES_, int RUN_, int TALL_>
+// WAVES of a SIMD that registers and LDS have to last for.  RUN of them at a time are an XCD's, in
+// blocks TALL tiles high.  GROUPS of four waves take a part of the stages each, with SLOTS of their
+// own, and add their sums up in the groups' order.
+template <int BM_, int BN_, int KB_, int SLOTS_, int WAVES_, int RUN_, int TALL_, int GROUPS_ = 1>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, KB = KB_, SLOTS = SLOTS_, WAVES = WAVES_;
-  static constexpr int RUN = RUN_, TALL = TALL_;
+  static constexpr int RUN = RUN_, TALL = TALL_, GROUPS = GROUPS_;
   static constexpr int kSlot = (BM + BN) * KB;
-  static constexpr int kLds = SLOTS * kSlot;
-  static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024);
+  static constexpr int kLds = SLOTS * kSlot;  // of a group
+  static constexpr int kThreads = 256 * GROUPS;
+  static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024 && WAVES % GROUPS == 0);
 };
 
 // Place of 16-byte chunk c in row r of a staged operand with k contiguous: the 16 rows that a
@@ -173,6 +175,11 @@ struct Feed {
     p += step;
     k += kBK;
   }
+  // from the first stage of all to stage `in_term` of a later term
+  __device__ __forceinline__ void skip(int64_t next0, int64_t next1, int32_t in_term) {
+    p += next0 + next1 + in_term * step;
+    k += in_term * kBK;
+  }
   // to the next term after `stages` stages
   __device__ __forceinline__ void turn(int64_t next, int32_t stages) {
     p += next - stages * step;
@@ -237,12 +244,15 @@ constexpr int kProductThreads = 256;
 // are the wave's first row and column in the tile.  All threads of the workgroup come; room is LDS
 // that no other wave reads any more.
 template <typename T, bool TRA, bool TRB, class TILE, class EPI>
-__global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Product p, EPI epi) {
+__global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Product p, EPI epi) {
   constexpr int kThr = kProductThreads, BM = TILE::BM, BN = TILE::BN, KB = TILE::KB;
   constexpr int MT = BM / 32, NT = BN / 32, kSlot = TILE::kSlot, SLOTS = TILE::SLOTS;
   static_assert(SLOTS == 2 || SLOTS == 3);
-  __shared__ __attribute__((aligned(1024))) char smem[TILE::kLds];
-  const int tid = threadIdx.x, lane = tid % kWave;
+  constexpr int GROUPS = TILE::GROUPS;
+  __shared__ __attribute__((aligned(1024))) char lds_all[GROUPS * TILE::kLds];
+  const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThr);
+  char* const smem = lds_all + group * TILE::kLds;
+  const int tid = threadIdx.x - group * kThr, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int mw = (wave >> 1) * (BM / 2), nw = (wave & 1) * (BN / 2);
   Place at;
@@ -254,7 +264,11 @@ __global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Produ
   const int32_t k0 = at.split * p.part;
   const int32_t k_end = k0 + p.part < p.k ? k0 + p.part : p.k;
   const int32_t each = k_end > k0 ? (k_end - k0 + kBK - 1) / kBK : 0;  // stages of a term
-  const int32_t stages = each * p.terms;
+  const int32_t all = each * p.terms;
+  // this group's: `most` of them or what is left
+  const int32_t most = (all + GROUPS - 1) / GROUPS;
+  const int32_t before = group * most < all ? group * most : all;
+  const int32_t stages = all - before < most ? all - before : most;
   FeedA fa;
   FeedB fb;
   fa.begin(p.a, at.pair, at.m0, k0, k_end, tid);
@@ -263,6 +277,12 @@ __global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Produ
       reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem)) +
       wave * (kWave * 16);
   int32_t in_term = 0, term = 0;
+  if constexpr (GROUPS > 1) {
+    if (each > 0) term = before / each;
+    in_term = before - term * each;
+    fa.skip(term > 0 ? p.a.next[0] : 0, term > 1 ? p.a.next[1] : 0, in_term);
+    fb.skip(term > 0 ? p.b.next[0] : 0, term > 1 ? p.b.next[1] : 0, in_term);
+  }
   const auto load = [&](int slot) {
     fa.load(lds + slot * kSlot);
     fb.load(lds + slot * kSlot + BM * KB);
@@ -283,9 +303,10 @@ __global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Produ
   if (stages > 0) load(0);
   if (SLOTS > 2 && stages > 1) load(1);
   int slot = 0;
-  for (int32_t h = 0; h < stages; ++h) {
+  for (int32_t h = 0; h < most; ++h) {
     if (SLOTS > 2 && h + 1 < stages) meet_loaded<kLoads>();
     else meet_loaded<0>();
+    if (GROUPS > 1 && h >= stages) continue;
     if (h + SLOTS - 1 < stages) load(slot == 0 ? SLOTS - 1 : slot - 1);
     const char* const sa = smem + slot * kSlot;
     const char* const sb = sa + BM * KB;
@@ -306,6 +327,22 @@ __global__ __launch_bounds__(kProductThreads, TILE::WAVES) void mt_product(Produ
     slot = slot + 1 == SLOTS ? 0 : slot + 1;
   }
   meet_read();
+  if constexpr (GROUPS > 1) {
+    constexpr int kSums = kThr * MT * NT * 16;
+    static_assert(kSums <= TILE::kLds);
+    auto* const sums = reinterpret_cast<AccOf<T>*>(smem);
+    if (group > 0)
+#pragma unroll
+      for (int i = 0; i < MT * NT; ++i) sums[i * kThr + tid] = acc[i / NT][i % NT];
+    meet_read();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+      for (int i = 0; i < MT * NT; ++i)
+        acc[i / NT][i % NT] +=
+            *reinterpret_cast<const AccOf<T>*>(smem + g * TILE::kLds + (i * kThr + tid) * 16);
+  }
   epi.template tile<TILE, MT, NT>(acc, at, mw, nw, lane, smem);
 }
 
@@ -316,7 +353,7 @@ void run_tiles(Product p, const EPI& epi, hipStream_t st) {
   const int32_t grid = numbers_of<TILE>(p);
   if (grid > 0)
     mt_product<T, TRA, TRB, TILE, EPI>
-        <<<static_cast<uint32_t>(grid), kProductThreads, 0, st>>>(p, epi);
+        <<<static_cast<uint32_t>(grid), TILE::kThreads, 0, st>>>(p, epi);
 }
 
 // Which tiles a product takes.  Of 2-byte elements, us, C of bfloat16, tiles of 128 x 256, 128 x
@@ -329,9 +366,16 @@ void run_tiles(Product p, const EPI& epi, hipStream_t st) {
 // With k contiguous a stage of 64 bytes reads half lines of memory, and the middle tiles' 128 bytes
 // make up for their size.  Binary32 products are bound by the matrix cores, and small tiles fill
 // the CUs more evenly.
+// Up to about one workgroup a CU its SIMDs have a wave each, which waits for its own loads: two
+// groups of waves share k.  With one group and two: tiles of 128: 2,048 x 2,048 x 2,048 (256) 28,
+// 23; tiles of 64 from 8 stages on: 1,024 x 1,024 x 2,048 (256) 15, 12; 2,048 x 1,024 x 2,048 (512)
+// 19, 16; 1,024 x 768 x 512 7.2, 7.2; 8 bits, 64 rows by 16,384 of 4,096 (256, memory) 14.6, 13.1.
 using LargeTile = Tile<128, 256, 64, 2, 2, 32, 8>;
 using MiddleTile = Tile<128, 128, 128, 2, 2, 16, 4>;
+using MiddleTwo = Tile<128, 128, 128, 2, 2, 16, 4, 2>;
 using SmallTile = Tile<64, 64, 128, 3, 3, 1, 4>;
+using SmallTwo = Tile<64, 64, 128, 2, 4, 1, 4, 2>;      // two workgroups a CU
+using SmallTwoAlone = Tile<64, 64, 128, 3, 2, 1, 4, 2>;  // one
 
 // f(a tile's type) for the tiles of a product.
 template <typename T, bool TRA, bool TRB, class F>
@@ -342,15 +386,20 @@ void with_tile(Product p, const F& f) {
     const int64_t all = int64_t{p.tiles_m} * p.tiles_n * p.batch * p.splits;
     return p.symmetric ? all / 2 : all;
   };
+  const int64_t middle = tiles(MiddleTile::BM, MiddleTile::BN);
+  const int64_t bytes = int64_t{p.part} * p.terms * static_cast<int64_t>(sizeof(T));
   if constexpr (sizeof(T) < 4) {
     if constexpr (TRA || TRB)
       if (!p.symmetric && tiles(LargeTile::BM, LargeTile::BN) >= 512) return f(LargeTile());
     // (few rows: bound by reading the other operand, of which small tiles have more on its way: 64
     // rows by 16,384 of 4,096, 26 us and 43)
-    if (p.a.rows > SmallTile::BM && tiles(MiddleTile::BM, MiddleTile::BN) >= 256)
-      return f(MiddleTile());
+    if (p.a.rows > SmallTile::BM && middle > 256) return f(MiddleTile());
+    if (p.a.rows > SmallTile::BM && middle >= 144) return f(MiddleTwo());
   }
-  f(SmallTile());
+  const int64_t small = tiles(SmallTile::BM, SmallTile::BN);
+  if (bytes < 8 * SmallTile::KB || small > 512) return f(SmallTile());
+  if (small <= 256) f(SmallTwoAlone());
+  else f(SmallTwo());
 }
 
 template <typename T, bool TRA, bool TRB, class EPI>

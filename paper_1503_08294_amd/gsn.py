@@ -686,13 +686,6 @@ def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, s
 # ------------------------------ C-named calls: training and serving over the units ----
 # (paper_1503_08294_amd.learning holds the calls on torch tensors that allocate their outputs.)
 
-def make_entropy(x, w) -> gsn_entropy_params:
-    """Parameters of the cross entropy of these tensors."""
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be 2-dimensional")
-    return gsn_entropy_params(_type(x, "x"), x.shape[1], w.shape[0], x.shape[0])
-
-
 def gsn_cross_entropy_workspace_bytes(params: gsn_entropy_params, backward: bool) -> int:
     return int(_lib.gsn_cross_entropy_workspace_bytes(params, 1 if backward else 0))
 
@@ -729,15 +722,6 @@ def gsn_cross_entropy_backward(params: gsn_entropy_params, dloss, x, w, targets,
         _dev(workspace, torch.uint8, what="workspace"), workspace.numel())
 
 
-def make_orthogonal(x, steps: int, coefficients, eps: float) -> gsn_orthogonal_params:
-    """Parameters of the orthogonalised matrices of x (..., rows, cols)."""
-    if x.dim() < 2:
-        raise ValueError(f"a matrix or a batch of them is needed, got {tuple(x.shape)}")
-    rows, cols = x.shape[-2:]
-    batch = x.numel() // (rows * cols) if rows * cols > 0 else 0
-    return gsn_orthogonal_params(_type(x, "x"), rows, cols, steps, batch, *coefficients, eps)
-
-
 def gsn_orthogonal_workspace_bytes(params: gsn_orthogonal_params, update: bool) -> int:
     return int(_lib.gsn_orthogonal_workspace_bytes(params, 1 if update else 0))
 
@@ -771,13 +755,6 @@ def gsn_quantise(x, q, scales, stream=None):
     qp, qs = _matrix(q, torch.int8, rows, dim, "q")
     return _run(_lib.gsn_quantise, x, stream, _type(x, "x"), rows, dim, xp, xs, qp, qs,
                 _flat(scales, torch.float32, (rows,), "scales"))
-
-
-def make_linear8(x, w) -> gsn_linear_params:
-    """Parameters of the 8-bit product of these tensors."""
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w must be 2-dimensional")
-    return gsn_linear_params(_type(x, "x"), x.shape[1], w.shape[0], x.shape[0])
 
 
 def gsn_linear_quantised_workspace_bytes(params: gsn_linear_params) -> int:

@@ -15,6 +15,8 @@ options out of the kernels' range ``gsn.GsnError``.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import gsn
@@ -23,10 +25,30 @@ from .mixture import _bytes, _no_tangent, _once, _rows, _same_device
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # five steps take singular values of 0.002 to 1 near 1
 
 
-def _workspace(size: int, x: torch.Tensor, what: str) -> torch.Tensor:
+# (parameters and workspace sizes go by sizes and types alone: they are made once for each of them,
+# and never written to)
+def _sized(name: str, p, size: int):
     if size == 0:
-        raise gsn.GsnError(gsn.GSN_E_INVAL, what)
-    return _bytes(size, x)
+        raise gsn.GsnError(gsn.GSN_E_INVAL, name)
+    return p, size
+
+
+@functools.lru_cache(maxsize=256)
+def _entropy(code, dim, classes, tokens, backward):
+    p = gsn.gsn_entropy_params(code, dim, classes, tokens)
+    return _sized("gsn_cross_entropy", p, gsn.gsn_cross_entropy_workspace_bytes(p, backward))
+
+
+@functools.lru_cache(maxsize=256)
+def _orthogonal(code, rows, cols, batch, steps, coefficients, eps, update):
+    p = gsn.gsn_orthogonal_params(code, rows, cols, steps, batch, *coefficients, eps)
+    return _sized("gsn_orthogonalise", p, gsn.gsn_orthogonal_workspace_bytes(p, update))
+
+
+@functools.lru_cache(maxsize=256)
+def _linear(code, dim, out, tokens):
+    p = gsn.gsn_linear_params(code, dim, out, tokens)
+    return _sized("gsn_linear_quantised", p, gsn.gsn_linear_quantised_workspace_bytes(p))
 
 
 def _no_gradient(what: str, *tensors):
@@ -36,17 +58,23 @@ def _no_gradient(what: str, *tensors):
                          "detached tensors")
 
 
+def _operands(x, w):
+    """(type, columns of both, rows of w, rows of x) of the operands of x w^T."""
+    if w.dim() != 2:
+        raise ValueError(f"w must be 2-dimensional, got {tuple(w.shape)}")
+    tokens, dim = x.shape
+    return gsn._type(x, "x"), dim, w.shape[0], tokens
+
+
 # -------------------------------------------------------------------- cross entropy ----
 
 def _cross_entropy(x, w, targets, valid, save):
     _rows(x, "x")
     _same_device(x, w, targets, valid)
-    p = gsn.make_entropy(x, w)
-    ws = _workspace(gsn.gsn_cross_entropy_workspace_bytes(p, False), x,
-                    "gsn_cross_entropy_workspace_bytes")
+    p, size = _entropy(*_operands(x, w), False)
     loss = x.new_empty(x.shape[0], dtype=torch.float32)
     stats = x.new_empty(2, x.shape[0], dtype=torch.float32) if save else None
-    gsn.gsn_cross_entropy(p, x, w, targets, valid, loss, stats, ws)
+    gsn.gsn_cross_entropy(p, x, w, targets, valid, loss, stats, _bytes(size, x))
     return loss, stats
 
 
@@ -59,12 +87,11 @@ def cross_entropy_backward(dloss, x, w, targets, valid, stats, need=(True, True)
     """(dx, dw) from dloss (tokens,) float32; None for what is not needed."""
     _rows(x, "x")
     _same_device(x, dloss, w, targets, valid, stats)
-    p = gsn.make_entropy(x, w)
-    ws = _workspace(gsn.gsn_cross_entropy_workspace_bytes(p, True), x,
-                    "gsn_cross_entropy_workspace_bytes")
+    p, size = _entropy(*_operands(x, w), True)
     dx, dw = (torch.empty_like(t, memory_format=torch.contiguous_format) if n else None
               for t, n in zip((x, w), need))
-    gsn.gsn_cross_entropy_backward(p, dloss, x, w, targets, valid, stats, dx, dw, ws)
+    gsn.gsn_cross_entropy_backward(p, dloss, x, w, targets, valid, stats, dx, dw,
+                                   _bytes(size, x))
     return dx, dw
 
 
@@ -98,20 +125,26 @@ def cross_entropy(x, w, targets, valid=None):
 
 # -------------------------------------------------------------- orthogonalised updates ----
 
+def _matrices(x):
+    """(type, rows, columns, number) of the matrices of x."""
+    if x.dim() < 2:
+        raise ValueError(f"a matrix or a batch of them is needed, got {tuple(x.shape)}")
+    rows, cols = x.shape[-2:]
+    if rows == 0 or cols == 0:
+        raise ValueError(f"matrices without elements: {tuple(x.shape)}")
+    return gsn._type(x, "x"), rows, cols, x.numel() // (rows * cols)
+
+
 def orthogonalise(x, *, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
     """The orthogonalised matrices of x (..., rows, cols): their singular vectors with singular
     values near 1 (0.7 to 1.2 with the usual coefficients and steps, where a value is above some
     0.002 of the matrix's norm).  See gsn_orthogonalise in include/gsn.h for the products."""
     _no_tangent(x)
     _no_gradient("orthogonalise", x)
-    p = gsn.make_orthogonal(x, steps, coefficients, eps)
+    p, size = _orthogonal(*_matrices(x), steps, tuple(coefficients), eps, False)
     x = x.contiguous()
     out = torch.empty_like(x)
-    if x.numel() == 0:
-        return out
-    ws = _workspace(gsn.gsn_orthogonal_workspace_bytes(p, False), x,
-                    "gsn_orthogonal_workspace_bytes")
-    gsn.gsn_orthogonalise(p, x, out, ws)
+    gsn.gsn_orthogonalise(p, x, out, _bytes(size, x))
     return out
 
 
@@ -129,19 +162,15 @@ def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=Tr
     place; new ones if None."""
     _no_tangent(weights, gradient, momentum)
     _no_gradient("orthogonal_step", weights, gradient, momentum)
-    p = gsn.make_orthogonal(weights, steps, coefficients, eps)
+    p, size = _orthogonal(*_matrices(weights), steps, tuple(coefficients), eps, True)
     new_weights, new_momentum = out if out is not None else (
         torch.empty_like(weights, memory_format=torch.contiguous_format),
         torch.empty_like(momentum, memory_format=torch.contiguous_format))
     _same_device(weights, gradient, momentum, new_weights, new_momentum)
-    if weights.numel() == 0:
-        return new_weights, new_momentum
     if scale is None:
         scale = max(1.0, p.rows / p.cols) ** 0.5
-    ws = _workspace(gsn.gsn_orthogonal_workspace_bytes(p, True), weights,
-                    "gsn_orthogonal_workspace_bytes")
     gsn.gsn_orthogonal_step(p, weights, gradient, momentum, rate * scale, beta, rate * decay,
-                            nesterov, new_weights, new_momentum, ws)
+                            nesterov, new_weights, new_momentum, _bytes(size, weights))
     return new_weights, new_momentum
 
 
@@ -169,9 +198,7 @@ def linear_8bit(x, w, scales):
     _no_tangent(x)
     _no_gradient("linear_8bit", x, scales)
     _same_device(x, w, scales)
-    p = gsn.make_linear8(x, w)
+    p, size = _linear(*_operands(x, w))
     y = x.new_empty(x.shape[0], w.shape[0])
-    ws = _workspace(gsn.gsn_linear_quantised_workspace_bytes(p), x,
-                    "gsn_linear_quantised_workspace_bytes")
-    gsn.gsn_linear_quantised(p, x, w, scales, y, ws)
+    gsn.gsn_linear_quantised(p, x, w, scales, y, _bytes(size, x))
     return y
