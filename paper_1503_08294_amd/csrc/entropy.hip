@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "experts_rule.h"
+#include "few.h"
 
 namespace gsn {
 namespace {
@@ -18,10 +19,11 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 // Workgroups that a product of few tiles is split up into, along k, where a part keeps 1,024 bytes
 // of k at least.
 constexpr int64_t kFill = 512;
-constexpr int64_t kFewTokens = 32;  // that few_rows() takes
-constexpr int64_t kPartCols = 32;   // columns of a part, at least
-// Tokens from which on binary32 operands are split up into two float16 values.
-constexpr int64_t kTwoTokens = 192;
+// Tokens from which on binary32 operands are split up into two float16 values, which takes more
+// memory traffic and fewer cycles of the matrix cores.  As they are and in two values, us, 60,000
+// classes of 1,024: forward 128 tokens 161 and 174, 160 215 and 213, 191 217 and 220; backward 64
+// tokens 303 and 377, 96 467 and 366, 191 700 and 488.
+constexpr int64_t kTwoTokens = 160, kTwoTokensBack = 80;
 
 bool params_ok(const gsn_entropy_params* p) {
   return p && p->dtype >= GSN_F32 && p->dtype <= GSN_F16 && p->tokens >= 0 &&
@@ -55,18 +57,18 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   x.dim = p.dim;
   // (rows of the copies and of d are whole lines of 128 bytes: products read rows that begin inside
   // a line up to a fifth slower)
-  x.two = p.dtype == GSN_F32 && p.tokens >= kTwoTokens;
+  x.two = p.dtype == GSN_F32 && p.tokens >= (backward ? kTwoTokensBack : kTwoTokens);
   x.pitch = static_cast<int32_t>(up_to(p.dim, 64));
   int64_t piece = kPieceBytes / (size * x.pitch);
   if (backward) piece = std::min(piece, kPieceBytes / (size * tokens));
   else piece = std::min(piece, kPartBytes / (8 * tokens) * kSmallRows);
   piece = std::max<int64_t>(piece / 256 * 256, 256);
   // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
-  x.few = !backward && p.tokens <= kFewTokens;
-  if (x.few) piece = up_to(p.classes, 256);
+  x.few = !backward && p.tokens <= few_at_most(p.dtype == GSN_F32, true);
   x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 64)));
   x.pieces = (p.classes - 1) / x.piece + 1;
-  x.parts = static_cast<int32_t>(up_to(x.piece, kPartCols) / kPartCols);
+  const bool may_be_few = p.tokens <= few_at_most(p.dtype == GSN_F32, false);
+  x.parts = static_cast<int32_t>(up_to(may_be_few ? p.classes : x.piece, kFewCols) / kFewCols);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
   x.splits_w = split_of(x.piece, x.pitch, tokens, p.dtype);
   return x;
@@ -173,6 +175,7 @@ int gsn_cross_entropy(const gsn_entropy_params* p, const void* x, int64_t x_stri
   a.stats = stats;
   a.copy_x = a.two || !gsn::in_place(x, x_stride, p->dim, p->dtype);
   a.copy_w = a.two || !gsn::in_place(w, w_stride, p->dim, p->dtype);
+  if (p->tokens <= gsn::few_at_most(p->dtype == GSN_F32, !a.copy_w)) a.few = true;
   gsn::carve_forward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32    ? gsn::launch_entropy<float>(a, st)

@@ -205,8 +205,9 @@ template <typename T>
 hipError_t launch(const Linear8& x, hipStream_t st) {
   // A few tokens: w is read once, as it is.  Otherwise its rows have to begin and end at multiples
   // of 16 bytes.
-  const bool few = x.tokens <= kFewRows;
-  const bool copy = !few && (!aligned16(x.w) || x.w_stride % 16 != 0 || x.dim % 16 != 0);
+  const bool aligned = aligned16(x.w) && x.w_stride % 16 == 0 && x.dim % 16 == 0;
+  const bool few = x.tokens <= few_at_most(false, aligned);
+  const bool copy = !few && !aligned;
   const uint32_t blocks = row_blocks(x.tokens);
   const int64_t copies =
       (static_cast<int64_t>(x.out) * (x.pitch / 16) + kRowThreads - 1) / kRowThreads;
