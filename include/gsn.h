@@ -623,8 +623,9 @@ int gsn_orthogonalise(const gsn_orthogonal_params* params, const void* x, void* 
  *     new_momentum = beta momentum + gradient
  *     u = gradient + beta new_momentum (nesterov != 0) or new_momentum
  *     new_weights = (1 - decay) weights - rate orthogonal(u)
- * gradient of type dtype, momentum float.  new_weights may be the memory of weights, new_momentum
- * that of momentum. */
+ * gradient of type dtype, momentum float.  new_weights may be the memory of weights or of gradient,
+ * new_momentum that of momentum; other outputs that are the memory of another array are refused
+ * (GSN_E_INVAL), as far as they begin at one place. */
 int gsn_orthogonal_step(const gsn_orthogonal_params* params, const void* weights,
                         const void* gradient, const float* momentum, float rate, float beta,
                         float decay, int32_t nesterov, void* new_weights, float* new_momentum,

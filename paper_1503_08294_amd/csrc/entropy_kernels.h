@@ -108,7 +108,7 @@ struct Reduce {
         for (int j = 0; j < NT; ++j)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            if (place == 16 * j + q && acc[i][j][q] != -INFINITY) x.chosen[t] = acc[i][j][q];
+            if (place == 16 * j + q) x.chosen[t] = acc[i][j][q];
       }
       float top = acc[i][0][0];
 #pragma unroll

@@ -686,6 +686,10 @@ int gsn_orthogonal_step(const gsn_orthogonal_params* p, const void* weights, con
     return GSN_E_INVAL;
   if (p->batch == 0) return GSN_OK;
   if (!weights || !gradient || !momentum || !new_weights || !new_momentum) return GSN_E_INVAL;
+  // (the new momentum is written while both are still read, the new weights after it is)
+  if (new_momentum == gradient || new_momentum == weights || new_weights == new_momentum ||
+      new_weights == momentum)
+    return GSN_E_INVAL;
   gsn::Orthogonal a = gsn::orthogonal_of(*p, true);
   a.x = gradient;
   a.momentum = momentum;

@@ -79,13 +79,16 @@ struct Tile {
   static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024 && WAVES % GROUPS == 0);
 };
 
-// Place of 16-byte chunk c in row r of a staged operand with k contiguous: the 16 rows that a
-// quarter wave reads at one k fall on different banks.
+// Place of 16-byte chunk c in row r of a staged operand with k contiguous.  LDS serves a wave's reads
+// of 16 bytes 16 lanes at a time, of 0 to 31 first lanes 0-3, 12-15, 20-23 and 24-27, then the rest:
+// a fragment's rows 0-3 and 12-15 at one chunk and 4-11 at the next have to fall on different banks.
+// (Rows of 64 bytes with c ^ ((r >> 2) & 3), which keeps 16 rows of one chunk apart: a quarter of the
+// reads' cycles were conflicts.)
 template <int KB>
 __device__ __forceinline__ int chunk_row(int r, int c) {
   static_assert(KB == 128 || KB == 64);
   if constexpr (KB == 128) return chunk_k(r, c);
-  else return c ^ ((r >> 2) & 3);
+  else return c ^ ((r >> 2 & 1) * 3);
 }
 
 // Fragment of 16 rows at r0 and the s-th 64 bytes of a stage's k; R rows, or columns, in all.
@@ -370,7 +373,7 @@ void run_tiles(Product p, const EPI& epi, hipStream_t st) {
 // groups of waves share k.  With one group and two: tiles of 128: 2,048 x 2,048 x 2,048 (256) 28,
 // 23; tiles of 64 from 8 stages on: 1,024 x 1,024 x 2,048 (256) 15, 12; 2,048 x 1,024 x 2,048 (512)
 // 19, 16; 1,024 x 768 x 512 7.2, 7.2; 8 bits, 64 rows by 16,384 of 4,096 (256, memory) 14.6, 13.1.
-using LargeTile = Tile<128, 256, 64, 2, 2, 32, 8>;
+using LargeTile = Tile<128, 256, 64, 3, 2, 32, 8>;
 using MiddleTile = Tile<128, 128, 128, 2, 2, 16, 4>;
 using MiddleTwo = Tile<128, 128, 128, 2, 2, 16, 4, 2>;
 using SmallTile = Tile<64, 64, 128, 3, 3, 1, 4>;

@@ -158,8 +158,8 @@ def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=Tr
 
     (of the momentum alone without nesterov).  scale: sqrt(max(1, rows / cols)) if None, so that
     the update moves outputs as far whatever the shape.  momentum is float32, gradient of the type
-    of weights.  out: the two tensors that take the results, (weights, momentum) for an update in
-    place; new ones if None."""
+    of weights, all contiguous.  out: the two tensors that take the results, (weights, momentum) for
+    an update in place; new ones if None."""
     _no_tangent(weights, gradient, momentum)
     _no_gradient("orthogonal_step", weights, gradient, momentum)
     p, size = _orthogonal(*_matrices(weights), steps, tuple(coefficients), eps, True)

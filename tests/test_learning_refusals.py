@@ -78,8 +78,13 @@ def test_orthogonal_arguments():
     each(gsn._lib.gsn_orthogonalise, [p, FAKE, FAKE, FAKE, LOTS, None],
          [(0, None, INVAL), (1, None, INVAL), (2, None, INVAL), (3, None, INVAL),
           (3, FAKE + 128, INVAL), (4, size(p, False) - 1, CAPACITY)])
-    good = [p, FAKE, FAKE, FAKE, 0.1, 0.9, 0.0, 1, FAKE, FAKE, FAKE, LOTS, None]
+    w, g, m, new_w, new_m = (FAKE * i for i in range(1, 6))
+    good = [p, w, g, m, 0.1, 0.9, 0.0, 1, new_w, new_m, FAKE, LOTS, None]
     nan = float("nan")
+    # outputs over what is still read: not the weights or the gradient for the momentum, nor either
+    # momentum for the weights
+    each(gsn._lib.gsn_orthogonal_step, good,
+         [(9, g, INVAL), (9, w, INVAL), (9, new_w, INVAL), (8, m, INVAL)])
     each(gsn._lib.gsn_orthogonal_step, good,
          [(0, None, INVAL), (1, None, INVAL), (2, None, INVAL), (3, None, INVAL), (4, nan, INVAL),
           (5, nan, INVAL), (6, float("inf"), INVAL), (8, None, INVAL), (9, None, INVAL),
