@@ -123,6 +123,27 @@ def test_entropy_strides(learn, dtype, dim, pad):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [3, 200])
+def test_entropy_of_an_impossible_target(learn, dtype, tokens):
+    """A target whose logit is -inf has an infinite loss; the other tokens keep theirs."""
+    x, w, t, _, _ = entropy_inputs(tokens, 24, 50, dtype, 14)
+    x[1] = 0
+    x[1, 3] = torch.inf
+    w[:, 3] = w[:, 3].abs() + 0.1
+    w[t[1].long(), 3] = -1
+    w[:, 3] *= -1  # every logit of token 1 is -inf but its target's, which is inf: NaN
+    t[2] = t[1]
+    loss = learn.cross_entropy(x.cuda(), w.cuda(), t.cuda()).cpu()
+    assert torch.isnan(loss[1])
+    w[:, 3] *= -1  # every logit is inf but the target's: NaN too, as inf - inf is
+    loss = learn.cross_entropy(x.cuda(), w.cuda(), t.cuda()).cpu()
+    assert not torch.isfinite(loss[1])
+    keep = torch.arange(tokens) != 1
+    want = ref.cross_entropy(x[keep], w, t[keep])
+    close(loss[keep], want["loss"], want["loss_tol"], "the others")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_entropy_large_and_small_logits(learn, dtype):
     """Logits of some hundreds (exp would overflow), a token that is sure, and a dloss far below the
     others'."""
@@ -137,9 +158,12 @@ def test_entropy_large_and_small_logits(learn, dtype):
 @pytest.mark.parametrize("dtype,tokens,dim,classes", [
     (BF16, 300, 128, 33_000), (F16, 2_100, 64, 9_000), (F32, 1_100, 72, 5_000),
     (BF16, 5_000, 264, 130), (F32, 40, 16, 40_000), (F32, 5_000, 264, 130),
-    (F32, 300, 1_100, 900)])
+    (F32, 300, 1_100, 900), (BF16, 300, 1_100, 2_000), (F16, 700, 520, 2_100),
+    (BF16, 40, 33, 500), (F16, 61, 1_000, 700), (F32, 100, 48, 300), (F32, 70, 600, 1_000),
+    (F32, 33, 130, 200), (BF16, 1_500, 300, 1_700)])
 def test_entropy_many_classes_or_tokens(learn, dtype, tokens, dim, classes):
-    """Tiles of 128, sums split up along the classes and along the tokens."""
+    """Tiles of every size, groups of waves that share k, sums split up along the classes and along
+    the tokens, few tokens of rows that begin anywhere."""
     check_entropy(learn, *entropy_inputs(tokens, dim, classes, dtype, 6, shut=0.02, lost=0.02),
                   f"{dtype}")
 
@@ -319,13 +343,31 @@ def test_orthogonalise_shapes(learn):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("batch,rows,cols", [(1, 520, 1100), (5, 700, 300), (40, 136, 200)])
+@pytest.mark.parametrize("batch,rows,cols", [(1, 520, 1100), (5, 700, 300), (40, 136, 200),
+                                             (14, 300, 260), (70, 300, 520), (70, 520, 300)])
 def test_orthogonalise_larger(learn, dtype, batch, rows, cols):
-    """Tiles of 128 too."""
+    """Tiles of every size; after one step little is passed on, and the bound is tight."""
     x = randn(batch, rows, cols, seed=24, dtype=dtype)
-    got = learn.orthogonalise(x.cuda())
     pick = sorted({0, batch // 2, batch - 1})
-    check_orthogonal(got[pick], x[pick], dtype, 2, f"{dtype}")
+    for steps in (5, 1):
+        got = learn.orthogonalise(x.cuda(), steps=steps)
+        check_orthogonal(got[pick], x[pick], dtype, 2, f"{dtype}", steps=steps)
+
+
+def test_orthogonal_step_of_a_large_batch(learn):
+    """One float16 value a number, in the largest tiles."""
+    w, g = (randn(70, 520, 300, seed=s, dtype=BF16) for s in (48, 49))
+    m = randn(70, 520, 300, seed=50)
+    got, got_m = learn.orthogonal_step(w.cuda(), g.cuda(), m.cuda(), 0.5, steps=2)
+    for i in (0, 33, 69):
+        want_m = 0.95 * m[i].double() + g[i].double()
+        u = g[i].double() + 0.95 * want_m
+        o = ref.orthogonalise(u, steps=2)
+        want = w[i].double() - 0.5 * (520 / 300) ** 0.5 * o
+        tol = 0.5 * (520 / 300) ** 0.5 * ref.orthogonal_error(u, 1, steps=2) * (1 + 2.0 ** -10) \
+            + (want * 2.0 ** -8).norm() + 1e-5 * want.norm()
+        assert (got[i].double().cpu() - want).norm() <= tol
+        close(got_m[i], want_m, 3 * ref.U * (m[i].abs().double() + g[i].abs().double()), "momentum")
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -405,7 +447,9 @@ def test_quantise_borders_and_odd_rows(learn, dtype):
 @pytest.mark.parametrize("tokens,dim,out", [(1, 1, 1), (1, 64, 100), (1, 4096, 333), (2, 17, 33),
                                             (5, 16, 64), (16, 1000, 129), (17, 80, 70),
                                             (64, 512, 1000), (65, 33, 257), (200, 1111, 130),
-                                            (2_000, 96, 2_100)])
+                                            (2_000, 96, 2_100), (300, 2_048, 1_000),
+                                            (1_500, 200, 1_704), (700, 1_024, 2_104),
+                                            (40, 1_001, 500), (17, 4_096, 64)])
 def test_linear(learn, dtype, tokens, dim, out):
     x = randn(tokens, dim, seed=32, dtype=dtype, scale=2.0)
     check_linear(learn, x, dtype, out, f"{dtype}")
@@ -420,6 +464,32 @@ def test_linear_strides(learn, dtype, tokens, pad):
         return b.cuda()[:, pad:-pad]
 
     check_linear(learn, randn(tokens, 60, seed=33, dtype=dtype), dtype, 90, f"{dtype}", wide)
+
+
+@pytest.mark.parametrize("tokens", [3, 70])
+@pytest.mark.parametrize("pad", [3, 16])
+def test_what_is_beside_the_results_stays(learn, tokens, pad):
+    """Outputs in the middle of wider buffers: what is around them is left as it was."""
+    from paper_1503_08294_amd import gsn
+    x = randn(tokens, 48, seed=51, dtype=BF16).cuda()
+    q = torch.full((tokens + 2, 48 + 2 * pad), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((tokens + 2,), -7.0, device="cuda")
+    gsn.gsn_quantise(x, q[1:-1, pad:-pad], s[1:-1])
+    want_q, want_s = ref.quantise(x.cpu())
+    assert torch.equal(q[1:-1, pad:-pad].cpu().long(), want_q)
+    assert torch.equal(s[1:-1].cpu(), want_s) and (s[[0, -1]] == -7).all()
+    q[1:-1, pad:-pad] = 99
+    assert (q == 99).all()
+    w, ws = learn.quantise(randn(90, 48, seed=52).cuda())
+    y = torch.full((tokens + 2, 90 + 2 * pad), 5.0, dtype=BF16, device="cuda")
+    p = gsn.gsn_linear_params(gsn.GSN_BF16, 48, 90, tokens)
+    room = torch.empty(gsn.gsn_linear_quantised_workspace_bytes(p), dtype=torch.uint8,
+                       device="cuda")
+    gsn.gsn_linear_quantised(p, x, w, ws, y[1:-1, pad:-pad], room)
+    want, tol = ref.linear_8bit(x.cpu(), w.cpu(), ws.cpu())
+    close(y[1:-1, pad:-pad], want, tol, "y")
+    y[1:-1, pad:-pad] = 5
+    assert (y == 5).all()
 
 
 def test_linear_largest_sums(learn):
