@@ -197,6 +197,90 @@ struct Scaled {
   }
 };
 
+// One or two tokens in one launch: every workgroup brings the tokens to 8 bits for itself, in LDS,
+// while its first rows of w are on their way, and takes 32 columns as few_rows() does.  One token
+// through 4,096 x 16,384: 12.6 us, 15.7 as two launches.
+constexpr int64_t kTokensAlone = 2;
+constexpr int32_t kDimAlone = 16384;
+template <typename T>
+__global__ __launch_bounds__(256) void q8_alone(Linear8 x) {
+  constexpr int kStep = kRowBytes, GT = kFewCols / 16;
+  __shared__ __attribute__((aligned(16))) int8_t q[kTokensAlone * kDimAlone];
+  __shared__ float scale[kTokensAlone];
+  __shared__ i32x4 part[4][GT][kWave];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int g = lane >> 4, i = lane & 15;
+  const int32_t n0 = blockIdx.x * kFewCols, dim = x.dim;
+  const int8_t* w[GT];
+#pragma unroll
+  for (int t = 0; t < GT; ++t) {
+    const int32_t n = n0 + 16 * t + i;
+    w[t] = x.w + (n < x.out ? n : x.out - 1) * x.w_stride;
+  }
+  const int32_t steps = (dim + kStep - 1) / kStep, per = (steps + 3) / 4;
+  const int32_t k_begin = wave * per * kStep;
+  const int32_t k_end = k_begin + per * kStep < dim ? k_begin + per * kStep : dim;
+  Frag fw[2][GT];
+  const auto load = [&](auto inside, int32_t k0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < GT; ++t)
+        fw[h][t] = row_chunk<decltype(inside)::value>(w[t], k0 + (4 * h + g) * 16, dim);
+  };
+  const bool whole = k_begin + kStep <= k_end;
+  if (whole) load(std::true_type(), k_begin);
+  const int32_t pitch = x.pitch;
+  quantise_rows(static_cast<const T*>(x.x), x.x_stride, x.tokens, dim, q, pitch, pitch, scale, 0,
+                1);
+  __syncthreads();
+
+  i32x4 acc[GT] = {};
+  const bool live = i < x.tokens;
+  const auto multiply_these = [&](const Frag (&a)[2][GT], int32_t k0) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t k = k0 + (4 * h + g) * 16;
+      Frag f;
+      f.u = u32x4{0, 0, 0, 0};
+      if (live && k < pitch) f.u = *reinterpret_cast<const u32x4*>(q + i * pitch + k);
+#pragma unroll
+      for (int t = 0; t < GT; ++t) acc[t] = multiply_any<int8_t>(a[h][t], f, acc[t], 0);
+    }
+  };
+  int32_t k0 = k_begin;
+  if (whole) {
+    for (; k0 + 2 * kStep <= k_end; k0 += kStep) {
+      Frag a[2][GT];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < GT; ++t) a[h][t] = fw[h][t];
+      load(std::true_type(), k0 + kStep);
+      multiply_these(a, k0);
+    }
+    multiply_these(fw, k0);
+    k0 += kStep;
+  }
+  if (k0 < k_end) {
+    load(std::false_type(), k0);
+    multiply_these(fw, k0);
+  }
+#pragma unroll
+  for (int t = 0; t < GT; ++t) part[wave][t][lane] = acc[t];
+  __syncthreads();
+  const int m = tid >> 3, c = tid & 7, n = n0 + 4 * c;
+  if (m >= x.tokens || n >= x.out) return;
+  i32x4 sum = {};
+#pragma unroll
+  for (int u = 0; u < 4; ++u) sum += part[u][c >> 2][(c & 3) * 16 + m];
+  float v[4];
+  load4(x.scales, n, x.out, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = static_cast<float>(sum[e]) * scale[m] * v[e];
+  store4(static_cast<T*>(x.y) + m * x.y_stride, n, x.out, v);
+}
+
 uint32_t row_blocks(int64_t rows) {
   return static_cast<uint32_t>(std::min<int64_t>(rows, 1 << 16));
 }
@@ -208,6 +292,10 @@ hipError_t launch(const Linear8& x, hipStream_t st) {
   const bool aligned = aligned16(x.w) && x.w_stride % 16 == 0 && x.dim % 16 == 0;
   const bool few = x.tokens <= few_at_most(false, aligned);
   const bool copy = !few && !aligned;
+  if (x.tokens <= kTokensAlone && x.pitch <= kDimAlone) {
+    q8_alone<T><<<static_cast<uint32_t>((x.out + kFewCols - 1) / kFewCols), 256, 0, st>>>(x);
+    return hipGetLastError();
+  }
   const uint32_t blocks = row_blocks(x.tokens);
   const int64_t copies =
       (static_cast<int64_t>(x.out) * (x.pitch / 16) + kRowThreads - 1) / kRowThreads;

@@ -79,11 +79,11 @@ struct Tile {
   static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024 && WAVES % GROUPS == 0);
 };
 
-// Place of 16-byte chunk c in row r of a staged operand with k contiguous.  LDS serves a wave's reads
-// of 16 bytes 16 lanes at a time, of 0 to 31 first lanes 0-3, 12-15, 20-23 and 24-27, then the rest:
-// a fragment's rows 0-3 and 12-15 at one chunk and 4-11 at the next have to fall on different banks.
-// (Rows of 64 bytes with c ^ ((r >> 2) & 3), which keeps 16 rows of one chunk apart: a quarter of the
-// reads' cycles were conflicts.)
+// Place of 16-byte chunk c in row r of a staged operand with k contiguous.  LDS serves a wave's
+// reads of 16 bytes 16 lanes at a time, of 0 to 31 first lanes 0-3, 12-15, 20-23 and 24-27, then
+// the rest: a fragment's rows 0-3 and 12-15 at one chunk and 4-11 at the next have to fall on different
+// banks.  (Rows of 64 bytes with c ^ ((r >> 2) & 3), which keeps 16 rows of one chunk apart: a
+// quarter of the reads' cycles were conflicts.)
 template <int KB>
 __device__ __forceinline__ int chunk_row(int r, int c) {
   static_assert(KB == 128 || KB == 64);
@@ -379,6 +379,10 @@ using MiddleTwo = Tile<128, 128, 128, 2, 2, 16, 4, 2>;
 using SmallTile = Tile<64, 64, 128, 3, 3, 1, 4>;
 using SmallTwo = Tile<64, 64, 128, 2, 4, 1, 4, 2>;      // two workgroups a CU
 using SmallTwoAlone = Tile<64, 64, 128, 3, 2, 1, 4, 2>;  // one
+// Few rows: small tiles of which some are left after the 768 that the CUs take at a time; wider
+// ones are one round (64 rows by 50,000 of 1,024, 782 tiles: 18 us and 22; by 49,152 19 and 18; by
+// 100,000 40 and 35).
+using FlatTile = Tile<64, 128, 128, 2, 3, 1, 4>;
 
 // f(a tile's type) for the tiles of a product.
 template <typename T, bool TRA, bool TRB, class F>
@@ -400,6 +404,8 @@ void with_tile(Product p, const F& f) {
     if (p.a.rows > SmallTile::BM && middle >= 144) return f(MiddleTwo());
   }
   const int64_t small = tiles(SmallTile::BM, SmallTile::BN);
+  if (p.a.rows <= SmallTile::BM && small > 768 && small <= 1024 && sizeof(T) < 4)
+    return f(FlatTile());
   if (bytes < 8 * SmallTile::KB || small > 512) return f(SmallTile());
   if (small <= 256) f(SmallTwoAlone());
   else f(SmallTwo());

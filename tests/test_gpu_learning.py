@@ -160,7 +160,7 @@ def test_entropy_large_and_small_logits(learn, dtype):
     (BF16, 5_000, 264, 130), (F32, 40, 16, 40_000), (F32, 5_000, 264, 130),
     (F32, 300, 1_100, 900), (BF16, 300, 1_100, 2_000), (F16, 700, 520, 2_100),
     (BF16, 40, 33, 500), (F16, 61, 1_000, 700), (F32, 100, 48, 300), (F32, 70, 600, 1_000),
-    (F32, 33, 130, 200), (BF16, 1_500, 300, 1_700)])
+    (F32, 33, 130, 200), (BF16, 1_500, 300, 1_700), (F16, 40, 64, 50_001)])
 def test_entropy_many_classes_or_tokens(learn, dtype, tokens, dim, classes):
     """Tiles of every size, groups of waves that share k, sums split up along the classes and along
     the tokens, few tokens of rows that begin anywhere."""
@@ -449,7 +449,8 @@ def test_quantise_borders_and_odd_rows(learn, dtype):
                                             (64, 512, 1000), (65, 33, 257), (200, 1111, 130),
                                             (2_000, 96, 2_100), (300, 2_048, 1_000),
                                             (1_500, 200, 1_704), (700, 1_024, 2_104),
-                                            (40, 1_001, 500), (17, 4_096, 64)])
+                                            (40, 1_001, 500), (17, 4_096, 64), (2, 16_384, 40),
+                                            (1, 16_385, 40), (2, 1_000, 33)])
 def test_linear(learn, dtype, tokens, dim, out):
     x = randn(tokens, dim, seed=32, dtype=dtype, scale=2.0)
     check_linear(learn, x, dtype, out, f"{dtype}")
