@@ -65,44 +65,29 @@ __device__ __forceinline__ AccOf<T> multiply_any(const Frag& n, const Frag& m, A
     return multiply<T>(n, m, acc, q);
 }
 
-// Tiles of BM x BN by four waves, 2 x 2 of them: stages of KB bytes of k, SLOTS of them in LDS, and
-// WAVES of a SIMD that registers and LDS have to last for.  RUN of them at a time are an XCD's, in
-// blocks TALL tiles high.  GROUPS of four waves take a part of the stages each, with SLOTS of their
+// Tiles of BM x BN by four waves, 2 x 2 of them: stages of 128 bytes of k, SLOTS of them in LDS,
+// and WAVES of a SIMD that registers and LDS have to last for.  RUN of them at a time are an XCD's,
+// in blocks TALL tiles high.  GROUPS of four waves take a part of the stages each, with SLOTS of their
 // own, and add their sums up in the groups' order.
-template <int BM_, int BN_, int KB_, int SLOTS_, int WAVES_, int RUN_, int TALL_, int GROUPS_ = 1>
+template <int BM_, int BN_, int SLOTS_, int WAVES_, int RUN_, int TALL_, int GROUPS_ = 1>
 struct Tile {
-  static constexpr int BM = BM_, BN = BN_, KB = KB_, SLOTS = SLOTS_, WAVES = WAVES_;
+  static constexpr int BM = BM_, BN = BN_, SLOTS = SLOTS_, WAVES = WAVES_;
   static constexpr int RUN = RUN_, TALL = TALL_, GROUPS = GROUPS_;
-  static constexpr int kSlot = (BM + BN) * KB;
+  static constexpr int kSlot = (BM + BN) * kRowBytes;
   static constexpr int kLds = SLOTS * kSlot;  // of a group
   static constexpr int kThreads = 256 * GROUPS;
   static_assert(BN % BM == 0 && kLds * WAVES <= 160 * 1024 && WAVES % GROUPS == 0);
 };
 
-// Place of 16-byte chunk c in row r of a staged operand with k contiguous.  LDS serves a wave's
-// reads of 16 bytes 16 lanes at a time, of 0 to 31 first lanes 0-3, 12-15, 20-23 and 24-27, then
-// the rest: a fragment's rows 0-3 and 12-15 at one chunk and 4-11 at the next have to fall on different
-// banks.  (Rows of 64 bytes with c ^ ((r >> 2) & 3), which keeps 16 rows of one chunk apart: a
-// quarter of the reads' cycles were conflicts.)
-template <int KB>
-__device__ __forceinline__ int chunk_row(int r, int c) {
-  static_assert(KB == 128 || KB == 64);
-  if constexpr (KB == 128) return chunk_k(r, c);
-  else return c ^ ((r >> 2 & 1) * 3);
-}
-
-// Fragment of 16 rows at r0 and the s-th 64 bytes of a stage's k; R rows, or columns, in all.
-template <typename T, bool TR, int R, int KB>
+// Fragment of 16 rows at r0 and the s-th half of a stage's k; R rows, or columns, in all.  (8-bit
+// elements lie as the bytes of wider ones do.)
+template <typename T, bool TR, int R>
 __device__ __forceinline__ Frag fragment_any(const char* tile, int r0, int s, int lane) {
-  if constexpr (TR) {
-    static_assert(sizeof(T) > 1);
-    return fragment<T, true, R>(tile, r0, s, lane);
+  if constexpr (sizeof(T) == 1) {
+    static_assert(!TR);
+    return fragment<float, false, R>(tile, r0, s, lane);
   } else {
-    const int r = r0 + (lane & 15);
-    Frag f;
-    f.u = *reinterpret_cast<const u32x4*>(tile + r * KB +
-                                          chunk_row<KB>(r, 4 * s + (lane >> 4)) * 16);
-    return f;
+    return fragment<T, TR, R>(tile, r0, s, lane);
   }
 }
 
@@ -115,15 +100,15 @@ __device__ __forceinline__ float settled(float v) {
 }
 
 // What this lane loads of one operand's stages: of stage h the chunks j THR + thread for j = 0, 1,
-// ..., SIDE rows (or columns) of KB bytes of k in all.
-template <typename T, bool TR, int SIDE, int KB, int THR>
+// ..., SIDE rows (or columns) of 128 bytes of k in all.
+template <typename T, bool TR, int SIDE, int THR>
 struct Feed {
   static constexpr int kE = 16 / static_cast<int>(sizeof(T));
-  static constexpr int kBK = KB / static_cast<int>(sizeof(T));
-  static constexpr int kC = TR ? SIDE / kE : KB / 16;  // chunks of a row
-  static constexpr int kLoads = SIDE * KB / 16 / THR;
+  static constexpr int kBK = kRowBytes / static_cast<int>(sizeof(T));
+  static constexpr int kC = TR ? SIDE / kE : 8;  // chunks of a row
+  static constexpr int kLoads = SIDE * 8 / THR;
   static constexpr int kStep = THR / kC;  // rows from one j to the next
-  static_assert(THR % kC == 0 && SIDE * KB / 16 % THR == 0);
+  static_assert(THR % kC == 0 && SIDE * 8 % THR == 0);
 
   const char* p;   // the chunk j = 0 of the next stage
   int64_t ld, step;
@@ -133,7 +118,7 @@ struct Feed {
 
   __device__ __forceinline__ static int chunk(int row, int c) {
     if constexpr (TR) return chunk_n<T, kC>(row, c);
-    else return chunk_row<KB>(row, c);
+    else return chunk_k(row, c);
   }
   __device__ __forceinline__ void begin(const Operand& o, int32_t pair, int32_t row0, int32_t k0,
                                         int32_t k_end, int tid) {
@@ -150,7 +135,7 @@ struct Feed {
     } else {
       p = base + static_cast<int64_t>(row0 + r) * ld +
           (static_cast<int64_t>(k0) + c * kE) * static_cast<int>(sizeof(T));
-      step = KB;
+      step = kRowBytes;
       k = k0 + c * kE;
       left = o.rows - row0 - r;
     }
@@ -248,9 +233,9 @@ constexpr int kProductThreads = 256;
 // that no other wave reads any more.
 template <typename T, bool TRA, bool TRB, class TILE, class EPI>
 __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Product p, EPI epi) {
-  constexpr int kThr = kProductThreads, BM = TILE::BM, BN = TILE::BN, KB = TILE::KB;
+  constexpr int kThr = kProductThreads, BM = TILE::BM, BN = TILE::BN;
   constexpr int MT = BM / 32, NT = BN / 32, kSlot = TILE::kSlot, SLOTS = TILE::SLOTS;
-  static_assert(SLOTS == 2 || SLOTS == 3);
+  static_assert(SLOTS >= 1 && SLOTS <= 3);
   constexpr int GROUPS = TILE::GROUPS;
   __shared__ __attribute__((aligned(1024))) char lds_all[GROUPS * TILE::kLds];
   const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kThr);
@@ -261,8 +246,8 @@ __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Produc
   Place at;
   if (!place_of<TILE>(p, blockIdx.x, &at)) return;
 
-  using FeedA = Feed<T, TRA, BM, KB, kThr>;
-  using FeedB = Feed<T, TRB, BN, KB, kThr>;
+  using FeedA = Feed<T, TRA, BM, kThr>;
+  using FeedB = Feed<T, TRB, BN, kThr>;
   constexpr int kBK = FeedA::kBK, kLoads = FeedA::kLoads + FeedB::kLoads;
   const int32_t k0 = at.split * p.part;
   const int32_t k_end = k0 + p.part < p.k ? k0 + p.part : p.k;
@@ -288,7 +273,7 @@ __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Produc
   }
   const auto load = [&](int slot) {
     fa.load(lds + slot * kSlot);
-    fb.load(lds + slot * kSlot + BM * KB);
+    fb.load(lds + slot * kSlot + BM * kRowBytes);
     if (++in_term == each) {
       in_term = 0;
       fa.turn(term == 0 ? p.a.next[0] : p.a.next[1], each);
@@ -307,19 +292,29 @@ __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Produc
   if (SLOTS > 2 && stages > 1) load(1);
   int slot = 0;
   for (int32_t h = 0; h < most; ++h) {
-    if (SLOTS > 2 && h + 1 < stages) meet_loaded<kLoads>();
-    else meet_loaded<0>();
-    if (GROUPS > 1 && h >= stages) continue;
-    if (h + SLOTS - 1 < stages) load(slot == 0 ? SLOTS - 1 : slot - 1);
+    if constexpr (SLOTS == 1) {
+      // (the other workgroups of the CU multiply while this one's stage is on its way)
+      if (h > 0) {
+        meet_read();
+        if (h < stages) load(0);
+      }
+      meet_loaded<0>();
+      if (GROUPS > 1 && h >= stages) continue;
+    } else {
+      if (SLOTS > 2 && h + 1 < stages) meet_loaded<kLoads>();
+      else meet_loaded<0>();
+      if (GROUPS > 1 && h >= stages) continue;
+      if (h + SLOTS - 1 < stages) load(slot == 0 ? SLOTS - 1 : slot - 1);
+    }
     const char* const sa = smem + slot * kSlot;
-    const char* const sb = sa + BM * KB;
+    const char* const sb = sa + BM * kRowBytes;
 #pragma unroll
-    for (int s = 0; s < KB / 64; ++s) {
+    for (int s = 0; s < 2; ++s) {
       Frag ra[MT], rb[NT];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) rb[j] = fragment_any<T, TRB, BN, KB>(sb, nw + j * 16, s, lane);
+      for (int j = 0; j < NT; ++j) rb[j] = fragment_any<T, TRB, BN>(sb, nw + j * 16, s, lane);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) ra[i] = fragment_any<T, TRA, BM, KB>(sa, mw + i * 16, s, lane);
+      for (int i = 0; i < MT; ++i) ra[i] = fragment_any<T, TRA, BM>(sa, mw + i * 16, s, lane);
 #pragma unroll
       for (int q = 0; q < kParts<T>; ++q)
 #pragma unroll
@@ -327,7 +322,7 @@ __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Produc
 #pragma unroll
           for (int j = 0; j < NT; ++j) acc[i][j] = multiply_any<T>(rb[j], ra[i], acc[i][j], q);
     }
-    slot = slot + 1 == SLOTS ? 0 : slot + 1;
+    if constexpr (SLOTS > 1) slot = slot + 1 == SLOTS ? 0 : slot + 1;
   }
   meet_read();
   if constexpr (GROUPS > 1) {
@@ -361,28 +356,36 @@ void run_tiles(Product p, const EPI& epi, hipStream_t st) {
 
 // Which tiles a product takes.  Of 2-byte elements, us, C of bfloat16, tiles of 128 x 256, 128 x
 // 128 and 64 x 64 (two workgroups a CU of the first two, three of the last):
-//   k contiguous: 8,192 x 8,192 x 2,048: 280, 277, 613; 4,096 x 4,096 x 1,024: 42, 41, 63;
-//     2,048 x 2,048 x 1,024 (256 tiles of 128): 25, 16, 18; 1,536 x 1,536 x 1,024: 25, 15, 13
-//   n contiguous in B: 257, 283, 655; 40, 42, 68; 27, 17, 20; 26, 16, 14
-//   m and n contiguous: 256, 300, 671; 40, 45, 69; 27, 18, 21; 27, 17, 15
-//     (4,096 x 2,048 x 1,024, 256 tiles of 128 x 256: 30, 25, 35)
-// With k contiguous a stage of 64 bytes reads half lines of memory, and the middle tiles' 128 bytes
-// make up for their size.  Binary32 products are bound by the matrix cores, and small tiles fill
-// the CUs more evenly.
+//   k contiguous: 8,192 x 4,096 x 1,024: 75, 84, 118; 4,096 x 4,096 (512 tiles of 128 x 256): 39,
+//     44, 62; 4,096 x 2,048: 29, 24, 31; 2,048 x 2,048 (256 of 128): 24, 16, 20; 1,536 x 1,536: 24,
+//     15, 13
+//   n contiguous in B: 77, 87, 134; 41, 44, 67; 32, 24, 35; 25, 17, 20; 27, 16, 14
+//   m and n contiguous: 76, 90, 134; 41, 46, 69; 33, 25, 34; 26, 17, 21; 28, 17, 15
+//   8 bits, 4,096 x 4,096 x 4,096: 65, 76, 159
+// The large tiles have one place for a stage: a workgroup waits for its loads while the other one
+// multiplies, and the registers that a stage ahead would take and the half lines that two stages of
+// half the size would read cost more (8,192 x 32,768 x 2,048, k contiguous: 1,007 us; 1,099 with
+// three places for 64 bytes of k; tiles of 128 with two places for 128 bytes 1,130, with one 1,003;
+// 8,192 x 2,048 x 32,768: 978, 957, 1,085, 1,161).  MFMAs of 32 x 32 in place of 16 x 16 were 8 to
+// 12% slower.  The CUs hold 512 of the large or of the middle tiles: the large ones are taken where
+// their rounds, at 0.9 of the time for their size, are not the longer (1,777 x 10,007 x 1,512, 560
+// large tiles or 1,106: 484 and 408 us of a training step).
+// Binary32 products are bound by the matrix cores, and small tiles fill the CUs more evenly.
 // Up to about one workgroup a CU its SIMDs have a wave each, which waits for its own loads: two
 // groups of waves share k.  With one group and two: tiles of 128: 2,048 x 2,048 x 2,048 (256) 28,
 // 23; tiles of 64 from 8 stages on: 1,024 x 1,024 x 2,048 (256) 15, 12; 2,048 x 1,024 x 2,048 (512)
 // 19, 16; 1,024 x 768 x 512 7.2, 7.2; 8 bits, 64 rows by 16,384 of 4,096 (256, memory) 14.6, 13.1.
-using LargeTile = Tile<128, 256, 64, 3, 2, 32, 8>;
-using MiddleTile = Tile<128, 128, 128, 2, 2, 16, 4>;
-using MiddleTwo = Tile<128, 128, 128, 2, 2, 16, 4, 2>;
-using SmallTile = Tile<64, 64, 128, 3, 3, 1, 4>;
-using SmallTwo = Tile<64, 64, 128, 2, 4, 1, 4, 2>;      // two workgroups a CU
-using SmallTwoAlone = Tile<64, 64, 128, 3, 2, 1, 4, 2>;  // one
+using LargeTile = Tile<128, 256, 1, 2, 32, 8>;
+using MiddleTile = Tile<128, 128, 2, 2, 16, 4>;
+using MiddleMany = Tile<128, 128, 1, 3, 16, 4>;
+using MiddleTwo = Tile<128, 128, 2, 2, 16, 4, 2>;
+using SmallTile = Tile<64, 64, 3, 3, 1, 4>;
+using SmallTwo = Tile<64, 64, 2, 4, 1, 4, 2>;      // two workgroups a CU
+using SmallTwoAlone = Tile<64, 64, 3, 2, 1, 4, 2>;  // one
 // Few rows: small tiles of which some are left after the 768 that the CUs take at a time; wider
 // ones are one round (64 rows by 50,000 of 1,024, 782 tiles: 18 us and 22; by 49,152 19 and 18; by
 // 100,000 40 and 35).
-using FlatTile = Tile<64, 128, 128, 2, 3, 1, 4>;
+using FlatTile = Tile<64, 128, 2, 3, 1, 4>;
 
 // f(a tile's type) for the tiles of a product.
 template <typename T, bool TRA, bool TRB, class F>
@@ -396,17 +399,22 @@ void with_tile(Product p, const F& f) {
   const int64_t middle = tiles(MiddleTile::BM, MiddleTile::BN);
   const int64_t bytes = int64_t{p.part} * p.terms * static_cast<int64_t>(sizeof(T));
   if constexpr (sizeof(T) < 4) {
-    if constexpr (TRA || TRB)
-      if (!p.symmetric && tiles(LargeTile::BM, LargeTile::BN) >= 512) return f(LargeTile());
     // (few rows: bound by reading the other operand, of which small tiles have more on its way: 64
-    // rows by 16,384 of 4,096, 26 us and 43)
-    if (p.a.rows > SmallTile::BM && middle > 256) return f(MiddleTile());
-    if (p.a.rows > SmallTile::BM && middle >= 144) return f(MiddleTwo());
+    // rows by 16,384 of 4,096, 26 us and 43; of a symmetric product large tiles would hold more
+    // that is below the diagonal)
+    const bool few = p.a.rows <= SmallTile::BM;
+    const int64_t large = tiles(LargeTile::BM, LargeTile::BN);
+    const auto rounds = [](int64_t n) { return (n + 511) / 512; };
+    if (!few && !p.symmetric && large >= 512 && 18 * rounds(large) <= 10 * rounds(middle))
+      return f(LargeTile());
+    if (!few && middle > 768) return f(MiddleMany());
+    if (!few && middle > 256) return f(MiddleTile());
+    if (!few && middle >= 144) return f(MiddleTwo());
   }
   const int64_t small = tiles(SmallTile::BM, SmallTile::BN);
   if (p.a.rows <= SmallTile::BM && small > 768 && small <= 1024 && sizeof(T) < 4)
     return f(FlatTile());
-  if (bytes < 8 * SmallTile::KB || small > 512) return f(SmallTile());
+  if (bytes < 8 * kRowBytes || small > 512) return f(SmallTile());
   if (small <= 256) f(SmallTwoAlone());
   else f(SmallTwo());
 }
