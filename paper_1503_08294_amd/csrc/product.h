@@ -67,8 +67,8 @@ __device__ __forceinline__ AccOf<T> multiply_any(const Frag& n, const Frag& m, A
 
 // Tiles of BM x BN by four waves, 2 x 2 of them: stages of 128 bytes of k, SLOTS of them in LDS,
 // and WAVES of a SIMD that registers and LDS have to last for.  RUN of them at a time are an XCD's,
-// in blocks TALL tiles high.  GROUPS of four waves take a part of the stages each, with SLOTS of their
-// own, and add their sums up in the groups' order.
+// in blocks TALL tiles high.  GROUPS of four waves take a part of the stages each, with SLOTS of
+// their own, and add their sums up in the groups' order.
 template <int BM_, int BN_, int SLOTS_, int WAVES_, int RUN_, int TALL_, int GROUPS_ = 1>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, SLOTS = SLOTS_, WAVES = WAVES_;
@@ -367,9 +367,12 @@ void run_tiles(Product p, const EPI& epi, hipStream_t st) {
 // half the size would read cost more (8,192 x 32,768 x 2,048, k contiguous: 1,007 us; 1,099 with
 // three places for 64 bytes of k; tiles of 128 with two places for 128 bytes 1,130, with one 1,003;
 // 8,192 x 2,048 x 32,768: 978, 957, 1,085, 1,161).  MFMAs of 32 x 32 in place of 16 x 16 were 8 to
-// 12% slower.  The CUs hold 512 of the large or of the middle tiles: the large ones are taken where
-// their rounds, at 0.9 of the time for their size, are not the longer (1,777 x 10,007 x 1,512, 560
-// large tiles or 1,106: 484 and 408 us of a training step).
+// 12% slower.  The middle tiles have two places where all of them are on the CUs at a time, and
+// one, in three workgroups a CU, where there are more (64 products of 1,024 x 1,024 x 2,048 of
+// which half is made, 2,304 tiles: 212 and 196 us; 4,096 x 2,560 x 1,024, 640 tiles 34 and 33,
+// 4,096 x 2,048, 512 tiles 24 and 24).  The CUs hold 512 of the large or of the middle tiles: the
+// large ones are taken where their rounds, at 0.9 of the time for their size, are not the longer
+// (1,777 x 10,007 x 1,512, 560 large tiles or 1,106: 484 and 408 us of a training step).
 // Binary32 products are bound by the matrix cores, and small tiles fill the CUs more evenly.
 // Up to about one workgroup a CU its SIMDs have a wave each, which waits for its own loads: two
 // groups of waves share k.  With one group and two: tiles of 128: 2,048 x 2,048 x 2,048 (256) 28,
@@ -389,12 +392,10 @@ using FlatTile = Tile<64, 128, 2, 3, 1, 4>;
 
 // f(a tile's type) for the tiles of a product.
 template <typename T, bool TRA, bool TRB, class F>
-void with_tile(Product p, const F& f) {
+void with_tile(const Product& p, const F& f) {
   const auto tiles = [&](int32_t bm, int32_t bn) {
-    p.tiles_m = tiles_of(p.a.rows, bm);
-    p.tiles_n = tiles_of(p.b.rows, bn);
-    const int64_t all = int64_t{p.tiles_m} * p.tiles_n * p.batch * p.splits;
-    return p.symmetric ? all / 2 : all;
+    const int64_t m = tiles_of(p.a.rows, bm), n = tiles_of(p.b.rows, bn);
+    return (p.symmetric && bm == bn ? n * (n + 1) / 2 : m * n) * p.batch * p.splits;
   };
   const int64_t middle = tiles(MiddleTile::BM, MiddleTile::BN);
   const int64_t bytes = int64_t{p.part} * p.terms * static_cast<int64_t>(sizeof(T));
@@ -407,7 +408,7 @@ void with_tile(Product p, const F& f) {
     const auto rounds = [](int64_t n) { return (n + 511) / 512; };
     if (!few && !p.symmetric && large >= 512 && 18 * rounds(large) <= 10 * rounds(middle))
       return f(LargeTile());
-    if (!few && middle > 768) return f(MiddleMany());
+    if (!few && middle > 512) return f(MiddleMany());
     if (!few && middle > 256) return f(MiddleTile());
     if (!few && middle >= 144) return f(MiddleTwo());
   }
