@@ -10,6 +10,11 @@
 // kept times a power of two, which takes its largest element to 2^14 to 2^15, as hi = float16(v)
 // and lo = float16(v - hi): 22 bits of every element down to 2^-18 of the largest, 2^-40 of it
 // below.  A product is hi lo + lo hi + hi hi, three products of one binary32 sum.
+//
+// Bound by the products.  8,192 tokens, 131,072 classes of 2,048, bfloat16: logits reduced 4.0 ms,
+// made again as d 4.7 (in four pieces, 2.1 GB written), dx 3.9, dw 3.9; joins, sums and copies
+// 0.05.  1,777 tokens, 10,007 classes of 501, two values: 82, 103, 67 and 104 us, and 60 for the
+// copies and joins; the tiles of each are one or two rounds of what the CUs hold.
 #pragma once
 
 #include "entropy.h"

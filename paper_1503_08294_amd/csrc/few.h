@@ -21,8 +21,9 @@ struct Few {
 
 // Rows of x up to which this is taken in place of tiles, which read x once a tile from LDS.  The
 // two in us: 50,001 classes of 1,024, bfloat16, 16 rows 28 and 28, 24 rows 32 and 28, 64 rows 48
-// and 28; 60,000 of 1,024, binary32, 32 rows 70 and 88, 33 rows 102 and 88.  Tiles of a w whose rows
-// do not begin at multiples of 16 bytes take a copy of it, which is twice its bytes more to move.
+// and 28; 60,000 of 1,024, binary32, 32 rows 70 and 88, 33 rows 102 and 88.  Tiles of a w whose
+// rows do not begin at multiples of 16 bytes take a copy of it, which is twice its bytes more to
+// move.
 constexpr int64_t few_at_most(bool binary32, bool aligned) {
   return !aligned ? 64 : binary32 ? 32 : 16;
 }

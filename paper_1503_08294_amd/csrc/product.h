@@ -34,8 +34,8 @@ struct Product {
   // with one XCD: 64 pairs, 2,048 x 1,024 by 1,024 x 1,024 of float16, 310 us in eighths and 342 in
   // runs; 4 pairs, 2,048 x 4,096 by its transposed self, three products, 315 and 356; 7 of 666 x
   // 501, 20 and 27.  One pair with few rows and very many columns: 8,192 x 131,072 x 2,048, nothing
-  // written, 4.5 and 4.9 ms; but with its results written a piece of 32,768 columns takes 1.23 and
-  // 1.18, and 8,192 x 2,048 x 32,768 1.10 and 0.96.
+  // written, 4.0 and 4.3 ms; but with its results written (tiles of 128) a piece of 32,768 columns
+  // took 1.23 and 1.18, and 8,192 x 2,048 x 32,768 1.10 and 0.96.
   int32_t eighths;
   int32_t symmetric;  // C = C^T: tiles with n0 >= m0 alone
 };
@@ -224,9 +224,16 @@ __device__ __forceinline__ bool place_of(const Product& p, int32_t number, Place
 constexpr int kProductThreads = 256;
 
 // A tile by four waves.  Stages go from memory straight to LDS; a stage is awaited by all waves
-// together, then a later one is sent out and this one multiplied.  Two or three workgroups share a
-// CU: one's waits, start and results hide behind another's products.  What becomes of the results
-// is the functor's:
+// together, then a later one is sent out (with one place, after this one is multiplied) and this
+// one multiplied.  Two or three workgroups share a CU: one's waits, start and results hide behind
+// another's products.
+//
+// 8,192 tokens, 131,072 classes of 2,048, bfloat16: logits at 1.10 PFLOP/s, the gradients' products
+// at 1.13 (a large library product: 1.31); 8,191 through 4,096 x 8,192 in 8 bits 2.09 POP/s (2.12).
+// There the matrix cores are busy for half of the cycles and LDS for a fifth: what is left is the
+// wait for loads.  A k of a few stages pays for its start and results: 1,024 in float16 0.83.
+//
+// What becomes of the results is the functor's:
 //   EPI::tile<TILE, MT, NT>(acc, place, mw, nw, lane, room)
 // acc[i][j][q] is C(m0 + mw + 16 i + (lane & 15), n0 + nw + 16 j + 4 (lane >> 4) + q); mw and nw
 // are the wave's first row and column in the tile.  All threads of the workgroup come; room is LDS
