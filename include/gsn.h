@@ -566,6 +566,8 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
  * valid: uint8 [classes] or NULL, 0 for a class that is not there: it is in no sum and its row of
  * w means nothing.  A token whose target is out of range or not valid has none: its loss is 0
  * and its x means nothing.  tokens 0 to 2^24, dim 1 to 2^16, classes 1 to 2^28.
+ * GSN_F32 of many tokens (160, backward 80) takes x and w in two float16 values an element, of
+ * which 22 bits are left down to 2^-18 of the largest of its row, and 2^-40 of that below.
  * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128 (GSN_F32: 64 x 64). */
 typedef struct gsn_entropy_params {
   int32_t dtype;
@@ -586,8 +588,10 @@ int gsn_cross_entropy(const gsn_entropy_params* params, const void* x, int64_t x
 /* Gradients from dloss float [tokens]: dx [tokens][dim] and dw [classes][dim] of type dtype,
  * every element written, 0 for tokens without a target and classes that are not valid; each may
  * be NULL (not computed).  The logits' gradients dloss (exp(l) / sum - [c = target]) are rounded
- * to dtype before they are multiplied with w and x; in GSN_F16 as multiples of the largest
- * |dloss|, so that a small dloss loses no digits there. */
+ * to dtype before they are multiplied with w and x; in GSN_F16 as multiples of the largest finite
+ * |dloss|, so that a small dloss loses no digits there; in GSN_F32 of many tokens to two float16
+ * values as above, with the largest of all (times the size of a row of w or x and dloss) in place
+ * of a row's. */
 int gsn_cross_entropy_backward(const gsn_entropy_params* params, const float* dloss,
                                const void* x, int64_t x_stride, const void* w, int64_t w_stride,
                                const int32_t* targets, const uint8_t* valid, const float* stats,
@@ -603,7 +607,8 @@ int gsn_cross_entropy_backward(const gsn_entropy_params* params, const float* dl
  * batch 0 to 2^20, rows and cols 1 to 2^15, steps 1 to 64, eps >= 0.  Coefficients that let a
  * singular value that starts at 1 or less grow past 5, or a + b s^2 + c s^4 past 28 for a value s
  * on its way, are refused (GSN_E_INVAL).  A matrix of zeros stays one (eps = 0 too); one that holds
- * a NaN or an infinity becomes NaN. */
+ * a NaN or an infinity becomes NaN.  GSN_E_CAPACITY if the matrices have some 2^23 tiles of 128 x
+ * 128 or parts of 8,192 elements (256 a matrix at most) in all. */
 typedef struct gsn_orthogonal_params {
   int32_t dtype;
   int32_t rows, cols;

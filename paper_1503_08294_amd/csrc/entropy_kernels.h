@@ -24,6 +24,9 @@
 namespace gsn {
 namespace {
 
+// What gradients of logits that are kept in float16 are at most.
+constexpr float kMostKept = 0x1p15f;
+
 // A token's target, -1 where there is none: out of range, or a class that is not valid.
 __device__ __forceinline__ int32_t target_of(const Entropy& x, int64_t t) {
   const int32_t c = x.targets[t];
@@ -254,8 +257,8 @@ __device__ __forceinline__ void store_two(const Entropy& x, void* d, f32x4 (&v)[
 
 // A tile of the logits -> their gradients, as the operands of the two products that take them: of
 // one type rounded to it; of binary32 in two values as d for the product with w, times the class's
-// power of two (at most 2^11) and without dloss, and as dt for the product with x, times the
-// token's power of two and dloss (at most 2^11).
+// power of two and without dloss, and as dt for the product with x, times the token's power of two
+// and dloss (at most kMostKept each).
 template <typename T, bool TWO>
 struct Gradient {
   Entropy x;
@@ -280,7 +283,7 @@ struct Gradient {
       const float most_w = 1.0f / __uint_as_float(x.most[1 + index]);
 #pragma unroll
       for (int j = 0; j < NT; ++j)
-        cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j) * most_w * 2048.0f;
+        cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j) * most_w * kMostKept;
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -510,9 +513,10 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
     atomicMax(most, largest);
 }
 
-// Gradients of the logits in float16 are kept times 2^11 / max |dloss|: at most 2^11, and those of
-// small probabilities are not lost (2^-25 of the largest dloss still has all of its 11 bits).  And
-// the largest powers of two of the rows in two values begin (2^-126, were all rows zeros).
+// Gradients of the logits in float16 are kept times 2^15 / max |dloss|: at most 2^15, and those of
+// small probabilities are not lost (2^-29 of the largest dloss still has all of its 11 bits).  A
+// dloss that is not finite is its own token's matter.  And the largest powers of two of the rows in
+// two values begin (2^-126, were all rows zeros).
 __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   __shared__ float some[16];
   for (int32_t i = threadIdx.x; i <= x.pieces; i += 1024)
@@ -521,20 +525,17 @@ __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   for (int64_t t = threadIdx.x; t < x.tokens; t += 1024) {
     if (target_of(x, t) < 0) continue;
     const float v = fabsf(x.dloss[t]);
-    m = v > m || v != v ? v : m;  // (NaN stays)
+    if (v < INFINITY) m = fmaxf(m, v);
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float v = __shfl_xor(m, o);
-    m = v > m || v != v ? v : m;
-  }
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   if (threadIdx.x % kWave == 0) some[threadIdx.x / kWave] = m;
   __syncthreads();
   if (threadIdx.x > 0) return;
-  for (int w = 1; w < 16; ++w) m = some[w] > m || some[w] != some[w] ? some[w] : m;
-  const float base = m < 0x1p-100f ? 0x1p-100f : m;
-  x.factor[0] = 2048.0f / base;
-  x.factor[1] = base / 2048.0f;
+  for (int w = 1; w < 16; ++w) m = fmaxf(m, some[w]);
+  const float base = fmaxf(m, 0x1p-100f);
+  x.factor[0] = kMostKept / base;
+  x.factor[1] = base / kMostKept;
 }
 
 // A wave a row; few enough workgroups that they have little to tell each other (ce_pairs).
@@ -658,7 +659,7 @@ void backward(const Entropy& x, hipStream_t st) {
       const int64_t each = x.tokens * x.pitch;
       run_product<E, false, true>(
           p, Partial{x.dxp, each, static_cast<int32_t>(x.tokens), x.pitch, first > 0,
-                     TWO ? x.most + 1 + index : nullptr, nullptr, 1.0f / 2048.0f}, st);
+                     TWO ? x.most + 1 + index : nullptr, nullptr, 1.0f / kMostKept}, st);
     }
     if (x.dw) {
       Product p{};

@@ -110,6 +110,18 @@ __global__ __launch_bounds__(kNormThreads) void or_norm(Orthogonal x) {
   x.norms[blockIdx.x] = s;
 }
 
+// v -> 2^11 v / norm, by a power of two before where the quotient would leave binary32's range (an
+// eps of 0).  A matrix of zeros without an eps stays one; an infinite norm gives NaN.
+struct Inverse {
+  float before, factor;
+  __device__ __forceinline__ explicit Inverse(double norm) {
+    before = norm < 0x1p-100 ? 0x1p60f : norm > 0x1p120 ? 0x1p-40f : 1.0f;
+    factor = norm > 0.0 ? norm < INFINITY ? static_cast<float>(kScale / (norm * before)) : NAN
+                        : norm != norm ? NAN : 0.0f;
+  }
+  __device__ __forceinline__ float of(float v) const { return v * before * factor; }
+};
+
 // X of the first step, times 2^11, as one or two float16 values a number.
 template <typename T, bool UPDATE>
 __global__ __launch_bounds__(256) void or_begin(Orthogonal x) {
@@ -124,8 +136,7 @@ __global__ __launch_bounds__(256) void or_begin(Orthogonal x) {
   __syncthreads();
   s = some[0] + some[1] + some[2] + some[3];
   const double norm = sqrt(s) + static_cast<double>(x.eps);
-  // (a matrix of zeros without an eps; infinities become NaN)
-  const float factor = norm > 0.0 ? static_cast<float>(kScale / norm) : s != s ? NAN : 0.0f;
+  const Inverse inverse(norm);
   const uint32_t each = static_cast<uint32_t>(x.cols8) / 8, n = each * x.rows8;
   const int64_t other = x.batch * (int64_t{8} * n);
   for (uint32_t i = part * 256 + tid; i < n; i += x.blocks * 256) {
@@ -136,7 +147,7 @@ __global__ __launch_bounds__(256) void or_begin(Orthogonal x) {
     Vec<f16_t, 8> hi, lo;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const float w = settled(v[q] * factor);
+      const float w = settled(inverse.of(v[q]));
       hi.v[q] = from_float<f16_t>(w);
       lo.v[q] = from_float<f16_t>(w - to_float(hi.v[q]));
     }
@@ -293,8 +304,8 @@ struct Finish {
 
 // A small matrix by one workgroup, all steps in LDS: X, A and B as above, with S (the short side)
 // rows and L columns.  A wave takes tiles of 16 x 16 of A and of B, and columns of 16 of X, which
-// it alone reads and writes.  Bound by latency: 15 products that wait for each other,
-// with a barrier after each; one matrix of 64 x 192 in two values 34 us, 88 as launches.
+// it alone reads and writes.  Bound by latency: 15 products that wait for each other, with a barrier
+// after each; one matrix of 64 x 192 in two values 34 us, 88 as launches.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallLds = 152 * 1024;
 constexpr int small_side(int values) { return values == 1 ? 128 : 96; }  // of S at most
@@ -363,7 +374,7 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) sum += some[w];
   const double norm = sqrt(sum) + static_cast<double>(x.eps);
-  const float factor = norm > 0.0 ? static_cast<float>(kScale / norm) : sum != sum ? NAN : 0.0f;
+  const Inverse inverse(norm);
   // one or two float16 values of v at element i of X, A or B
   const auto keep = [&](f16_t* to, int32_t other, int32_t i, float v) {
     v = settled(v);
@@ -384,7 +395,7 @@ __global__ __launch_bounds__(kSmallThreads) void or_small(Orthogonal x) {
     int32_t r = i / x.cols, c = i - r * x.cols;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      if (i + q < n) keep(xs, z.many_x, wide ? r * z.x + c : c * z.x + r, v[q] * factor);
+      if (i + q < n) keep(xs, z.many_x, wide ? r * z.x + c : c * z.x + r, inverse.of(v[q]));
       if (++c == x.cols) {
         c = 0;
         ++r;

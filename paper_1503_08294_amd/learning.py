@@ -141,7 +141,8 @@ def orthogonalise(x, *, steps=5, coefficients=COEFFICIENTS, eps=1e-7):
     0.002 of the matrix's norm).  See gsn_orthogonalise in include/gsn.h for the products."""
     _no_tangent(x)
     _no_gradient("orthogonalise", x)
-    p, size = _orthogonal(*_matrices(x), steps, tuple(coefficients), eps, False)
+    p, size = _orthogonal(*_matrices(x), steps, tuple(map(float, coefficients)),
+                          float(eps), False)
     x = x.contiguous()
     out = torch.empty_like(x)
     gsn.gsn_orthogonalise(p, x, out, _bytes(size, x))
@@ -162,7 +163,8 @@ def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=Tr
     an update in place; new ones if None."""
     _no_tangent(weights, gradient, momentum)
     _no_gradient("orthogonal_step", weights, gradient, momentum)
-    p, size = _orthogonal(*_matrices(weights), steps, tuple(coefficients), eps, True)
+    p, size = _orthogonal(*_matrices(weights), steps, tuple(map(float, coefficients)), float(eps),
+                          True)
     new_weights, new_momentum = out if out is not None else (
         torch.empty_like(weights, memory_format=torch.contiguous_format),
         torch.empty_like(momentum, memory_format=torch.contiguous_format))

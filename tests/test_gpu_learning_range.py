@@ -1,0 +1,61 @@
+"""Numbers at the ends of binary32 in the learning calls: matrices of tiny and of huge norms, tokens
+whose dloss is not finite."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_1503_08294_amd import learning
+
+pytestmark = pytest.mark.gpu
+
+SIZES = ((33, 70), (70, 33), (200, 312), (312, 200))  # in one workgroup each, and in tiles
+
+
+def _whole(rows, cols, seed):
+    """Whole numbers: times a power of two they are the same binary32 values, subnormal too."""
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-8, 9, (2, rows, cols), generator=g).float().cuda()
+
+
+@pytest.mark.parametrize("rows,cols", SIZES)
+@pytest.mark.parametrize("power", (-145, -130, -110, -60, 60, 110, 123))
+def test_a_matrix_times_a_power_of_two_is_the_same_one(rows, cols, power):
+    x = _whole(rows, cols, 5)
+    half = power // 2  # (2^-145 itself is no normal number)
+    scaled = x * 2.0 ** half * 2.0 ** (power - half)
+    want = learning.orthogonalise(x, eps=0.0)
+    got = learning.orthogonalise(scaled, eps=0.0)
+    torch.cuda.synchronize()
+    assert torch.isfinite(want).all() and want.abs().max() > 0.01
+    assert torch.equal(got, want)
+    # an update by the gradient alone
+    zeros = torch.zeros_like(x)
+    for w in (torch.float32, torch.bfloat16):
+        if w == torch.bfloat16 and not -120 <= power <= 120:
+            continue
+        a, b = (learning.orthogonal_step(zeros.to(w), v.to(w), zeros, 1.0, beta=0.0,
+                                         nesterov=False, eps=0.0)[0] for v in (x, scaled))
+        torch.cuda.synchronize()
+        assert torch.equal(a, b) and a.abs().max() > 0.01
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16, torch.float16))
+@pytest.mark.parametrize("tokens", (17, 130))
+@pytest.mark.parametrize("value", (torch.inf, -torch.inf, torch.nan))
+def test_a_dloss_that_is_not_finite_is_its_own_tokens_matter(dtype, tokens, value):
+    g = torch.Generator().manual_seed(tokens)
+    x = torch.randn(tokens, 72, generator=g).to(dtype).cuda()
+    w = torch.randn(301, 72, generator=g).to(dtype).cuda()
+    targets = torch.randint(0, 301, (tokens,), generator=g, dtype=torch.int32).cuda()
+    dloss = torch.rand(tokens, generator=g).cuda()
+    stats = learning.cross_entropy_forward(x, w, targets)[1]
+    other = targets.clone()
+    other[5] = -1
+    want = learning.cross_entropy_backward(dloss, x, w, other, None, stats)[0]
+    dloss[5] = value
+    got = learning.cross_entropy_backward(dloss, x, w, targets, None, stats)[0]
+    torch.cuda.synchronize()
+    rest = torch.arange(tokens, device="cuda") != 5
+    assert torch.equal(got[rest], want[rest]) and torch.isfinite(got[rest]).all()
+    assert not torch.isfinite(got[5].float()).any()
