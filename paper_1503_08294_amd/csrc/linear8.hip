@@ -35,109 +35,163 @@ __device__ __forceinline__ float beside_border(float q, float v, float s) {
   if (below < 0.0f || (below == 0.0f && odd)) return q - 1.0f;
   return q;
 }
-// Eight of them (|v / s| <= 127 but for rounding).  What is left of v after q s has an error of
-// 2^-24 of itself: up to 0.4999 s no other integer is nearer, and few values are looked at again.
-__device__ __forceinline__ Vec<int8_t, 8> quantised(const float* v, float s, float inverse) {
-  float q[8];
-  bool again = false;
-  const float sure = 0.4999f * s;
+// Eight of them (|v / s| <= 127 but for rounding) as bytes.  The quotient goes next to 1.5 2^23,
+// where binary32 values are 1 apart and their last byte is the integer's.  What is left of v after q
+// s has an error of 2^-24 of itself: up to 0.4999 s no other integer is nearer, and few values are
+// looked at again.
+__device__ __forceinline__ uint2 quantised(const float* v, float s, float inverse) {
+  constexpr float kOnes = 0x1.8p23f;
+  float at[8], most = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    q[i] = rintf(v[i] * inverse);
-    again |= !(fabsf(fmaf(-q[i], s, v[i])) < sure);
+    at[i] = fmaf(v[i], inverse, kOnes);
+    most = fmaxf(most, fabsf(fmaf(kOnes - at[i], s, v[i])));
   }
-  if (__any(again)) {
+  if (__any(most >= 0.4999f * s)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = beside_border(q[i], v[i], s);
+    for (int i = 0; i < 8; ++i) at[i] = beside_border(at[i] - kOnes, v[i], s) + kOnes;
   }
-  Vec<int8_t, 8> o;
+  uint32_t four[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o.v[i] = static_cast<int8_t>(static_cast<int>(q[i]));
-  return o;
+  for (int h = 0; h < 2; ++h) {
+    const float* const a = at + 4 * h;
+    const auto two = [](float lo, float hi) {  // last bytes of both, in the low half
+      return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x0c0c0400u);
+    };
+    four[h] = __builtin_amdgcn_perm(two(a[2], a[3]), two(a[0], a[1]), 0x05040100u);
+  }
+  return uint2{four[0], four[1]};
 }
 
-// Rows in 8 bits, a workgroup a row: the largest value, then the quotients, the row kept in
-// registers in between where it has up to 8,192 elements.  `pitch` bytes of q are written (at most
-// up to the next multiple of 16 bytes), zeros past the end.  Bound by memory.
-constexpr int kRowThreads = 256;
+// The largest magnitude of some elements, as bits (larger for larger numbers, largest for NaN).
 template <typename T>
+struct Largest {
+  typedef uint16_t Two __attribute__((ext_vector_type(2)));
+  uint32_t top = 0;
+  __device__ __forceinline__ void take(uint32_t bits) {
+    if constexpr (sizeof(T) == 4)
+      top = max(top, bits & 0x7fffffffu);
+    else
+      top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+                                             __builtin_bit_cast(Two, top),
+                                             __builtin_bit_cast(Two, bits & 0x7fff7fffu)));
+  }
+  // as bits of a binary32 value
+  __device__ __forceinline__ uint32_t value() const {
+    if constexpr (sizeof(T) == 4) {
+      return top;
+    } else {
+      const uint16_t one = static_cast<uint16_t>(max(top & 0xffffu, top >> 16));
+      return __float_as_uint(to_float(__builtin_bit_cast(T, one)));
+    }
+  }
+};
+
+// Rows in 8 bits, a row by THREADS, a workgroup or a wave: the largest value, then the quotients, 8
+// KEPT elements a thread kept in registers in between.  `pitch` bytes of q are written (at most up
+// to the next multiple of 16 bytes), zeros past the end.  8,191 rows of 4,096: bfloat16 27 us (3.7
+// TB/s), binary32 31 us (5.5 TB/s, bound by memory).
+constexpr int kRowThreads = 256;
+template <int THREADS, int KEPT, typename T>
 __device__ __forceinline__ void quantise_rows(const T* __restrict__ x, int64_t stride,
                                               int64_t rows, int32_t dim, int8_t* __restrict__ q,
                                               int64_t q_stride, int32_t pitch,
                                               float* __restrict__ scales, int64_t block,
                                               int64_t blocks) {
-  constexpr int kKept = 4, kEach = 8 * kRowThreads;
-  typedef T Eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-  __shared__ uint32_t some[kRowThreads / kWave];
-  const int tid = threadIdx.x;
+  // (elements go in eights; up to 7 that are left, and the zeros behind them, are one a thread:
+  // eights that may all end early take registers for twice the waves, 35 us in place of 27)
+  constexpr int kE = 16 / static_cast<int>(sizeof(T)), kParts = 8 / kE;
+  struct Eight {
+    Frag f[kParts];
+  };
+  __shared__ uint32_t some[THREADS / kWave];
+  const int tid = threadIdx.x % THREADS;
+  const int32_t chunks = dim / 8, rest = dim - 8 * chunks;
   for (int64_t r = block; r < rows; r += blocks) {
     const T* const row = x + r * stride;
-    Eight kept[kKept];
-    uint32_t top = 0;  // bits without the sign: larger for larger numbers, largest for NaN
-    const auto load = [&](int32_t k, bool inside) {
+    Eight kept[KEPT];
+    Largest<T> most;
+    const auto load = [&](int32_t c) {
       Eight v;
-      if (inside || k + 8 <= dim) return *reinterpret_cast<const Eight*>(row + k);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = k + i < dim ? row[k + i] : from_float<T>(0.0f);
+      for (int h = 0; h < kParts; ++h) {
+        if (c < chunks) v.f[h] = row_chunk<true>(row, c * 8 + h * kE, dim);
+        else v.f[h].u = u32x4{0, 0, 0, 0};
+      }
       return v;
     };
     const auto largest = [&](const Eight& v) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(to_float(v[i])) & 0x7fffffffu);
+      for (int h = 0; h < kParts; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most.take(v.f[h].u[i]);
     };
-    // (whole parts without a branch a lane: the loads of all of them are under way together)
 #pragma unroll
-    for (int i = 0; i < kKept; ++i)
-      if (i * kEach < dim) kept[i] = load(i * kEach + tid * 8, (i + 1) * kEach <= dim);
+    for (int i = 0; i < KEPT; ++i)
+      if (i * THREADS < chunks) kept[i] = load(i * THREADS + tid);
+    const float left = tid < rest ? to_float(row[8 * chunks + tid]) : 0.0f;
 #pragma unroll
-    for (int i = 0; i < kKept; ++i)
-      if (i * kEach < dim) largest(kept[i]);
-    for (int32_t k = kKept * kEach + tid * 8; k < dim; k += kEach) largest(load(k, false));
+    for (int i = 0; i < KEPT; ++i)
+      if (i * THREADS < chunks) largest(kept[i]);
+    for (int32_t c = KEPT * THREADS + tid; c < chunks; c += THREADS) largest(load(c));
+    uint32_t top = max(most.value(), __float_as_uint(left) & 0x7fffffffu);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o));
-    __syncthreads();
-    if (tid % kWave == 0) some[tid / kWave] = top;
-    __syncthreads();
+    if constexpr (THREADS > kWave) {
+      __syncthreads();
+      if (tid % kWave == 0) some[tid / kWave] = top;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kRowThreads / kWave; ++w) top = max(top, some[w]);
+      for (int w = 0; w < THREADS / kWave; ++w) top = max(top, some[w]);
+    }
     const bool bad = top >= 0x7f800000u;
     const float s = fmaxf(__uint_as_float(bad ? 0 : top) / 127.0f, 0x1p-126f), inverse = 1.0f / s;
     int8_t* const to = q + r * q_stride;
-    const auto store = [&](int32_t k, const Eight& v) {
+    const auto store = [&](int32_t c, const Eight& v) {
+      if (c >= chunks) return;
       float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = bad ? 0.0f : to_float(v[i]);
-      const Vec<int8_t, 8> o = quantised(f, s, inverse);
-      if (k + 8 <= pitch) {
-        typedef uint8_t Loose __attribute__((ext_vector_type(8), aligned(1)));
-        *reinterpret_cast<Loose*>(to + k) = __builtin_bit_cast(Loose, o);
-      } else {
-        for (int i = 0; i < 8; ++i)
-          if (k + i < pitch) to[k + i] = o.v[i];
+      for (int h = 0; h < kParts; ++h) {
+        const Vec<T, kE> e = __builtin_bit_cast(Vec<T, kE>, v.f[h].u);
+#pragma unroll
+        for (int i = 0; i < kE; ++i) f[h * kE + i] = bad ? 0.0f : to_float(e.v[i]);
       }
+      const uint2 o = quantised(f, s, inverse);
+      typedef uint32_t Loose __attribute__((ext_vector_type(2), aligned(1)));
+      *reinterpret_cast<Loose*>(to + 8 * c) = Loose{o.x, o.y};
     };
 #pragma unroll
-    for (int i = 0; i < kKept; ++i)
-      if (i * kEach + tid * 8 < pitch) store(i * kEach + tid * 8, kept[i]);
-    for (int32_t k = kKept * kEach + tid * 8; k < pitch; k += kEach) store(k, load(k, false));
+    for (int i = 0; i < KEPT; ++i)
+      if (i * THREADS < chunks) store(i * THREADS + tid, kept[i]);
+    for (int32_t c = KEPT * THREADS + tid; c < chunks; c += THREADS) store(c, load(c));
+    if (8 * chunks + tid < pitch) {
+      const float v = bad ? 0.0f : left;
+      to[8 * chunks + tid] =
+          static_cast<int8_t>(static_cast<int>(beside_border(rintf(v * inverse), v, s)));
+    }
     if (tid == 0) scales[r] = bad ? NAN : s;
   }
 }
 
-template <typename T>
+template <typename T, int THREADS, int KEPT>
 __global__ __launch_bounds__(kRowThreads) void q8_rows(const T* x, int64_t stride, int64_t rows,
                                                        int32_t dim, int8_t* q, int64_t q_stride,
                                                        float* scales) {
-  quantise_rows(x, stride, rows, dim, q, q_stride, dim, scales, blockIdx.x, gridDim.x);
+  constexpr int kRows = kRowThreads / THREADS;
+  quantise_rows<THREADS, KEPT>(x, stride, rows, dim, q, q_stride, dim, scales,
+                               int64_t{blockIdx.x} * kRows + threadIdx.x / THREADS,
+                               int64_t{gridDim.x} * kRows);
 }
 
 // x in 8 bits by the first `blocks` workgroups, and by the others w in rows of `pitch` bytes with
 // zeros at their ends.
-template <typename T>
+template <typename T, int THREADS, int KEPT>
 __global__ __launch_bounds__(kRowThreads) void q8_begin(Linear8 x, uint32_t blocks) {
+  constexpr int kRows = kRowThreads / THREADS;  // of a workgroup at a time
   if (blockIdx.x < blocks)
-    return quantise_rows(static_cast<const T*>(x.x), x.x_stride, x.tokens, x.dim, x.q, x.pitch,
-                         x.pitch, x.x_scales, blockIdx.x, blocks);
+    return quantise_rows<THREADS, KEPT>(
+        static_cast<const T*>(x.x), x.x_stride, x.tokens, x.dim, x.q, x.pitch, x.pitch,
+        x.x_scales, int64_t{blockIdx.x} * kRows + threadIdx.x / THREADS, int64_t{blocks} * kRows);
   const int32_t each = x.pitch / 16;
   const int64_t all = static_cast<int64_t>(x.out) * each;
   for (int64_t i = static_cast<int64_t>(blockIdx.x - blocks) * kRowThreads + threadIdx.x; i < all;
@@ -231,8 +285,8 @@ __global__ __launch_bounds__(256) void q8_alone(Linear8 x) {
   const bool whole = k_begin + kStep <= k_end;
   if (whole) load(std::true_type(), k_begin);
   const int32_t pitch = x.pitch;
-  quantise_rows(static_cast<const T*>(x.x), x.x_stride, x.tokens, dim, q, pitch, pitch, scale, 0,
-                1);
+  quantise_rows<kRowThreads, 4>(static_cast<const T*>(x.x), x.x_stride, x.tokens, dim, q, pitch,
+                                pitch, scale, 0, 1);
   __syncthreads();
 
   i32x4 acc[GT] = {};
@@ -281,8 +335,16 @@ __global__ __launch_bounds__(256) void q8_alone(Linear8 x) {
   store4(static_cast<T*>(x.y) + m * x.y_stride, n, x.out, v);
 }
 
-uint32_t row_blocks(int64_t rows) {
-  return static_cast<uint32_t>(std::min<int64_t>(rows, 1 << 16));
+// Rows by a wave each, where they fit its registers and there are enough: no wait for other waves.
+// By workgroups and by waves, us, bfloat16: 65,536 rows of 64 76 and 22, 8,191 of 1,001 15.1 and
+// 9.4, 2,048 of 1,024 5.9 and 4.6, 1,024 of 1,024 3.9 and 3.9; 16,384 of 2,048 34 and 26, 4,096 of
+// 2,048 10.4 and 9.6, 2,048 of 2,048 6.6 and 7.1; 16,384 of 4,096 48.6 and 47.7, 8,191 27 and 31.
+constexpr int32_t kWaveDim = 2048;
+bool by_waves(int64_t rows, int32_t dim) {
+  return dim <= kWaveDim && rows >= 2 * std::max(dim, 1024);
+}
+uint32_t row_blocks(int64_t rows, bool waves) {
+  return static_cast<uint32_t>(std::min<int64_t>(waves ? (rows + 3) / 4 : rows, 1 << 16));
 }
 
 template <typename T>
@@ -296,11 +358,14 @@ hipError_t launch(const Linear8& x, hipStream_t st) {
     q8_alone<T><<<static_cast<uint32_t>((x.out + kFewCols - 1) / kFewCols), 256, 0, st>>>(x);
     return hipGetLastError();
   }
-  const uint32_t blocks = row_blocks(x.tokens);
+  const bool waves = by_waves(x.tokens, x.dim);
+  const uint32_t blocks = row_blocks(x.tokens, waves);
   const int64_t copies =
       (static_cast<int64_t>(x.out) * (x.pitch / 16) + kRowThreads - 1) / kRowThreads;
-  q8_begin<T><<<blocks + (copy ? static_cast<uint32_t>(std::min<int64_t>(copies, 1 << 14)) : 0),
-                kRowThreads, 0, st>>>(x, blocks);
+  const uint32_t grid =
+      blocks + (copy ? static_cast<uint32_t>(std::min<int64_t>(copies, 1 << 14)) : 0);
+  if (waves) q8_begin<T, kWave, kWaveDim / 512><<<grid, kRowThreads, 0, st>>>(x, blocks);
+  else q8_begin<T, kRowThreads, 4><<<grid, kRowThreads, 0, st>>>(x, blocks);
   if (few) {
     run_few<int8_t>(Few{x.q, x.pitch, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.out,
                         x.dim}, Scaled<T>{x}, st);
@@ -359,9 +424,16 @@ int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_
   if (rows == 0) return GSN_OK;
   if (!x || !q || !scales || x_stride < dim || q_stride < dim) return GSN_E_INVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const uint32_t blocks = gsn::row_blocks(rows);
+  const bool waves = gsn::by_waves(rows, dim);
+  const uint32_t blocks = gsn::row_blocks(rows, waves);
   const auto run = [&](auto* p) {
-    gsn::q8_rows<<<blocks, gsn::kRowThreads, 0, st>>>(p, x_stride, rows, dim, q, q_stride, scales);
+    using T = std::remove_const_t<std::remove_pointer_t<decltype(p)>>;
+    if (waves)
+      gsn::q8_rows<T, gsn::kWave, gsn::kWaveDim / 512><<<blocks, gsn::kRowThreads, 0, st>>>(
+          p, x_stride, rows, dim, q, q_stride, scales);
+    else
+      gsn::q8_rows<T, gsn::kRowThreads, 4><<<blocks, gsn::kRowThreads, 0, st>>>(
+          p, x_stride, rows, dim, q, q_stride, scales);
   };
   if (dtype == GSN_F32) run(static_cast<const float*>(x));
   else if (dtype == GSN_BF16) run(static_cast<const gsn::bf16_t*>(x));
