@@ -588,10 +588,10 @@ int gsn_cross_entropy(const gsn_entropy_params* params, const void* x, int64_t x
 /* Gradients from dloss float [tokens]: dx [tokens][dim] and dw [classes][dim] of type dtype,
  * every element written, 0 for tokens without a target and classes that are not valid; each may
  * be NULL (not computed).  The logits' gradients dloss (exp(l) / sum - [c = target]) are rounded
- * to dtype before they are multiplied with w and x; in GSN_F16 as multiples of the largest finite
- * |dloss|, so that a small dloss loses no digits there; in GSN_F32 of many tokens to two float16
- * values as above, with the largest of all (times the size of a row of w or x and dloss) in place
- * of a row's. */
+ * to dtype (to two values of it for up to 32 tokens) before they are multiplied with w and x; in
+ * GSN_F16 as multiples of the largest finite |dloss|, so that a small dloss loses no digits
+ * there; in GSN_F32 of many tokens to two float16 values as above, with the largest of all (times
+ * the size of a row of w or x and dloss) in place of a row's. */
 int gsn_cross_entropy_backward(const gsn_entropy_params* params, const float* dloss,
                                const void* x, int64_t x_stride, const void* w, int64_t w_stride,
                                const int32_t* targets, const uint8_t* valid, const float* stats,

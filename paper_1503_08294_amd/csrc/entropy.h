@@ -20,7 +20,9 @@ struct Entropy {
   bool copy_x, copy_w;
   bool few;       // tokens that read w once, as it is
   bool two;       // binary32 operands in two float16 values, copies always
-  void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the ends
+  bool two_d;     // gradients of the logits in two values of a 2-byte type, backward
+  void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the
+                  // ends; of two_d twice, one behind the other
   void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
   float* fx;      // of operands in two values: the powers of two of the rows of xc,
   float* fw;      // and of wc
@@ -34,10 +36,10 @@ struct Entropy {
   // backward
   const float* dloss;
   float* factor;  // 2: what dloss is multiplied by where the logits' gradients are kept, and back
-  void* d;        // [tokens][piece] gradients of the logits
+  void* d;        // [tokens][piece] gradients of the logits; of two_d the second values behind them
   void* dt;       // of operands in two values those for the product with x
   int32_t splits_x, splits_w;
-  float* dxp;     // [splits_x][tokens][pitch]
+  float* dxp;     // [splits_x][tokens][pitch]; of two_d [splits_x][2][tokens][pitch]
   float* dwp;     // [splits_w][piece][pitch], where splits_w > 1
   void* dx;
   void* dw;

@@ -25,6 +25,13 @@ constexpr int64_t kFill = 512;
 // tokens 303 and 377, 96 467 and 366, 191 700 and 488.
 constexpr int64_t kTwoTokens = 160, kTwoTokensBack = 80;
 
+// Tokens up to which gradients of the logits are kept in two values of a 2-byte type.  In one, a
+// token's dx and its class's row of dw are off by the rounding of its target's gradient, up to half
+// a step all of them; over many tokens these differ, over a few they may all be large.  us of a
+// backward pass in one value and in two, bfloat16: 50,001 classes of 1,024, 1 token 79 and 82, 16
+// 83 and 90, 32 88 and 98, 64 96 and 110, 128 110 and 141; 10,007 of 501, 32 tokens 37 and 39.
+constexpr int64_t kTwoGradients = 32;
+
 bool params_ok(const gsn_entropy_params* p) {
   return p && p->dtype >= GSN_F32 && p->dtype <= GSN_F16 && p->tokens >= 0 &&
          p->tokens <= (1 << 24) && p->dim >= 1 && p->dim <= (1 << 16) && p->classes >= 1 &&
@@ -58,9 +65,10 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   // (rows of the copies and of d are whole lines of 128 bytes: products read rows that begin inside
   // a line up to a fifth slower)
   x.two = p.dtype == GSN_F32 && p.tokens >= (backward ? kTwoTokensBack : kTwoTokens);
+  x.two_d = backward && p.dtype != GSN_F32 && p.tokens <= kTwoGradients;
   x.pitch = static_cast<int32_t>(up_to(p.dim, 64));
   int64_t piece = kPieceBytes / (size * x.pitch);
-  if (backward) piece = std::min(piece, kPieceBytes / (size * tokens));
+  if (backward) piece = std::min(piece, kPieceBytes / (size * tokens * (x.two_d ? 2 : 1)));
   else piece = std::min(piece, kPartBytes / (8 * tokens) * kSmallRows);
   piece = std::max<int64_t>(piece / 256 * 256, 256);
   // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
@@ -103,11 +111,12 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
   Carver c{static_cast<char*>(base)};
   const size_t s = size_of(dtype), t = static_cast<size_t>(x->tokens);
   x->factor = static_cast<float*>(c.take(8));
-  x->xc = c.take(s * t * x->pitch);
+  x->xc = c.take(s * t * x->pitch * (x->two_d ? 2 : 1));
   x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
-  x->d = c.take(s * t * x->piece);
+  x->d = c.take(s * t * x->piece * (x->two_d ? 2 : 1));
   carve_two(&c, x, true);
-  x->dxp = static_cast<float*>(c.take(4 * t * x->pitch * static_cast<size_t>(x->splits_x)));
+  x->dxp = static_cast<float*>(
+      c.take(4 * t * x->pitch * static_cast<size_t>(x->splits_x) * (x->two_d ? 2 : 1)));
   x->dwp = x->splits_w > 1
                ? static_cast<float*>(c.take(4 * static_cast<size_t>(x->piece) * x->pitch *
                                             static_cast<size_t>(x->splits_w)))

@@ -21,7 +21,7 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
     out: 8 U more.  exp(l - largest) is off by that twice, by (|l - largest| + 3) 2 U of the
     exponential (its argument and itself), and the sum of the exponentials by one U for each of the
     additions that a term goes through, 64 + classes / 64 at most.  The gradients of the logits are
-    rounded to the operands' type, those of float16 as multiples of 2^-11 of the largest dloss; in
+    rounded to the operands' type, those of float16 as multiples of 2^-15 of the largest dloss; in
     two values to 2^-23, and to 2^-36 of the largest that one could be beside w's, or x's, largest.
     Their products with w and x are sums of binary32, the results are rounded once."""
     dtype = x.dtype
@@ -61,7 +61,7 @@ def cross_entropy(x, w, targets, valid=None, dloss=None):
     ulp = 2.0 ** -23 if two else HALF_ULP[dtype]
     step = HALF_STEP[dtype]
     if dtype == torch.float16:
-        step = step * 2.0 ** -11 * g.abs().max()
+        step = step * 2.0 ** -15 * g.abs().max()
     d_tol = (p * rel_p + 4 * U) * g.abs() + ulp * d.abs() + step
     d_tol = torch.where(live[:, None] & there, d_tol, 0.0)
     for name, a, b in (("dx", d, w), ("dw", d.t(), x)):
