@@ -330,11 +330,13 @@ struct Gradient {
         for (int j = 0; j < NT; ++j) v[j] = acc[i][j] * h;
         store_two<f16_t>(x, x.dt, v, t0, at.n0 + nw, lane, room);
       } else {
-        if (x.two_d) {
-          store_two<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
-        } else {
-          store_rows<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
+        if constexpr (sizeof(T) == 2) {
+          if (x.two_d) {
+            store_two<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
+            continue;
+          }
         }
+        store_rows<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
       }
     }
   }

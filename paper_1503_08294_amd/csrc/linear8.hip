@@ -253,7 +253,7 @@ struct Scaled {
 
 // One or two tokens in one launch: every workgroup brings the tokens to 8 bits for itself, in LDS,
 // while its first rows of w are on their way, and takes 32 columns as few_rows() does.  One token
-// through 4,096 x 16,384: 13.3 us, 15.7 as two launches (67 MB at 5.0 TB/s).
+// through 4,096 x 16,384: 13.0 us, 15.7 as two launches (67 MB at 5.2 TB/s).
 constexpr int64_t kTokensAlone = 2;
 constexpr int32_t kDimAlone = 16384;
 template <typename T>
