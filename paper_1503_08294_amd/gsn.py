@@ -726,11 +726,21 @@ def gsn_orthogonal_workspace_bytes(params: gsn_orthogonal_params, update: bool) 
     return int(_lib.gsn_orthogonal_workspace_bytes(params, 1 if update else 0))
 
 
+def _matrices(p: gsn_orthogonal_params, x, what: str):
+    """The shape of the matrices that the parameters tell of."""
+    shape = x.shape
+    if tuple(shape[-2:]) != (p.rows, p.cols) or x.numel() != p.batch * p.rows * p.cols:
+        raise ValueError(f"{what} must be {p.batch} matrices of {p.rows} x {p.cols}, got "
+                         f"{tuple(shape)}")
+    return shape
+
+
 def gsn_orthogonalise(params: gsn_orthogonal_params, x, out, workspace, stream=None):
     """x, out: (..., rows, cols), contiguous."""
+    shape = _matrices(params, x, "x")
     return _run(
-        _lib.gsn_orthogonalise, x, stream, params, _flat(x, x.dtype, x.shape, "x"),
-        _flat(out, x.dtype, x.shape, "out"), _dev(workspace, torch.uint8, what="workspace"),
+        _lib.gsn_orthogonalise, x, stream, params, _flat(x, x.dtype, shape, "x"),
+        _flat(out, x.dtype, shape, "out"), _dev(workspace, torch.uint8, what="workspace"),
         workspace.numel())
 
 
@@ -738,7 +748,7 @@ def gsn_orthogonal_step(params: gsn_orthogonal_params, weights, gradient, moment
                         beta: float, decay: float, nesterov: bool, new_weights, new_momentum,
                         workspace, stream=None):
     """weights, gradient: (..., rows, cols) of one type; momentum: float32 of that shape."""
-    w, shape = weights, weights.shape
+    w, shape = weights, _matrices(params, weights, "weights")
     return _run(
         _lib.gsn_orthogonal_step, w, stream, params, _flat(w, w.dtype, shape, "weights"),
         _flat(gradient, w.dtype, shape, "gradient"),

@@ -1,0 +1,63 @@
+"""Tensors that are not those that a call's parameters tell of: the kernels go by the parameters and
+would read and write past the tensors' ends, so the binding refuses them before the library is called
+(no GPU needed: tensors, devices and the library are stand-ins)."""
+import pytest
+import torch
+
+from paper_1503_08294_amd import gsn, learning
+from test_mixture_devices import OnDevice
+
+F32, BF16, U8 = torch.float32, torch.bfloat16, torch.uint8
+
+
+def t(*shape, dtype=F32):
+    return OnDevice(0, shape, dtype)
+
+
+@pytest.fixture
+def called(monkeypatch):
+    """Names of the library's functions that were called."""
+    names = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                names.append(name)
+                return gsn.GSN_OK
+            call.__name__ = name
+            return call
+
+    monkeypatch.setattr(gsn, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(gsn, "_raw_stream", lambda index: 1000)
+    monkeypatch.setattr(gsn, "_lib", Library())
+    return names
+
+
+def matrices(rows=6, cols=8, batch=3, code=gsn.GSN_F32):
+    return gsn.gsn_orthogonal_params(code, rows, cols, 5, batch, *learning.COEFFICIENTS, 1e-7)
+
+
+ROOM = 1 << 16
+
+
+@pytest.mark.parametrize("shape,fits", [
+    ((3, 6, 8), True), ((1, 3, 6, 8), True), ((2, 6, 8), False), ((4, 6, 8), False),
+    ((3, 8, 6), False), ((6, 8), False), ((3, 48), False), ((144,), False), ((3, 5, 8), False)])
+def test_matrices_of_other_sizes(called, shape, fits):
+    x = t(*shape)
+    calls = [lambda: gsn.gsn_orthogonalise(matrices(), x, x, t(ROOM, dtype=U8)),
+             lambda: gsn.gsn_orthogonal_step(matrices(), x, x, x, 0.1, 0.9, 0.0, True, x, x,
+                                             t(ROOM, dtype=U8))]
+    for call in calls:
+        if fits:
+            call()
+        else:
+            with pytest.raises(ValueError, match="must be 3 matrices of 6 x 8"):
+                call()
+    assert called == (["gsn_orthogonalise", "gsn_orthogonal_step"] if fits else [])
+
+
+def test_one_matrix_by_itself(called):
+    x = t(6, 8)
+    gsn.gsn_orthogonalise(matrices(batch=1), x, x, t(ROOM, dtype=U8))
+    assert called == ["gsn_orthogonalise"]
