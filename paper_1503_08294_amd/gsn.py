@@ -498,6 +498,15 @@ def _type(t: torch.Tensor, what: str) -> int:
     return code
 
 
+def _type_of(p, t: torch.Tensor, what: str) -> torch.dtype:
+    """t's type, which has to be that of the parameters p: kernels go by them."""
+    if _DTYPES.get(t.dtype) != p.dtype:
+        _type(t, what)
+        raise ValueError(f"{what} is of {t.dtype}, not of the type that the parameters name "
+                         f"({p.dtype})")
+    return t.dtype
+
+
 def _refuse(t, dtype, shape, what: str):
     """The first reason why t is not a device tensor of this type and shape."""
     if not t.is_cuda:
@@ -654,7 +663,7 @@ def gsn_experts_saved_bytes(params: gsn_experts_params) -> int:
 def gsn_experts(params: gsn_experts_params, x, ids, weights, w1, w2, out, saved, workspace,
                 stream=None):
     p = params
-    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    xp, xs = _matrix(x, _type_of(p, x, "x"), p.tokens, p.dim, "x")
     pairs = (p.tokens, p.top)
     return _run(
         _lib.gsn_experts, x, stream, p, xp, xs, _flat(ids, torch.int32, pairs, "ids"),
@@ -669,7 +678,7 @@ def gsn_experts(params: gsn_experts_params, x, ids, weights, w1, w2, out, saved,
 def gsn_experts_backward(params: gsn_experts_params, dout, x, weights, w1, w2, saved, dx,
                          dweights, dw1, dw2, workspace, stream=None):
     p = params
-    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    xp, xs = _matrix(x, _type_of(p, x, "x"), p.tokens, p.dim, "x")
     pairs = (p.tokens, p.top)
     s1, s2 = (p.experts, 2 * p.hidden, p.dim), (p.experts, p.dim, p.hidden)
     return _run(
@@ -695,7 +704,7 @@ def gsn_cross_entropy(params: gsn_entropy_params, x, w, targets, valid, loss, st
     """x: (tokens, dim); w: (classes, dim); targets: (tokens,) int32; valid: (classes,) uint8 or
     None; loss: (tokens,) float32; stats: (2, tokens) float32 or None."""
     p = params
-    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    xp, xs = _matrix(x, _type_of(p, x, "x"), p.tokens, p.dim, "x")
     wp, ws = _matrix(w, x.dtype, p.classes, p.dim, "w")
     return _run(
         _lib.gsn_cross_entropy, x, stream, p, xp, xs, wp, ws,
@@ -710,7 +719,7 @@ def gsn_cross_entropy_backward(params: gsn_entropy_params, dloss, x, w, targets,
                                dw, workspace, stream=None):
     """Gradients of gsn_cross_entropy; dx and dw may be None."""
     p = params
-    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    xp, xs = _matrix(x, _type_of(p, x, "x"), p.tokens, p.dim, "x")
     wp, ws = _matrix(w, x.dtype, p.classes, p.dim, "w")
     return _run(
         _lib.gsn_cross_entropy_backward, x, stream, p,
@@ -728,6 +737,7 @@ def gsn_orthogonal_workspace_bytes(params: gsn_orthogonal_params, update: bool) 
 
 def _matrices(p: gsn_orthogonal_params, x, what: str):
     """The shape of the matrices that the parameters tell of."""
+    _type_of(p, x, what)
     shape = x.shape
     if tuple(shape[-2:]) != (p.rows, p.cols) or x.numel() != p.batch * p.rows * p.cols:
         raise ValueError(f"{what} must be {p.batch} matrices of {p.rows} x {p.cols}, got "
@@ -774,7 +784,7 @@ def gsn_linear_quantised_workspace_bytes(params: gsn_linear_params) -> int:
 def gsn_linear_quantised(params: gsn_linear_params, x, w, scales, y, workspace, stream=None):
     """x: (tokens, dim); w: (out, dim) int8; scales: (out,) float32; y: (tokens, out)."""
     p = params
-    xp, xs = _matrix(x, x.dtype, p.tokens, p.dim, "x")
+    xp, xs = _matrix(x, _type_of(p, x, "x"), p.tokens, p.dim, "x")
     wp, ws = _matrix(w, torch.int8, p.out, p.dim, "w")
     yp, ys = _matrix(y, x.dtype, p.tokens, p.out, "y")
     return _run(

@@ -61,3 +61,31 @@ def test_one_matrix_by_itself(called):
     x = t(6, 8)
     gsn.gsn_orthogonalise(matrices(batch=1), x, x, t(ROOM, dtype=U8))
     assert called == ["gsn_orthogonalise"]
+
+
+@pytest.mark.parametrize("code,fits", [(gsn.GSN_F32, False), (gsn.GSN_BF16, True),
+                                       (gsn.GSN_F16, False), (7, False)])
+def test_tensors_of_another_type(called, code, fits):
+    """(An element of the parameters' type may be twice as long as the tensors'.)"""
+    ep = gsn.gsn_entropy_params(code, 8, 20, 5)
+    lp = gsn.gsn_linear_params(code, 8, 20, 5)
+    xp = gsn.gsn_experts_params(code, 3, 2, 8, 4, 5)
+    x, w, m, ws = t(5, 8, dtype=BF16), t(20, 8, dtype=BF16), t(3, 6, 8, dtype=BF16), t(ROOM, dtype=U8)
+    targets, ids, pairs = t(5, dtype=torch.int32), t(5, 2, dtype=torch.int32), t(5, 2)
+    w1, w2, f = t(3, 8, 8, dtype=BF16), t(3, 8, 4, dtype=BF16), t(3, 6, 8)
+    calls = [
+        lambda: gsn.gsn_cross_entropy(ep, x, w, targets, None, t(5), None, ws),
+        lambda: gsn.gsn_cross_entropy_backward(ep, t(5), x, w, targets, None, t(2, 5), x, w, ws),
+        lambda: gsn.gsn_orthogonalise(matrices(code=code), m, m, ws),
+        lambda: gsn.gsn_orthogonal_step(matrices(code=code), m, m, f, 0.1, 0.9, 0.0, True, m, f, ws),
+        lambda: gsn.gsn_linear_quantised(lp, x, t(20, 8, dtype=torch.int8), t(20),
+                                         t(5, 20, dtype=BF16), ws),
+        lambda: gsn.gsn_experts(xp, x, ids, pairs, w1, w2, x, ws, ws),
+        lambda: gsn.gsn_experts_backward(xp, x, x, pairs, w1, w2, ws, x, pairs, w1, w2, ws)]
+    for call in calls:
+        if fits:
+            call()
+        else:
+            with pytest.raises(ValueError, match="type that the parameters"):
+                call()
+    assert len(called) == (len(calls) if fits else 0)
