@@ -498,6 +498,12 @@ def _type(t: torch.Tensor, what: str) -> int:
     return code
 
 
+def _int32(n: int) -> int:
+    """n for a field of 32 bits, -1, which every call refuses, for what it cannot hold (ctypes would
+    take that modulo 2^32)."""
+    return n if -0x80000000 <= n < 0x80000000 else -1
+
+
 def _type_of(p, t: torch.Tensor, what: str) -> torch.dtype:
     """t's type, which has to be that of the parameters p: kernels go by them."""
     if _DTYPES.get(t.dtype) != p.dtype:
@@ -573,13 +579,13 @@ def gsn_layer_norm(x, weight, bias, eps: float, y, stats=None, stream=None):
     yp, ys = _matrix(y, x.dtype, rows, dim, "y")
     pt = _params_type(x.dtype, weight, bias)
     return _run(
-        _lib.gsn_layer_norm, x, stream, code, _DTYPES.get(pt, -1), rows, dim, xp, xs,
+        _lib.gsn_layer_norm, x, stream, code, _DTYPES.get(pt, -1), rows, _int32(dim), xp, xs,
         _flat(weight, pt, (dim,), "weight"), _flat(bias, pt, (dim,), "bias"), eps, yp, ys,
         _flat(stats, torch.float32, (2, rows), "stats"))
 
 
 def gsn_layer_norm_workspace_bytes(rows: int, dim: int) -> int:
-    return int(_lib.gsn_layer_norm_workspace_bytes(rows, dim))
+    return int(_lib.gsn_layer_norm_workspace_bytes(rows, _int32(dim)))
 
 
 def gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, workspace, stream=None):
@@ -591,8 +597,8 @@ def gsn_layer_norm_backward(dy, x, weight, stats, dx, dweight, dbias, workspace,
     dxp, dxs = (None, dim) if dx is None else _matrix(dx, x.dtype, rows, dim, "dx")
     pt = _params_type(x.dtype, weight if weight is not None else dweight, dbias)
     return _run(
-        _lib.gsn_layer_norm_backward, x, stream, code, _DTYPES.get(pt, -1), rows, dim, dyp, dys,
-        xp, xs, _flat(weight, pt, (dim,), "weight"),
+        _lib.gsn_layer_norm_backward, x, stream, code, _DTYPES.get(pt, -1), rows, _int32(dim), dyp,
+        dys, xp, xs, _flat(weight, pt, (dim,), "weight"),
         _flat(stats, torch.float32, (2, rows), "stats"),
         dxp, dxs, _flat(dweight, pt, (dim,), "dweight"), _flat(dbias, pt, (dim,), "dbias"),
         _dev(workspace, torch.uint8), 0 if workspace is None else workspace.numel())
@@ -773,8 +779,8 @@ def gsn_quantise(x, q, scales, stream=None):
     rows, dim = x.shape
     xp, xs = _matrix(x, x.dtype, rows, dim, "x")
     qp, qs = _matrix(q, torch.int8, rows, dim, "q")
-    return _run(_lib.gsn_quantise, x, stream, _type(x, "x"), rows, dim, xp, xs, qp, qs,
-                _flat(scales, torch.float32, (rows,), "scales"))
+    return _run(_lib.gsn_quantise, x, stream, _type(x, "x"), rows, _int32(dim), xp, xs,
+                qp, qs, _flat(scales, torch.float32, (rows,), "scales"))
 
 
 def gsn_linear_quantised_workspace_bytes(params: gsn_linear_params) -> int:

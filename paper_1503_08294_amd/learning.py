@@ -20,6 +20,7 @@ import functools
 import torch
 
 from . import gsn
+from .gsn import _int32
 from .mixture import _bytes, _no_tangent, _once, _rows, _same_device
 
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # five steps take singular values of 0.002 to 1 near 1
@@ -35,19 +36,20 @@ def _sized(name: str, p, size: int):
 
 @functools.lru_cache(maxsize=256)
 def _entropy(code, dim, classes, tokens, backward):
-    p = gsn.gsn_entropy_params(code, dim, classes, tokens)
+    p = gsn.gsn_entropy_params(code, _int32(dim), _int32(classes), tokens)
     return _sized("gsn_cross_entropy", p, gsn.gsn_cross_entropy_workspace_bytes(p, backward))
 
 
 @functools.lru_cache(maxsize=256)
 def _orthogonal(code, rows, cols, batch, steps, coefficients, eps, update):
-    p = gsn.gsn_orthogonal_params(code, rows, cols, steps, batch, *coefficients, eps)
+    p = gsn.gsn_orthogonal_params(code, _int32(rows), _int32(cols), _int32(steps), batch,
+                                  *coefficients, eps)
     return _sized("gsn_orthogonalise", p, gsn.gsn_orthogonal_workspace_bytes(p, update))
 
 
 @functools.lru_cache(maxsize=256)
 def _linear(code, dim, out, tokens):
-    p = gsn.gsn_linear_params(code, dim, out, tokens)
+    p = gsn.gsn_linear_params(code, _int32(dim), _int32(out), tokens)
     return _sized("gsn_linear_quantised", p, gsn.gsn_linear_quantised_workspace_bytes(p))
 
 

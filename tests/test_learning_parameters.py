@@ -89,3 +89,43 @@ def test_tensors_of_another_type(called, code, fits):
             with pytest.raises(ValueError, match="type that the parameters"):
                 call()
     assert len(called) == (len(calls) if fits else 0)
+
+
+def test_sizes_beyond_32_bits(monkeypatch):
+    """They are out of every call's range, and not taken modulo 2^32 for one that is in it."""
+    far = (1 << 32) + 8
+    x = torch.zeros(1, 1)
+    for call in (lambda: learning.orthogonalise(x, steps=(1 << 32) + 5),
+                 lambda: learning.orthogonal_step(x, x, x, 0.1, steps=(1 << 32) + 5),
+                 lambda: learning.orthogonalise(x, steps=-(1 << 32) + 5),
+                 lambda: learning.cross_entropy(x.expand(1, far), x.expand(1, far), x),
+                 lambda: learning.cross_entropy(x, x.expand(far, 1), x),
+                 lambda: learning.linear_8bit(x.expand(1, far), x.expand(1, far), x)):
+        with pytest.raises(gsn.GsnError):
+            call()
+
+
+def test_rows_beyond_32_bits(monkeypatch):
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                seen.append((name, args))
+                return gsn.GSN_E_INVAL
+            call.__name__ = name
+            return call
+
+    monkeypatch.setattr(gsn, "_current_device", lambda: 0, raising=False)
+    monkeypatch.setattr(gsn, "_raw_stream", lambda index: 1000)
+    monkeypatch.setattr(gsn, "_lib", Library())
+    far = (1 << 32) + 8
+    x, s = t(2, far), t(2, 2)
+    for call in (lambda: gsn.gsn_quantise(x, t(2, far, dtype=torch.int8), t(2)),
+                 lambda: gsn.gsn_layer_norm(x, None, None, 1e-5, x),
+                 lambda: gsn.gsn_layer_norm_backward(x, x, None, s, x, None, None, None)):
+        with pytest.raises(gsn.GsnError):
+            call()
+    assert len(seen) == 3
+    for name, args in seen:
+        assert far not in args[:4] and -1 in args[:4], name
