@@ -652,6 +652,8 @@ typedef struct gsn_linear_params {
   int32_t dim, out;
   int64_t tokens;
 } gsn_linear_params;
+/* Device bytes of a call's workspace: x in 8 bits, and beyond 64 tokens room for a copy of w; 0 if
+ * the parameters are invalid. */
 size_t gsn_linear_quantised_workspace_bytes(const gsn_linear_params* params);
 int gsn_linear_quantised(const gsn_linear_params* params, const void* x, int64_t x_stride,
                 const int8_t* w, int64_t w_stride, const float* scales, void* y,

@@ -20,7 +20,7 @@ struct Linear8 {
   int64_t y_stride;
   int8_t* q;        // [tokens][pitch], zeros at the rows' ends
   float* x_scales;  // [tokens]
-  int8_t* wc;       // [out][pitch] w, where its rows are not at multiples of 16 bytes
+  int8_t* wc;       // [out][pitch] w, where its rows are not at multiples of 16 bytes; many tokens
   bool lines;       // rows of y begin and end at multiples of 16 bytes
 };
 
@@ -408,7 +408,9 @@ size_t carve(void* base, Linear8* x) {
   const size_t pitch = static_cast<size_t>(x->pitch);
   x->q = static_cast<int8_t*>(take(static_cast<size_t>(x->tokens) * pitch));
   x->x_scales = static_cast<float*>(take(4 * static_cast<size_t>(x->tokens)));
-  x->wc = static_cast<int8_t*>(take(static_cast<size_t>(x->out) * pitch));
+  // (launch() copies w for no fewer tokens)
+  if (x->tokens > few_at_most(false, false))
+    x->wc = static_cast<int8_t*>(take(static_cast<size_t>(x->out) * pitch));
   return used;
 }
 
