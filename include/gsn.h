@@ -566,8 +566,9 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
  * valid: uint8 [classes] or NULL, 0 for a class that is not there: it is in no sum and its row of
  * w means nothing.  A token whose target is out of range or not valid has none: its loss is 0
  * and its x means nothing.  tokens 0 to 2^24, dim 1 to 2^16, classes 1 to 2^28.
- * GSN_F32 of many tokens (160, backward 80) takes x and w in two float16 values an element, of
- * which 22 bits are left down to 2^-18 of the largest of its row, and 2^-40 of that below.
+ * GSN_F32 of many tokens (160, backward 224) makes the logits of x and w in two float16 values an
+ * element, of which 22 bits are left down to 2^-18 of the largest of its row, and 2^-40 of that
+ * below; an infinity in a row makes its logits NaN.
  * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128 (GSN_F32: 64 x 64). */
 typedef struct gsn_entropy_params {
   int32_t dtype;
@@ -590,8 +591,7 @@ int gsn_cross_entropy(const gsn_entropy_params* params, const void* x, int64_t x
  * be NULL (not computed).  The logits' gradients dloss (exp(l) / sum - [c = target]) are rounded
  * to dtype (to two values of it for up to 32 tokens) before they are multiplied with w and x; in
  * GSN_F16 as multiples of the largest finite |dloss|, so that a small dloss loses no digits
- * there; in GSN_F32 of many tokens to two float16 values as above, with the largest of all (times
- * the size of a row of w or x and dloss) in place of a row's. */
+ * there. */
 int gsn_cross_entropy_backward(const gsn_entropy_params* params, const float* dloss,
                                const void* x, int64_t x_stride, const void* w, int64_t w_stride,
                                const int32_t* targets, const uint8_t* valid, const float* stats,

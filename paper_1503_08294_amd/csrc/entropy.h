@@ -19,15 +19,15 @@ struct Entropy {
   int32_t piece, parts;  // classes of a piece; tiles of its columns, at most
   bool copy_x, copy_w;
   bool few;       // tokens that read w once, as it is
-  bool two;       // binary32 operands in two float16 values, copies always
+  bool two;       // binary32 logits of x and w in two float16 values
   bool two_d;     // gradients of the logits in two values of a 2-byte type, backward
   void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the
                   // ends; of two_d twice, one behind the other
   void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
-  float* fx;      // of operands in two values: the powers of two of the rows of xc,
-  float* fw;      // and of wc
-  int32_t pieces;
-  uint32_t* most;  // [1 + pieces] bits of the largest of fx, of each piece's fw; backward
+  void* x2;       // x and a piece of w in two values, the second ones behind all of the first
+  void* w2;
+  float* fx;      // the powers of two of the rows of x2,
+  float* fw;      // and of w2
   // forward
   float* loss;
   float* stats;   // [2][tokens]: the largest logit, and the sum of exp(logit - largest)
@@ -37,7 +37,6 @@ struct Entropy {
   const float* dloss;
   float* factor;  // 2: what dloss is multiplied by where the logits' gradients are kept, and back
   void* d;        // [tokens][piece] gradients of the logits; of two_d the second values behind them
-  void* dt;       // of operands in two values those for the product with x
   int32_t splits_x, splits_w;
   float* dxp;     // [splits_x][tokens][pitch]; of two_d [splits_x][2][tokens][pitch]
   float* dwp;     // [splits_w][piece][pitch], where splits_w > 1

@@ -19,11 +19,13 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 // Workgroups that a product of few tiles is split up into, along k, where a part keeps 1,024 bytes
 // of k at least.
 constexpr int64_t kFill = 512;
-// Tokens from which on binary32 operands are split up into two float16 values, which takes more
-// memory traffic and fewer cycles of the matrix cores.  As they are and in two values, us, 60,000
-// classes of 1,024: forward 128 tokens 161 and 174, 160 215 and 213, 191 217 and 220; backward 64
-// tokens 303 and 377, 96 467 and 366, 191 700 and 488.
-constexpr int64_t kTwoTokens = 160, kTwoTokensBack = 80;
+// Tokens from which on the logits of binary32 operands are made of two float16 values, which takes
+// more memory traffic and fewer cycles of the matrix cores.  As they are and in two values, us:
+// forward, 60,000 classes of 1,024, 128 tokens 161 and 174, 160 228 and 211, 224 284 and 220; 10,007
+// of 501, 160 tokens 44 and 41.  Backward, where they are one product of three, and copied for the
+// two others as well: 60,000 of 1,024, 192 tokens 681 and 688, 224 849 and 788, 320 1,116 and 1,028;
+// 10,007 of 501, 192 tokens 97 and 109, 224 112 and 116, 320 139 and 130.
+constexpr int64_t kTwoTokens = 160, kTwoTokensBack = 224;
 
 // Tokens up to which gradients of the logits are kept in two values of a 2-byte type.  In one, a
 // token's dx and its class's row of dw are off by the rounding of its target's gradient, up to half
@@ -74,7 +76,6 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
   x.few = !backward && p.tokens <= few_at_most(p.dtype == GSN_F32, true);
   x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 64)));
-  x.pieces = (p.classes - 1) / x.piece + 1;
   const bool may_be_few = p.tokens <= few_at_most(p.dtype == GSN_F32, false);
   x.parts = static_cast<int32_t>(up_to(may_be_few ? p.classes : x.piece, kFewCols) / kFewCols);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
@@ -82,24 +83,24 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   return x;
 }
 
-// What operands in two values need besides (a tile reads the powers of two of whole tiles).
-void carve_two(Carver* c, Entropy* x, bool backward) {
-  if (!x->two) return;
-  x->fx = static_cast<float*>(c->take(4 * static_cast<size_t>(x->tokens)));
-  x->fw = static_cast<float*>(c->take(4 * (static_cast<size_t>(x->piece) + kTileRows)));
-  if (!backward) return;
-  x->most = static_cast<uint32_t*>(c->take(4 * (1 + static_cast<size_t>(x->pieces))));
-  x->dt = c->take(4 * static_cast<size_t>(x->tokens) * x->piece);
+// x and w in two values (a tile reads the powers of two of whole tiles).
+void carve_two(Carver* c, Entropy* x) {
+  const size_t t = static_cast<size_t>(x->tokens), n = static_cast<size_t>(x->piece);
+  x->x2 = c->take(4 * t * x->pitch);
+  x->w2 = c->take(4 * n * x->pitch);
+  x->fx = static_cast<float*>(c->take(4 * t));
+  x->fw = static_cast<float*>(c->take(4 * (n + kTileRows)));
 }
 
 size_t carve_forward(void* base, int32_t dtype, Entropy* x) {
   Carver c{static_cast<char*>(base)};
   const size_t s = size_of(dtype), t = static_cast<size_t>(x->tokens);
-  if (!x->few) {
+  if (x->two) {
+    carve_two(&c, x);
+  } else if (!x->few) {
     x->xc = c.take(s * t * x->pitch);
     x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
   }
-  carve_two(&c, x, false);
   x->part = static_cast<float2*>(c.take(8 * t * x->parts));
   x->chosen = static_cast<float*>(c.take(4 * t));
   float* const stats = static_cast<float*>(c.take(8 * t));
@@ -114,7 +115,7 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
   x->xc = c.take(s * t * x->pitch * (x->two_d ? 2 : 1));
   x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
   x->d = c.take(s * t * x->piece * (x->two_d ? 2 : 1));
-  carve_two(&c, x, true);
+  if (x->two) carve_two(&c, x);
   x->dxp = static_cast<float*>(
       c.take(4 * t * x->pitch * static_cast<size_t>(x->splits_x) * (x->two_d ? 2 : 1)));
   x->dwp = x->splits_w > 1
@@ -126,7 +127,7 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
 
 // Whether the grids of a call's products stay below 2^32 threads of 256.
 bool grids_ok(const Entropy& x, int32_t dtype, bool backward) {
-  const int64_t side = dtype == GSN_F32 && !x.two ? kSmallRows : kMiddleRows;
+  const int64_t side = dtype == GSN_F32 && (backward || !x.two) ? kSmallRows : kMiddleRows;
   const auto tiles = [&](int64_t m, int64_t n) {
     return up_to(m, side) / side * (up_to(n, side) / side);
   };
@@ -182,8 +183,8 @@ int gsn_cross_entropy(const gsn_entropy_params* p, const void* x, int64_t x_stri
   a.valid = valid;
   a.loss = loss;
   a.stats = stats;
-  a.copy_x = a.two || !gsn::in_place(x, x_stride, p->dim, p->dtype);
-  a.copy_w = a.two || !gsn::in_place(w, w_stride, p->dim, p->dtype);
+  a.copy_x = !gsn::in_place(x, x_stride, p->dim, p->dtype);
+  a.copy_w = !gsn::in_place(w, w_stride, p->dim, p->dtype);
   if (p->tokens <= gsn::few_at_most(p->dtype == GSN_F32, !a.copy_w)) a.few = true;
   gsn::carve_forward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -217,9 +218,9 @@ int gsn_cross_entropy_backward(const gsn_entropy_params* p, const float* dloss, 
   a.stats = const_cast<float*>(stats);
   a.dx = p->tokens > 0 ? dx : nullptr;
   a.dw = dw;
-  a.copy_x = a.two || !gsn::in_place(x, x_stride, p->dim, p->dtype);
+  a.copy_x = !gsn::in_place(x, x_stride, p->dim, p->dtype);
   // (the product with w meets its classes that are not valid as zeros)
-  a.copy_w = a.two || valid || !gsn::in_place(w, w_stride, p->dim, p->dtype);
+  a.copy_w = valid || !gsn::in_place(w, w_stride, p->dim, p->dtype);
   gsn::carve_backward(workspace, p->dtype, &a);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = p->dtype == GSN_F32 ? gsn::launch_entropy_backward<float>(a, st)

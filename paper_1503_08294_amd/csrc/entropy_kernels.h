@@ -5,16 +5,20 @@
 // The logits are not kept: a tile of them is reduced to its rows' largest value and sum of
 // exponentials, and the backward pass makes them again, a piece of the classes at a time, as d.
 //
-// Binary32 operands in two values (TWO): the matrix cores multiply float16 at 9 times the rate that
-// they multiply binary32 at (1.43 and 0.153 PFLOP/s in large library products).  A row of x or w is
-// kept times a power of two, which takes its largest element to 2^14 to 2^15, as hi = float16(v)
-// and lo = float16(v - hi): 22 bits of every element down to 2^-18 of the largest, 2^-40 of it
-// below.  A product is hi lo + lo hi + hi hi, three products of one binary32 sum.
+// Logits of binary32 operands in two values (TWO): the matrix cores multiply float16 at 9 times the
+// rate that they multiply binary32 at (1.43 and 0.153 PFLOP/s in large library products).  A row of
+// x or w is kept times a power of two, which takes its largest element to 2^14 to 2^15, as hi =
+// float16(v) and lo = float16(v - hi): 22 bits of every element down to 2^-18 of the largest, 2^-40
+// of it below.  A product is hi lo + lo hi + hi hi, three products of one binary32 sum.  What a
+// logit loses so is small beside the row's others; the gradients' products take binary32 operands:
+// a class that every token finds improbable has a row of dw that is a sum of small terms alone, and
+// a token's or a feature's may be, so that no one scale has room for all of them in float16.
 //
 // Bound by the products.  8,192 tokens, 131,072 classes of 2,048, bfloat16: logits reduced 4.0 ms,
 // made again as d 4.7 (in four pieces, 2.1 GB written), dx 3.9, dw 3.9; joins, sums and copies
-// 0.05.  1,777 tokens, 10,007 classes of 501, two values: 82, 103, 67 and 104 us, and 60 for the
-// copies and joins; the tiles of each are one or two rounds of what the CUs hold.
+// 0.05.  1,777 tokens, 10,007 classes of 501, binary32, logits in two values: 78,
+// 85, 191 and 202 us, and 57 for copies and joins (with d, w and x in two values as well dx and dw
+// took 67 and 104, and lost classes whose probabilities are below some 2^-24 of the largest).
 #pragma once
 
 #include "entropy.h"
@@ -255,14 +259,12 @@ __device__ __forceinline__ void store_two(const Entropy& x, void* d, f32x4 (&v)[
   store_rows<E>(x, static_cast<E*>(d) + x.tokens * x.piece, v, t0, n0, lane, room);
 }
 
-// A tile of the logits -> their gradients, as the operands of the two products that take them: of
-// one type rounded to it (two_d: to two values of it); of binary32 in two values as d for the
-// product with w, times the class's power of two and without dloss, and as dt for the product with
-// x, times the token's power of two and dloss (at most kMostKept each).
+// A tile of the logits -> their gradients, as the operand of the two products that take them:
+// rounded to the operands' type (two_d: to two values of it).
 template <typename T, bool TWO>
 struct Gradient {
   Entropy x;
-  int32_t first, index;  // the piece's first class, and its number
+  int32_t first;  // the piece's first class
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
@@ -270,21 +272,12 @@ struct Gradient {
     const int li = lane & 15, lg = (lane >> 4) * 4;
     const int32_t n = at.n0 + nw + lg;
     const uint32_t shut = shut_columns<NT>(x.valid, x.classes, first + n);
-    constexpr bool kScaled = TWO || __is_same(T, f16_t);
+    constexpr bool kScaled = __is_same(T, f16_t);
     const float factor = kScaled ? x.factor[0] : 1.0f;
     const bool masked = __any(shut != 0);
     char* const room = smem + threadIdx.x / kWave * (TILE::kLds / 4);
-    static_assert(Turn<std::conditional_t<TWO, f16_t, T>, 16 * NT>::kBytes <= TILE::kLds / 4);
-    f32x4 cols[TWO ? NT : 1];
-    float most_x = 1.0f;
-    if constexpr (TWO) {
-      unscale(x, acc, int64_t{at.m0} + mw, at.n0 + nw, lane);
-      most_x = 1.0f / __uint_as_float(x.most[0]);
-      const float most_w = 1.0f / __uint_as_float(x.most[1 + index]);
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j) * most_w * kMostKept;
-    }
+    static_assert(Turn<T, 16 * NT>::kBytes <= TILE::kLds / 4);
+    if constexpr (TWO) unscale(x, acc, int64_t{at.m0} + mw, at.n0 + nw, lane);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int64_t t0 = at.m0 + mw + 16 * i, t = t0 + li;
@@ -292,7 +285,7 @@ struct Gradient {
       const int64_t tt = t < x.tokens ? t : x.tokens - 1;
       const int32_t target = target_of(x, tt);
       const int32_t place = target - first - n;
-      const float top = x.stats[tt], g = TWO ? 1.0f : x.dloss[tt] * factor;
+      const float top = x.stats[tt], g = x.dloss[tt] * factor;
       const float each = g / x.stats[x.tokens + tt];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
@@ -312,32 +305,13 @@ struct Gradient {
           for (int q = 0; q < 4; ++q)
             if (target < 0 || (shut >> (4 * j + q) & 1)) acc[i][j][q] = 0.0f;
       }
-      if constexpr (TWO) {
-        f32x4 v[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = acc[i][j] * cols[j];
-        // (columns past the last class have no power of two: their zeros are made again)
-        if (masked)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (shut >> (4 * j + q) & 1) v[j][q] = 0.0f;
-        store_two<f16_t>(x, x.d, v, t0, at.n0 + nw, lane, room);
-        // (a token without a target may have any dloss)
-        const float h = target < 0 ? 0.0f : x.dloss[tt] * factor * (x.fx[tt] * most_x);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = acc[i][j] * h;
-        store_two<f16_t>(x, x.dt, v, t0, at.n0 + nw, lane, room);
-      } else {
-        if constexpr (sizeof(T) == 2) {
-          if (x.two_d) {
-            store_two<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
-            continue;
-          }
+      if constexpr (sizeof(T) == 2) {
+        if (x.two_d) {
+          store_two<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
+          continue;
         }
-        store_rows<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
       }
+      store_rows<T>(x, x.d, acc[i], t0, at.n0 + nw, lane, room);
     }
   }
 };
@@ -348,18 +322,11 @@ struct Partial {
   int64_t split;  // elements from a split to the next
   int32_t rows, pitch;
   int32_t add;
-  // of operands in two values: what the sums are multiplied by, bits of a power of two, a number
-  // (or null) and a constant
-  const uint32_t* power;
-  const float* number;
-  float constant;
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
-    const float factor =
-        power ? __uint_as_float(*power) * constant * (number ? *number : 1.0f) : 1.0f;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
@@ -369,15 +336,14 @@ struct Partial {
       for (int j = 0; j < NT; ++j) {
         if (n + 16 * j >= pitch) break;
         f32x4* const p = reinterpret_cast<f32x4*>(row + n + 16 * j);
-        const f32x4 v = acc[i][j] * factor;
-        *p = add ? v + *p : v;
+        *p = add ? acc[i][j] + *p : acc[i][j];
       }
     }
   }
 };
 
 // A tile of dw, rounded to its type.
-template <typename T, bool TWO>
+template <typename T>
 struct Weights {
   Entropy x;
   int32_t first, count;
@@ -386,9 +352,7 @@ struct Weights {
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
                                        int lane, char*) const {
     const int32_t n = at.n0 + nw + (lane >> 4) * 4;
-    const float factor = TWO                    ? x.factor[1] * __uint_as_float(x.most[0])
-                         : __is_same(T, f16_t) ? x.factor[1]
-                                               : 1.0f;
+    const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int32_t m = at.m0 + mw + 16 * i + (lane & 15);
@@ -408,11 +372,11 @@ struct Weights {
 
 // The splits' sums, and their one rounding.  Rows without a target, or that are no valid class, are
 // zeros.
-template <typename T, bool OF_TOKENS, bool TWO>
+template <typename T, bool OF_TOKENS>
 __global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict__ part,
                                               int32_t splits, int64_t rows, int32_t first,
                                               int64_t split, T* __restrict__ out) {
-  const float all = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
+  const float factor = __is_same(T, f16_t) ? x.factor[1] : 1.0f;
   const int32_t each = (x.dim + 3) / 4;
   for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < rows * each;
        at += static_cast<int64_t>(gridDim.x) * 256) {
@@ -425,7 +389,6 @@ __global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict
 #pragma unroll 16
       for (int32_t i = 0; i < splits; ++i)
         s += *reinterpret_cast<const f32x4*>(part + i * split + r * x.pitch + d);
-    const float factor = TWO && OF_TOKENS && live ? x.dloss[r] : all;
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) v[q] = s[q] * factor;
@@ -456,32 +419,26 @@ __global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t 
   }
 }
 
-// Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends; the power of
-// two that gives the row back, and the largest of them (as bits of positive numbers, whose largest
-// is the same in any order).
-template <bool OF_TOKENS, bool DEAD>
+// Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends, and the power
+// of two that gives the row back.
+template <bool OF_TOKENS>
 __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t first,
-                                                f16_t* __restrict__ out, float* __restrict__ power,
-                                                uint32_t* __restrict__ most) {
+                                                f16_t* __restrict__ out,
+                                                float* __restrict__ power) {
   const float* const from = static_cast<const float*>(OF_TOKENS ? x.x : x.w);
   const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
   const int lane = threadIdx.x % kWave;
   const int64_t other = (OF_TOKENS ? x.tokens : int64_t{x.piece}) * x.pitch;
-  __shared__ uint32_t some[4];
-  uint32_t largest = 0;
   for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; r < rows;
        r += static_cast<int64_t>(gridDim.x) * 4) {
-    const bool live =
-        !DEAD || (OF_TOKENS ? target_of(x, r) >= 0 : !(x.valid && !x.valid[first + r]));
     const float* const row = from + (first + r) * stride;
     float top = 0.0f;
-    if (live)
-      for (int32_t k = lane * 4; k < x.dim; k += kWave * 4) {
-        float v[4];
-        load4(row, k, x.dim, v);
+    for (int32_t k = lane * 4; k < x.dim; k += kWave * 4) {
+      float v[4];
+      load4(row, k, x.dim, v);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) top = fmaxf(top, fabsf(v[q]));
-      }
+      for (int q = 0; q < 4; ++q) top = fmaxf(top, fabsf(v[q]));
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     // (rows below 2^-86 keep fewer bits, so that the power and its inverse are normal numbers; what
@@ -491,13 +448,10 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
       frexpf(top, &up);
       up = 15 - up < 100 ? 15 - up : 100;
     }
-    const float back = top > 0.0f ? ldexpf(1.0f, -up) : 0x1p-126f;  // (zeros: the smallest)
     for (int32_t k = lane * 8; k < x.pitch; k += kWave * 8) {
-      float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-      if (live) {
-        load4(row, k, x.dim, v);
-        load4(row, k + 4, x.dim, v + 4);
-      }
+      float v[8];
+      load4(row, k, x.dim, v);
+      load4(row, k + 4, x.dim, v + 4);
       Vec<f16_t, 8> hi, lo;
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
@@ -509,27 +463,15 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
       *reinterpret_cast<Vec<f16_t, 8>*>(to) = hi;
       *reinterpret_cast<Vec<f16_t, 8>*>(to + other) = lo;
     }
-    if (lane == 0) power[r] = back;
-    largest = max(largest, __float_as_uint(back));
+    if (lane == 0) power[r] = ldexpf(1.0f, -up);
   }
-  if (!most) return;
-  if (lane == 0) some[threadIdx.x / kWave] = largest;
-  __syncthreads();
-  if (threadIdx.x > 0) return;
-  largest = max(max(some[0], some[1]), max(some[2], some[3]));
-  // (most workgroups have nothing larger to tell: 10,007 rows took 118 us when all did)
-  if (largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
-    atomicMax(most, largest);
 }
 
 // Gradients of the logits in float16 are kept times 2^15 / max |dloss|: at most 2^15, and those of
 // small probabilities are not lost (2^-29 of the largest dloss still has all of its 11 bits).  A
-// dloss that is not finite is its own token's matter.  And the largest powers of two of the rows in
-// two values begin (2^-126, were all rows zeros).
+// dloss that is not finite is its own token's matter.
 __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   __shared__ float some[16];
-  for (int32_t i = threadIdx.x; i <= x.pieces; i += 1024)
-    if (x.most) x.most[i] = 0x00800000u;
   float m = 0.0f;
   for (int64_t t = threadIdx.x; t < x.tokens; t += 1024) {
     if (target_of(x, t) < 0) continue;
@@ -547,7 +489,7 @@ __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   x.factor[1] = base / kMostKept;
 }
 
-// A wave a row; few enough workgroups that they have little to tell each other (ce_pairs).
+// A wave a row.
 inline uint32_t row_blocks(int64_t rows) {
   return static_cast<uint32_t>(rows < 4 ? 1 : rows < 4096 ? rows / 4 : 1024);
 }
@@ -564,7 +506,7 @@ Operand operand_of(const void* p, int64_t ld, int64_t rows) {
 
 // An operand in two values: of the terms hi lo, lo hi, hi hi (the small ones first: fewer roundings
 // of a large sum), where `lo` is `other` elements behind hi.
-Operand pair_of(const void* p, int64_t ld, int64_t rows, int64_t other, bool first) {
+inline Operand pair_of(const void* p, int64_t ld, int64_t rows, int64_t other, bool first) {
   const int64_t lo = 2 * other;
   return Operand{static_cast<const char*>(p) + (first ? 0 : lo),
                  {first ? lo : -lo, first ? -lo : 0}, 2 * ld, 0, static_cast<int32_t>(rows)};
@@ -578,13 +520,13 @@ void split(Product* p, int32_t splits) {
   p->part = ((p->k + splits - 1) / splits + kBK - 1) / kBK * kBK;
 }
 
-// x or its copy by w from class `first` on or its copy.
+// x or its copy by w from class `first` on or its copy (or both in two values).
 template <typename T, bool TWO>
 Product logits_of(const Entropy& x, int32_t first, int32_t count) {
   Product p{};
   if constexpr (TWO) {
-    p.a = pair_of(x.xc, x.pitch, x.tokens, x.tokens * x.pitch, true);
-    p.b = pair_of(x.wc, x.pitch, count, int64_t{x.piece} * x.pitch, false);
+    p.a = pair_of(x.x2, x.pitch, x.tokens, x.tokens * x.pitch, true);
+    p.b = pair_of(x.w2, x.pitch, count, int64_t{x.piece} * x.pitch, false);
     p.terms = 3;
   } else {
     p.a = x.copy_x ? operand_of<T>(x.xc, x.pitch, x.tokens)
@@ -601,35 +543,37 @@ Product logits_of(const Entropy& x, int32_t first, int32_t count) {
 }
 
 // The copies of x and of a piece of w.
-template <typename T, bool TWO, bool DEAD>
+template <typename T, bool DEAD>
 void copy_tokens(const Entropy& x, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
-  if constexpr (TWO)
-    ce_pairs<true, DEAD><<<row_blocks(x.tokens), 256, 0, st>>>(
-        x, x.tokens, 0, static_cast<f16_t*>(x.xc), x.fx, x.most);
-  else
-    ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
-                                                                        static_cast<T*>(x.xc));
+  ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
+                                                                      static_cast<T*>(x.xc));
 }
-template <typename T, bool TWO, bool DEAD>
+template <typename T, bool DEAD>
 void copy_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
-  if constexpr (TWO)
-    ce_pairs<false, DEAD><<<row_blocks(count), 256, 0, st>>>(
-        x, count, first, static_cast<f16_t*>(x.wc), x.fw,
-        x.most ? x.most + 1 + first / x.piece : nullptr);
-  else
-    ce_rows<T, false, DEAD><<<some_blocks(count * row), 256, 0, st>>>(x, count, first,
-                                                                      static_cast<T*>(x.wc));
+  ce_rows<T, false, DEAD><<<some_blocks(count * row), 256, 0, st>>>(x, count, first,
+                                                                    static_cast<T*>(x.wc));
+}
+// The same in two values.
+inline void pair_tokens(const Entropy& x, hipStream_t st) {
+  ce_pairs<true><<<row_blocks(x.tokens), 256, 0, st>>>(x, x.tokens, 0, static_cast<f16_t*>(x.x2),
+                                                       x.fx);
+}
+inline void pair_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
+  ce_pairs<false><<<row_blocks(count), 256, 0, st>>>(x, count, first, static_cast<f16_t*>(x.w2),
+                                                     x.fw);
 }
 
 template <typename T, bool TWO>
 void forward(const Entropy& x, hipStream_t st) {
   using E = std::conditional_t<TWO, f16_t, T>;
-  if (x.copy_x) copy_tokens<T, TWO, false>(x, st);
+  if constexpr (TWO) pair_tokens(x, st);
+  else if (x.copy_x) copy_tokens<T, false>(x, st);
   for (int32_t first = 0; first < x.classes; first += x.piece) {
     const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    if (x.copy_w) copy_classes<T, TWO, false>(x, first, count, st);
+    if constexpr (TWO) pair_classes(x, first, count, st);
+    else if (x.copy_w) copy_classes<T, false>(x, first, count, st);
     Product p = logits_of<T, TWO>(x, first, count);
     p.eighths = 1;
     int32_t parts = 0;
@@ -649,53 +593,46 @@ void forward(const Entropy& x, hipStream_t st) {
 template <typename T, bool TWO>
 void backward(const Entropy& x, hipStream_t st) {
   using E = std::conditional_t<TWO, f16_t, T>;
-  if (TWO || __is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
-  copy_tokens<T, TWO, true>(x, st);
+  if (__is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
+  copy_tokens<T, true>(x, st);
+  if constexpr (TWO) pair_tokens(x, st);
   for (int32_t first = 0; first < x.classes; first += x.piece) {
     const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    const int32_t index = first / x.piece;
-    if (x.copy_w) copy_classes<T, TWO, true>(x, first, count, st);
-    const Product l = logits_of<T, TWO>(x, first, count);
+    if (x.copy_w) copy_classes<T, true>(x, first, count, st);
+    if constexpr (TWO) pair_classes(x, first, count, st);
+    run_product<E, false, false>(logits_of<T, TWO>(x, first, count), Gradient<T, TWO>{x, first},
+                                 st);
     // (second values of d are tokens of their own in both products: two terms would read w once
     // more, and take a stage more for dw)
     const int64_t rows = x.two_d ? 2 * x.tokens : x.tokens;
-    run_product<E, false, false>(l, Gradient<T, TWO>{x, first, index}, st);
-    const int64_t other_d = x.tokens * x.piece;
     if (x.dx) {
-      Product p = l;
-      p.a = TWO ? pair_of(x.d, x.piece, x.tokens, other_d, true)
-                : operand_of<E>(x.d, x.piece, rows);
+      Product p = logits_of<T, false>(x, first, count);
+      p.a = operand_of<T>(x.d, x.piece, rows);
       p.b.rows = x.dim;
       p.k = count;
-      split<E>(&p, x.splits_x);
-      run_product<E, false, true>(
-          p, Partial{x.dxp, rows * x.pitch, static_cast<int32_t>(rows), x.pitch, first > 0,
-                     TWO ? x.most + 1 + index : nullptr, nullptr, 1.0f / kMostKept}, st);
+      split<T>(&p, x.splits_x);
+      run_product<T, false, true>(
+          p, Partial{x.dxp, rows * x.pitch, static_cast<int32_t>(rows), x.pitch, first > 0}, st);
     }
     if (x.dw) {
       Product p{};
-      p.a = TWO ? pair_of(x.dt, x.piece, count, other_d, true)
-                : operand_of<E>(x.d, x.piece, count);
-      p.b = TWO ? pair_of(x.xc, x.pitch, x.dim, x.tokens * x.pitch, false)
-                : operand_of<E>(x.xc, x.pitch, x.dim);
-      p.terms = l.terms;
-      p.batch = 1;
+      p.a = operand_of<T>(x.d, x.piece, count);
+      p.b = operand_of<T>(x.xc, x.pitch, x.dim);
+      p.terms = p.batch = 1;
       p.k = static_cast<int32_t>(rows);
-      split<E>(&p, x.splits_w);
+      split<T>(&p, x.splits_w);
       if (x.splits_w > 1) {
         const int64_t each = int64_t{x.piece} * x.pitch;
-        run_product<E, true, true>(
-            p, Partial{x.dwp, each, count, x.pitch, 0, TWO ? x.most : nullptr,
-                       TWO ? x.factor + 1 : nullptr, 1.0f}, st);
-        ce_sum<T, false, TWO><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
+        run_product<T, true, true>(p, Partial{x.dwp, each, count, x.pitch, 0}, st);
+        ce_sum<T, false><<<some_blocks(int64_t{count} * ((x.dim + 3) / 4)), 256, 0, st>>>(
             x, x.dwp, x.splits_w, count, first, each, static_cast<T*>(x.dw));
       } else {
-        run_product<E, true, true>(p, Weights<T, TWO>{x, first, count}, st);
+        run_product<T, true, true>(p, Weights<T>{x, first, count}, st);
       }
     }
   }
   if (x.dx)
-    ce_sum<T, true, TWO><<<some_blocks(x.tokens * ((x.dim + 3) / 4)), 256, 0, st>>>(
+    ce_sum<T, true><<<some_blocks(x.tokens * ((x.dim + 3) / 4)), 256, 0, st>>>(
         x, x.dxp, x.two_d ? 2 * x.splits_x : x.splits_x, x.tokens, 0, x.tokens * x.pitch,
         static_cast<T*>(x.dx));
 }

@@ -1,0 +1,104 @@
+"""Gradients of the cross entropy in binary32 where they are small beside others: classes that every
+token finds improbable, classes whose rows of w are small beside another's, tokens that count for
+little.  Every element is held to what binary32 leaves of the terms of its own sum."""
+import pytest
+import torch
+
+from paper_1503_08294_amd import learning
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def check(x, w, t, dloss, valid=None):
+    """dx and dw against the formulas in 64 bits.
+
+    A logit is off by E = (dim + 8) U sum |x w| at most, where x and w may be kept in 22 bits, and
+    by dim 2^-39 of the largest x and w; exp(l - largest) by 2 E and by (|l - largest| + 3) 2 U of
+    itself, the sum of the exponentials by as much and by U an addition, 64 + classes / 64 at most.
+    So much of a probability, three roundings, and four roundings of dloss for the target's, is what
+    a gradient of a logit may be off by; dx and dw are sums of binary32 of their products."""
+    stats = learning.cross_entropy_forward(x.cuda(), w.cuda(), t.cuda(),
+                                           None if valid is None else valid.cuda())[1]
+    dx, dw = learning.cross_entropy_backward(dloss.cuda(), x.cuda(), w.cuda(), t.cuda(),
+                                             None if valid is None else valid.cuda(), stats)
+    there = torch.ones(len(w), dtype=torch.bool) if valid is None else valid != 0
+    x, g = x.double(), dloss.double()[:, None]
+    w = torch.where(there[:, None], w.double(), 0.0)
+    classes, dim = w.shape
+    logits = (x @ w.t()).masked_fill(~there, -torch.inf)
+    size = (x.abs() @ w.abs().t()).masked_fill(~there, 0.0)
+    e = ((dim + 8) * U * size).max(1, keepdim=True)[0] \
+        + dim * 2.0 ** -39 * x.abs().max() * w.abs().max()
+    p = logits.softmax(1)
+    far = (logits.max(1, keepdim=True)[0] - logits).masked_fill(~there, 0.0)
+    rel_sum = 2 * e + (64 + classes / 64) * U + (p * (far + 3)).sum(1, keepdim=True) * 2 * U
+    one = torch.zeros_like(p).scatter_(1, t.long()[:, None], 1.0)
+    d = (p - one) * g
+    off = (p * (rel_sum + 2 * e + (far + 6) * 2 * U) + 4 * U * one) * g.abs()
+    for got, a, b, o, name in ((dx, d, w, off, "dx"), (dw, d.t(), x, off.t(), "dw")):
+        want = a @ b
+        tol = (o + (a.shape[1] + 12) * U * (a.abs() + o)) @ b.abs()
+        tol = tol + U * (want.abs() + tol) + 2.0 ** -149
+        over = (got.double().cpu() - want).abs() / tol
+        assert torch.isfinite(got).all(), name
+        at = int(over.argmax())
+        assert over.max() <= 1, f"{name}: {over.max()} times the tolerance at {divmod(at, over.shape[1])}"
+        some = want.abs() > 2.0 ** -100
+        assert (got.cpu()[some] != 0).all(), name
+
+
+def randn(*shape, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed))
+
+
+TOKENS = [40, 80, 100, 160, 223, 224, 1_100]
+
+
+@pytest.mark.parametrize("tokens", TOKENS)
+def test_classes_that_every_token_finds_improbable(tokens):
+    """Probabilities from some tenths down to e^-60 or so."""
+    dim, classes = 40, 150
+    direction = torch.ones(dim) * dim ** -0.5
+    x = 3 * direction + 0.1 * randn(tokens, dim, seed=1)
+    w = -torch.linspace(0, 20, classes)[:, None] * direction + 0.1 * randn(classes, dim, seed=2)
+    t = torch.randint(0, 5, (tokens,), generator=torch.Generator().manual_seed(3)).int()
+    check(x, w, t, torch.rand(tokens, generator=torch.Generator().manual_seed(4)) / tokens)
+
+
+@pytest.mark.parametrize("tokens", TOKENS)
+def test_classes_whose_weights_are_small_beside_anothers(tokens):
+    """One class, which is improbable, has a row 2^28 times the others' in one of its columns."""
+    dim, classes = 24, 70
+    x, w = randn(tokens, dim, seed=5), randn(classes, dim, seed=6) * 2.0 ** -8
+    x[:, 0], w[:, 0] = 2.0 ** -15, 0.0
+    w[7] = 0
+    w[7, 0] = -2.0 ** 20
+    t = torch.randint(8, classes, (tokens,), generator=torch.Generator().manual_seed(7)).int()
+    check(x, w, t, torch.rand(tokens, generator=torch.Generator().manual_seed(8)) / tokens)
+
+
+@pytest.mark.parametrize("tokens", TOKENS)
+def test_tokens_that_count_for_little(tokens):
+    """Features that only tokens of a small dloss, or of a small x, have."""
+    dim, classes = 48, 60
+    x, w = randn(tokens, dim, seed=9), randn(classes, dim, seed=10) * 0.2
+    t = torch.randint(0, classes, (tokens,), generator=torch.Generator().manual_seed(11)).int()
+    dloss = 0.5 + torch.rand(tokens, generator=torch.Generator().manual_seed(12))
+    x[::2, :16] = 0           # columns 0 to 15: odd tokens alone, of which
+    dloss[1::2] *= 2.0 ** -30  # every one counts for little
+    x[3::4] *= 2.0 ** -20
+    check(x, w, t, dloss)
+
+
+def test_with_classes_that_are_not_there():
+    tokens, dim, classes = 170, 33, 90
+    direction = torch.ones(dim) * dim ** -0.5
+    x = 2 * direction + 0.1 * randn(tokens, dim, seed=13)
+    w = -torch.linspace(0, 20, classes)[:, None] * direction + 0.1 * randn(classes, dim, seed=14)
+    valid = torch.ones(classes, dtype=torch.uint8)
+    valid[10::7] = 0
+    w[valid == 0] = torch.nan
+    t = torch.randint(0, 5, (tokens,), generator=torch.Generator().manual_seed(15)).int()
+    check(x, w, t, torch.ones(tokens) / tokens, valid)
