@@ -566,9 +566,9 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
  * valid: uint8 [classes] or NULL, 0 for a class that is not there: it is in no sum and its row of
  * w means nothing.  A token whose target is out of range or not valid has none: its loss is 0
  * and its x means nothing.  tokens 0 to 2^24, dim 1 to 2^16, classes 1 to 2^28.
- * GSN_F32 of many tokens (160, backward 224) makes the logits of x and w in two float16 values an
- * element, of which 22 bits are left down to 2^-18 of the largest of its row, and 2^-40 of that
- * below; an infinity in a row makes its logits NaN.
+ * GSN_F32 of many tokens (256) makes the logits of x and w in two float16 values an element, 22
+ * bits, where a logit is off by no more than 2^-24 by what those have no room for: where the
+ * largest |x| times a row's largest sum of |w| and the other way round are 2^15 together at most.
  * GSN_E_CAPACITY if a product has more than some 2^23 tiles of 128 x 128 (GSN_F32: 64 x 64). */
 typedef struct gsn_entropy_params {
   int32_t dtype;

@@ -19,7 +19,7 @@ struct Entropy {
   int32_t piece, parts;  // classes of a piece; tiles of its columns, at most
   bool copy_x, copy_w;
   bool few;       // tokens that read w once, as it is
-  bool two;       // binary32 logits of x and w in two float16 values
+  bool two;       // binary32 logits of x and w in two float16 values, of pieces that allow it
   bool two_d;     // gradients of the logits in two values of a 2-byte type, backward
   void* xc;       // [tokens][pitch] x, zeros for tokens without a target (backward) and at the
                   // ends; of two_d twice, one behind the other
@@ -28,6 +28,9 @@ struct Entropy {
   void* w2;
   float* fx;      // the powers of two of the rows of x2,
   float* fw;      // and of w2
+  int32_t pieces;
+  uint32_t* sizes;  // [1 + pieces][2] of x and of each piece of w: bits of the largest magnitude
+                    // and of a row's largest sum of magnitudes
   // forward
   float* loss;
   float* stats;   // [2][tokens]: the largest logit, and the sum of exp(logit - largest)

@@ -20,12 +20,12 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 // of k at least.
 constexpr int64_t kFill = 512;
 // Tokens from which on the logits of binary32 operands are made of two float16 values, which takes
-// more memory traffic and fewer cycles of the matrix cores.  As they are and in two values, us:
-// forward, 60,000 classes of 1,024, 128 tokens 161 and 174, 160 228 and 211, 224 284 and 220; 10,007
-// of 501, 160 tokens 44 and 41.  Backward, where they are one product of three, and copied for the
-// two others as well: 60,000 of 1,024, 192 tokens 681 and 688, 224 849 and 788, 320 1,116 and 1,028;
-// 10,007 of 501, 192 tokens 97 and 109, 224 112 and 116, 320 139 and 130.
-constexpr int64_t kTwoTokens = 160, kTwoTokensBack = 224;
+// more memory traffic and launches, and fewer cycles of the matrix cores; of a backward pass they
+// are one product of three.  As they are and in two values, us: 60,000 classes of 1,024, forward 224
+// tokens 284 and 229, 256 285 and 235, 320 357 and 268, backward 849 and 790, 887 and 841, 1,116
+// and 1,034; 10,007 of 501, 256 tokens 52 and 56, backward 115 and 130, 512 tokens 70 and 65, 181
+// and 183; 2,000 of 2,048, 256 tokens 47 and 60, backward 110 and 120.
+constexpr int64_t kTwoTokens = 256;
 
 // Tokens up to which gradients of the logits are kept in two values of a 2-byte type.  In one, a
 // token's dx and its class's row of dw are off by the rounding of its target's gradient, up to half
@@ -66,7 +66,7 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   x.dim = p.dim;
   // (rows of the copies and of d are whole lines of 128 bytes: products read rows that begin inside
   // a line up to a fifth slower)
-  x.two = p.dtype == GSN_F32 && p.tokens >= (backward ? kTwoTokensBack : kTwoTokens);
+  x.two = p.dtype == GSN_F32 && p.tokens >= kTwoTokens;
   x.two_d = backward && p.dtype != GSN_F32 && p.tokens <= kTwoGradients;
   x.pitch = static_cast<int32_t>(up_to(p.dim, 64));
   int64_t piece = kPieceBytes / (size * x.pitch);
@@ -76,6 +76,7 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   // A few tokens: w is read once, whatever its rows' alignment, and no piece of it is copied.
   x.few = !backward && p.tokens <= few_at_most(p.dtype == GSN_F32, true);
   x.piece = static_cast<int32_t>(std::min(piece, up_to(p.classes, 64)));
+  x.pieces = (p.classes - 1) / x.piece + 1;
   const bool may_be_few = p.tokens <= few_at_most(p.dtype == GSN_F32, false);
   x.parts = static_cast<int32_t>(up_to(may_be_few ? p.classes : x.piece, kFewCols) / kFewCols);
   x.splits_x = split_of(tokens, x.pitch, x.piece, p.dtype);
@@ -90,14 +91,14 @@ void carve_two(Carver* c, Entropy* x) {
   x->w2 = c->take(4 * n * x->pitch);
   x->fx = static_cast<float*>(c->take(4 * t));
   x->fw = static_cast<float*>(c->take(4 * (n + kTileRows)));
+  x->sizes = static_cast<uint32_t*>(c->take(8 * (1 + static_cast<size_t>(x->pieces))));
 }
 
 size_t carve_forward(void* base, int32_t dtype, Entropy* x) {
   Carver c{static_cast<char*>(base)};
   const size_t s = size_of(dtype), t = static_cast<size_t>(x->tokens);
-  if (x->two) {
-    carve_two(&c, x);
-  } else if (!x->few) {
+  if (x->two) carve_two(&c, x);
+  if (!x->few) {
     x->xc = c.take(s * t * x->pitch);
     x->wc = c.take(s * x->piece * static_cast<size_t>(x->pitch));
   }
@@ -127,7 +128,7 @@ size_t carve_backward(void* base, int32_t dtype, Entropy* x) {
 
 // Whether the grids of a call's products stay below 2^32 threads of 256.
 bool grids_ok(const Entropy& x, int32_t dtype, bool backward) {
-  const int64_t side = dtype == GSN_F32 && (backward || !x.two) ? kSmallRows : kMiddleRows;
+  const int64_t side = dtype == GSN_F32 ? kSmallRows : kMiddleRows;
   const auto tiles = [&](int64_t m, int64_t n) {
     return up_to(m, side) / side * (up_to(n, side) / side);
   };

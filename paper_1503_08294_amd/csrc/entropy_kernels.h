@@ -10,7 +10,8 @@
 // x or w is kept times a power of two, which takes its largest element to 2^14 to 2^15, as hi =
 // float16(v) and lo = float16(v - hi): 22 bits of every element down to 2^-18 of the largest, 2^-40
 // of it below.  A product is hi lo + lo hi + hi hi, three products of one binary32 sum.  What a
-// logit loses so is small beside the row's others; the gradients' products take binary32 operands:
+// logit loses so is small beside the row's others, and in pieces of the classes for which it is not
+// they are made in binary32 (two_will_do()).  The gradients' products take binary32 operands:
 // a class that every token finds improbable has a row of dw that is a sum of small terms alone, and
 // a token's or a feature's may be, so that no one scale has room for all of them in float16.
 //
@@ -88,11 +89,30 @@ __device__ __forceinline__ void unscale(const Entropy& x, f32x4 (&acc)[MT][NT], 
   }
 }
 
+// Whether a piece's logits are made of two values.  An element that is kept so is off by 2^-23 of
+// itself or by 2^-39 of its row's largest, X or W, so that beside the errors of binary32 a logit
+// has one of 2^-39 (X sum |w| + W sum |x|).  It is at most 2^-24, a rounding of a number near 1, or
+// the logits are made in binary32: rows may hold a number far larger than the others, by which a
+// feature shuts classes out for some tokens, say, and infinities and NaN.
+__device__ __forceinline__ bool two_will_do(const Entropy& x, int32_t index) {
+  const uint32_t* const w = x.sizes + 2 * (1 + index);
+  return __uint_as_float(x.sizes[0]) * __uint_as_float(w[1]) +
+             __uint_as_float(w[0]) * __uint_as_float(x.sizes[1]) <= 0x1p15f;
+}
+// Whether these logits are the ones to make.
+template <typename T, bool TWO>
+__device__ __forceinline__ bool logits_wanted(const Entropy& x, int32_t index) {
+  if constexpr (sizeof(T) == 4) return !x.two || two_will_do(x, index) == TWO;
+  else return true;
+}
+
 // A tile of the logits -> (largest, sum) of each row, and the target's logit.
 template <typename T, bool TWO>
 struct Reduce {
   Entropy x;
-  int32_t first;  // the piece's first class
+  int32_t first, index;  // the piece's first class, and its number
+
+  __device__ __forceinline__ bool wanted() const { return logits_wanted<T, TWO>(x, index); }
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
@@ -185,13 +205,20 @@ __device__ __forceinline__ void finish_token(const Entropy& x, int64_t t, float2
   x.stats[x.tokens + t] = v.y;
 }
 
+// A piece's parts, of logits in two values and of others, and whether it is the first and the last.
+struct Parts {
+  int32_t two, one, index, begin, last;
+  __device__ __forceinline__ int32_t of(const Entropy& x) const {
+    return x.two && two_will_do(x, index) ? two : one;
+  }
+};
 // A workgroup a token, where there are few tokens.
 constexpr int kFewJoin = 512;
-__global__ __launch_bounds__(kFewJoin) void ce_join_few(Entropy x, int32_t parts, int32_t begin,
-                                                       int32_t last) {
+__global__ __launch_bounds__(kFewJoin) void ce_join_few(Entropy x, Parts p) {
   __shared__ float2 some[kFewJoin / kWave];
   const int tid = threadIdx.x;
   const int64_t t = blockIdx.x;
+  const int32_t parts = p.of(x);
   float2 v{-INFINITY, 0.0f};
 #pragma unroll 4
   for (int32_t i = tid; i < parts; i += kFewJoin) v = merged(v, x.part[i * x.tokens + t]);
@@ -203,15 +230,15 @@ __global__ __launch_bounds__(kFewJoin) void ce_join_few(Entropy x, int32_t parts
   if (tid > 0) return;
   v = some[0];
   for (int w = 1; w < kFewJoin / kWave; ++w) v = merged(v, some[w]);
-  if (!begin) v = merged(float2{x.stats[t], x.stats[x.tokens + t]}, v);
-  finish_token(x, t, v, last);
+  if (!p.begin) v = merged(float2{x.stats[t], x.stats[x.tokens + t]}, v);
+  finish_token(x, t, v, p.last);
 }
 constexpr int kJoinTokens = 64, kJoinWaves = 16;
-__global__ __launch_bounds__(kJoinTokens* kJoinWaves) void ce_join(Entropy x, int32_t parts,
-                                                                  int32_t begin, int32_t last) {
+__global__ __launch_bounds__(kJoinTokens* kJoinWaves) void ce_join(Entropy x, Parts p) {
   __shared__ float2 some[kJoinWaves][kJoinTokens];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * kJoinTokens + lane;
+  const int32_t parts = p.of(x);
   float2 v{-INFINITY, 0.0f};
   if (t < x.tokens) {
 #pragma unroll 4
@@ -220,9 +247,9 @@ __global__ __launch_bounds__(kJoinTokens* kJoinWaves) void ce_join(Entropy x, in
   some[wave][lane] = v;
   __syncthreads();
   if (wave > 0 || t >= x.tokens) return;
-  if (!begin) v = merged(float2{x.stats[t], x.stats[x.tokens + t]}, v);
+  if (!p.begin) v = merged(float2{x.stats[t], x.stats[x.tokens + t]}, v);
   for (int w = 1; w < kJoinWaves; ++w) v = merged(v, some[w][lane]);
-  finish_token(x, t, v, last);
+  finish_token(x, t, v, p.last);
 }
 
 // 16 rows from t0 on of the logits' gradients, columns n0 on, in 2- or 4-byte elements.
@@ -264,7 +291,9 @@ __device__ __forceinline__ void store_two(const Entropy& x, void* d, f32x4 (&v)[
 template <typename T, bool TWO>
 struct Gradient {
   Entropy x;
-  int32_t first;  // the piece's first class
+  int32_t first, index;  // the piece's first class, and its number
+
+  __device__ __forceinline__ bool wanted() const { return logits_wanted<T, TWO>(x, index); }
 
   template <class TILE, int MT, int NT>
   __device__ __forceinline__ void tile(f32x4 (&acc)[MT][NT], const Place& at, int mw, int nw,
@@ -397,10 +426,12 @@ __global__ __launch_bounds__(256) void ce_sum(Entropy x, const float* __restrict
 }
 
 // Rows of x (OF_TOKENS) or of w from `first` on, in rows of `pitch`, with zeros at their ends.
-// DEAD: rows of zeros where a token has no target or a class is not valid.
+// DEAD: rows of zeros where a token has no target or a class is not valid.  index >= 0: not if the
+// logits of this piece are made of two values.
 template <typename T, bool OF_TOKENS, bool DEAD>
 __global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t first,
-                                               T* __restrict__ out) {
+                                               int32_t index, T* __restrict__ out) {
+  if (index >= 0 && two_will_do(x, index)) return;
   constexpr int kE = 16 / sizeof(T);
   const T* const from = static_cast<const T*>(OF_TOKENS ? x.x : x.w);
   const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
@@ -419,28 +450,42 @@ __global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t 
   }
 }
 
-// Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends, and the power
-// of two that gives the row back.
+// Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends and for
+// tokens without a target and classes that are not valid; the power of two that gives the row back;
+// and the rows' sizes (as bits of numbers that are not negative, whose largest is the same in any
+// order, and NaN's are larger).
 template <bool OF_TOKENS>
 __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t first,
-                                                f16_t* __restrict__ out,
-                                                float* __restrict__ power) {
+                                                f16_t* __restrict__ out, float* __restrict__ power,
+                                                uint32_t* __restrict__ sizes) {
   const float* const from = static_cast<const float*>(OF_TOKENS ? x.x : x.w);
   const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
   const int lane = threadIdx.x % kWave;
   const int64_t other = (OF_TOKENS ? x.tokens : int64_t{x.piece}) * x.pitch;
+  __shared__ uint32_t some[2][4];
+  uint32_t largest = 0, longest = 0;
   for (int64_t r = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / kWave; r < rows;
        r += static_cast<int64_t>(gridDim.x) * 4) {
+    const bool live = OF_TOKENS ? target_of(x, r) >= 0 : !(x.valid && !x.valid[first + r]);
     const float* const row = from + (first + r) * stride;
-    float top = 0.0f;
-    for (int32_t k = lane * 4; k < x.dim; k += kWave * 4) {
-      float v[4];
-      load4(row, k, x.dim, v);
+    float top = 0.0f, sum = 0.0f;
+    if (live)
+      for (int32_t k = lane * 4; k < x.dim; k += kWave * 4) {
+        float v[4];
+        load4(row, k, x.dim, v);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) top = fmaxf(top, fabsf(v[q]));
+        for (int q = 0; q < 4; ++q) {
+          top = fmaxf(top, fabsf(v[q]));
+          sum += fabsf(v[q]);
+        }
+      }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      top = fmaxf(top, __shfl_xor(top, o));
+      sum += __shfl_xor(sum, o);
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    largest = max(largest, __float_as_uint(top));
+    longest = max(longest, __float_as_uint(sum) & 0x7fffffffu);
     // (rows below 2^-86 keep fewer bits, so that the power and its inverse are normal numbers; what
     // is not finite stays so)
     int up = 0;
@@ -449,9 +494,11 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
       up = 15 - up < 100 ? 15 - up : 100;
     }
     for (int32_t k = lane * 8; k < x.pitch; k += kWave * 8) {
-      float v[8];
-      load4(row, k, x.dim, v);
-      load4(row, k + 4, x.dim, v + 4);
+      float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (live) {
+        load4(row, k, x.dim, v);
+        load4(row, k + 4, x.dim, v + 4);
+      }
       Vec<f16_t, 8> hi, lo;
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
@@ -465,6 +512,21 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
     }
     if (lane == 0) power[r] = ldexpf(1.0f, -up);
   }
+  if (lane == 0) {
+    some[0][threadIdx.x / kWave] = largest;
+    some[1][threadIdx.x / kWave] = longest;
+  }
+  __syncthreads();
+  if (threadIdx.x > 1) return;
+  const uint32_t* const s = some[threadIdx.x];
+  largest = max(max(s[0], s[1]), max(s[2], s[3]));
+  // (most workgroups have nothing larger to tell: 10,007 rows took 118 us when all did)
+  uint32_t* const to = sizes + threadIdx.x;
+  if (largest > __hip_atomic_load(to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
+    atomicMax(to, largest);
+}
+__global__ __launch_bounds__(256) void ce_begin(Entropy x) {
+  for (int32_t i = threadIdx.x; i < 2 * (1 + x.pieces); i += 256) x.sizes[i] = 0;
 }
 
 // Gradients of the logits in float16 are kept times 2^15 / max |dloss|: at most 2^15, and those of
@@ -489,7 +551,7 @@ __global__ __launch_bounds__(1024) void ce_factor(Entropy x) {
   x.factor[1] = base / kMostKept;
 }
 
-// A wave a row.
+// A wave a row; few enough workgroups that they have little to tell each other (ce_pairs).
 inline uint32_t row_blocks(int64_t rows) {
   return static_cast<uint32_t>(rows < 4 ? 1 : rows < 4096 ? rows / 4 : 1024);
 }
@@ -542,66 +604,78 @@ Product logits_of(const Entropy& x, int32_t first, int32_t count) {
   return p;
 }
 
-// The copies of x and of a piece of w.
+// The copies of x and of a piece of w; index as of ce_rows().
 template <typename T, bool DEAD>
-void copy_tokens(const Entropy& x, hipStream_t st) {
+void copy_tokens(const Entropy& x, int32_t index, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
-  ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0,
+  ce_rows<T, true, DEAD><<<some_blocks(x.tokens * row), 256, 0, st>>>(x, x.tokens, 0, index,
                                                                       static_cast<T*>(x.xc));
 }
 template <typename T, bool DEAD>
-void copy_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
+void copy_classes(const Entropy& x, int32_t first, int32_t count, int32_t index, hipStream_t st) {
   const int64_t row = x.pitch / (16 / sizeof(T));
-  ce_rows<T, false, DEAD><<<some_blocks(count * row), 256, 0, st>>>(x, count, first,
+  ce_rows<T, false, DEAD><<<some_blocks(count * row), 256, 0, st>>>(x, count, first, index,
                                                                     static_cast<T*>(x.wc));
 }
 // The same in two values.
 inline void pair_tokens(const Entropy& x, hipStream_t st) {
+  ce_begin<<<1, 256, 0, st>>>(x);
   ce_pairs<true><<<row_blocks(x.tokens), 256, 0, st>>>(x, x.tokens, 0, static_cast<f16_t*>(x.x2),
-                                                       x.fx);
+                                                       x.fx, x.sizes);
 }
-inline void pair_classes(const Entropy& x, int32_t first, int32_t count, hipStream_t st) {
+inline void pair_classes(const Entropy& x, int32_t first, int32_t count, int32_t index,
+                         hipStream_t st) {
   ce_pairs<false><<<row_blocks(count), 256, 0, st>>>(x, count, first, static_cast<f16_t*>(x.w2),
-                                                     x.fw);
+                                                     x.fw, x.sizes + 2 * (1 + index));
 }
 
 template <typename T, bool TWO>
 void forward(const Entropy& x, hipStream_t st) {
-  using E = std::conditional_t<TWO, f16_t, T>;
   if constexpr (TWO) pair_tokens(x, st);
-  else if (x.copy_x) copy_tokens<T, false>(x, st);
+  else if (x.copy_x) copy_tokens<T, false>(x, -1, st);
   for (int32_t first = 0; first < x.classes; first += x.piece) {
     const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    if constexpr (TWO) pair_classes(x, first, count, st);
-    else if (x.copy_w) copy_classes<T, false>(x, first, count, st);
-    Product p = logits_of<T, TWO>(x, first, count);
+    const int32_t index = first / x.piece;
+    Parts parts{0, 0, index, first == 0, first + count == x.classes};
+    if constexpr (TWO) {
+      pair_classes(x, first, count, index, st);
+      Product p = logits_of<T, true>(x, first, count);
+      p.eighths = 1;
+      with_tile<f16_t, false, false>(p, [&](auto tile) { parts.two = tiles_of(count, tile.BN); });
+      run_product<f16_t, false, false>(p, Reduce<T, true>{x, first, index}, st);
+      // (of pieces whose logits are made in binary32 after all)
+      if (x.copy_x) copy_tokens<T, false>(x, index, st);
+    }
+    if (x.copy_w) copy_classes<T, false>(x, first, count, TWO ? index : -1, st);
+    Product p = logits_of<T, false>(x, first, count);
     p.eighths = 1;
-    int32_t parts = 0;
-    with_tile<E, false, false>(p, [&](auto tile) { parts = tiles_of(count, tile.BN); });
-    run_product<E, false, false>(p, Reduce<T, TWO>{x, first}, st);
+    with_tile<T, false, false>(p, [&](auto tile) { parts.one = tiles_of(count, tile.BN); });
+    run_product<T, false, false>(p, Reduce<T, false>{x, first, index}, st);
     // (of 64 tokens, 782 parts: 10.5 us by lanes)
     if (x.tokens <= 1024)
-      ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(
-          x, parts, first == 0, first + count == x.classes);
+      ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(x, parts);
     else
       ce_join<<<static_cast<uint32_t>((x.tokens + kJoinTokens - 1) / kJoinTokens),
-                kJoinTokens * kJoinWaves, 0, st>>>(x, parts, first == 0,
-                                                   first + count == x.classes);
+                kJoinTokens * kJoinWaves, 0, st>>>(x, parts);
   }
 }
 
 template <typename T, bool TWO>
 void backward(const Entropy& x, hipStream_t st) {
-  using E = std::conditional_t<TWO, f16_t, T>;
   if (__is_same(T, f16_t)) ce_factor<<<1, 1024, 0, st>>>(x);
-  copy_tokens<T, true>(x, st);
+  copy_tokens<T, true>(x, -1, st);
   if constexpr (TWO) pair_tokens(x, st);
   for (int32_t first = 0; first < x.classes; first += x.piece) {
     const int32_t count = x.classes - first < x.piece ? x.classes - first : x.piece;
-    if (x.copy_w) copy_classes<T, true>(x, first, count, st);
-    if constexpr (TWO) pair_classes(x, first, count, st);
-    run_product<E, false, false>(logits_of<T, TWO>(x, first, count), Gradient<T, TWO>{x, first},
-                                 st);
+    const int32_t index = first / x.piece;
+    if (x.copy_w) copy_classes<T, true>(x, first, count, -1, st);
+    if constexpr (TWO) {
+      pair_classes(x, first, count, index, st);
+      run_product<f16_t, false, false>(logits_of<T, true>(x, first, count),
+                                       Gradient<T, true>{x, first, index}, st);
+    }
+    run_product<T, false, false>(logits_of<T, false>(x, first, count),
+                                 Gradient<T, false>{x, first, index}, st);
     // (second values of d are tokens of their own in both products: two terms would read w once
     // more, and take a stage more for dw)
     const int64_t rows = x.two_d ? 2 * x.tokens : x.tokens;
@@ -645,7 +719,7 @@ hipError_t launch_entropy(const Entropy& x, hipStream_t st) {
     run_few<T>(Few{x.x, x.x_stride, x.w, x.w_stride, static_cast<int32_t>(x.tokens), x.classes,
                    x.dim}, ReduceFew{x}, st);
     ce_join_few<<<static_cast<uint32_t>(x.tokens), kFewJoin, 0, st>>>(
-        x, (x.classes + kFewCols - 1) / kFewCols, 1, 1);
+        x, Parts{0, (x.classes + kFewCols - 1) / kFewCols, 0, 1, 1});
     return hipGetLastError();
   }
   if constexpr (sizeof(T) == 4)

@@ -235,9 +235,19 @@ constexpr int kProductThreads = 256;
 //
 // What becomes of the results is the functor's:
 //   EPI::tile<TILE, MT, NT>(acc, place, mw, nw, lane, room)
+// and, where there is a bool EPI::wanted() that is false, nothing: the product is not made.
 // acc[i][j][q] is C(m0 + mw + 16 i + (lane & 15), n0 + nw + 16 j + 4 (lane >> 4) + q); mw and nw
 // are the wave's first row and column in the tile.  All threads of the workgroup come; room is LDS
 // that no other wave reads any more.
+template <class EPI>
+__device__ __forceinline__ auto wanted(const EPI& epi, int) -> decltype(epi.wanted()) {
+  return epi.wanted();
+}
+template <class EPI>
+__device__ __forceinline__ bool wanted(const EPI&, int64_t) {
+  return true;
+}
+
 template <typename T, bool TRA, bool TRB, class TILE, class EPI>
 __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Product p, EPI epi) {
   constexpr int kThr = kProductThreads, BM = TILE::BM, BN = TILE::BN;
@@ -250,6 +260,7 @@ __global__ __launch_bounds__(TILE::kThreads, TILE::WAVES) void mt_product(Produc
   const int tid = threadIdx.x - group * kThr, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int mw = (wave >> 1) * (BM / 2), nw = (wave & 1) * (BN / 2);
+  if (!wanted(epi, 0)) return;
   Place at;
   if (!place_of<TILE>(p, blockIdx.x, &at)) return;
 
