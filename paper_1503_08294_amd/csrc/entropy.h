@@ -26,8 +26,8 @@ struct Entropy {
   void* wc;       // [piece][pitch] a piece of w, zeros for classes that are not valid
   void* x2;       // x and a piece of w in two values, the second ones behind all of the first
   void* w2;
-  float* fx;      // the powers of two of the rows of x2,
-  float* fw;      // and of w2
+  int32_t* ex;    // the exponents of the powers of two that give back the rows of x2,
+  int32_t* ew;    // and of w2
   int32_t pieces;
   uint32_t* sizes;  // [1 + pieces][2] of x and of each piece of w: bits of the largest magnitude
                     // and of a row's largest sum of magnitudes

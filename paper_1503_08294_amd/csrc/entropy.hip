@@ -21,10 +21,10 @@ constexpr int64_t kPieceBytes = int64_t{1} << 29;
 constexpr int64_t kFill = 512;
 // Tokens from which on the logits of binary32 operands are made of two float16 values, which takes
 // more memory traffic and launches, and fewer cycles of the matrix cores; of a backward pass they
-// are one product of three.  As they are and in two values, us: 60,000 classes of 1,024, forward 224
-// tokens 284 and 229, 256 285 and 235, 320 357 and 268, backward 849 and 790, 887 and 841, 1,116
-// and 1,034; 10,007 of 501, 256 tokens 52 and 56, backward 115 and 130, 512 tokens 70 and 65, 181
-// and 183; 2,000 of 2,048, 256 tokens 47 and 60, backward 110 and 120.
+// are one product of three.  As they are and in two values, us: 60,000 classes of 1,024, forward
+// 224 tokens 284 and 229, 256 285 and 235, 320 357 and 268, backward 849 and 790, 887 and 841,
+// 1,116 and 1,034; 10,007 of 501, 256 tokens 52 and 56, backward 115 and 130, 512 tokens 70 and 65,
+// 181 and 183; 2,000 of 2,048, 256 tokens 47 and 60, backward 110 and 120.
 constexpr int64_t kTwoTokens = 256;
 
 // Tokens up to which gradients of the logits are kept in two values of a 2-byte type.  In one, a
@@ -84,13 +84,13 @@ Entropy entropy_of(const gsn_entropy_params& p, bool backward) {
   return x;
 }
 
-// x and w in two values (a tile reads the powers of two of whole tiles).
+// x and w in two values (a tile reads the exponents of whole tiles).
 void carve_two(Carver* c, Entropy* x) {
   const size_t t = static_cast<size_t>(x->tokens), n = static_cast<size_t>(x->piece);
   x->x2 = c->take(4 * t * x->pitch);
   x->w2 = c->take(4 * n * x->pitch);
-  x->fx = static_cast<float*>(c->take(4 * t));
-  x->fw = static_cast<float*>(c->take(4 * (n + kTileRows)));
+  x->ex = static_cast<int32_t*>(c->take(4 * t));
+  x->ew = static_cast<int32_t*>(c->take(4 * (n + kTileRows)));
   x->sizes = static_cast<uint32_t*>(c->take(8 * (1 + static_cast<size_t>(x->pieces))));
 }
 

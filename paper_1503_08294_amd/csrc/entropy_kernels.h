@@ -69,23 +69,24 @@ __device__ __forceinline__ float2 merged(float2 a, float2 b) {
   return float2{m, a.y * expf(a.x - base) + b.y * expf(b.x - base)};
 }
 
-// The logits of rows and columns that were kept times a power of two.
+// The logits of rows and columns that were kept times powers of two (which may be too small for
+// binary32 themselves).
 template <int MT, int NT>
 __device__ __forceinline__ void unscale(const Entropy& x, f32x4 (&acc)[MT][NT], int64_t m,
                                         int32_t n, int lane) {
-  f32x4 cols[NT];
-  // (columns past the last class are not used, but read: fw has room for them)
+  i32x4 cols[NT];
+  // (columns past the last class are not used, but read: ew has room for them)
 #pragma unroll
   for (int j = 0; j < NT; ++j)
-    cols[j] = *reinterpret_cast<const f32x4*>(x.fw + n + 16 * j + (lane >> 4) * 4);
+    cols[j] = *reinterpret_cast<const i32x4*>(x.ew + n + 16 * j + (lane >> 4) * 4);
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
     const int64_t t = m + 16 * i + (lane & 15);
-    const float row = x.fx[t < x.tokens ? t : x.tokens - 1];
+    const int32_t row = x.ex[t < x.tokens ? t : x.tokens - 1];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) acc[i][j][q] *= row * cols[j][q];
+      for (int q = 0; q < 4; ++q) acc[i][j][q] = ldexpf(acc[i][j][q], row + cols[j][q]);
   }
 }
 
@@ -451,12 +452,13 @@ __global__ __launch_bounds__(256) void ce_rows(Entropy x, int64_t rows, int32_t 
 }
 
 // Rows of x (OF_TOKENS) or of w in two values, a wave a row, with zeros at their ends and for
-// tokens without a target and classes that are not valid; the power of two that gives the row back;
-// and the rows' sizes (as bits of numbers that are not negative, whose largest is the same in any
-// order, and NaN's are larger).
+// tokens without a target and classes that are not valid; the exponent of the power of two that
+// gives the row back; and the rows' sizes (as bits of numbers that are not negative, whose largest
+// is the same in any order, and NaN's are larger).
 template <bool OF_TOKENS>
 __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t first,
-                                                f16_t* __restrict__ out, float* __restrict__ power,
+                                                f16_t* __restrict__ out,
+                                                int32_t* __restrict__ exponent,
                                                 uint32_t* __restrict__ sizes) {
   const float* const from = static_cast<const float*>(OF_TOKENS ? x.x : x.w);
   const int64_t stride = OF_TOKENS ? x.x_stride : x.w_stride;
@@ -486,13 +488,9 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
     }
     largest = max(largest, __float_as_uint(top));
     longest = max(longest, __float_as_uint(sum) & 0x7fffffffu);
-    // (rows below 2^-86 keep fewer bits, so that the power and its inverse are normal numbers; what
-    // is not finite stays so)
-    int up = 0;
-    if (top > 0.0f && top < INFINITY) {
-      frexpf(top, &up);
-      up = 15 - up < 100 ? 15 - up : 100;
-    }
+    int down = 15;  // (what is not finite stays so)
+    if (top > 0.0f && top < INFINITY) frexpf(top, &down);
+    const int up = 15 - down;
     for (int32_t k = lane * 8; k < x.pitch; k += kWave * 8) {
       float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if (live) {
@@ -510,7 +508,7 @@ __global__ __launch_bounds__(256) void ce_pairs(Entropy x, int64_t rows, int32_t
       *reinterpret_cast<Vec<f16_t, 8>*>(to) = hi;
       *reinterpret_cast<Vec<f16_t, 8>*>(to + other) = lo;
     }
-    if (lane == 0) power[r] = ldexpf(1.0f, -up);
+    if (lane == 0) exponent[r] = -up;
   }
   if (lane == 0) {
     some[0][threadIdx.x / kWave] = largest;
@@ -621,12 +619,12 @@ void copy_classes(const Entropy& x, int32_t first, int32_t count, int32_t index,
 inline void pair_tokens(const Entropy& x, hipStream_t st) {
   ce_begin<<<1, 256, 0, st>>>(x);
   ce_pairs<true><<<row_blocks(x.tokens), 256, 0, st>>>(x, x.tokens, 0, static_cast<f16_t*>(x.x2),
-                                                       x.fx, x.sizes);
+                                                       x.ex, x.sizes);
 }
 inline void pair_classes(const Entropy& x, int32_t first, int32_t count, int32_t index,
                          hipStream_t st) {
   ce_pairs<false><<<row_blocks(count), 256, 0, st>>>(x, count, first, static_cast<f16_t*>(x.w2),
-                                                     x.fw, x.sizes + 2 * (1 + index));
+                                                     x.ew, x.sizes + 2 * (1 + index));
 }
 
 template <typename T, bool TWO>

@@ -47,3 +47,22 @@ def test_a_large_row_by_a_small_one(tokens):
         got = learning.cross_entropy((x * 2.0 ** power).cuda(), (w * 2.0 ** -power).cuda(), t)
         # (powers of two change no digit, but for those that 2^-100 leaves no room for)
         assert ((got - want).abs() <= 1e-5).all()
+
+
+@pytest.mark.parametrize("tokens", [5, 160, 256, 300])
+@pytest.mark.parametrize("power", [-120, -110, 110, 120])
+def test_rows_near_both_ends_of_binary32(tokens, power):
+    """The logits of x times 2^power and w times 2^-power, all of them normal numbers, are those of x
+    and w, and so are the losses; each is off by dim + 8 roundings of a logit's sum of magnitudes,
+    below 24 x 3, and as many of its own."""
+    g = torch.Generator().manual_seed(tokens)
+    x, w = (torch.rand(n, 24, generator=g) + 0.5 for n in (tokens, 70))
+    x *= torch.randint(0, 2, x.shape, generator=g) * 2 - 1
+    w *= torch.randint(0, 2, w.shape, generator=g) * 2 - 1
+    t = torch.randint(0, 70, (tokens,), generator=g, dtype=torch.int32).cuda()
+    want = torch.nn.functional.cross_entropy(x.double() @ w.double().t(), t.long().cpu(),
+                                             reduction="none")
+    y, v = x * 2.0 ** power, w * 2.0 ** -power
+    assert y.abs().min() >= 2.0 ** -126 and v.abs().min() >= 2.0 ** -126
+    got = learning.cross_entropy(y.cuda(), v.cuda(), t).double().cpu()
+    assert ((got - want).abs() <= 3 * 32 * 2.0 ** -24 * 72).all()
