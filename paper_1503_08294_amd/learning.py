@@ -60,6 +60,14 @@ def _no_gradient(what: str, *tensors):
                          "detached tensors")
 
 
+def _written(*tensors):
+    """Counts as a write to them for autograd, as an operation of torch's in place does: what was
+    saved of them for a backward pass is no longer what it was."""
+    for t in tensors:
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
+
+
 def _operands(x, w):
     """(type, columns of both, rows of w, rows of x) of the operands of x w^T."""
     if w.dim() != 2:
@@ -162,12 +170,13 @@ def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=Tr
     (of the momentum alone without nesterov).  scale: sqrt(max(1, rows / cols)) if None, so that
     the update moves outputs as far whatever the shape.  momentum is float32, gradient of the type
     of weights, all contiguous.  out: the two tensors that take the results, (weights, momentum) for
-    an update in place; new ones if None."""
-    _no_tangent(weights, gradient, momentum)
-    _no_gradient("orthogonal_step", weights, gradient, momentum)
+    an update in place, which autograd sees as one; new ones if None."""
+    given = () if out is None else tuple(out)
+    _no_tangent(weights, gradient, momentum, *given)
+    _no_gradient("orthogonal_step", weights, gradient, momentum, *given)
     p, size = _orthogonal(*_matrices(weights), steps, tuple(map(float, coefficients)), float(eps),
                           True)
-    new_weights, new_momentum = out if out is not None else (
+    new_weights, new_momentum = given if out is not None else (
         torch.empty_like(weights, memory_format=torch.contiguous_format),
         torch.empty_like(momentum, memory_format=torch.contiguous_format))
     _same_device(weights, gradient, momentum, new_weights, new_momentum)
@@ -175,6 +184,7 @@ def orthogonal_step(weights, gradient, momentum, rate, *, beta=0.95, nesterov=Tr
         scale = max(1.0, p.rows / p.cols) ** 0.5
     gsn.gsn_orthogonal_step(p, weights, gradient, momentum, rate * scale, beta, rate * decay,
                             nesterov, new_weights, new_momentum, _bytes(size, weights))
+    _written(*given)
     return new_weights, new_momentum
 
 
