@@ -6,8 +6,9 @@ a unit has its units as classes: ``cross_entropy`` is that model's loss, without
 of all units.  ``orthogonal_step`` updates its matrices and those of the local experts of
 ``mixture`` by the orthogonalised momentum of their gradients, ``linear_8bit`` serves a layer in 8
 bits.  ``cross_entropy`` takes part in autograd, once: derivatives of its gradients raise
-``RuntimeError``.  The other calls have no derivatives and refuse tensors that want them, and all
-refuse tensors that carry a forward-mode tangent.
+``RuntimeError``; ``cross_entropy_forward`` and ``cross_entropy_backward`` are its two halves for
+programs that keep their own order.  The other calls have no derivatives and refuse tensors that
+want them, and all refuse tensors that carry a forward-mode tangent.
 
 Tensors are on one HIP device; work goes to torch's current stream of that device, where the
 outputs and workspaces are allocated too.  Tensors that do not fit raise ``ValueError``, sizes and
@@ -90,11 +91,13 @@ def _cross_entropy(x, w, targets, valid, save):
 
 def cross_entropy_forward(x, w, targets, valid=None):
     """(loss, stats): the loss of every token and what the backward pass takes."""
+    _no_tangent(x, w)
     return _cross_entropy(x, w, targets, valid, True)
 
 
 def cross_entropy_backward(dloss, x, w, targets, valid, stats, need=(True, True)):
     """(dx, dw) from dloss (tokens,) float32; None for what is not needed."""
+    _no_tangent(dloss, x, w, stats)
     _rows(x, "x")
     _same_device(x, dloss, w, targets, valid, stats)
     p, size = _entropy(*_operands(x, w), True)
