@@ -645,8 +645,9 @@ int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_
 
 /* y[t][n] = (sum over k of q[t][k] w[n][k]) scale[t] scales[n], with q and scale those of
  * gsn_quantise of x.  x [tokens][dim] and y [tokens][out] of type dtype; w int8 [out][dim], scales
- * float [out]; row strides.  The sum is exact.  tokens 0 to 2^24, dim 1 to 2^17 - 1, out 1 to
- * 2^28.  GSN_E_CAPACITY if the product has more than some 2^23 tiles of 128 x 128. */
+ * float [out]; row strides.  The sum is exact, its products with the scales are rounded to binary32
+ * each.  tokens 0 to 2^24, dim 1 to 2^17 - 1, out 1 to 2^28.  GSN_E_CAPACITY if the product has more
+ * than some 2^23 tiles of 128 x 128. */
 typedef struct gsn_linear_params {
   int32_t dtype;
   int32_t dim, out;
