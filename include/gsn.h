@@ -558,7 +558,8 @@ int gsn_experts_backward(const gsn_experts_params* params, const void* dout, con
  * the rules of the mixture's calls above: no handle, async, may be captured, allocate nothing,
  * the same bits on every run, sums in binary32 (products of 8 bits: in 32-bit integers), a
  * result rounded once to nearest even.  Workspaces are 256-byte aligned; two calls that may run
- * at a time need one each. */
+ * at a time need one each.  Outputs are memory of their own where nothing else is said; those that
+ * begin where an input does that is read after them are refused (GSN_E_INVAL). */
 
 /* Softmax cross entropy of every token, the logits never kept as a whole:
  *     l[c] = x[t] . w[c],  loss[t] = log(sum over the valid classes of exp(l[c])) - l[targets[t]]

@@ -143,6 +143,12 @@ bool in_place(const void* p, int64_t stride, int32_t dim, int32_t dtype) {
   return aligned16(p) && stride % elements == 0 && dim % elements == 0;
 }
 
+// Whether an output begins where one of the inputs does.
+template <class... IN>
+bool over(const void* out, const IN*... in) {
+  return out && ((out == in) || ...);
+}
+
 bool workspace_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 256 == 0; }
 
 }  // namespace
@@ -176,6 +182,8 @@ int gsn_cross_entropy(const gsn_entropy_params* p, const void* x, int64_t x_stri
   if (workspace_bytes < gsn_cross_entropy_workspace_bytes(p, 0)) return GSN_E_CAPACITY;
   gsn::Entropy a = gsn::entropy_of(*p, false);
   if (!gsn::grids_ok(a, p->dtype, false)) return GSN_E_CAPACITY;
+  if (gsn::over(loss, x, w, targets, valid, stats) || gsn::over(stats, x, w, targets, valid))
+    return GSN_E_INVAL;
   a.x = x;
   a.x_stride = x_stride;
   a.w = w;
@@ -209,6 +217,10 @@ int gsn_cross_entropy_backward(const gsn_entropy_params* p, const float* dloss, 
   if (workspace_bytes < gsn_cross_entropy_workspace_bytes(p, 1)) return GSN_E_CAPACITY;
   gsn::Entropy a = gsn::entropy_of(*p, true);
   if (!gsn::grids_ok(a, p->dtype, true)) return GSN_E_CAPACITY;
+  // (dx is written when all else has been read but the targets and dloss)
+  if (gsn::over(dx, dw, targets, valid, dloss) ||
+      gsn::over(dw, x, targets, valid, stats, dloss))
+    return GSN_E_INVAL;
   a.dloss = dloss;
   a.x = x;
   a.x_stride = x_stride;

@@ -474,6 +474,7 @@ int gsn_quantise(int32_t dtype, int64_t rows, int32_t dim, const void* x, int64_
     return GSN_E_INVAL;
   if (rows == 0) return GSN_OK;
   if (!x || !q || !scales || x_stride < dim || q_stride < dim) return GSN_E_INVAL;
+  if (q == x || scales == x || q == static_cast<const void*>(scales)) return GSN_E_INVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool waves = gsn::by_waves(rows, dim);
   const uint32_t blocks = gsn::row_blocks(rows, waves);
@@ -511,6 +512,7 @@ int gsn_linear_quantised(const gsn_linear_params* p, const void* x, int64_t x_st
   if (int64_t{gsn::tiles_of(p->tokens, gsn::kMiddleRows)} *
           gsn::tiles_of(p->out, gsn::kMiddleRows) >= (1 << 23))
     return GSN_E_CAPACITY;
+  if (y == x || y == w || y == scales) return GSN_E_INVAL;
   gsn::Linear8 a = gsn::linear8_of(*p);
   a.x = x;
   a.x_stride = x_stride;
