@@ -12,7 +12,9 @@ want them, and all refuse tensors that carry a forward-mode tangent.
 
 Tensors are on one HIP device; work goes to torch's current stream of that device, where the
 outputs and workspaces are allocated too.  Tensors that do not fit raise ``ValueError``, sizes and
-options out of the kernels' range ``gsn.GsnError``.
+options out of the kernels' range ``gsn.GsnError``.  All calls can be recorded into a HIP graph; a
+backward pass through autograd, as any of torch's, only while no eager graph of the same leaves
+lives.
 """
 from __future__ import annotations
 
