@@ -128,7 +128,8 @@ def train(model, points, normals, steps: int, batch: int, rate=3e-3, balance_rat
         opt.step()
         with torch.no_grad():
             for p, m in zip(matrices, momenta):
-                learning.orthogonal_step(p, p.grad.contiguous(), m, orthogonal_rate, out=(p, m))
+                if p.grad is not None:  # (the classes' is, where they are not learned)
+                    learning.orthogonal_step(p, p.grad.contiguous(), m, orthogonal_rate, out=(p, m))
         counts = mixture.route_counts(ids, model.balance.numel())
         mixture.route_balance(counts, model.balance, balance_rate)
 
