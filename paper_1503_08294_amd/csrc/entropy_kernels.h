@@ -17,9 +17,10 @@
 //
 // Bound by the products.  8,192 tokens, 131,072 classes of 2,048, bfloat16: logits reduced 4.0 ms,
 // made again as d 4.7 (in four pieces, 2.1 GB written), dx 3.9, dw 3.9; joins, sums and copies
-// 0.05.  1,777 tokens, 10,007 classes of 501, binary32, logits in two values: 78,
-// 85, 191 and 202 us, and 57 for copies and joins (with d, w and x in two values as well dx and dw
-// took 67 and 104, and lost classes whose probabilities are below some 2^-24 of the largest).
+// 0.05.  1,777 tokens, 10,007 classes of 501, binary32, logits in two values: 78, 84, 189 and 200 us,
+// 90 for splitting into two values, copies and joins, and for launches that end at once.  (With d, w
+// and x in two values as well dx and dw took 67 and 104, and lost classes whose probabilities are
+// below some 2^-24 of the largest.)
 #pragma once
 
 #include "entropy.h"
